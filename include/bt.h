@@ -253,6 +253,99 @@ bt_status bt_block_prefill_attn(const bt_config* cfg, const void* q, const void*
                                 void* stream);
 
 /*
+ * ---- Long and shared contexts.  The paper's block decoder attends over every cached block (section 2.3) and
+ * its decoding is bound by reading that cache (appendix E.2).  These calls, which the paper has no counterpart for, bound
+ * what is read or held: a window, a prefix held once for the batch, eviction.  They run over the same block cache.
+ *
+ * Attention under a sliding window with sinks: of the n rows of a sequence the query of the newest block sees the first
+ * min(sinks, n) and the last min(window, n) (a row that is both counts once):
+ *   out[b,h,:] = sum_j softmax_j(scale * q[b,h,:] . K[b,h,j,:]) * V[b,h,j,:],  j < sinks or n - window <= j < n.
+ * Rows outside are neither read nor waited for, whatever they hold.  window >= 1, sinks >= 0 (else BT_ERR_SHAPE); either may
+ * exceed the cache.  Everything else - empty sequences, the workspace (bt_workspace_bytes), errors - is that of
+ * bt_block_decode_attn, and for the step form that of bt_block_decode_step: the row is appended first, so n counts it
+ * and it is always visible.
+ */
+bt_status bt_block_decode_attn_window(const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q,
+                                      int window, int sinks, void* out, void* workspace, size_t workspace_bytes,
+                                      uint32_t* dev_status, void* stream);
+bt_status bt_block_decode_step_window(const bt_config* cfg, bt_block_cache* cache, int layer, const void* q,
+                                      const void* k_new, const void* v_new, int window, int sinks, void* out,
+                                      void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/*
+ * bt_block_prefill_attn under the same rule, counted from every query: position t sees row j <= t with
+ * j > t - window or j < sinks.  Only the key/value tiles that hold a visible pair are read and multiplied.  A row that a
+ * query does not see has no part in its result even if it holds an infinity or a NaN (such query rows are worked
+ * out again without the tensor cores, which is slow).  Arguments and errors as for bt_block_prefill_attn, except that
+ * cfg->prefill_plain is refused with BT_ERR_UNSUPPORTED: there is no CUDA-core form.
+ */
+bt_status bt_block_prefill_attn_window(const bt_config* cfg, const void* q, const void* k, const void* v, int n_blocks,
+                                       int64_t kv_seq_stride, int window, int sinks, void* out, uint32_t* dev_status,
+                                       void* stream);
+
+/*
+ * Decode attention of a batch that shares a prefix (one instruction or document in front of every sequence), whose
+ * K and V are held once and read once for all sequences:
+ *   out[b,h,:] = softmax over the rows  { prefix rows 0 .. S-1 of head h }  then  { own rows 0 .. len[b]-1 of (b,h) }.
+ * prefix: a block cache of ONE sequence, [n_layers][1][H][prefix_max][hd] with S = prefix->len[layer] - what
+ * bt_block_kv_append, bt_block_qkv_project_append and the prefill calls fill under a config of batch 1 and max_blocks =
+ * prefix_max.  It is only read.  Either part may be empty; both empty gives zeros and BT_DEV_EMPTY.
+ * The prefix part is a dense product per head on the tensor cores (the softmax weights are rounded to bf16 where
+ * they meet V, as in the prefill), the own part is bt_block_decode_attn's; two launches that overlap.  The step form
+ * appends a row to the sequence's own cache first, exactly as bt_block_decode_step.
+ * workspace: required, bt_workspace_bytes_shared bytes (0 on an invalid config), initialised by bt_workspace_init under the
+ * same config; one call at a time.  Other arguments and errors as for bt_block_decode_attn / bt_block_decode_step.
+ */
+size_t bt_workspace_bytes_shared(const bt_config* cfg, int prefix_max);
+bt_status bt_block_decode_attn_shared(const bt_config* cfg, const bt_block_cache* prefix, int prefix_max,
+                                      const bt_block_cache* cache, int layer, const void* q, void* out, void* workspace,
+                                      size_t workspace_bytes, uint32_t* dev_status, void* stream);
+bt_status bt_block_decode_step_shared(const bt_config* cfg, const bt_block_cache* prefix, int prefix_max,
+                                      bt_block_cache* cache, int layer, const void* q, const void* k_new, const void* v_new,
+                                      void* out, void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/*
+ * Decode attention that also sums the weight each cached row gets (what bt_block_kv_evict chooses by):
+ *   out as bt_block_decode_attn, and for j < len[b]
+ *   weights_out[b,h,j] = weights_in[b,h,j] + softmax_j(scale * q[b,h,:] . K[b,h,j,:])     (fp32)
+ * weights_in, weights_out: float [n_layers][B][H][N_max], 16-byte aligned; the same array for a running sum, or
+ * weights_in = NULL to start the sums here (all zeros).  Entries at or past len[b] are neither read nor written.
+ * The step form appends a row first, as bt_block_decode_step; the sum of the appended row starts with its weight of
+ * this step, whatever weights_in holds there.
+ * workspace: bt_workspace_bytes_weights bytes, initialised by bt_workspace_init; it may be NULL for the attn form where
+ * that equals bt_workspace_bytes and bt_decode_splits is 1.  Other arguments and errors as above.
+ */
+size_t bt_workspace_bytes_weights(const bt_config* cfg);
+bt_status bt_block_decode_attn_weights(const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q, void* out,
+                                       const float* weights_in, float* weights_out, void* workspace,
+                                       size_t workspace_bytes, uint32_t* dev_status, void* stream);
+bt_status bt_block_decode_step_weights(const bt_config* cfg, bt_block_cache* cache, int layer, const void* q,
+                                       const void* k_new, const void* v_new, void* out, const float* weights_in,
+                                       float* weights_out, void* workspace, size_t workspace_bytes, uint32_t* dev_status,
+                                       void* stream);
+
+/*
+ * Eviction.  Every sequence of the layer with len[b] >= n_trigger is cut to n_keep rows (n_trigger <= n_keep means
+ * n_keep + 1: every longer sequence); the others are left as they are.  Per head of a cut sequence the rows that stay are
+ * the first n_sinks, the last n_recent, and of the rows between the n_keep - n_sinks - n_recent with the largest `weights`
+ * (equal ones: the lowest index first; a NaN counts as lower than any number, -0 as 0).  They keep their
+ * order and move, with their weights, to rows 0 .. n_keep-1; len[b] = n_keep.  The heads of a sequence choose
+ * independently.  n_keep >= 1, 0 <= n_sinks + n_recent <= n_keep (else BT_ERR_SHAPE).
+ *   weights : float [n_layers][B][H][N_max], 16-byte aligned.
+ *   kept    : int32 [B][H][n_keep], required: the old row of every new one, or -1 throughout for a sequence that was not cut.
+ *   dst     : NULL = in place (dst_weights NULL, dst_max ignored).  Else another cache [n_layers][B][H][dst_max][hd] with
+ *             sums [n_layers][B][H][dst_max] that receives the result, rows of uncut sequences included (a prompt's
+ *             cache trimmed into a smaller one); the source is only read.  None of its arrays may overlap the
+ *             source's (BT_ERR_UNSUPPORTED where they are the same); BT_ERR_CAPACITY if a sequence that is not cut,
+ *             or n_keep rows, might not fit dst_max.
+ * Rows and sums at or past the new length keep what they held.  workspace: in place bt_workspace_bytes bytes, initialised;
+ * not used (may be NULL) with dst.  One launch.
+ */
+bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* weights, int layer, int n_keep,
+                            int n_trigger, int n_sinks, int n_recent, bt_block_cache* dst, float* dst_weights, int dst_max,
+                            int32_t* kept, void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/*
  * One block-decoder decode step of one layer driven from HOST buffers (bt_block_decode_step with
  * the copies around it, section 2.3): q_host, k_new_host,
  * v_new_host [B][H][hd] bf16 are copied to the caller's device staging buffers q_dev, k_dev,

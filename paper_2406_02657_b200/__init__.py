@@ -4,5 +4,5 @@ Importing the package loads (building first if needed) the CUDA library; there i
 CPU or framework fallback.
 """
 from .binding import *  # noqa: F401,F403
-from .binding import (BlockCache, BtError, LocalCache, alloc_workspace, bt_config, lib, make_config,  # noqa: F401
-                      status_string)
+from .binding import (BlockCache, BtError, LocalCache, alloc_workspace, alloc_workspace_shared,  # noqa: F401
+                      alloc_workspace_weights, bt_config, lib, make_config, status_string)

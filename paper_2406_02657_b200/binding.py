@@ -23,6 +23,9 @@ EXPORTS = [
     "bt_block_prefill_attn", "bt_block_decode_step_host", "bt_block_decode_attn_noalloc",
     "bt_workspace_init", "bt_block_decode_step", "bt_block_decode_step_multi", "bt_selftest_bounded_wait",
     "bt_prefix_project", "bt_block_qkv_project_append", "bt_local_qkv_project_append",
+    "bt_workspace_bytes_shared", "bt_workspace_bytes_weights", "bt_block_decode_attn_window", "bt_block_decode_step_window",
+    "bt_block_prefill_attn_window", "bt_block_decode_attn_shared", "bt_block_decode_step_shared",
+    "bt_block_decode_attn_weights", "bt_block_decode_step_weights", "bt_block_kv_evict",
 ]
 
 
@@ -77,8 +80,21 @@ def _load() -> ctypes.CDLL:
     lib.bt_prefix_project.argtypes = [cfgp, vp, vp, vp, vp, vp, vp]
     lib.bt_block_qkv_project_append.argtypes = [cfgp, ctypes.POINTER(bt_block_cache), i32, vp, i32, vp, vp, vp, vp, vp]
     lib.bt_local_qkv_project_append.argtypes = [cfgp, ctypes.POINTER(bt_local_cache), i32, vp, i32, vp, vp, i32, vp, vp, vp, vp]
+    cachep = ctypes.POINTER(bt_block_cache)
+    lib.bt_workspace_bytes_shared.argtypes = [cfgp, i32]
+    lib.bt_workspace_bytes_weights.argtypes = [cfgp]
+    lib.bt_block_decode_attn_window.argtypes = [cfgp, cachep, i32, vp, i32, i32, vp, vp, u64, vp, vp]
+    lib.bt_block_decode_step_window.argtypes = [cfgp, cachep, i32, vp, vp, vp, i32, i32, vp, vp, u64, vp, vp]
+    lib.bt_block_prefill_attn_window.argtypes = [cfgp, vp, vp, vp, i32, ctypes.c_int64, i32, i32, vp, vp, vp]
+    lib.bt_block_decode_attn_shared.argtypes = [cfgp, cachep, i32, cachep, i32, vp, vp, vp, u64, vp, vp]
+    lib.bt_block_decode_step_shared.argtypes = [cfgp, cachep, i32, cachep, i32, vp, vp, vp, vp, vp, u64, vp, vp]
+    lib.bt_block_decode_attn_weights.argtypes = [cfgp, cachep, i32, vp, vp, vp, vp, vp, u64, vp, vp]
+    lib.bt_block_decode_step_weights.argtypes = [cfgp, cachep, i32, vp, vp, vp, vp, vp, vp, vp, u64, vp, vp]
+    lib.bt_block_kv_evict.argtypes = [cfgp, cachep, vp, i32, i32, i32, i32, i32, cachep, vp, i32, vp, vp, u64, vp, vp]
     for name in EXPORTS[4:]:
         getattr(lib, name).restype = ctypes.c_int
+    for name in ("bt_workspace_bytes_shared", "bt_workspace_bytes_weights"):
+        getattr(lib, name).restype = ctypes.c_size_t
     return lib
 
 
@@ -164,6 +180,30 @@ def alloc_workspace(cfg, device="cuda"):
     ws = torch.empty((max(n, 4) + 3) // 4, dtype=torch.float32, device=device)
     bt_workspace_init(cfg, ws)
     return ws
+
+
+def bt_workspace_bytes_shared(cfg, prefix_max) -> int:
+    return _lib.bt_workspace_bytes_shared(ctypes.byref(cfg), prefix_max)
+
+
+def bt_workspace_bytes_weights(cfg) -> int:
+    return _lib.bt_workspace_bytes_weights(ctypes.byref(cfg))
+
+
+def _alloc_initialised(cfg, n, device):
+    ws = torch.empty((max(n, 4) + 3) // 4, dtype=torch.float32, device=device)
+    bt_workspace_init(cfg, ws)
+    return ws
+
+
+def alloc_workspace_shared(cfg, prefix_max, device="cuda"):
+    """A workspace for the calls over a shared prefix of up to prefix_max rows, initialised and ready."""
+    return _alloc_initialised(cfg, bt_workspace_bytes_shared(cfg, prefix_max), device)
+
+
+def alloc_workspace_weights(cfg, device="cuda"):
+    """A workspace for the decode calls that sum attention weights, initialised and ready."""
+    return _alloc_initialised(cfg, bt_workspace_bytes_weights(cfg), device)
 
 
 def bt_block_kv_append(cfg, cache: BlockCache, layer, k_new, v_new, n_new=None, dev_status=None, stream=None):
@@ -259,6 +299,76 @@ def bt_block_prefill_attn(cfg, q, k, v, out, n_blocks=None, kv_seq_stride=None, 
     kv_seq_stride = n_blocks if kv_seq_stride is None else kv_seq_stride
     _check(_lib.bt_block_prefill_attn(ctypes.byref(cfg), _ptr(q), _ptr(k), _ptr(v), n_blocks, kv_seq_stride,
                                       _ptr(out), _ptr(dev_status), _stream(stream)), "bt_block_prefill_attn")
+
+
+def _ws(workspace):
+    return (_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+
+
+def bt_block_decode_attn_window(cfg, cache: BlockCache, layer, q, window, sinks, out, workspace=None, dev_status=None, stream=None):
+    """Decode attention over the first `sinks` and the last `window` rows of each sequence."""
+    _check(_lib.bt_block_decode_attn_window(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), window, sinks, _ptr(out),
+                                            *_ws(workspace), _ptr(dev_status), _stream(stream)), "bt_block_decode_attn_window")
+
+
+def bt_block_decode_step_window(cfg, cache: BlockCache, layer, q, k_new, v_new, window, sinks, out, workspace, dev_status=None,
+                                stream=None):
+    """Append the new block's row, then attend over the first `sinks` and the last `window` rows, in one launch."""
+    _check(_lib.bt_block_decode_step_window(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(k_new), _ptr(v_new),
+                                            window, sinks, _ptr(out), *_ws(workspace), _ptr(dev_status), _stream(stream)),
+           "bt_block_decode_step_window")
+
+
+def bt_block_prefill_attn_window(cfg, q, k, v, window, sinks, out, n_blocks=None, kv_seq_stride=None, dev_status=None, stream=None):
+    """Prefill attention; position t sees rows j <= t with j > t - window or j < sinks."""
+    n_blocks = q.shape[2] if n_blocks is None else n_blocks
+    kv_seq_stride = n_blocks if kv_seq_stride is None else kv_seq_stride
+    _check(_lib.bt_block_prefill_attn_window(ctypes.byref(cfg), _ptr(q), _ptr(k), _ptr(v), n_blocks, kv_seq_stride, window, sinks,
+                                             _ptr(out), _ptr(dev_status), _stream(stream)), "bt_block_prefill_attn_window")
+
+
+def bt_block_decode_attn_shared(cfg, prefix: BlockCache, cache: BlockCache, layer, q, out, workspace, dev_status=None, stream=None):
+    """Decode attention over a prefix that all sequences share (a BlockCache of one sequence) and each one's own rows."""
+    _check(_lib.bt_block_decode_attn_shared(ctypes.byref(cfg), ctypes.byref(prefix.c), prefix.k.shape[3], ctypes.byref(cache.c),
+                                            layer, _ptr(q), _ptr(out), *_ws(workspace), _ptr(dev_status), _stream(stream)),
+           "bt_block_decode_attn_shared")
+
+
+def bt_block_decode_step_shared(cfg, prefix: BlockCache, cache: BlockCache, layer, q, k_new, v_new, out, workspace,
+                                dev_status=None, stream=None):
+    """Append the new block's row to each sequence's own cache, then bt_block_decode_attn_shared."""
+    _check(_lib.bt_block_decode_step_shared(ctypes.byref(cfg), ctypes.byref(prefix.c), prefix.k.shape[3], ctypes.byref(cache.c),
+                                            layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), *_ws(workspace),
+                                            _ptr(dev_status), _stream(stream)), "bt_block_decode_step_shared")
+
+
+def bt_block_decode_attn_weights(cfg, cache: BlockCache, layer, q, out, weights_in, weights_out, workspace=None, dev_status=None,
+                                 stream=None):
+    """Decode attention that adds each row's weight to fp32 sums [layers,B,H,N_max] (weights_in None: sums start here)."""
+    _check(_lib.bt_block_decode_attn_weights(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(out), _ptr(weights_in),
+                                             _ptr(weights_out), *_ws(workspace), _ptr(dev_status), _stream(stream)),
+           "bt_block_decode_attn_weights")
+
+
+def bt_block_decode_step_weights(cfg, cache: BlockCache, layer, q, k_new, v_new, out, weights_in, weights_out, workspace,
+                                 dev_status=None, stream=None):
+    """Append the new block's row, then bt_block_decode_attn_weights (the new row's sum starts with its weight)."""
+    _check(_lib.bt_block_decode_step_weights(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(k_new), _ptr(v_new),
+                                             _ptr(out), _ptr(weights_in), _ptr(weights_out), *_ws(workspace), _ptr(dev_status),
+                                             _stream(stream)), "bt_block_decode_step_weights")
+
+
+def bt_block_kv_evict(cfg, cache: BlockCache, weights, layer, n_keep, n_sinks, n_recent, workspace=None, n_trigger=0, dst=None,
+                      dst_weights=None, kept=None, dev_status=None, stream=None):
+    """Cut every sequence of at least n_trigger rows to n_keep: the first n_sinks, the last n_recent and those with the largest
+    sums; in place, or into the BlockCache `dst`.  Returns `kept` (allocated when not passed): int32 [B,H,n_keep]."""
+    if kept is None:
+        kept = torch.empty((cfg.batch, cfg.heads, max(n_keep, 1)), dtype=torch.int32, device=cache.k.device)
+    _check(_lib.bt_block_kv_evict(ctypes.byref(cfg), ctypes.byref(cache.c), _ptr(weights), layer, n_keep, n_trigger, n_sinks, n_recent,
+                                  None if dst is None else ctypes.byref(dst.c), _ptr(dst_weights),
+                                  0 if dst is None else dst.k.shape[3], _ptr(kept), *_ws(workspace), _ptr(dev_status),
+                                  _stream(stream)), "bt_block_kv_evict")
+    return kept
 
 
 def bt_block_decode_step_host(cfg, cache: BlockCache, layer, q_host, k_new_host, v_new_host, out_host, q_dev, k_dev,

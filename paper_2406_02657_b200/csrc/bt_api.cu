@@ -33,7 +33,8 @@ float scale_log2(const bt_config* c)
     return s * kLog2e;
 }
 
-int choose_splits(const bt_config* c)
+// `rows`: how many a query may have to read
+int choose_splits_for(const bt_config* c, int rows)
 {
     if (c->decode_splits > 0) return c->decode_splits;
     // enough work items to reach every SM several times over, each of at least 128 rows (four chunks of the
@@ -42,8 +43,8 @@ int choose_splits(const bt_config* c)
     const long long bh = (long long)c->batch * c->heads;
     const long long target = 512;
     long long s = (target + bh - 1) / bh;
-    long long by_rows = c->max_blocks / 128;
-    const long long small = c->max_blocks / 16 < 4 ? c->max_blocks / 16 : 4;
+    long long by_rows = rows / 128;
+    const long long small = rows / 16 < 4 ? rows / 16 : 4;
     if (by_rows < small) by_rows = small;
     if (by_rows < 1) by_rows = 1;
     if (s > by_rows) s = by_rows;
@@ -51,6 +52,7 @@ int choose_splits(const bt_config* c)
     if (s < 1) s = 1;
     return (int)s;
 }
+int choose_splits(const bt_config* c) { return choose_splits_for(c, c->max_blocks); }
 
 inline size_t block_layer_elems(const bt_config* c) { return (size_t)c->batch * c->heads * c->max_blocks * c->head_dim; }
 inline int local_cap(const bt_config* c) { return c->prefix_len + c->block_len; }
@@ -182,16 +184,12 @@ bt_status bt_block_kv_append(const bt_config* cfg, bt_block_cache* cache, int la
                                             k_new, v_new, n_new, dev_status, (cudaStream_t)stream));
 }
 
-// append (optional) + attention in one launch; the arguments have passed decode_validate
-static bt_status decode_launch(const bt_config* cfg, bt_block_cache* cache, int layer, const void* q, const void* k_new,
-                               const void* v_new, void* out, void* workspace, size_t workspace_bytes,
-                               uint32_t* dev_status, void* stream)
+// the arguments of the streaming decode kernel (k_new == NULL: nothing is appended)
+static void fill_decode_args(bt::DecodeArgs& a, const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q,
+                             const void* k_new, const void* v_new, void* out, void* workspace, int splits, uint32_t* dev_status)
 {
-    const int splits = choose_splits(cfg);
     const bool need_ws = splits > 1 || k_new != nullptr;
-    (void)workspace_bytes;
     bt::CacheView v = block_view(cfg, cache, layer);
-    bt::DecodeArgs a;
     a.q = q;
     a.k = v.k;
     a.v = v.v;
@@ -208,6 +206,16 @@ static bt_status decode_launch(const bt_config* cfg, bt_block_cache* cache, int 
     a.n_max = cfg->max_blocks;
     a.splits = splits;
     a.scale_log2 = scale_log2(cfg);
+}
+
+// append (optional) + attention in one launch; the arguments have passed decode_validate
+static bt_status decode_launch(const bt_config* cfg, bt_block_cache* cache, int layer, const void* q, const void* k_new,
+                               const void* v_new, void* out, void* workspace, size_t workspace_bytes,
+                               uint32_t* dev_status, void* stream)
+{
+    (void)workspace_bytes;
+    bt::DecodeArgs a;
+    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, choose_splits(cfg), dev_status);
     return cuda_status(bt::launch_block_decode(a, (cudaStream_t)stream));
 }
 
@@ -318,15 +326,15 @@ bt_status bt_token_decode_attn(const bt_config* cfg, bt_local_cache* cache, int 
     return cuda_status(bt::launch_token_decode(a, (cudaStream_t)stream));
 }
 
-bt_status bt_block_prefill_attn(const bt_config* cfg, const void* q, const void* k, const void* v, int n_blocks,
-                                int64_t kv_seq_stride, void* out, uint32_t* dev_status, void* stream)
+// the arguments of the prefill kernels, checked
+static bt_status prefill_args(bt::PrefillArgs& a, const bt_config* cfg, const void* q, const void* k, const void* v, int n_blocks,
+                              int64_t kv_seq_stride, void* out, const uint32_t* dev_status)
 {
     bt_status st = check_config(cfg, 0);
     if (st != BT_OK) return st;
     if (!q || !k || !v || !out) return BT_ERR_NULL;
     if (n_blocks <= 0 || kv_seq_stride < n_blocks) return BT_ERR_SHAPE;
     if (!al16(q) || !al16(k) || !al16(v) || !al16(out) || !al4(dev_status)) return BT_ERR_UNSUPPORTED;
-    bt::PrefillArgs a;
     a.q = q;
     a.k = k;
     a.v = v;
@@ -337,6 +345,15 @@ bt_status bt_block_prefill_attn(const bt_config* cfg, const void* q, const void*
     a.T = n_blocks;
     a.kv_seq_stride = kv_seq_stride;
     a.scale_log2 = scale_log2(cfg);
+    return BT_OK;
+}
+
+bt_status bt_block_prefill_attn(const bt_config* cfg, const void* q, const void* k, const void* v, int n_blocks,
+                                int64_t kv_seq_stride, void* out, uint32_t* dev_status, void* stream)
+{
+    bt::PrefillArgs a;
+    const bt_status st = prefill_args(a, cfg, q, k, v, n_blocks, kv_seq_stride, out, dev_status);
+    if (st != BT_OK) return st;
     // the kernel is the caller's choice, never a silent switch: the tensor-core one unless the config asks
     // for the CUDA-core one
     if (cfg->prefill_plain) return cuda_status(bt::launch_block_prefill_simple(a, (cudaStream_t)stream));
@@ -364,6 +381,235 @@ bt_status bt_block_decode_step_host(const bt_config* cfg, bt_block_cache* cache,
     if (st != BT_OK) return st;
     if (cudaMemcpyAsync(out_host, out_dev, bytes, cudaMemcpyDeviceToHost, s) != cudaSuccess) return BT_ERR_CUDA;
     return BT_OK;
+}
+
+// ---- long and shared contexts
+
+static bt_status decode_window(const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q, const void* k_new,
+                               const void* v_new, bool step, int window, int sinks, void* out, void* workspace,
+                               size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    bt_status st = decode_validate(cfg, cache, layer, q, k_new, v_new, step, out, workspace, workspace_bytes, dev_status);
+    if (st != BT_OK) return st;
+    if (window < 1 || sinks < 0) return BT_ERR_SHAPE;
+    bt::WindowDecodeArgs a;
+    a.window = window < cfg->max_blocks ? window : cfg->max_blocks;
+    a.sinks = sinks < cfg->max_blocks ? sinks : cfg->max_blocks;
+    const long long rows = (long long)a.window + a.sinks;
+    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace,
+                     choose_splits_for(cfg, rows < cfg->max_blocks ? (int)rows : cfg->max_blocks), dev_status);
+    return cuda_status(bt::launch_block_decode_window(a, (cudaStream_t)stream));
+}
+
+bt_status bt_block_decode_attn_window(const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q, int window,
+                                      int sinks, void* out, void* workspace, size_t workspace_bytes, uint32_t* dev_status,
+                                      void* stream)
+{
+    return decode_window(cfg, cache, layer, q, nullptr, nullptr, false, window, sinks, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+bt_status bt_block_decode_step_window(const bt_config* cfg, bt_block_cache* cache, int layer, const void* q, const void* k_new,
+                                      const void* v_new, int window, int sinks, void* out, void* workspace,
+                                      size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    return decode_window(cfg, cache, layer, q, k_new, v_new, true, window, sinks, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+bt_status bt_block_prefill_attn_window(const bt_config* cfg, const void* q, const void* k, const void* v, int n_blocks,
+                                       int64_t kv_seq_stride, int window, int sinks, void* out, uint32_t* dev_status, void* stream)
+{
+    bt::PrefillArgs a;
+    bt_status st = prefill_args(a, cfg, q, k, v, n_blocks, kv_seq_stride, out, dev_status);
+    if (st != BT_OK) return st;
+    if (window < 1 || sinks < 0) return BT_ERR_SHAPE;
+    if (cfg->prefill_plain || !bt::prefill_tc_supported(a)) return BT_ERR_UNSUPPORTED;
+    return cuda_status(bt::launch_block_prefill_window(a, window < n_blocks ? window : n_blocks, sinks < n_blocks ? sinks : n_blocks,
+                                                       dev_status, (cudaStream_t)stream));
+}
+
+// Parts into which the shared prefix is cut: with the heads and the tiles of 128 sequences enough CTAs for the SMs
+// (148 on a B200; the number fixes the workspace, so it does not depend on the device), each of at least 128 rows.
+static int shared_parts(const bt_config* cfg, int prefix_max)
+{
+    const long long tiles = (long long)cfg->heads * ((cfg->batch + 127) / 128);
+    long long parts = 148 / tiles;
+    const long long most = (prefix_max + 127) / 128;
+    if (parts > most) parts = most;
+    if (parts > 32) parts = 32;
+    return parts < 1 ? 1 : (int)parts;
+}
+static size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+size_t bt_workspace_bytes_shared(const bt_config* cfg, int prefix_max)
+{
+    if (check_config(cfg, 0) != BT_OK || prefix_max <= 0) return 0;
+    return align16(bt_workspace_bytes(cfg)) + (size_t)shared_parts(cfg, prefix_max) * cfg->batch * cfg->heads * (cfg->head_dim + 4) * sizeof(float);
+}
+
+static bt_status decode_shared(const bt_config* cfg, const bt_block_cache* prefix, int prefix_max, const bt_block_cache* cache,
+                               int layer, const void* q, const void* k_new, const void* v_new, bool step, void* out,
+                               void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    bt_status st = check_config(cfg, layer);
+    if (st != BT_OK) return st;
+    if (!prefix || !prefix->k || !prefix->v || !prefix->len) return BT_ERR_NULL;
+    if (prefix_max <= 0) return BT_ERR_SHAPE;
+    st = decode_validate(cfg, cache, layer, q, k_new, v_new, step, out, workspace, workspace_bytes, dev_status);
+    if (st != BT_OK) return st;
+    if (!workspace || workspace_bytes < bt_workspace_bytes_shared(cfg, prefix_max)) return BT_ERR_WORKSPACE;
+    if (!block_cache_aligned(prefix) || !al16(workspace)) return BT_ERR_UNSUPPORTED;
+    const size_t prefix_layer = (size_t)cfg->heads * prefix_max * cfg->head_dim * 2;
+    bt::SharedPrefixArgs p;
+    p.q = q;
+    p.k = (const char*)prefix->k + prefix_layer * layer;
+    p.v = (const char*)prefix->v + prefix_layer * layer;
+    p.len = prefix->len + layer;
+    p.pre = (float*)((char*)workspace + align16(bt_workspace_bytes(cfg)));
+    p.dev_status = dev_status;
+    p.B = cfg->batch;
+    p.H = cfg->heads;
+    p.hd = cfg->head_dim;
+    p.cap = prefix_max;
+    p.n_pre = shared_parts(cfg, prefix_max);
+    p.scale_log2 = scale_log2(cfg);
+    if (!bt::shared_prefix_supported(p)) return BT_ERR_UNSUPPORTED;
+    bt::SharedDecodeArgs a;
+    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, choose_splits(cfg), dev_status);
+    a.pre = p.pre;
+    a.n_pre = p.n_pre;
+    a.prefix_len = p.len;
+    const cudaError_t e = bt::launch_shared_prefix(p, (cudaStream_t)stream);
+    if (e != cudaSuccess) return cuda_status(e);
+    return cuda_status(bt::launch_block_decode_shared(a, (cudaStream_t)stream));
+}
+
+bt_status bt_block_decode_attn_shared(const bt_config* cfg, const bt_block_cache* prefix, int prefix_max, const bt_block_cache* cache,
+                                      int layer, const void* q, void* out, void* workspace, size_t workspace_bytes,
+                                      uint32_t* dev_status, void* stream)
+{
+    return decode_shared(cfg, prefix, prefix_max, cache, layer, q, nullptr, nullptr, false, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+bt_status bt_block_decode_step_shared(const bt_config* cfg, const bt_block_cache* prefix, int prefix_max, bt_block_cache* cache,
+                                      int layer, const void* q, const void* k_new, const void* v_new, void* out, void* workspace,
+                                      size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    return decode_shared(cfg, prefix, prefix_max, cache, layer, q, k_new, v_new, true, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+// Do the scores of an item stay in its warp's shared memory (else they go through the workspace)?
+static bool weights_in_smem(const bt_config* cfg) { return choose_splits(cfg) == 1 && cfg->max_blocks <= bt::kWeightsSmemRows; }
+
+size_t bt_workspace_bytes_weights(const bt_config* cfg)
+{
+    if (check_config(cfg, 0) != BT_OK) return 0;
+    if (weights_in_smem(cfg)) return bt_workspace_bytes(cfg);
+    const size_t bh = (size_t)cfg->batch * cfg->heads;
+    return align16(bt_workspace_bytes(cfg)) + bh * 16 + bh * cfg->max_blocks * sizeof(float);
+}
+
+static bt_status decode_weights(const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q, const void* k_new,
+                                const void* v_new, bool step, void* out, const float* weights_in, float* weights_out,
+                                void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    bt_status st = decode_validate(cfg, cache, layer, q, k_new, v_new, step, out, workspace, workspace_bytes, dev_status);
+    if (st != BT_OK) return st;
+    if (!weights_out) return BT_ERR_NULL;
+    if (!weights_in_smem(cfg) && (!workspace || workspace_bytes < bt_workspace_bytes_weights(cfg))) return BT_ERR_WORKSPACE;
+    if (!al16(weights_in) || !al16(weights_out) || (!weights_in_smem(cfg) && !al16(workspace))) return BT_ERR_UNSUPPORTED;
+    const size_t bh = (size_t)cfg->batch * cfg->heads, layer_sums = bh * cfg->max_blocks * layer;
+    bt::WeightsDecodeArgs a;
+    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, choose_splits(cfg), dev_status);
+    a.w_in = weights_in ? weights_in + layer_sums : nullptr;
+    a.w_out = weights_out + layer_sums;
+    a.smem_rows = 0;
+    a.info = nullptr;
+    a.scores = nullptr;
+    if (weights_in_smem(cfg)) {
+        a.smem_rows = (cfg->max_blocks + 3) & ~3;
+    } else {
+        a.info = (int4*)((char*)workspace + align16(bt_workspace_bytes(cfg)));
+        a.scores = (float*)(a.info + bh);
+    }
+    return cuda_status(bt::launch_block_decode_weights(a, (cudaStream_t)stream));
+}
+
+bt_status bt_block_decode_attn_weights(const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q, void* out,
+                                       const float* weights_in, float* weights_out, void* workspace, size_t workspace_bytes,
+                                       uint32_t* dev_status, void* stream)
+{
+    return decode_weights(cfg, cache, layer, q, nullptr, nullptr, false, out, weights_in, weights_out, workspace, workspace_bytes,
+                          dev_status, stream);
+}
+
+bt_status bt_block_decode_step_weights(const bt_config* cfg, bt_block_cache* cache, int layer, const void* q, const void* k_new,
+                                       const void* v_new, void* out, const float* weights_in, float* weights_out, void* workspace,
+                                       size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    return decode_weights(cfg, cache, layer, q, k_new, v_new, true, out, weights_in, weights_out, workspace, workspace_bytes,
+                          dev_status, stream);
+}
+
+bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* weights, int layer, int n_keep, int n_trigger,
+                            int n_sinks, int n_recent, bt_block_cache* dst, float* dst_weights, int dst_max, int32_t* kept,
+                            void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    bt_status st = check_config(cfg, layer);
+    if (st != BT_OK) return st;
+    if (!cache || !cache->k || !cache->v || !cache->len || !weights || !kept) return BT_ERR_NULL;
+    if (dst && (!dst->k || !dst->v || !dst->len || !dst_weights)) return BT_ERR_NULL;
+    if (n_keep < 1 || n_sinks < 0 || n_recent < 0 || n_trigger < 0 || n_sinks > n_keep || n_recent > n_keep - n_sinks) return BT_ERR_SHAPE;
+    if (n_trigger <= n_keep) n_trigger = n_keep + 1;
+    if (dst) {
+        if (dst_max < 1) return BT_ERR_SHAPE;
+        // the longest sequence that is left whole has to fit, and so do the rows kept
+        const int whole = n_trigger - 1 < cfg->max_blocks ? n_trigger - 1 : cfg->max_blocks;
+        const int most = n_keep < cfg->max_blocks && n_keep > whole ? n_keep : whole;
+        if (dst_max < most) return BT_ERR_CAPACITY;
+        // another cache throughout, or none: the kernel for another cache does not order its reads before its writes
+        if (dst->k == cache->k || dst->v == cache->v || dst->len == cache->len || dst_weights == weights) return BT_ERR_UNSUPPORTED;
+    } else {
+        if (dst_weights) return BT_ERR_NULL;   // sums for another cache without the cache
+        if (!workspace || workspace_bytes < bt_workspace_bytes(cfg)) return BT_ERR_WORKSPACE;
+        if (!al16(workspace)) return BT_ERR_UNSUPPORTED;
+    }
+    if (!block_cache_aligned(cache) || !al16(weights) || !al4(kept) || !al4(dev_status)) return BT_ERR_UNSUPPORTED;
+    if (dst && (!block_cache_aligned(dst) || !al16(dst_weights))) return BT_ERR_UNSUPPORTED;
+    const bt::CacheView v = block_view(cfg, cache, layer);
+    const size_t bh = (size_t)cfg->batch * cfg->heads;
+    bt::EvictArgs a;
+    a.k = v.k;
+    a.v = v.v;
+    a.w = weights + bh * cfg->max_blocks * layer;
+    a.len = v.len;
+    a.in_place = dst == nullptr;
+    if (dst) {
+        const size_t dst_layer = bh * dst_max * cfg->head_dim * 2 * layer;
+        a.dst_k = (char*)dst->k + dst_layer;
+        a.dst_v = (char*)dst->v + dst_layer;
+        a.dst_w = dst_weights + bh * dst_max * layer;
+        a.dst_len = dst->len + (size_t)layer * cfg->batch;
+        a.dst_max = dst_max;
+        a.counters = nullptr;
+    } else {
+        a.dst_k = v.k;
+        a.dst_v = v.v;
+        a.dst_w = weights + bh * cfg->max_blocks * layer;
+        a.dst_len = v.len;
+        a.dst_max = cfg->max_blocks;
+        a.counters = (int32_t*)((char*)workspace + partial_bytes(cfg)) + bh;
+    }
+    a.kept = kept;
+    a.dev_status = dev_status;
+    a.B = cfg->batch;
+    a.H = cfg->heads;
+    a.hd = cfg->head_dim;
+    a.n_max = cfg->max_blocks;
+    a.n_keep = n_keep;
+    a.trigger = n_trigger;
+    a.n_sinks = n_sinks;
+    a.n_recent = n_recent;
+    return cuda_status(bt::launch_block_kv_evict(a, (cudaStream_t)stream));
 }
 
 // ---- the linear maps either side of the attention path

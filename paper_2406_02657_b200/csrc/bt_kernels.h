@@ -51,6 +51,46 @@ struct DecodeArgs {
 // The streaming kernel: per-item results, or per-split partials merged by the split that finishes last.
 cudaError_t launch_block_decode(const DecodeArgs& a, cudaStream_t stream);
 
+// The same over rows j < sinks and j >= n - window only (splits counts parts of the visible rows).
+struct WindowDecodeArgs : DecodeArgs {
+    int window, sinks;   // window >= 1, sinks >= 0
+};
+cudaError_t launch_block_decode_window(const WindowDecodeArgs& a, cudaStream_t stream);
+
+// The same, joined with the partial results over a prefix that all sequences share (launch_shared_prefix, which has
+// to be the launch right before this one on the stream).
+struct SharedDecodeArgs : DecodeArgs {
+    const float* pre;            // [B*H][n_pre][hd+4]: normalised partials and their log2-sum-exp
+    int n_pre;
+    const int32_t* prefix_len;   // rows of the prefix (device)
+};
+cudaError_t launch_block_decode_shared(const SharedDecodeArgs& a, cudaStream_t stream);
+
+// Partial results of every sequence's query over the shared prefix.
+struct SharedPrefixArgs {
+    const void* q;               // [B][H][hd]
+    const void* k;               // [H][cap][hd]
+    const void* v;
+    const int32_t* len;          // valid rows (device)
+    float* pre;                  // [B*H][n_pre][hd+4]
+    uint32_t* dev_status;
+    int B, H, hd, cap, n_pre;
+    float scale_log2;
+};
+bool shared_prefix_supported(const SharedPrefixArgs& a);
+cudaError_t launch_shared_prefix(const SharedPrefixArgs& a, cudaStream_t stream);
+
+// The same, with 2^(score - lse) of every row added to a sum.
+struct WeightsDecodeArgs : DecodeArgs {
+    const float* w_in;   // [B*H][n_max] or NULL (zeros)
+    float* w_out;        // may be w_in
+    int smem_rows;       // rows of a warp's score buffer in shared memory (a multiple of 4, >= n_max; splits == 1), or 0:
+    float* scores;       // ... then [B*H][n_max] in the workspace
+    int4* info;          // ... and per (b,h): lse, rows, appended row or -1
+};
+constexpr int kWeightsSmemRows = 2048;   // capacity up to which a warp keeps its scores in shared memory
+cudaError_t launch_block_decode_weights(const WeightsDecodeArgs& a, cudaStream_t stream);
+
 // Decode step with m queries and m new rows per (sequence, head) (query i sees the cache and new rows 0..i).
 struct MultiDecodeArgs {
     const void* q;       // [B][H][m][hd]
@@ -67,6 +107,24 @@ struct MultiDecodeArgs {
 };
 bool multi_decode_supported(const MultiDecodeArgs& a);
 cudaError_t launch_block_decode_multi(const MultiDecodeArgs& a, cudaStream_t stream);
+
+// Keeps n_keep rows of every (sequence, head) whose sequence has at least `trigger` rows; see bt_block_kv_evict.
+struct EvictArgs {
+    const void* k;       // layer base, [B][H][n_max][hd]
+    const void* v;
+    const float* w;      // [B*H][n_max]
+    const int32_t* len;  // [B]
+    void* dst_k;         // [B][H][dst_max][hd]; the source itself when in place
+    void* dst_v;
+    float* dst_w;
+    int32_t* dst_len;
+    int32_t* kept;       // [B*H][n_keep]
+    int32_t* counters;   // [B], zero on entry and on exit (in place only)
+    uint32_t* dev_status;
+    int B, H, hd, n_max, dst_max, n_keep, trigger, n_sinks, n_recent;
+    bool in_place;
+};
+cudaError_t launch_block_kv_evict(const EvictArgs& a, cudaStream_t stream);
 
 struct TokenArgs {
     void* kv;            // layer base, [B][H][C][2][hd]
@@ -96,6 +154,8 @@ cudaError_t launch_block_prefill_simple(const PrefillArgs& a, cudaStream_t strea
 // Tensor-core kernel (TMA + tcgen05 + TMEM): needs 16-byte aligned pointers.
 bool prefill_tc_supported(const PrefillArgs& a);
 cudaError_t launch_block_prefill_tc(const PrefillArgs& a, uint32_t* dev_status, cudaStream_t stream);
+// The same kernel under a window: query t sees row j iff j <= t and (j > t - window or j < sinks).  window >= 1, sinks >= 0.
+cudaError_t launch_block_prefill_window(const PrefillArgs& a, int window, int sinks, uint32_t* dev_status, cudaStream_t stream);
 
 
 // y = W x + b on the tensor cores.  x [M][K], w [N][K] (row o = weights of output feature o), bias [N] or

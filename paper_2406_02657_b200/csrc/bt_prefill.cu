@@ -22,6 +22,14 @@
 //                     S = Q K^T into tensor memory, O += P V with P read from tensor memory (the
 //                     probabilities never visit shared memory), each in the order PV(j) S(j+2)
 // All waits are bounded in wall time: one that runs out raises BT_DEV_TIMEOUT and the CTA winds down.
+//
+// The windowed form (query t sees row j iff j <= t and (j > t - window or j < sinks)) is the same kernel compiled with
+// WINDOW: an item walks only the key/value tiles that hold a visible pair - those of the sinks, then those from the
+// first one in the window of the item's earlier query tile up to the diagonal - so the work falls from T^2 / 2 to
+// about T (window + 128).  The tiles that are past for query tile A but not yet for B are read by B alone.  On the
+// tiles at an edge of the mask each thread applies a 32-bit mask per column chunk.  Those tiles also bring V rows
+// that some of their queries must not see: a weight of 0 does not silence an infinity or a NaN there, so a query row
+// whose result is not finite is worked out again over its visible rows alone (prefill_row_plain).
 #include <cuda.h>
 
 #include <memory>
@@ -110,6 +118,23 @@ struct Params {
     long long n_items;
     float scale_log2;
 };
+struct WindowParams : Params {
+    int window, sinks;
+    const bf16* q;           // for rows that are worked out again
+    const bf16* k;
+    const bf16* v;
+    int64_t kv_seq_stride;   // rows
+};
+template <bool WINDOW>
+struct ParamsSelect {
+    using type = Params;
+};
+template <>
+struct ParamsSelect<true> {
+    using type = WindowParams;
+};
+template <bool WINDOW>
+using ParamsOf = typename ParamsSelect<WINDOW>::type;
 
 // warps 0-3: softmax warpgroup of tile A, warps 4-7: of tile B
 constexpr int kProducerWarp = 8, kMmaWarp = 9;  // warp 9 issues for tile A, warp 10 for tile B
@@ -152,20 +177,103 @@ constexpr int smem_bytes()
 
 constexpr uint32_t kTmemCols = 512;  // S_A0, S_A1, S_B0, S_B1 (64 columns each), O_A, O_B (head_dim columns each)
 
-// The class-k item of a (sequence, head) with n query tiles.
+// The class-k item of a (sequence, head) with n query tiles.  It walks `na` key/value tiles (steps of tile A; tile B takes
+// the first nb of them).  With a window the list of tiles has a gap and A leaves some out: step i of the list is
+// tile i below `ns` (tiles with sinks) and tile i - ns + lo from there on, and A skips steps skip_at .. skip_at + skip_n - 1,
+// which are past its window.
 struct Item {
     int bh, qa, qb, na, nb;  // qb = -1 and nb = 0 when the item has one tile only
+    int ns, lo, skip_at, skip_n;
 };
-__device__ __forceinline__ Item decode_item(long long item, const Params& p)
+// What class k does, whichever (sequence, head) it belongs to.
+__host__ __device__ __forceinline__ Item class_item(int k, int n_qtiles)
 {
-    Item it;
-    it.bh = (int)(item / p.n_classes);
-    const int k = (int)(item - (long long)it.bh * p.n_classes);
-    it.qa = p.n_qtiles - 1 - 2 * k;
+    Item it = {};
+    it.qa = n_qtiles - 1 - 2 * k;
     it.qb = it.qa - 1;
     it.na = 2 * it.qa + 2;
     it.nb = 2 * it.qb + 2;  // 0 when qb == -1
     return it;
+}
+__host__ __device__ __forceinline__ int first_window_tile(int qt, int window) { return qt * BM >= window ? (qt * BM - window + 1) / BN : 0; }
+__host__ __device__ __forceinline__ Item class_item_window(int k, int n_qtiles, int window, int sinks)
+{
+    Item it = class_item(k, n_qtiles);
+    const int sink_tiles = sinks / BN + (sinks % BN ? 1 : 0);
+    const int lo_a = first_window_tile(it.qa, window), lo_b = it.qb >= 0 ? first_window_tile(it.qb, window) : lo_a;
+    it.lo = lo_b;
+    it.ns = sink_tiles < lo_b ? sink_tiles : lo_b;
+    const int past = lo_b > sink_tiles ? lo_b : sink_tiles;   // first tile without sinks that B may see
+    it.skip_at = it.ns + past - lo_b;
+    it.skip_n = lo_a > past ? lo_a - past : 0;
+    it.na = it.ns + 2 * it.qa + 2 - lo_b;
+    it.nb = it.qb >= 0 ? it.na - 2 : 0;
+    return it;
+}
+template <bool WINDOW>
+__device__ __forceinline__ Item decode_item(long long item, const ParamsOf<WINDOW>& p)
+{
+    const int bh = (int)(item / p.n_classes);
+    const int k = (int)(item - (long long)bh * p.n_classes);
+    Item it;
+    if constexpr (WINDOW) it = class_item_window(k, p.n_qtiles, p.window, p.sinks);
+    else it = class_item(k, p.n_qtiles);
+    it.bh = bh;
+    return it;
+}
+template <bool WINDOW>
+__device__ __forceinline__ int list_tile(const Item& it, int i)
+{
+    if constexpr (WINDOW) return i < it.ns ? i : i - it.ns + it.lo;
+    return i;
+}
+// Step k of tile x as a step of the list, and whether tile A leaves that step of the list out.
+template <bool WINDOW>
+__device__ __forceinline__ int list_step(const Item& it, int x, int k)
+{
+    if constexpr (WINDOW) return x == 0 && k >= it.skip_at ? k + it.skip_n : k;
+    return k;
+}
+template <bool WINDOW>
+__device__ __forceinline__ bool skipped_by_a(const Item& it, int i)
+{
+    if constexpr (WINDOW) return i >= it.skip_at && i < it.skip_at + it.skip_n;
+    return false;
+}
+
+// One query row over its visible rows alone, by one warp, straight from global memory; the bf16 results go into the staged
+// output row.  For the rows that the tiled product cannot answer: see the head of the file.
+template <int HD>
+__device__ __noinline__ void prefill_row_plain(const WindowParams& p, int bh, int t, uint32_t stage, int row, int lane)
+{
+    constexpr int PER = HD / 32;   // dims of a lane: PER * lane ..
+    const bf16* qr = p.q + ((size_t)bh * p.T + t) * HD + lane * PER;
+    const bf16* kr = p.k + (size_t)bh * p.kv_seq_stride * HD + lane * PER;
+    const bf16* vr = p.v + (size_t)bh * p.kv_seq_stride * HD + lane * PER;
+    float q[PER], acc[PER], m = kNegInf, l = 0.f;
+    for (int i = 0; i < PER; ++i) {
+        q[i] = __bfloat162float(qr[i]) * p.scale_log2;
+        acc[i] = 0.f;
+    }
+    const int first = t >= p.window ? t - p.window + 1 : 0;
+    for (int j = 0; j <= t; ++j) {
+        if (j >= p.sinks && j < first) j = first;
+        float s = 0.f;
+        for (int i = 0; i < PER; ++i) s = fmaf(q[i], __bfloat162float(kr[(size_t)j * HD + i]), s);
+        s = row_sum<32>(s);
+        const float mn = s > m || s != s ? s : m;      // a NaN score makes the row NaN
+        const float cf = m == kNegInf ? 0.f : ex2(m - mn), pj = s == kNegInf ? 0.f : ex2(s - mn);
+        l = l * cf + pj;
+        if (s != kNegInf)
+            for (int i = 0; i < PER; ++i) acc[i] = acc[i] * cf + pj * __bfloat162float(vr[(size_t)j * HD + i]);
+        m = mn;
+    }
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    for (int i = 0; i < PER; ++i) {
+        const int d = lane * PER + i;
+        const __nv_bfloat16_raw o = __float2bfloat16_rn(acc[i] * inv);
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(stage + (d >> 6) * kQBoxBytes + ((((d & 63) >> 3) ^ (row & 7)) << 4) + (d & 7) * 2), "h"(o.x) : "memory");
+    }
 }
 
 // Position i of this CTA's walk over its items.
@@ -177,10 +285,10 @@ __device__ __forceinline__ bool walk_done(const Schedule& sc, const Params& p, l
 __device__ __forceinline__ long long walk_next(const Schedule& sc, long long i) { return sc.use_table ? i + 1 : i + gridDim.x; }
 __device__ __forceinline__ long long walk_item(const Schedule& sc, long long i) { return sc.use_table ? sc.order[i] : i; }
 
-template <int HD>
+template <int HD, bool WINDOW>
 __global__ void __launch_bounds__(kThreads, 1)
 block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
-                        const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapO, Params p,
+                        const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapO, ParamsOf<WINDOW> p,
                         const __grid_constant__ Schedule sched)
 {
     constexpr int NB = HD / 64;                 // TMA boxes per operand tile
@@ -227,13 +335,13 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
         asm volatile("prefetch.tensormap [%0];" ::"l"(&mapQ) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&mapK) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&mapV) : "memory");
-        const Item it = decode_item(walk_item(sched, walk_begin(sched)), p);
+        const Item it = decode_item<WINDOW>(walk_item(sched, walk_begin(sched)), p);
         for (int bx = 0; bx < NB; ++bx) {
             tma_prefetch_l2_3d(&mapQ, bx * 64, it.qa * BM, it.bh);
             if (it.nb > 0) tma_prefetch_l2_3d(&mapQ, bx * 64, it.qb * BM, it.bh);
             for (int j = 0; j < it.na && j < kKvStages; ++j) {
-                tma_prefetch_l2_3d(&mapK, bx * 64, j * BN, it.bh);
-                tma_prefetch_l2_3d(&mapV, bx * 64, j * BN, it.bh);
+                tma_prefetch_l2_3d(&mapK, bx * 64, list_tile<WINDOW>(it, j) * BN, it.bh);
+                tma_prefetch_l2_3d(&mapV, bx * 64, list_tile<WINDOW>(it, j) * BN, it.bh);
             }
         }
     }
@@ -254,7 +362,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
             bool ok = true;
             for (long long wi = walk_begin(sched); ok && !walk_done(sched, p, wi); wi = walk_next(sched, wi), ++n_done) {
                 const long long item = walk_item(sched, wi);
-                const Item it = decode_item(item, p);
+                const Item it = decode_item<WINDOW>(item, p);
                 auto load_q = [&](int buf, int qt) {
                     ok = ok && mbar_wait(bar(B_QEMPTY + buf), (q_uses[buf] & 1) ^ 1, abort_flag, p.dev_status);
                     if (!ok) return;
@@ -263,7 +371,8 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                     for (int bx = 0; bx < NB; ++bx)
                         tma_load_3d(sQ + buf * Q_TILE_BYTES + bx * kQBoxBytes, &mapQ, bar(B_QFULL + buf), bx * 64, qt * BM, it.bh);
                 };
-                auto load_kv = [&](int j) {
+                auto load_kv = [&](int i) {
+                    const int j = list_tile<WINDOW>(it, i);
                     const uint32_t st = kv_count % kKvStages, par = ((kv_count / kKvStages) & 1) ^ 1;
                     ok = ok && mbar_wait(bar(B_KEMPTY + st), par, abort_flag, p.dev_status);
                     if (!ok) return;
@@ -302,16 +411,18 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
             uint32_t q_uses[4] = {0, 0, 0, 0};
             uint32_t kv_base = 0;                 // key/value tiles consumed by earlier items
             uint32_t p_count = 0;                 // P tiles consumed so far
+            uint32_t s_base = 0;                  // steps of earlier items (even without a window, so the buffer is j & 1)
             bool ok = true;
             uint32_t n_done = 0;
             for (long long wi = walk_begin(sched); ok && !walk_done(sched, p, wi); wi = walk_next(sched, wi), ++n_done) {
                 const long long item = walk_item(sched, wi);
-                const Item it = decode_item(item, p);
+                const Item it = decode_item<WINDOW>(item, p);
                 const int qbuf = x ? qbuf_b(n_done) : qbuf_a(n_done);
-                const int steps = x ? it.nb : it.na;
+                const int steps = x ? it.nb : it.na - it.skip_n;
+                const uint32_t odd = WINDOW ? s_base & 1 : 0;   // score buffer of step 0
                 // S_x(j) = Q_x K_j^T, then the barriers that fire when it (and all before it) is done
                 auto issue_s = [&](int j) {
-                    const uint32_t kc = kv_base + j, st = kc % kKvStages;
+                    const uint32_t kc = kv_base + list_step<WINDOW>(it, x, j), st = kc % kKvStages;
                     ok = ok && wait_all(bar(B_KFULL + st), (kc / kKvStages) & 1);
                     if (ok && j == 0) {
                         ok = wait_all(bar(B_QFULL + qbuf), q_uses[qbuf] & 1);
@@ -324,7 +435,8 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                     // the next 64 head dims are one box further.
                     const uint32_t qlo = ((sQ + qbuf * Q_TILE_BYTES) >> 4) | (1u << 16);
                     const uint32_t klo = ((sK + st * KV_TILE_BYTES) >> 4) | (1u << 16);
-                    const uint32_t d_s = tmem + COL_S0 + (uint32_t)(x * 2 + (j & 1)) * BN;
+                    const uint32_t buf = (j + odd) & 1;
+                    const uint32_t d_s = tmem + COL_S0 + (uint32_t)(x * 2 + buf) * BN;
                     if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < HD / 16; ++kk) {
@@ -332,13 +444,14 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                             const uint32_t koff = (uint32_t)(((kk >> 2) * kKvBoxBytes + (kk & 3) * 32) >> 4);
                             mma_bf16(d_s, desc_words(qlo + qoff, kDescHiSw128), desc_words(klo + koff, kDescHiSw128), IDESC_S, kk > 0 ? 1u : 0u);
                         }
-                        mma_commit(bar(B_SFULL + x * 2 + (j & 1)));
+                        mma_commit(bar(B_SFULL + x * 2 + buf));
                     }
                     __syncwarp();
                 };
                 // O_x (+)= P_x(j) V_j
                 auto issue_pv = [&](int j) {
-                    const uint32_t kc = kv_base + j, st = kc % kKvStages;
+                    const int i = list_step<WINDOW>(it, x, j);
+                    const uint32_t kc = kv_base + i, st = kc % kKvStages;
                     ok = ok && wait_all(bar(B_PFULL + x * 2 + (p_count & 1)), (p_count >> 1) & 1);
                     if (!ok) return;
                     ++p_count;
@@ -346,7 +459,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                     // A = P from tensor memory: 16 kv columns = 8 packed 32-bit columns;
                     // B = V, MN-major: 16 kv rows = 2048 bytes; the next 64 head dims are one box further
                     const uint32_t vlo = ((sV + st * KV_TILE_BYTES) >> 4) | ((uint32_t)(kKvBoxBytes >> 4) << 16);
-                    const uint32_t a_p = tmem + COL_S0 + (uint32_t)(x * 2 + (j & 1)) * BN;
+                    const uint32_t a_p = tmem + COL_S0 + (uint32_t)(x * 2 + ((j + odd) & 1)) * BN;
                     if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < BN / 16; ++kk)
@@ -355,20 +468,22 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                         mma_commit(bar(B_PVDONE + x));
                         // the stage (K_j and V_j) is free after its last reader
                         mma_commit(bar(B_KEMPTY + st));
-                        if (x == 0 && j >= it.nb) mma_commit(bar(B_KEMPTY + st));  // tile B does not read this one
+                        if (x == 0 && i >= it.nb) mma_commit(bar(B_KEMPTY + st));  // tile B does not read this one
+                        if (x == 1 && skipped_by_a<WINDOW>(it, i)) mma_commit(bar(B_KEMPTY + st));  // nor tile A this one
                         if (j == steps - 1) mma_commit(bar(B_OFULL + x));
                     }
                     __syncwarp();
                 };
                 if (steps > 0) {
                     issue_s(0);
-                    issue_s(1);
+                    if (!WINDOW || steps > 1) issue_s(1);
                     for (int j = 0; ok && j < steps; ++j) {
                         issue_pv(j);
                         if (j + 2 < steps) issue_s(j + 2);
                     }
                 }
                 kv_base += it.na;
+                if (WINDOW) s_base += steps;
             }
         }
     } else {
@@ -383,15 +498,16 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
         bool ok = true;
         for (long long wi = walk_begin(sched); ok && !walk_done(sched, p, wi); wi = walk_next(sched, wi), ++n_done) {
             const long long item = walk_item(sched, wi);
-            const Item it = decode_item(item, p);
-            const int qt = x ? it.qb : it.qa, n_kv = x ? it.nb : it.na;
+            const Item it = decode_item<WINDOW>(item, p);
+            const int qt = x ? it.qb : it.qa, n_kv = x ? it.nb : it.na - it.skip_n;
             const int qbuf = x ? qbuf_b(n_done) : qbuf_a(n_done);
             if (n_kv == 0) continue;                       // single-tile item: warpgroup B has nothing to do
             float m_ref = kNegInf, l = 0.f;
             for (int j = 0; j < n_kv; ++j, ++s_count) {
-                const uint32_t buf = s_count & 1;          // = j & 1: every tile takes an even number of steps
+                const uint32_t buf = s_count & 1;          // = j & 1 without a window: every tile takes an even number of steps
                 const uint32_t s_addr = lane_base + COL_S0 + (uint32_t)(x * 2 + buf) * BN;
                 ok = mbar_wait(bar(B_SFULL + x * 2 + buf), (s_count >> 1) & 1, abort_flag, p.dev_status);
+                if (WINDOW) ok = __all_sync(0xffffffffu, ok) != 0;
                 if (!ok) break;
                 tc_fence_after();
                 // The last two key/value tiles straddle the diagonal.  Row r of the query tile sees column c of
@@ -401,17 +517,40 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                 const int dj = j - 2 * qt;                 // 0 or 1 on the diagonal tiles, negative before them
                 const int part = dj >= 0 ? wq - 2 * dj : BN / 32;
                 const int nch = part < 0 ? 0 : (part + 1 < BN / 32 ? part + 1 : BN / 32);
+                // With a window, per 32-column chunk: is any pair of this warp visible (else the chunk is left out), and if not
+                // all of them are, the columns that this thread's row sees.
+                bool any_seen[BN / 32] = {}, all_seen[BN / 32] = {};
+                uint32_t seen[BN / 32] = {};
+                if constexpr (WINDOW) {
+                    const int tile = list_tile<WINDOW>(it, list_step<WINDOW>(it, x, j));
+                    const int r_min = qt * BM + wq * 32, t = r_min + lane;
+#pragma unroll
+                    for (int c = 0; c < BN / 32; ++c) {
+                        const int c_min = tile * BN + c * 32, c_max = c_min + 31;
+                        any_seen[c] = c_min <= r_min + 31 && (c_max > r_min - p.window || c_min < p.sinks);
+                        all_seen[c] = c_max <= r_min && (c_min > r_min + 31 - p.window || c_max < p.sinks);
+                        auto low = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };   // the first n columns
+                        seen[c] = low(t - c_min + 1) & (~low(t - p.window + 1 - c_min) | low(p.sinks - c_min));
+                    }
+                }
+                auto used = [&](int c) { return WINDOW ? any_seen[c] : c < nch; };
                 uint32_t sr[BN];
 #pragma unroll
                 for (int c = 0; c < BN / 32; ++c)
-                    if (c < nch) tmem_ld32_issue(s_addr + c * 32, sr + c * 32);
+                    if (used(c)) tmem_ld32_issue(s_addr + c * 32, sr + c * 32);
                 tmem_wait_ld();
 #pragma unroll
                 for (int c = 0; c < BN / 32; ++c)
-                    if (c < nch) tmem_ld_fence32(sr + c * 32);
+                    if (used(c)) tmem_ld_fence32(sr + c * 32);
 #pragma unroll
                 for (int c = 0; c < BN / 32; ++c)
-                    if (c == part) {  // masked scores become -inf: they drop out of the maximum and exponentiate to 0
+                    if constexpr (WINDOW) {
+                        if (any_seen[c] && !all_seen[c]) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!(seen[c] >> i & 1u)) sr[c * 32 + i] = __float_as_uint(kNegInf);
+                        }
+                    } else if (c == part) {  // masked scores become -inf: they drop out of the maximum and exponentiate to 0
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (i > lane) sr[c * 32 + i] = __float_as_uint(kNegInf);
@@ -419,7 +558,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                 float mx4[4] = {kNegInf, kNegInf, kNegInf, kNegInf};  // independent chains: the maximum is latency-bound
 #pragma unroll
                 for (int c = 0; c < BN / 32; ++c)
-                    if (c < nch) {
+                    if (used(c)) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
 #pragma unroll
@@ -460,12 +599,13 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                 // P = 2^(s*scale - m_ref) as bf16 pairs over the S columns (chunk c of P lands in columns
                 // 16c .. 16c+15; every S column is already in registers).  The row sum is taken in fp32
                 // before the rounding: the rounding errors of the terms average out in the normaliser.
-                const uint64_t sc2 = pack2(p.scale_log2, p.scale_log2), nm2 = pack2(-m_ref, -m_ref);
+                const float m_use = WINDOW && m_ref == kNegInf ? 0.f : m_ref;   // a row may see nothing of its first tiles
+                const uint64_t sc2 = pack2(p.scale_log2, p.scale_log2), nm2 = pack2(-m_use, -m_use);
                 uint64_t l2a = pack2(0.f, 0.f), l2b = l2a;
 #pragma unroll
                 for (int c = 0; c < BN / 32; ++c) {
                     uint32_t packed[16];
-                    if (c < nch) {
+                    if (used(c)) {
                         // three passes over the chunk, in place, so that 32 independent exponentials are in flight
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
@@ -516,6 +656,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
             // 128-byte-swizzled box layout, then one TMA store per box; rows past T are dropped by the
             // store.  The buffer goes back to the producer once read.
             const uint32_t stage = sQ + qbuf * Q_TILE_BYTES + row * 128;
+            float worst = 0.f;   // with a window: NaN or infinite if any of the row's results is
 #pragma unroll 1
             for (int c0 = 0; c0 < HD; c0 += 64) {
                 uint32_t o[64];
@@ -529,9 +670,21 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                     float f[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[q8 * 8 + i]) * inv;
+                    if constexpr (WINDOW) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) worst = fmaf(f[i], 0.f, worst);
+                    }
                     const uint4 w = pack8(f);
                     const uint32_t dst = stage + (c0 >> 6) * kQBoxBytes + ((q8 ^ (row & 7)) << 4);
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+                }
+            }
+            if constexpr (WINDOW) {
+                uint32_t again = __ballot_sync(0xffffffffu, worst != 0.f && ok && qt * BM + row < p.T);   // NaN != 0
+                while (again) {
+                    const int who = __ffs(again) - 1, r = wq * 32 + who;
+                    prefill_row_plain<HD>(p, it.bh, qt * BM + r, sQ + qbuf * Q_TILE_BYTES + r * 128, r, lane);
+                    again &= again - 1;
                 }
             }
             tc_fence_before();
@@ -590,7 +743,7 @@ static int gcd_int(int a, int b)
 // them.  Waves of `wave` slabs are dealt one after the other, each heaviest class first, every item to the CTA
 // with the least work so far; a CTA's list keeps the order of dealing, so the slabs of a wave are in flight
 // together and find each other's K and V in the L2.
-static bool build_schedule(Schedule* sc, long long slabs, int n_qtiles, int n_classes, int grid, int hd, int T)
+static bool build_schedule(Schedule* sc, long long slabs, int n_qtiles, int n_classes, int grid, int hd, int T, int window, int sinks)
 {
     const long long n_items = slabs * n_classes;
     if (n_items > kMaxTableItems || grid > kMaxTableCtas) return false;
@@ -605,7 +758,7 @@ static bool build_schedule(Schedule* sc, long long slabs, int n_qtiles, int n_cl
     for (long long w0 = 0; w0 < slabs; w0 += wave) {
         const long long w1 = w0 + wave < slabs ? w0 + wave : slabs;
         for (int k = 0; k < n_classes; ++k) {
-            const int cost = 2 * (n_qtiles - 2 * k) + 2;
+            const int cost = window ? class_item_window(k, n_qtiles, window, sinks).na + 2 : 2 * (n_qtiles - 2 * k) + 2;
             for (long long bh = w0; bh < w1; ++bh) {
                 int best = 0;
                 for (int c = 1; c < grid; ++c)
@@ -628,13 +781,16 @@ static bool build_schedule(Schedule* sc, long long slabs, int n_qtiles, int n_cl
 // Tables are kept per shape: building one costs a few hundred microseconds.
 struct ScheduleKey {
     long long slabs;
-    int n_qtiles, grid, hd, T;
-    bool operator==(const ScheduleKey& o) const { return slabs == o.slabs && n_qtiles == o.n_qtiles && grid == o.grid && hd == o.hd && T == o.T; }
+    int n_qtiles, grid, hd, T, window, sinks;   // window = 0: none
+    bool operator==(const ScheduleKey& o) const
+    {
+        return slabs == o.slabs && n_qtiles == o.n_qtiles && grid == o.grid && hd == o.hd && T == o.T && window == o.window && sinks == o.sinks;
+    }
 };
-static void cached_schedule(Schedule* out, long long slabs, int n_qtiles, int n_classes, int grid, int hd, int T)
+static void cached_schedule(Schedule* out, long long slabs, int n_qtiles, int n_classes, int grid, int hd, int T, int window, int sinks)
 {
     static std::vector<std::pair<ScheduleKey, std::unique_ptr<Schedule>>> cache;
-    const ScheduleKey key{slabs, n_qtiles, grid, hd, T};
+    const ScheduleKey key{slabs, n_qtiles, grid, hd, T, window, sinks};
     std::lock_guard<std::mutex> lock(setup_mutex());
     for (auto& e : cache)
         if (e.first == key) {
@@ -642,27 +798,35 @@ static void cached_schedule(Schedule* out, long long slabs, int n_qtiles, int n_
             return;
         }
     std::unique_ptr<Schedule> sc(new Schedule());
-    if (!build_schedule(sc.get(), slabs, n_qtiles, n_classes, grid, hd, T)) sc->use_table = 0;
+    if (!build_schedule(sc.get(), slabs, n_qtiles, n_classes, grid, hd, T, window, sinks)) sc->use_table = 0;
     if (cache.size() >= 32) cache.erase(cache.begin());
     *out = *sc;
     cache.emplace_back(key, std::move(sc));
 }
 
-template <int HD>
-static cudaError_t launch_t(const PrefillArgs& a, uint32_t* dev_status, cudaStream_t stream)
+template <int HD, bool WINDOW>
+static cudaError_t launch_t(const PrefillArgs& a, int window, int sinks, uint32_t* dev_status, cudaStream_t stream)
 {
     static PerDeviceOnce limit_raised;
     int dev = 0, sms = 0;
     cudaError_t e = current_device(&dev, &sms);
     if (e != cudaSuccess) return e;
-    e = raise_smem_limit_once(limit_raised, dev, block_prefill_tc_kernel<HD>, smem_bytes<HD>());
+    e = raise_smem_limit_once(limit_raised, dev, block_prefill_tc_kernel<HD, WINDOW>, smem_bytes<HD>());
     if (e != cudaSuccess) return e;
     const long long slabs = (long long)a.B * a.H;
     CUtensorMap mq, mk, mv, mo;
     if (!make_map(&mq, a.q, HD, a.T, a.T, slabs, BM) || !make_map(&mk, a.k, HD, a.T, a.kv_seq_stride, slabs, BN) ||
         !make_map(&mv, a.v, HD, a.T, a.kv_seq_stride, slabs, BN) || !make_map(&mo, a.out, HD, a.T, a.T, slabs, BM))
         return cudaErrorInvalidValue;
-    Params p;
+    ParamsOf<WINDOW> p;
+    if constexpr (WINDOW) {
+        p.window = window;
+        p.sinks = sinks;
+        p.q = reinterpret_cast<const bf16*>(a.q);
+        p.k = reinterpret_cast<const bf16*>(a.k);
+        p.v = reinterpret_cast<const bf16*>(a.v);
+        p.kv_seq_stride = a.kv_seq_stride;
+    }
     p.dev_status = dev_status;
     p.T = a.T;
     p.n_qtiles = (a.T + BM - 1) / BM;
@@ -672,13 +836,13 @@ static cudaError_t launch_t(const PrefillArgs& a, uint32_t* dev_status, cudaStre
     // one persistent CTA per SM
     long long grid = p.n_items < sms ? p.n_items : sms;
     static thread_local Schedule sc;  // 8 KB: passed to the kernel by value
-    cached_schedule(&sc, slabs, p.n_qtiles, p.n_classes, (int)grid, HD, a.T);
+    cached_schedule(&sc, slabs, p.n_qtiles, p.n_classes, (int)grid, HD, a.T, WINDOW ? window : 0, WINDOW ? sinks : 0);
     if (!sc.use_table) {
         // no table: a grid size coprime to the number of classes makes every CTA cycle through all classes
         // (heavy and light items alike)
         while (grid > 1 && p.n_items > grid && gcd_int((int)grid, p.n_classes) != 1) --grid;
     }
-    return launch_pdl(block_prefill_tc_kernel<HD>, dim3((unsigned)grid), dim3(kThreads), (size_t)smem_bytes<HD>(), stream, mq, mk, mv, mo, p, sc);
+    return launch_pdl(block_prefill_tc_kernel<HD, WINDOW>, dim3((unsigned)grid), dim3(kThreads), (size_t)smem_bytes<HD>(), stream, mq, mk, mv, mo, p, sc);
 }
 
 }  // namespace pf
@@ -691,7 +855,12 @@ bool prefill_tc_supported(const PrefillArgs& a)
 
 cudaError_t launch_block_prefill_tc(const PrefillArgs& a, uint32_t* dev_status, cudaStream_t stream)
 {
-    return a.hd == 64 ? pf::launch_t<64>(a, dev_status, stream) : pf::launch_t<128>(a, dev_status, stream);
+    return a.hd == 64 ? pf::launch_t<64, false>(a, 0, 0, dev_status, stream) : pf::launch_t<128, false>(a, 0, 0, dev_status, stream);
+}
+
+cudaError_t launch_block_prefill_window(const PrefillArgs& a, int window, int sinks, uint32_t* dev_status, cudaStream_t stream)
+{
+    return a.hd == 64 ? pf::launch_t<64, true>(a, window, sinks, dev_status, stream) : pf::launch_t<128, true>(a, window, sinks, dev_status, stream);
 }
 
 }  // namespace bt
