@@ -1,14 +1,23 @@
 // bt_block_kv_evict: per (sequence, head), keep the first rows, the last rows and those with the largest summed
 // attention weights, in their order, and move them together.
 //
-// A CTA finds the threshold of its (sequence, head) by a radix select over order-preserving 32-bit keys (four passes
-// of 8 bits, histograms per warp in shared memory; sums of up to kKeyCache rows stay there as keys), turns it into the
-// list of kept rows by two ballot walks (each warp a contiguous piece of rows), and moves the rows in 16-byte pieces.
-// Ties go to the lowest index, so the result does not depend on the order of any atomic.
+// Selection works on order-preserving 32-bit keys in registers and finds the smallest key that stays.  Ties go to the lowest
+// index, so the result does not depend on the order of any atomic.
+//   A warp alone (select_rows_warp, up to 1024 rows): bisection, one bit a step from the top, each step 32 compares and
+//   a warp reduction; it ends as soon as the count is the number wanted, long before the last bit if sums are distinct.
+//   A CTA (select_rows): a radix select over digits of 12, 10 and 10 bits.  The first digit holds the exponent and three
+//   bits more: real sums crowd into few exponents, and with an 8-bit digit the lanes of a warp met in the same bins (35 us
+//   for 16384 rows; bisection with a barrier per step took as long).  Counts per warp and register,
+//   scanned, then place every row.
 //
-// In place, row i of the result comes from row list[i] >= i, and list grows: a chunk of rows is read into
-// registers, the CTA meets, and only then is it written.  What chunk c writes (rows <= its own sources) is above no
-// source of a later chunk and was read by every earlier one, so one barrier per chunk is enough.
+// Moving: rows travel in 16-byte pieces through registers.  Into another cache all pieces are independent.  In place, row
+// i of the result comes from row list[i] >= i, and list grows: a chunk is read, its readers meet, and only then is it
+// written.  What a chunk writes (rows <= its own sources) is below every source of a later chunk, so one barrier per
+// chunk is enough.
+//
+// Two shapes.  Many (sequence, head) pairs with short caches: a warp selects and moves a pair by itself, one launch, no
+// barriers.  Else a launch with a CTA per pair selects, and a second one moves with several CTAs per pair - in place, a
+// cluster of them that meets once per chunk.
 //
 // Bound by HBM: the kept rows are read and written once, the sums read once.
 #include "bt_common.cuh"
@@ -18,10 +27,12 @@
 namespace bt {
 namespace ev {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kKeyCache = 4096;   // rows whose keys stay in shared memory
+constexpr int kMoveThreads = 256;
+constexpr int kSelectThreads = 1024;
+constexpr int kKeys = 16;         // rows a thread holds in a selection round
 constexpr int kUnroll = 4;        // rows a thread moves per chunk (of K and of V each)
+constexpr int kSelectBits = 12;
+constexpr int kFusedThreads = 128, kFusedKeys = 8, kFusedBits = 10, kFusedRows = kFusedThreads * kFusedKeys;
 
 // Larger sum <=> larger key.  -0 counts as +0; a NaN is below everything.
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -31,138 +42,215 @@ __device__ __forceinline__ uint32_t key_of(float x)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-template <int HD, bool IN_PLACE>
-__global__ void __launch_bounds__(kThreads) evict_kernel(EvictArgs a, int parts)
+template <int THREADS, int BITS>
+struct SelectSmem {
+    uint32_t hist[1 << BITS];
+    uint32_t cand[THREADS];
+    uint32_t warp_sum[32];
+    uint32_t key, left, in_bin, n_cand;
+};
+
+// Writes the list of rows that stay: rows outside [lo, hi) and the `want` (< hi - lo) largest of those inside.  All
+// threads of the CTA call it; the list is complete for them after the caller's next barrier.  A thread owns KEYS
+// neighbouring rows per round of KEYS * THREADS.
+template <int THREADS, int KEYS, int BITS>
+__device__ __forceinline__ void select_rows(const float* w, int n, int lo, int hi, int want, int32_t* list, SelectSmem<THREADS, BITS>& sm)
 {
-    __shared__ uint32_t keys[kKeyCache];
-    __shared__ uint32_t hist[kWarps][256];
-    __shared__ uint32_t sel_key, sel_left;
-    __shared__ int seg_sure[kWarps], seg_eq[kWarps];
+    constexpr int ROUND = THREADS * KEYS, BINS = 1 << BITS, PER = BINS / THREADS;
+    static_assert(ROUND < 65536, "the packed counts hold 16 bits each");
+    static_assert(THREADS <= 1024 && PER * THREADS == BINS && KEYS % 4 == 0 && KEYS <= 32, "");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    pdl_launch_dependents();
-    pdl_wait();
-
-    const int bh = blockIdx.x / parts, part = blockIdx.x - bh * parts, b = bh / a.H;
-    int n = a.len[b];
-    n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
-    const bool cut = n >= a.trigger && n > a.n_keep;
-    // In place the length changes once all heads of the sequence have read it: whoever arrives last writes it.
-    if (IN_PLACE && tid == 0) {
-        int one;
-        asm volatile("and.b32 %0, %1, 0;\n\tadd.s32 %0, %0, 1;" : "=r"(one) : "r"(n));   // issued after the read above has returned
-        if (atomicAdd(a.counters + b, one) == a.H * parts - 1) {
-            a.counters[b] = 0;
-            if (cut) a.dst_len[b] = a.n_keep;
+    const bool vec = (reinterpret_cast<uintptr_t>(w) & 15) == 0;   // the same for all threads
+    uint32_t key[KEYS], in = 0;   // in: which of them compete
+    auto load = [&](int base) {
+        const int j0 = base + tid * KEYS;
+        // bits lo - j0 .. hi - j0 - 1 of the thread's rows
+        auto first = [](int x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1u; };
+        in = first(hi - j0) & ~first(lo - j0) & first(KEYS);
+#pragma unroll
+        for (int i = 0; i < KEYS; i += 4) {
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (vec && j0 + i + 3 < n) {
+                x = *reinterpret_cast<const float4*>(w + j0 + i);
+            } else {
+                if (j0 + i < n) x.x = w[j0 + i];
+                if (j0 + i + 1 < n) x.y = w[j0 + i + 1];
+                if (j0 + i + 2 < n) x.z = w[j0 + i + 2];
+                if (j0 + i + 3 < n) x.w = w[j0 + i + 3];
+            }
+            key[i] = key_of(x.x);
+            key[i + 1] = key_of(x.y);
+            key[i + 2] = key_of(x.z);
+            key[i + 3] = key_of(x.w);
         }
-    }
-    if (!IN_PLACE && tid == 0 && part == 0 && bh == b * a.H) a.dst_len[b] = cut ? a.n_keep : min(n, a.dst_max);
-
-    const int total = cut ? a.n_keep : (IN_PLACE ? 0 : min(n, a.dst_max));   // rows of the result that are written
-    const int d0 = (int)((long long)total * part / parts), d1 = (int)((long long)total * (part + 1) / parts);
-    const float* w = a.w + (size_t)bh * a.n_max;
-    int32_t* list = a.kept + (size_t)bh * a.n_keep;
-    if (!cut) {
-        for (int i = part * kThreads + tid; i < a.n_keep; i += parts * kThreads) list[i] = -1;
-    } else {
-        const int lo = a.n_sinks, hi = n - a.n_recent;            // rows that compete
-        const int want = a.n_keep - a.n_sinks - a.n_recent;       // how many of them stay: fewer than hi - lo
-        const bool cached = n <= kKeyCache;
-        auto key_at = [&](int j) { return cached ? keys[j] : key_of(w[j]); };
-        if (cached) {
-            for (int j = tid; j < n; j += kThreads) keys[j] = key_of(w[j]);
+    };
+    // exclusive sum over the threads in order; sm.warp_sum is free again after the caller's next barrier
+    auto scan = [&](uint32_t mine, uint32_t& total) {
+        uint32_t incl = mine;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += v;
         }
-        uint32_t prefix = 0, left = (uint32_t)want;               // the want-th largest key, 8 bits at a time from the top
-        if (want > 0) {
-            for (int shift = 24; shift >= 0; shift -= 8) {
-                for (int i = tid; i < kWarps * 256; i += kThreads) (&hist[0][0])[i] = 0;
-                __syncthreads();
-                for (int j = lo + tid; j < hi; j += kThreads) {
-                    const uint32_t key = key_at(j);
-                    if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[warp][(key >> shift) & 255u], 1u);
+        if (lane == 31) sm.warp_sum[warp] = incl;
+        __syncthreads();
+        const uint32_t ws = lane < THREADS / 32 ? sm.warp_sum[lane] : 0u;
+        total = __reduce_add_sync(0xffffffffu, ws);
+        return incl - mine + __reduce_add_sync(0xffffffffu, lane < warp ? ws : 0u);
+    };
+    const bool one_round = n <= ROUND;
+    if (one_round) load(0);
+    // rows with a key above `stay` stay for sure, and the first `left` of those equal to it
+    uint32_t stay = 0xffffffffu, left = (uint32_t)want, prefix = 0;
+    int shift = 32;
+    while (want > 0 && shift > 0) {   // one digit at a time from the top
+        const int bits = shift < BITS ? shift : BITS, above = shift;
+        shift -= bits;
+        for (int i = tid; i < BINS; i += THREADS) sm.hist[i] = 0;
+        if (tid == 0) sm.n_cand = 0;
+        __syncthreads();
+        for (int base = 0; base < n; base += ROUND) {
+            if (!one_round) load(base);
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const bool counts = (in >> i & 1u) && (above == 32 || (key[i] >> above) == (prefix >> above));
+                if (__any_sync(0xffffffffu, counts)) {
+                    const uint32_t digit = counts ? (key[i] >> shift) & (uint32_t)(BINS - 1) : ~0u;
+                    // a warp's run of equal digits (equal sums, often zeros) counts at once
+                    const bool run = __all_sync(0xffffffffu, digit == __shfl_sync(0xffffffffu, digit, 0));
+                    if (counts && (!run || lane == 0)) atomicAdd(&sm.hist[digit & (uint32_t)((1 << bits) - 1)], run ? 32u : 1u);
                 }
-                __syncthreads();
-                if (warp == 0) {   // lane l: bins 255 - 8 l downwards
-                    uint32_t c[8], sum = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        c[i] = 0;
-                        for (int q = 0; q < kWarps; ++q) c[i] += hist[q][255 - (lane * 8 + i)];
-                        sum += c[i];
-                    }
-                    uint32_t incl = sum;
-#pragma unroll
-                    for (int off = 1; off < 32; off <<= 1) {
-                        const uint32_t t = __shfl_up_sync(0xffffffffu, incl, off);
-                        if (lane >= off) incl += t;
-                    }
-                    uint32_t before = incl - sum;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (before < left && left <= before + c[i]) {
-                            sel_key = prefix | ((uint32_t)(255 - (lane * 8 + i)) << shift);
-                            sel_left = left - before;
-                        }
-                        before += c[i];
-                    }
-                }
-                __syncthreads();
-                prefix = sel_key;
-                left = sel_left;
             }
         }
         __syncthreads();
-        // rows above the threshold stay, and the first `left` of those equal to it
-        const int seg = ((n + 31) / 32 + kWarps - 1) / kWarps * 32, s0 = min(n, warp * seg), s1 = min(n, s0 + seg);
-        auto look = [&](int j, bool& sure, bool& eq) {
-            const bool in = j < s1, competes = in && j >= lo && j < hi;
-            const uint32_t key = competes ? key_at(j) : 0u;
-            sure = in && (!competes || (want > 0 && key > prefix));
-            eq = competes && want > 0 && key == prefix;
-        };
-        int n_sure = 0, n_eq = 0;
-        for (int j0 = s0; j0 < s1; j0 += 32) {
-            bool sure, eq;
-            look(j0 + lane, sure, eq);
-            n_sure += __popc(__ballot_sync(0xffffffffu, sure));
-            n_eq += __popc(__ballot_sync(0xffffffffu, eq));
-        }
-        if (lane == 0) {
-            seg_sure[warp] = n_sure;
-            seg_eq[warp] = n_eq;
-        }
-        __syncthreads();
-        int eq_at = 0, at = 0;
-        for (int q = 0; q < warp; ++q) {
-            at += seg_sure[q];
-            eq_at += seg_eq[q];
-        }
-        at += min(eq_at, (int)left);
-        const uint32_t below = (1u << lane) - 1u;
-        for (int j0 = s0; j0 < s1; j0 += 32) {
-            bool sure, eq;
-            look(j0 + lane, sure, eq);
-            const uint32_t eqs = __ballot_sync(0xffffffffu, eq);
-            const bool take = sure || (eq && eq_at + __popc(eqs & below) < (int)left);
-            const uint32_t taken = __ballot_sync(0xffffffffu, take);
-            const int pos = at + __popc(taken & below);
-            if (take && pos >= d0 && pos < d1) list[pos] = j0 + lane;
-            eq_at += __popc(eqs);
-            at += __popc(taken);
+        // thread t has bins BINS - 1 - t * PER, downwards
+        const int b0 = BINS - 1 - tid * PER;
+        uint32_t sum = 0, total;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) sum += sm.hist[b0 - i];
+        uint32_t before = scan(sum, total);
+        if (before < left && left <= before + sum) {    // one thread of the CTA
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t c = sm.hist[b0 - i];
+                if (left <= before + c) {
+                    sm.key = prefix | ((uint32_t)(b0 - i) << shift);
+                    sm.left = left - before;
+                    sm.in_bin = c;
+                    break;
+                }
+                before += c;
+            }
         }
         __syncthreads();
+        prefix = sm.key;
+        left = sm.left;
+        const uint32_t in_bin = sm.in_bin;
+        if (in_bin == left && prefix != 0u) {   // the bin stays whole: everything from its first key up
+            stay = prefix - 1;
+            left = 0;
+            break;
+        }
+        if (shift == 0) {
+            stay = prefix;
+        } else if (in_bin <= THREADS) {         // few enough for one key per thread: the rest bit by bit
+            for (int base = 0; base < n; base += ROUND) {
+                if (!one_round) load(base);
+#pragma unroll
+                for (int i = 0; i < KEYS; ++i)
+                    if ((in >> i & 1u) && (key[i] >> shift) == (prefix >> shift)) sm.cand[atomicAdd(&sm.n_cand, 1u)] = key[i];
+            }
+            __syncthreads();
+            const bool have = tid < (int)in_bin;
+            const uint32_t mine = have ? sm.cand[tid] : 0u;
+            uint32_t t = prefix;
+            bool exact = false;
+            for (uint32_t bit = 1u << (shift - 1); bit && !exact; bit >>= 1) {
+                const uint32_t c = (uint32_t)__syncthreads_count(have && mine >= (t | bit));
+                if (c >= left) t |= bit;
+                exact = c == left;              // the keys >= t are the ones: no need to know the smallest of them
+            }
+            stay = exact ? t - 1 : t;
+            left = exact ? 0u : left - (uint32_t)__syncthreads_count(have && mine > t);
+            break;
+        }
     }
+    uint32_t sure_before = 0, eq_before = 0;    // rows of earlier rounds
+    for (int base = 0; base < n; base += ROUND) {
+        if (!one_round) load(base);
+        const int j0 = base + tid * KEYS;
+        uint32_t sure = 0, eq = 0;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            sure |= (key[i] > stay ? 1u : 0u) << i;
+            eq |= (key[i] == stay ? 1u : 0u) << i;
+        }
+        const uint32_t exists = n - j0 >= KEYS ? (KEYS == 32 ? ~0u : (1u << (KEYS & 31)) - 1u) : n - j0 <= 0 ? 0u : (1u << (n - j0)) - 1u;
+        sure = exists & (~in | sure);
+        eq = left > 0 ? in & eq : 0u;
+        uint32_t total;
+        const uint32_t at = scan((uint32_t)__popc(sure) << 16 | (uint32_t)__popc(eq), total);
+        uint32_t eq_rank = eq_before + (at & 0xffffu), pos = sure_before + (at >> 16) + min(eq_rank, left);
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const bool e = eq >> i & 1u;
+            if ((sure >> i & 1u) || (e && eq_rank < left)) list[pos++] = j0 + i;
+            eq_rank += e ? 1u : 0u;
+        }
+        sure_before += total >> 16;
+        eq_before += total & 0xffffu;
+        if (!one_round) __syncthreads();        // the next round's scan reuses the sums
+    }
+}
 
-    // ---- move rows d0 .. d1 - 1 of the result
+struct Pair {
+    int bh, b, n;
+    bool cut;
+};
+__device__ __forceinline__ Pair pair_of(const EvictArgs& a, int bh)
+{
+    Pair p;
+    p.bh = bh;
+    p.b = bh / a.H;
+    const int n = a.len[p.b];
+    p.n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
+    p.cut = p.n >= a.trigger && p.n > a.n_keep;
+    return p;
+}
+
+// New length of the pair's sequence.  In place it changes once all heads have read the old one: whoever arrives last
+// writes it.  (One thread of one CTA per pair.)
+__device__ __forceinline__ void settle_length(const EvictArgs& a, const Pair& p)
+{
+    if (a.in_place) {
+        int one;
+        asm volatile("and.b32 %0, %1, 0;\n\tadd.s32 %0, %0, 1;" : "=r"(one) : "r"(p.n));   // issued after that read has returned
+        if (atomicAdd(a.counters + p.b, one) == a.H - 1) {
+            a.counters[p.b] = 0;
+            if (p.cut) a.dst_len[p.b] = a.n_keep;
+        }
+    } else if (p.bh == p.b * a.H) {
+        a.dst_len[p.b] = p.cut ? a.n_keep : min(p.n, a.dst_max);
+    }
+}
+
+// Moves rows d0 .. d1 - 1 of the pair's result with a group of THREADS threads (this one is `tid`).  In place, group
+// `rank` of `ctas` takes every ctas-th chunk, and `meet` is their barrier.
+template <int HD, bool IN_PLACE, int THREADS, class Meet>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const int32_t* list, int bh, bool cut, int d0, int d1, int rank, int ctas, int tid, Meet meet)
+{
     using G = RowGeo<HD>;
-    constexpr int ROWS = kThreads / G::LPR;          // rows one pass of the CTA covers
+    constexpr int ROWS = THREADS / G::LPR;      // rows one pass of the group covers
     constexpr int CHUNK = ROWS * kUnroll;
+    static_assert(CHUNK <= THREADS, "a thread carries one sum");
     const int sub = tid % G::LPR, rg = tid / G::LPR;
     const bf16* K = reinterpret_cast<const bf16*>(a.k) + (size_t)bh * a.n_max * HD + sub * 8;
     const bf16* V = reinterpret_cast<const bf16*>(a.v) + (size_t)bh * a.n_max * HD + sub * 8;
     bf16* DK = reinterpret_cast<bf16*>(a.dst_k) + (size_t)bh * a.dst_max * HD + sub * 8;
     bf16* DV = reinterpret_cast<bf16*>(a.dst_v) + (size_t)bh * a.dst_max * HD + sub * 8;
+    const float* w = a.w + (size_t)bh * a.n_max;
     float* dw = a.dst_w + (size_t)bh * a.dst_max;
-    for (int c0 = d0; c0 < d1; c0 += CHUNK) {
+    for (int r0 = d0; r0 < d1; r0 += CHUNK * ctas) {
+        const int c0 = r0 + rank * CHUNK;
         uint4 kr[kUnroll], vr[kUnroll];
         int src[kUnroll];
 #pragma unroll
@@ -171,17 +259,17 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(EvictArgs a, int parts)
             src[u] = i < d1 ? (cut ? list[i] : i) : -1;
             if (IN_PLACE && src[u] == i) src[u] = -1;   // already where it belongs
         }
+        const int wi = c0 + tid;
+        const bool has_w = tid < CHUNK && wi < d1;
+        const int wsrc = has_w ? (cut ? list[wi] : wi) : 0;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
             if (src[u] >= 0) {
                 kr[u] = *reinterpret_cast<const uint4*>(K + (size_t)src[u] * HD);
                 vr[u] = *reinterpret_cast<const uint4*>(V + (size_t)src[u] * HD);
             }
-        float wr = 0.f;
-        const int wi = c0 + tid;                         // CHUNK <= kThreads: a thread carries one sum
-        const bool has_w = tid < CHUNK && wi < d1;
-        if (has_w) wr = w[cut ? list[wi] : wi];
-        if (IN_PLACE) __syncthreads();
+        const float wr = has_w ? w[wsrc] : 0.f;
+        if (IN_PLACE) meet();
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
             if (src[u] >= 0) {
@@ -190,9 +278,70 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(EvictArgs a, int parts)
                 *reinterpret_cast<uint4*>(DV + i) = vr[u];
             }
         if (has_w) dw[wi] = wr;
-        static_assert(CHUNK <= kThreads, "one sum per thread");
     }
 }
+
+// ---- many pairs, short caches: one CTA per pair, one launch
+template <int HD, bool IN_PLACE>
+__global__ void __launch_bounds__(kFusedThreads, 1024 / kFusedThreads) evict_fused_kernel(EvictArgs a)
+{
+    __shared__ SelectSmem<kFusedThreads, kFusedBits> sm;
+    __shared__ int32_t list[kFusedRows];
+    pdl_launch_dependents();
+    pdl_wait();
+    const Pair p = pair_of(a, blockIdx.x);
+    if (threadIdx.x == 0) settle_length(a, p);
+    int32_t* kept = a.kept + (size_t)p.bh * a.n_keep;
+    if (p.cut) {
+        select_rows<kFusedThreads, kFusedKeys, kFusedBits>(a.w + (size_t)p.bh * a.n_max, p.n, a.n_sinks, p.n - a.n_recent, a.n_keep - a.n_sinks - a.n_recent, list, sm);
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.n_keep; i += kFusedThreads) kept[i] = list[i];
+    } else {
+        for (int i = threadIdx.x; i < a.n_keep; i += kFusedThreads) kept[i] = -1;
+        if (IN_PLACE) return;
+    }
+    move_rows<HD, IN_PLACE, kFusedThreads>(a, list, p.bh, p.cut, 0, p.cut ? a.n_keep : min(p.n, a.dst_max), 0, 1, threadIdx.x, [] { __syncthreads(); });
+}
+
+// ---- few pairs or long caches: select, then move
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a)
+{
+    __shared__ SelectSmem<THREADS, kSelectBits> sm;
+    pdl_launch_dependents();
+    pdl_wait();
+    const Pair p = pair_of(a, blockIdx.x);
+    if (threadIdx.x == 0) settle_length(a, p);
+    int32_t* list = a.kept + (size_t)p.bh * a.n_keep;
+    if (p.cut)
+        select_rows<THREADS, kKeys, kSelectBits>(a.w + (size_t)p.bh * a.n_max, p.n, a.n_sinks, p.n - a.n_recent, a.n_keep - a.n_sinks - a.n_recent, list, sm);
+    else
+        for (int i = threadIdx.x; i < a.n_keep; i += THREADS) list[i] = -1;
+}
+
+// parts CTAs per pair; in place they are a cluster.  The list says whether the sequence was cut (in place its length has
+// changed by now).
+template <int HD, bool IN_PLACE>
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a, int parts)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int bh = blockIdx.x / parts, part = blockIdx.x - bh * parts;
+    const int32_t* list = a.kept + (size_t)bh * a.n_keep;
+    const bool cut = list[0] >= 0;
+    if constexpr (IN_PLACE) {
+        if (!cut) return;   // the whole cluster
+        move_rows<HD, true, kMoveThreads>(a, list, bh, true, 0, a.n_keep, part, parts, threadIdx.x, [] {
+            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        });
+    } else {
+        const int total = cut ? a.n_keep : pair_of(a, bh).n;
+        const int rows = min(total, a.dst_max);
+        move_rows<HD, false, kMoveThreads>(a, list, bh, cut, (int)((long long)rows * part / parts), (int)((long long)rows * (part + 1) / parts), 0, 1, threadIdx.x, [] {});
+    }
+}
+
+constexpr int kMaxCluster = 8;
 
 template <int HD>
 static cudaError_t launch_t(const EvictArgs& a, cudaStream_t stream)
@@ -200,17 +349,40 @@ static cudaError_t launch_t(const EvictArgs& a, cudaStream_t stream)
     int dev = 0, sms = 0;
     cudaError_t e = current_device(&dev, &sms);
     if (e != cudaSuccess) return e;
-    const long long items = (long long)a.B * a.H;
-    long long parts = 1;
-    if (!a.in_place) {   // into another cache the parts of a (sequence, head) do not depend on each other
-        parts = (4ll * sms + items - 1) / items;
-        const long long most = (a.n_keep + 127) / 128;
-        if (parts > most) parts = most;
-        if (parts < 1) parts = 1;
+    const long long pairs = (long long)a.B * a.H;
+    if (pairs * kMaxCluster > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    if (pairs >= 4ll * sms && a.n_max <= kFusedRows) {
+        if (a.in_place) return launch_pdl(evict_fused_kernel<HD, true>, dim3((unsigned)pairs), dim3(kFusedThreads), 0, stream, a);
+        return launch_pdl(evict_fused_kernel<HD, false>, dim3((unsigned)pairs), dim3(kFusedThreads), 0, stream, a);
     }
-    if (items * parts > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    if (a.in_place) return launch_pdl(evict_kernel<HD, true>, dim3((unsigned)items), dim3(kThreads), 0, stream, a, 1);
-    return launch_pdl(evict_kernel<HD, false>, dim3((unsigned)(items * parts)), dim3(kThreads), 0, stream, a, (int)parts);
+    if (a.n_max <= kMoveThreads * kKeys) e = launch_pdl(evict_select_kernel<kMoveThreads>, dim3((unsigned)pairs), dim3(kMoveThreads), 0, stream, a);
+    else e = launch_pdl(evict_select_kernel<kSelectThreads>, dim3((unsigned)pairs), dim3(kSelectThreads), 0, stream, a);   // enough threads for one round
+    if (e != cudaSuccess) return e;
+    // four CTAs fit an SM; a part is at least one chunk
+    constexpr int CHUNK = kMoveThreads / RowGeo<HD>::LPR * kUnroll;
+    long long parts = 4ll * sms / pairs;
+    if (parts < 1) parts = 1;
+    const long long most = (a.n_keep + CHUNK - 1) / CHUNK;
+    if (parts > most) parts = most;
+    if (!a.in_place) {
+        if (pairs * parts > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+        return launch_pdl(evict_move_kernel<HD, false>, dim3((unsigned)(pairs * parts)), dim3(kMoveThreads), 0, stream, a, (int)parts);
+    }
+    int cluster = 1;
+    while (cluster < kMaxCluster && cluster < parts) cluster *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(pairs * cluster));
+    cfg.blockDim = dim3(kMoveThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, evict_move_kernel<HD, true>, a, cluster);
 }
 
 }  // namespace ev
