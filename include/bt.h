@@ -291,7 +291,7 @@ bt_status bt_block_prefill_attn_window(const bt_config* cfg, const void* q, cons
  * bt_block_kv_append, bt_block_qkv_project_append and the prefill calls fill under a config of batch 1 and max_blocks =
  * prefix_max.  It is only read.  Either part may be empty; both empty gives zeros and BT_DEV_EMPTY.
  * The prefix part is a dense product per head on the tensor cores (the softmax weights are rounded to bf16 where
- * they meet V, as in the prefill), the own part is bt_block_decode_attn's; two launches that overlap.  The step form
+ * they meet V, as in the prefill), the own part on the CUDA cores while the first one computes; two or three launches.  The step form
  * appends a row to the sequence's own cache first, exactly as bt_block_decode_step.
  * workspace: required, bt_workspace_bytes_shared bytes (0 on an invalid config), initialised by bt_workspace_init under the
  * same config; one call at a time.  Other arguments and errors as for bt_block_decode_attn / bt_block_decode_step.

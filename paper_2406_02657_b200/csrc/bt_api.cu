@@ -440,10 +440,24 @@ static int shared_parts(const bt_config* cfg, int prefix_max)
 }
 static size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
 
+// Parts into which a sequence's own rows are cut: one while 512 rows at most or enough (sequence, head) pairs, else enough for
+// eight CTAs on each of 148 SMs, each of at least 128 rows.
+static int shared_splits(const bt_config* cfg)
+{
+    if (cfg->decode_splits > 0) return cfg->decode_splits;
+    const long long bh = (long long)cfg->batch * cfg->heads;
+    long long s = 8 * 148 / bh;
+    const long long most = cfg->max_blocks / 128;
+    if (s > most) s = most;
+    if (s > 32) s = 32;
+    return s < 1 || cfg->max_blocks <= 512 ? 1 : (int)s;
+}
+
 size_t bt_workspace_bytes_shared(const bt_config* cfg, int prefix_max)
 {
     if (check_config(cfg, 0) != BT_OK || prefix_max <= 0) return 0;
-    return align16(bt_workspace_bytes(cfg)) + (size_t)shared_parts(cfg, prefix_max) * cfg->batch * cfg->heads * (cfg->head_dim + 4) * sizeof(float);
+    return align16(bt_workspace_bytes(cfg)) +
+           (size_t)(shared_parts(cfg, prefix_max) + shared_splits(cfg)) * cfg->batch * cfg->heads * (cfg->head_dim + 4) * sizeof(float);
 }
 
 static bt_status decode_shared(const bt_config* cfg, const bt_block_cache* prefix, int prefix_max, const bt_block_cache* cache,
@@ -459,28 +473,19 @@ static bt_status decode_shared(const bt_config* cfg, const bt_block_cache* prefi
     if (!workspace || workspace_bytes < bt_workspace_bytes_shared(cfg, prefix_max)) return BT_ERR_WORKSPACE;
     if (!block_cache_aligned(prefix) || !al16(workspace)) return BT_ERR_UNSUPPORTED;
     const size_t prefix_layer = (size_t)cfg->heads * prefix_max * cfg->head_dim * 2;
-    bt::SharedPrefixArgs p;
-    p.q = q;
-    p.k = (const char*)prefix->k + prefix_layer * layer;
-    p.v = (const char*)prefix->v + prefix_layer * layer;
-    p.len = prefix->len + layer;
-    p.pre = (float*)((char*)workspace + align16(bt_workspace_bytes(cfg)));
-    p.dev_status = dev_status;
-    p.B = cfg->batch;
-    p.H = cfg->heads;
-    p.hd = cfg->head_dim;
-    p.cap = prefix_max;
-    p.n_pre = shared_parts(cfg, prefix_max);
-    p.scale_log2 = scale_log2(cfg);
-    if (!bt::shared_prefix_supported(p)) return BT_ERR_UNSUPPORTED;
     bt::SharedDecodeArgs a;
-    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, choose_splits(cfg), dev_status);
-    a.pre = p.pre;
-    a.n_pre = p.n_pre;
-    a.prefix_len = p.len;
-    const cudaError_t e = bt::launch_shared_prefix(p, (cudaStream_t)stream);
+    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, shared_splits(cfg), dev_status);
+    a.counters = (int32_t*)((char*)workspace + partial_bytes(cfg));
+    a.pk = (const char*)prefix->k + prefix_layer * layer;
+    a.pv = (const char*)prefix->v + prefix_layer * layer;
+    a.prefix_len = prefix->len + layer;
+    a.cap = prefix_max;
+    a.parts = (float*)((char*)workspace + align16(bt_workspace_bytes(cfg)));
+    a.n_pre = shared_parts(cfg, prefix_max);
+    if (!bt::shared_decode_supported(a)) return BT_ERR_UNSUPPORTED;
+    const cudaError_t e = bt::launch_shared_prefix(a, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_status(e);
-    return cuda_status(bt::launch_block_decode_shared(a, (cudaStream_t)stream));
+    return cuda_status(bt::launch_shared_own(a, (cudaStream_t)stream));
 }
 
 bt_status bt_block_decode_attn_shared(const bt_config* cfg, const bt_block_cache* prefix, int prefix_max, const bt_block_cache* cache,

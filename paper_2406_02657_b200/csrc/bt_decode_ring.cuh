@@ -1,5 +1,5 @@
 // Block-decoder decode attention (paper section 2.3; appendix E.2), streaming form, shared by the plain decode
-// calls and by their variants (a window with sinks, a shared prefix, summed weights).  The kernel
+// calls and by their variants (a window with sinks, summed weights).  The kernel
 // is bound by how many bytes of K and V it keeps in flight, so the bytes are moved by the bulk-copy
 // engine into shared-memory rings and the warps only compute.
 //
@@ -24,9 +24,6 @@
 //   kWindow  : an item walks its VISIBLE rows - the first min(sinks, n) and the last `window` - numbered without
 //              the gap between them; a chunk that spans the gap is two copies per tensor, nothing else changes.
 //              Rows that are not visible are neither copied nor looked at, whatever they hold.
-//   kShared  : the partials of the shared prefix (another kernel's work, in the workspace) are folded in by the
-//              log-sum-exp rule where the item folds its own row groups.  The two kernels overlap: this one streams
-//              the sequences' own rows and waits for the other only when its first item is folded.
 //   kWeights : the scores of an item are kept (in shared memory when the cache is short and the range is not
 //              split, else in the workspace) until its maximum and sum are known, then 2^(s - lse) is added
 //              to the caller's sums - by the same warp, or by a second launch.
@@ -70,7 +67,7 @@ constexpr uint32_t kPollLimit = 1u << 24;  // polls of one wait before giving up
 constexpr int kSmemPerCta = 227 * 1024;     // what one CTA may have
 
 // modes of the kernel, and the argument block of each
-enum { kPlain = 0, kWindow = 1, kShared = 2, kWeights = 3 };
+enum { kPlain = 0, kWindow = 1, kWeights = 2 };
 template <int MODE>
 struct ArgsSelect {
     using type = DecodeArgs;
@@ -78,10 +75,6 @@ struct ArgsSelect {
 template <>
 struct ArgsSelect<kWindow> {
     using type = WindowDecodeArgs;
-};
-template <>
-struct ArgsSelect<kShared> {
-    using type = SharedDecodeArgs;
 };
 template <>
 struct ArgsSelect<kWeights> {
@@ -282,7 +275,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
         }
         if (lane == 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const bf16*>(a.q) + (size_t)first * HD));
     }
-    if constexpr (MODE != kShared) pdl_wait();  // nothing above wrote global memory, or used a value read from it for more than a prefetch hint
+    pdl_wait();  // nothing above wrote global memory, or used a value read from it for more than a prefetch hint
 
     // ---- producer cursor (kept by every lane, acted on by lane 0): next chunk to request
     const Step step = step_of(stride, a);
@@ -541,20 +534,6 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
             for (int i = 0; i < 8; ++i) o[i] = st.acc[i] * inv;
             *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)w.bh * HD + sub * 8) = pack8(o);
         };
-        // kShared: the partials of the shared prefix join the row groups' states
-        auto fold_prefix = [&]() {
-            if constexpr (MODE == kShared) {
-                pdl_wait();   // they are complete and visible from here on
-                for (int s2 = rg; s2 < a.n_pre; s2 += RPW) {
-                    const float* ws = a.pre + ((size_t)w.bh * a.n_pre + s2) * (HD + 4);
-                    const float lse = __ldcg(ws + HD);
-                    const float4 x = __ldcg(reinterpret_cast<const float4*>(ws + sub * 8));
-                    const float4 y = __ldcg(reinterpret_cast<const float4*>(ws + sub * 8 + 4));
-                    const float a2[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                    st.merge(lse, 1.f, a2);
-                }
-            }
-        };
         // kWeights: what turns the kept scores into weights - at once when this warp has them all, else for the second launch
         auto add_weights = [&]() {
             if constexpr (MODE == kWeights) {
@@ -569,7 +548,6 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
             }
         };
         if (a.splits == 1) {
-            fold_prefix();
             merge_row_groups();
             if (rg == 0) write_out();
             add_weights();
@@ -606,17 +584,14 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
                     const float a2[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                     st.merge(lse, 1.f, a2);
                 }
-                fold_prefix();
-                merge_row_groups();
+                    merge_row_groups();
                 if (rg == 0) write_out();
                 add_weights();
                 if (lane == 0) a.counters[w.bh] = 0;
             }
         }
         if (w.sp == 0 && cc.h == 0 && lane == 0) {
-            bool empty = w.n == 0;
-            if constexpr (MODE == kShared) empty = empty && *a.prefix_len <= 0;
-            if (empty) raise_status(a.dev_status, BT_DEV_EMPTY);
+            if (w.n == 0) raise_status(a.dev_status, BT_DEV_EMPTY);
             if (w.overflow) raise_status(a.dev_status, BT_DEV_OVERFLOW);
         }
         settle();   // the item before this one: its count has long come back
@@ -626,7 +601,6 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
         pend_overflow = w.overflow;
     }
     settle();
-    if constexpr (MODE == kShared) pdl_wait();   // whoever had no item: this kernel's end implies the other's
     if (!alive) {
         // a copy never completed: report it, give the copies still in flight one more bounded wait so
         // that none lands in shared memory after the CTA is gone, and leave

@@ -57,28 +57,20 @@ struct WindowDecodeArgs : DecodeArgs {
 };
 cudaError_t launch_block_decode_window(const WindowDecodeArgs& a, cudaStream_t stream);
 
-// The same, joined with the partial results over a prefix that all sequences share (launch_shared_prefix, which has
-// to be the launch right before this one on the stream).
-struct SharedDecodeArgs : DecodeArgs {
-    const float* pre;            // [B*H][n_pre][hd+4]: normalised partials and their log2-sum-exp
+// Decode attention over a prefix that all sequences share and over each sequence's own rows.  Three launches that overlap:
+// the prefix (launch_shared_prefix), the own rows (launch_shared_own, right behind it) - each leaves normalised partials with
+// their log2-sum-exp - and their join; with few sequences the second one joins.
+struct SharedDecodeArgs : DecodeArgs {   // counters: only for an appended row; ws unused
+    const void* pk;              // prefix, [H][cap][hd]
+    const void* pv;
+    const int32_t* prefix_len;   // its rows (device)
+    int cap;
+    float* parts;                // [B*H][n_pre + splits][hd+4]: the prefix's partials, then those of the own rows
     int n_pre;
-    const int32_t* prefix_len;   // rows of the prefix (device)
 };
-cudaError_t launch_block_decode_shared(const SharedDecodeArgs& a, cudaStream_t stream);
-
-// Partial results of every sequence's query over the shared prefix.
-struct SharedPrefixArgs {
-    const void* q;               // [B][H][hd]
-    const void* k;               // [H][cap][hd]
-    const void* v;
-    const int32_t* len;          // valid rows (device)
-    float* pre;                  // [B*H][n_pre][hd+4]
-    uint32_t* dev_status;
-    int B, H, hd, cap, n_pre;
-    float scale_log2;
-};
-bool shared_prefix_supported(const SharedPrefixArgs& a);
-cudaError_t launch_shared_prefix(const SharedPrefixArgs& a, cudaStream_t stream);
+bool shared_decode_supported(const SharedDecodeArgs& a);
+cudaError_t launch_shared_prefix(const SharedDecodeArgs& a, cudaStream_t stream);
+cudaError_t launch_shared_own(const SharedDecodeArgs& a, cudaStream_t stream);
 
 // The same, with 2^(score - lse) of every row added to a sum.
 struct WeightsDecodeArgs : DecodeArgs {

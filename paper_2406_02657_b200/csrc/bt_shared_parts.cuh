@@ -1,0 +1,76 @@
+// The partial results of a shared-prefix decode and their join: per (sequence, head) `n_pre + splits` of them - the prefix's,
+// then those of the sequence's own rows - each head_dim floats (a normalised output) and a log2-sum-exp, hd + 4 floats apart.
+// Internal to the library.
+#pragma once
+
+#include "bt_common.cuh"
+#include "bt_kernels.h"
+
+namespace bt {
+namespace parts {
+
+
+// the lane's 8 dims of partials 0 .. count-1, `stride` of them apart
+template <int HD>
+__device__ __forceinline__ void fold_partials(SoftmaxState& st, const float* ws, int count, int stride, int sub)
+{
+    // four at a time, all requested before the first is used
+    for (int i0 = 0; i0 < count; i0 += 4) {
+        float lse[4];
+        float4 x[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float* p = ws + (size_t)(i0 + i) * stride * (HD + 4);
+            const bool there = i0 + i < count;
+            lse[i] = there ? __ldcg(p + HD) : kNegInf;
+            x[i] = y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (there) {
+                x[i] = __ldcg(reinterpret_cast<const float4*>(p + sub * 8));
+                y[i] = __ldcg(reinterpret_cast<const float4*>(p + sub * 8 + 4));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float part[8] = {x[i].x, x[i].y, x[i].z, x[i].w, y[i].x, y[i].y, y[i].z, y[i].w};
+            st.merge(lse[i], 1.f, part);
+        }
+    }
+}
+
+__device__ __forceinline__ void normalised(const SoftmaxState& st, float (&o)[8])
+{
+    const float inv = st.l > 0.f ? 1.f / st.l : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = st.acc[i] * inv;
+}
+
+template <int LPR>
+__device__ __forceinline__ void merge_row_groups(SoftmaxState& st)
+{
+#pragma unroll
+    for (int off = LPR; off < 32; off <<= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, st.m, off);
+        const float l2 = __shfl_xor_sync(0xffffffffu, st.l, off);
+        float a2[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a2[i] = __shfl_xor_sync(0xffffffffu, st.acc[i], off);
+        st.merge(m2, l2, a2);
+    }
+}
+
+
+// The lane's 8 dims of the joined result of one (sequence, head).
+template <int HD>
+__device__ __forceinline__ void join(const SharedDecodeArgs& a, int bh, int sub)
+{
+    SoftmaxState st;
+    st.init();
+    const int count = a.n_pre + a.splits;
+    fold_partials<HD>(st, a.parts + (size_t)bh * count * (HD + 4), count, 1, sub);
+    float o[8];
+    normalised(st, o);
+    *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)bh * HD + sub * 8) = pack8(o);
+}
+
+}  // namespace parts
+}  // namespace bt

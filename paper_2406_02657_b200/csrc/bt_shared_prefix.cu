@@ -21,6 +21,7 @@
 #include "bt_device.h"
 #include "bt_kernels.h"
 #include "bt_mbarrier.cuh"
+#include "bt_shared_parts.cuh"
 #include "bt_tcgen05.cuh"
 #include "bt_tensor_map.h"
 
@@ -34,6 +35,10 @@ constexpr int kQBoxBytes = BM * 128, kKvBoxBytes = BN * 128;
 constexpr int kMmaWarp = 8, kKWarp = 10, kVWarp = 11;
 constexpr int kThreads = 384;
 constexpr int kStages = 2;             // of K, and of V
+// Shared memory that lets one CTA on an SM, not two: they would take turns at the SM's tensor memory while other SMs have
+// none (calls back to back: 181 vs 157 us at 512 sequences and 8000 rows of head_dim 128), and leaves room for the
+// streaming kernel's CTA beside it.
+constexpr int kSmemOnePerSm = 116 * 1024;
 constexpr uint32_t kTmemCols = 512;    // four score buffers of 64 columns, two outputs of head_dim columns
 constexpr uint32_t kSpinLimit = 1u << 26;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
@@ -55,7 +60,8 @@ enum {
 template <int HD>
 constexpr int smem_bytes()
 {
-    return 1024 + (HD / 64) * (kQBoxBytes + 2 * kStages * kKvBoxBytes) + 256;
+    const int used = 1024 + (HD / 64) * (kQBoxBytes + 2 * kStages * kKvBoxBytes) + 256;
+    return used > kSmemOnePerSm ? used : kSmemOnePerSm;
 }
 
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* dev_status)
@@ -68,7 +74,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 2)
 shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
-                     const __grid_constant__ CUtensorMap mapV, SharedPrefixArgs a, int n_qtiles)
+                     const __grid_constant__ CUtensorMap mapV, SharedDecodeArgs a, int n_qtiles)
 {
     constexpr int NB = HD / 64;
     constexpr uint32_t Q_TILE_BYTES = NB * kQBoxBytes, KV_TILE_BYTES = NB * kKvBoxBytes;
@@ -111,7 +117,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     pdl_launch_dependents();
 
     const int qt = blockIdx.x % n_qtiles, hk = blockIdx.x / n_qtiles, part = hk % a.n_pre, h = hk / a.n_pre;
-    int rows = *a.len;
+    int rows = *a.prefix_len;
     rows = rows < 0 ? 0 : (rows > a.cap ? a.cap : rows);
     const int n_tiles = (rows + BN - 1) / BN, per = (n_tiles + a.n_pre - 1) / a.n_pre;
     const int t0 = min(n_tiles, part * per), nt = min(n_tiles, t0 + per) - t0;   // this part's tiles t0 .. t0 + nt - 1
@@ -326,7 +332,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
         const float total = l * f1 + l2 * f2, inv = total > 0.f ? 1.f / total : 0.f;
         const float g1 = f1 * inv, g2 = f2 * inv;
         const int b = qt * BM + row;
-        float* dst = a.pre + (((size_t)(b < a.B ? b : 0) * a.H + h) * a.n_pre + part) * (HD + 4);
+        float* dst = a.parts + (((size_t)(b < a.B ? b : 0) * a.H + h) * (a.n_pre + a.splits) + part) * (HD + 4);
 #pragma unroll 1
         for (int c = 0; c < HALF; c += 32) {
             float o[32];
@@ -370,7 +376,7 @@ static bool make_query_map(CUtensorMap* m, const void* q, int hd, int B, int H)
 }
 
 template <int HD>
-static cudaError_t launch_t(const SharedPrefixArgs& a, cudaStream_t stream)
+static cudaError_t launch_t(const SharedDecodeArgs& a, cudaStream_t stream)
 {
     static PerDeviceOnce limit_raised;
     int dev = 0, sms = 0;
@@ -378,9 +384,14 @@ static cudaError_t launch_t(const SharedPrefixArgs& a, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     e = raise_smem_limit_once(limit_raised, dev, shared_prefix_kernel<HD>, smem_bytes<HD>());
     if (e != cudaSuccess) return e;
+    // an SM's split between L1 and shared memory cannot change while a CTA runs on it: take all of it, so that the
+    // streaming kernel's CTA still fits
+    static PerDeviceOnce carveout_set;
+    e = carveout_set.once(dev, []() { return cudaFuncSetAttribute(shared_prefix_kernel<HD>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); });
+    if (e != cudaSuccess) return e;
     CUtensorMap mq, mk, mv;
-    if (!make_query_map(&mq, a.q, HD, a.B, a.H) || !make_slab_map(&mk, a.k, HD, a.cap, a.cap, a.H, BN) ||
-        !make_slab_map(&mv, a.v, HD, a.cap, a.cap, a.H, BN))
+    if (!make_query_map(&mq, a.q, HD, a.B, a.H) || !make_slab_map(&mk, a.pk, HD, a.cap, a.cap, a.H, BN) ||
+        !make_slab_map(&mv, a.pv, HD, a.cap, a.cap, a.H, BN))
         return cudaErrorInvalidValue;
     const int n_qtiles = (a.B + BM - 1) / BM;
     const long long grid = (long long)n_qtiles * a.H * a.n_pre;
@@ -390,12 +401,12 @@ static cudaError_t launch_t(const SharedPrefixArgs& a, cudaStream_t stream)
 
 }  // namespace sp
 
-bool shared_prefix_supported(const SharedPrefixArgs& a)
+bool shared_decode_supported(const SharedDecodeArgs& a)
 {
     return (a.hd == 64 || a.hd == 128) && tensor_map_encode_fn() != nullptr;
 }
 
-cudaError_t launch_shared_prefix(const SharedPrefixArgs& a, cudaStream_t stream)
+cudaError_t launch_shared_prefix(const SharedDecodeArgs& a, cudaStream_t stream)
 {
     return a.hd == 64 ? sp::launch_t<64>(a, stream) : sp::launch_t<128>(a, stream);
 }
