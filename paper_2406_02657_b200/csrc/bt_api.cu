@@ -502,15 +502,30 @@ bt_status bt_block_decode_step_shared(const bt_config* cfg, const bt_block_cache
     return decode_shared(cfg, prefix, prefix_max, cache, layer, q, k_new, v_new, true, out, workspace, workspace_bytes, dev_status, stream);
 }
 
-// Do the scores of an item stay in its warp's shared memory (else they go through the workspace)?
-static bool weights_in_smem(const bt_config* cfg) { return choose_splits(cfg) == 1 && cfg->max_blocks <= bt::kWeightsSmemRows; }
+// Ways the row range is split when weights are summed.  Where the plain calls split, this one's workspace has room for
+// as many parts as fill the kernel's seven warps on each of 148 SMs (86.8 us at 4 x 16 heads of 16384 rows, head_dim 128, in 16
+// parts; 91.5 us in the plain calls' 8, two warps on each), each of at least 128 rows.
+static int weights_splits(const bt_config* cfg)
+{
+    const int base = choose_splits(cfg);
+    if (cfg->decode_splits > 0 || base == 1) return base;
+    const long long s = 7 * 148 / ((long long)cfg->batch * cfg->heads), most = cfg->max_blocks / 128;
+    const long long wide = s < most ? s : most;
+    return wide > base ? (wide < 64 ? (int)wide : 64) : base;
+}
 
+// Do the scores of an item stay in its warp's shared memory (else they go through the workspace)?
+static bool weights_in_smem(const bt_config* cfg) { return weights_splits(cfg) == 1 && cfg->max_blocks <= bt::kWeightsSmemRows; }
+
+// Workspace of the calls that sum weights: the plain one, and unless the scores stay in shared memory per (b,h) 16 bytes, the
+// scores (N_max floats) and the partials of the splits.
 size_t bt_workspace_bytes_weights(const bt_config* cfg)
 {
     if (check_config(cfg, 0) != BT_OK) return 0;
     if (weights_in_smem(cfg)) return bt_workspace_bytes(cfg);
     const size_t bh = (size_t)cfg->batch * cfg->heads;
-    return align16(bt_workspace_bytes(cfg)) + bh * 16 + bh * cfg->max_blocks * sizeof(float);
+    return align16(bt_workspace_bytes(cfg)) + bh * 16 + align16(bh * cfg->max_blocks * sizeof(float)) +
+           bh * weights_splits(cfg) * (cfg->head_dim + 4) * sizeof(float);
 }
 
 static bt_status decode_weights(const bt_config* cfg, const bt_block_cache* cache, int layer, const void* q, const void* k_new,
@@ -524,7 +539,7 @@ static bt_status decode_weights(const bt_config* cfg, const bt_block_cache* cach
     if (!al16(weights_in) || !al16(weights_out) || (!weights_in_smem(cfg) && !al16(workspace))) return BT_ERR_UNSUPPORTED;
     const size_t bh = (size_t)cfg->batch * cfg->heads, layer_sums = bh * cfg->max_blocks * layer;
     bt::WeightsDecodeArgs a;
-    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, choose_splits(cfg), dev_status);
+    fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, weights_splits(cfg), dev_status);
     a.w_in = weights_in ? weights_in + layer_sums : nullptr;
     a.w_out = weights_out + layer_sums;
     a.smem_rows = 0;
@@ -535,6 +550,7 @@ static bt_status decode_weights(const bt_config* cfg, const bt_block_cache* cach
     } else {
         a.info = (int4*)((char*)workspace + align16(bt_workspace_bytes(cfg)));
         a.scores = (float*)(a.info + bh);
+        a.ws = (float*)((char*)a.scores + align16(bh * cfg->max_blocks * sizeof(float)));
     }
     return cuda_status(bt::launch_block_decode_weights(a, (cudaStream_t)stream));
 }

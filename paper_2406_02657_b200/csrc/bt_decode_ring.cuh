@@ -111,6 +111,10 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr)
     return r;
 }
 
+// What one warp of a pair hands to the other: 8 accumulators a lane of row group 0, then maximum and sum.
+template <int HD>
+constexpr int kStateFloats = HD + 4;
+
 // Row range of one work item.  n counts the appended row when there is one; rows [r0, c1) come from
 // the cache, and row n-1 from the caller's buffer when new_row is set.  With a window the range counts visible
 // rows only: visible row r is cache row r below `gap_at` and r + gap from there on.
@@ -162,8 +166,8 @@ __device__ __forceinline__ void advance(Cursor& c, const Step& s, const Args& a)
     c.h -= carry_h ? a.H : 0;
     c.b += s.b + carry_h;
 }
-template <int MODE>
-__device__ __forceinline__ Work decode_work(const Cursor& c, const ArgsOf<MODE>& a)
+template <int MODE, int GROUP>
+__device__ __forceinline__ Work decode_work(const Cursor& c, const ArgsOf<MODE>& a, int member)
 {
     Work w;
     w.bh = c.bh;
@@ -189,6 +193,12 @@ __device__ __forceinline__ Work decode_work(const Cursor& c, const ArgsOf<MODE>&
     const int r1 = min(n, w.r0 + per);
     w.new_row = append && r1 == n && w.r0 < n;   // exactly one split ends at row n-1
     w.c1 = w.new_row ? r1 - 1 : r1;
+    if constexpr (GROUP > 1) {   // this warp's share of the cached rows; the appended row is the first warp's
+        const int share = ((w.c1 - w.r0 + GROUP - 1) / GROUP + 31) & ~31;
+        w.r0 = min(w.c1, w.r0 + member * share);
+        w.c1 = min(w.c1, w.r0 + share);
+        w.new_row = w.new_row && member == 0;
+    }
     return w;
 }
 
@@ -220,7 +230,7 @@ __device__ __forceinline__ void add_row_weights(const WeightsDecodeArgs& a, cons
 // output directly; otherwise each item writes its normalised partial (hd floats, then its
 // log2-sum-exp; hd+4 floats apart so that every partial is 16-byte aligned) to the workspace and the
 // last one to arrive combines them.
-template <int HD, int kStages, int MODE>
+template <int HD, int kStages, int MODE, int GROUP>
 __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsOf<MODE> a)
 {
     using G = Geo<HD>;
@@ -246,8 +256,10 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
     pdl_launch_dependents();
 
     const int n_items = a.B * a.H * a.splits;
-    const int stride = n_warps * gridDim.x;
-    const int first = warp * gridDim.x + blockIdx.x;   // neighbouring items go to different SMs
+    // GROUP neighbouring warps share an item (then the launch gives each group one item at most); usually a warp has its own
+    const int member = GROUP > 1 ? warp % GROUP : 0;
+    const int stride = n_warps / GROUP * gridDim.x;
+    const int first = warp / GROUP * gridDim.x + blockIdx.x;   // neighbouring items go to different SMs
     bf16* Kall = reinterpret_cast<bf16*>(a.k);
     bf16* Vall = reinterpret_cast<bf16*>(a.v);
     // While the kernel before this one drains, warm L2 with this warp's first item (up to kPrefetchChunks
@@ -285,7 +297,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
     Work pw = {};
     auto p_seek = [&]() {  // move to the next item that has rows
         while (pc.item < n_items) {
-            pw = decode_work<MODE>(pc, a);
+            pw = decode_work<MODE, GROUP>(pc, a, member);
             p_nchunks = (pw.c1 - pw.r0 + ROWS - 1) / ROWS;
             if (p_nchunks > 0) {
                 p_c = 0;
@@ -352,14 +364,22 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
     int pend_arrival = -1, pend_b = 0, pend_n = 0;
     bool pend_overflow = false;
     auto settle = [&]() {
-        if (pend_arrival == a.H * a.splits - 1) {
+        if (pend_arrival == a.H * a.splits * GROUP - 1) {
             // that item was the last of its sequence to read the old length: raise it
             if (!pend_overflow) a.len[pend_b] = pend_n;
             a.counters[(size_t)a.B * a.H + pend_b] = 0;
         }
     };
+    // GROUP > 1: the other warps' states reach the first one through shared memory, behind the rings and barriers
+    float* group_state = nullptr;
+    auto meet_group = [&]() {
+        if (member == 0) asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / GROUP), "n"(GROUP * 32) : "memory");
+        else asm volatile("bar.arrive %0, %1;" ::"r"(1 + warp / GROUP), "n"(GROUP * 32) : "memory");
+    };
+    if constexpr (GROUP > 1)
+        group_state = reinterpret_cast<float*>(smem + ((n_warps * kStages * (G::STAGE_BYTES + 8) + 15) & ~15)) + warp / GROUP * kStateFloats<HD>;
     for (; alive && cc.item < n_items; cc = cn, advance(cn, step, a)) {
-        const Work w = decode_work<MODE>(cc, a);
+        const Work w = decode_work<MODE, GROUP>(cc, a, member);
         // Fused append: the sequence's length goes up once all of its H * splits items have read the old
         // one.  An item counts itself in as soon as its own read has returned (the increment is computed
         // from the value read, so the count cannot be issued before that) and looks at the result only
@@ -498,7 +518,10 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
                 st.m = mn;
             }
         }
-        if (!alive) break;
+        if (!alive) {
+            if constexpr (GROUP > 1) meet_group();   // nobody is left waiting
+            break;
+        }
         if (w.new_row) {  // warp-uniform.  Row n-1 = the new row: scored from registers, stored into the cache
             const float sn = row_sum<LPR>(dot8(qf, kn));
             new_score = sn;
@@ -534,6 +557,33 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
             for (int i = 0; i < 8; ++i) o[i] = st.acc[i] * inv;
             *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)w.bh * HD + sub * 8) = pack8(o);
         };
+        if constexpr (GROUP > 1) {
+            static_assert(GROUP == 2, "one state per group");
+            merge_row_groups();
+            if (member > 0) {
+                if (rg == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) group_state[sub * 8 + i] = st.acc[i];
+                    if (sub == 0) {
+                        group_state[HD] = st.m;
+                        group_state[HD + 1] = st.l;
+                    }
+                }
+                __syncwarp();
+                meet_group();
+                pend_arrival = seq_arrival;   // settled below, as after every item
+                pend_b = w.b;
+                pend_n = w.n;
+                pend_overflow = w.overflow;
+                break;
+            }
+            meet_group();
+            float a2[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a2[i] = group_state[sub * 8 + i];
+            if (rg > 0) st.init();   // row group 0 carries the joined state on
+            else st.merge(group_state[HD], group_state[HD + 1], a2);
+        }
         // kWeights: what turns the kept scores into weights - at once when this warp has them all, else for the second launch
         auto add_weights = [&]() {
             if constexpr (MODE == kWeights) {
@@ -618,16 +668,17 @@ inline int extra_smem(const ArgsOf<MODE>& a)
     return 0;
 }
 
-template <int HD, int STAGES, int MODE>
+template <int HD, int STAGES, int MODE, int GROUP = 1>
 static cudaError_t launch_st(const ArgsOf<MODE>& a, long long grid, int warps, int dev, cudaStream_t stream)
 {
     static PerDeviceOnce limit_raised;
     // the mode with score buffers may take all an SM has; the launcher has checked that they fit
-    const int most = MODE == kWeights ? kSmemPerCta : smem_bytes<HD>(STAGES == 2 ? kMaxWarps : kMaxWarpsLong, STAGES);
-    cudaError_t e = raise_smem_limit_once(limit_raised, dev, block_decode_ring_kernel<HD, STAGES, MODE>, most);
+    const int most = MODE == kWeights || GROUP > 1 ? kSmemPerCta : smem_bytes<HD>(STAGES == 2 ? kMaxWarps : kMaxWarpsLong, STAGES);
+    cudaError_t e = raise_smem_limit_once(limit_raised, dev, block_decode_ring_kernel<HD, STAGES, MODE, GROUP>, most);
     if (e != cudaSuccess) return e;
-    const int bytes = smem_bytes<HD>(warps, STAGES) + (MODE == kWeights ? 16 + warps * extra_smem<MODE>(a) : 0);
-    return launch_pdl(block_decode_ring_kernel<HD, STAGES, MODE>, dim3((unsigned)grid), dim3(warps * 32), (size_t)bytes, stream, a);
+    const int bytes = smem_bytes<HD>(warps, STAGES) + (MODE == kWeights ? 16 + warps * extra_smem<MODE>(a) : 0) +
+                      (GROUP > 1 ? 16 + warps / GROUP * kStateFloats<HD> * 4 : 0);
+    return launch_pdl(block_decode_ring_kernel<HD, STAGES, MODE, GROUP>, dim3((unsigned)grid), dim3(warps * 32), (size_t)bytes, stream, a);
 }
 
 template <int HD, int MODE>
@@ -656,7 +707,16 @@ static cudaError_t launch_t(const ArgsOf<MODE>& a, cudaStream_t stream)
     // Short caches (the capacity bounds the rows): an item is then about a thousand instructions whatever its rows,
     // and what limits the launch is how many warps an SM has to interleave - twelve when all of them get items
     // (17.7 vs 21.6 us at 8192 items of 17 rows; at 272 rows the same, at 512 rows eight warps win).
-    if (a.n_max <= kShortCacheRows && items >= grid * kMaxWarps) warps = kMaxWarps;
+    int rows = a.n_max;
+    if constexpr (MODE == kWindow) rows = rows < a.window + a.sinks ? rows : a.window + a.sinks;
+    if (rows <= kShortCacheRows && items >= grid * kMaxWarps) warps = kMaxWarps;
+    if constexpr (MODE != kPlain) {
+        // at most four items per SM: two warps on each (101.8 -> 91.0 us at 512 items of 2056 rows, head_dim 128 - four warps
+        // cannot keep up with the stream, however deep their rings)
+        bool pair = items <= grid * 4;
+        if constexpr (MODE == kWeights) pair = pair && !a.smem_rows;
+        if (pair) return launch_st<HD, kDeepStages, MODE, 2>(a, grid, 2 * (int)((items + grid - 1) / grid), dev, stream);
+    }
     const bool shallow = items * 4 >= grid * warps * 3 || warps > kMaxWarpsLong;   // (nearly) every warp has an item: the shallow ring
     if constexpr (MODE == kWeights) {
         // score buffers beside a deep ring only where both fit

@@ -117,6 +117,27 @@ def test_window_as_wide_as_the_cache_is_the_plain_attention(bt):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("hd,H,N,window,sinks", [(64, 16, 150, 100, 4), (128, 8, 400, 37, 70), (64, 16, 20, 7, 0)])
+def test_window_decode_many_items(bt, hd, H, N, window, sinks):
+    """Several items per warp: appended rows, lengths around the window's edges, a third of the sequences checked."""
+    B = 130
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
+    k, v = rnd(21, 1, (B, H, N, hd)), rnd(21, 2, (B, H, N, hd))
+    lens = [(b * 13) % (N + 1) for b in range(B)]
+    cache = make_cache(bt, cfg, k, v, lens)
+    q, kn, vn = (rnd(22, i, (B, H, hd)) for i in range(3))
+    out, st, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), status_word(), bt.alloc_workspace(cfg)
+    bt.bt_block_decode_step_window(cfg, cache, 0, to_dev(q), to_dev(kn), to_dev(vn), window, sinks, out, ws, dev_status=st)
+    n = [min(x + 1, N) for x in lens]
+    for b in range(B):
+        if lens[b] < N:
+            k[b, :, lens[b]], v[b, :, lens[b]] = kn[b], vn[b]
+    some = list(range(0, B, 3))
+    ref, tol = ctx.decode_window(f64(q[some]), f64(k[some]), f64(v[some]), [n[b] for b in some], window, sinks)
+    check(out[some], ref, tol, "many items")
+    assert cache.len[0].tolist() == n and st.item() == (bt.BT_DEV_OVERFLOW if N in lens else 0)
+
+
 # ------------------------------------------------------------------------------------------------ window, prefill
 
 @pytest.mark.parametrize("hd", [64, 128])
