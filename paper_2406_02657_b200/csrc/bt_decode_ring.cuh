@@ -708,7 +708,7 @@ static cudaError_t launch_t(const ArgsOf<MODE>& a, cudaStream_t stream)
     // and what limits the launch is how many warps an SM has to interleave - twelve when all of them get items
     // (17.7 vs 21.6 us at 8192 items of 17 rows; at 272 rows the same, at 512 rows eight warps win).
     int rows = a.n_max;
-    if constexpr (MODE == kWindow) rows = rows < a.window + a.sinks ? rows : a.window + a.sinks;
+    if constexpr (MODE == kWindow) rows = (int)min((long long)rows, (long long)a.window + a.sinks);   // the visible ones
     if (rows <= kShortCacheRows && items >= grid * kMaxWarps) warps = kMaxWarps;
     if constexpr (MODE != kPlain) {
         // at most four items per SM: two warps on each (101.8 -> 91.0 us at 512 items of 2056 rows, head_dim 128 - four warps

@@ -437,7 +437,8 @@ def test_evict(bt, hd, into, kind, N, n_keep, trigger, sinks, recent):
 
 
 @pytest.mark.parametrize("into", ["in_place", "other"])
-@pytest.mark.parametrize("B,H,N,n_keep", [(2, 2, 9001, 4500), (1, 1, 5000, 4900), (700, 16, 96, 40)])
+@pytest.mark.parametrize("B,H,N,n_keep", [(2, 2, 9001, 4500), (1, 1, 5000, 4900), (700, 16, 96, 40), (1, 2, 40001, 17000), (1, 1, 16385, 16384),
+                                          (40, 16, 3000, 1100), (5, 4, 900, 333)])
 def test_evict_long_and_many(bt, into, B, H, N, n_keep):
     hd, sinks, recent = 64, 5, 20
     cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
@@ -562,3 +563,97 @@ def test_two_graphs_with_their_own_workspaces_on_two_streams(bt):
         for b, n in enumerate(lens):
             assert (np.abs(sums[b, :, :n] - 20 * new[b, :, :n]) <= 20 * new_tol[b, :, :n] + 20 * 20 * 2.0 ** -23 * new[b, :, :n]).all()
             assert not sums[b, :, n:].any()
+
+
+# ------------------------------------------------------------------------------------------------ nothing else is touched
+
+class Guarded:
+    """A device tensor between two guard regions of known bytes."""
+
+    SIDE, PATTERN = 4096, 0x5A
+
+    def __init__(self, shape, dtype, fill=None):
+        self.n = int(np.prod(shape)) * torch.empty((), dtype=dtype).element_size()
+        self.raw = torch.full((2 * self.SIDE + self.n + (-self.n) % 256,), self.PATTERN, dtype=torch.uint8, device="cuda")
+        self.t = self.raw[self.SIDE:self.SIDE + self.n].view(dtype).view(shape)
+        if fill is not None:
+            self.t.copy_(fill)
+        self.before = self.raw.clone()
+
+    def guards(self):
+        return bool((self.raw[:self.SIDE] == self.PATTERN).all() and (self.raw[self.SIDE + self.n:] == self.PATTERN).all())
+
+    def unchanged(self):
+        return torch.equal(self.raw, self.before)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("B,H,N,splits", [(37, 5, 97, 0), (3, 2, 700, 0), (5, 3, 130, 4), (90, 8, 33, 1)])
+def test_contexts_touch_nothing_outside_their_rows(bt, hd, B, H, N, splits):
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    bf, i32, f32 = torch.bfloat16, torch.int32, torch.float32
+    lens = torch.tensor([(b * 29) % (N + 1) for b in range(B)], dtype=i32)
+    lens[0], lens[-1] = N, 0
+    data = lambda seed, shape: gen.normal_bf16_device(30, seed, shape, device="cuda")   # noqa: E731
+    q, kn, vn, out = (Guarded((B, H, hd), bf, data(i, (B, H, hd))) for i in range(4))
+    cap, S = 90, 77
+    pk, pv = Guarded((1, 1, H, cap, hd), bf, data(5, (1, 1, H, cap, hd))), Guarded((1, 1, H, cap, hd), bf, data(6, (1, 1, H, cap, hd)))
+    plen = Guarded((1, 1), i32, torch.tensor([[S]], dtype=i32))
+    prefix = bt.BlockCache(bt.make_config(1, H, hd, 4, 1, cap, 1), k=pk.t, v=pv.t, length=plen.t)
+
+    def fresh():
+        k, v = Guarded((1, B, H, N, hd), bf, data(7, (1, B, H, N, hd))), Guarded((1, B, H, N, hd), bf, data(8, (1, B, H, N, hd)))
+        n = Guarded((1, B), i32, lens[None])
+        return k, v, n, bt.BlockCache(cfg, k=k.t, v=v.t, length=n.t)
+
+    def workspace(nbytes):
+        ws = Guarded((max(nbytes, 4) // 4,), f32)
+        bt.bt_workspace_init(cfg, ws.t)
+        return ws
+
+    at = torch.arange(N, device="cuda")
+    for call in ("window", "shared", "weights"):
+        k, v, n, cache = fresh()
+        sums = Guarded((1, B, H, N), f32, torch.ones(1, B, H, N))
+        ws = workspace({"window": bt.bt_workspace_bytes(cfg), "shared": bt.bt_workspace_bytes_shared(cfg, cap),
+                        "weights": bt.bt_workspace_bytes_weights(cfg)}[call])
+        k0, v0 = k.t.clone(), v.t.clone()
+        if call == "window":
+            bt.bt_block_decode_step_window(cfg, cache, 0, q.t, kn.t, vn.t, 20, 3, out.t, ws.t)
+        elif call == "shared":
+            bt.bt_block_decode_step_shared(cfg, prefix, cache, 0, q.t, kn.t, vn.t, out.t, ws.t)
+        else:
+            bt.bt_block_decode_step_weights(cfg, cache, 0, q.t, kn.t, vn.t, out.t, sums.t, sums.t, ws.t)
+        torch.cuda.synchronize()
+        assert all(g.guards() for g in (k, v, n, ws, out, sums)), call
+        assert all(g.unchanged() for g in (q, kn, vn, pk, pv, plen)), call
+        new = (at[None] == lens.cuda()[:, None])[:, None, :, None]            # the appended rows
+        assert torch.equal(k.t[0], torch.where(new, kn.t[:, :, None], k0[0])) and torch.equal(v.t[0], torch.where(new, vn.t[:, :, None], v0[0]))
+        assert torch.equal(n.t[0].cpu(), (lens + 1).clamp(max=N))
+        past = (at[None] >= n.t[0][:, None])[:, None].expand(-1, H, -1)
+        assert (sums.t[0][past] == 1).all()
+        assert not ws.t.view(i32)[:bt.bt_workspace_bytes(cfg) // 4][-(B * H + B):].any()   # the counters are back at zero
+    keep = max(1, N // 3)
+    for into in (False, True):
+        k, v, n, cache = fresh()
+        sums = Guarded((1, B, H, N), f32, torch.rand((1, B, H, N), device="cuda", generator=torch.Generator("cuda").manual_seed(3)))
+        kept, ws = Guarded((B, H, keep), i32), workspace(bt.bt_workspace_bytes(cfg))
+        dk, dv, dw, dn = Guarded((1, B, H, keep, hd), bf), Guarded((1, B, H, keep, hd), bf), Guarded((1, B, H, keep), f32), Guarded((1, B), i32)
+        if into:
+            dst = bt.BlockCache(bt.make_config(B, H, hd, 4, 1, keep, 1), k=dk.t, v=dv.t, length=dn.t)
+            bt.bt_block_kv_evict(cfg, cache, sums.t, 0, keep, 0, keep // 2, dst=dst, dst_weights=dw.t, kept=kept.t)
+        else:
+            bt.bt_block_kv_evict(cfg, cache, sums.t, 0, keep, 0, keep // 2, ws.t, kept=kept.t)
+        torch.cuda.synchronize()
+        assert all(g.guards() for g in (k, v, n, sums, kept, ws, dk, dv, dw, dn))
+        assert all(g.unchanged() for g in ((k, v, n, sums) if into else (dk, dv, dw, dn)))
+        assert torch.equal((dn if into else n).t[0].cpu(), lens.clamp(max=keep))
+    T = min(N, 300)
+    x, y, z, o = (Guarded((2, H, T, hd), bf, data(10 + i, (2, H, T, hd))) for i in range(4))
+    bt.bt_block_prefill_attn_window(cfg_of(bt, 2, H, hd, T), x.t, y.t, z.t, 17, 2, o.t)
+    torch.cuda.synchronize()
+    assert o.guards() and all(g.unchanged() for g in (x, y, z)) and torch.isfinite(o.t).all()
+
+
+def cfg_of(bt, B, H, hd, N):
+    return bt.make_config(B, H, hd, 4, 1, N, 1)
