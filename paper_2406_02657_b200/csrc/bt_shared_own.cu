@@ -14,6 +14,8 @@
 // Join: a CTA that waited for the prefix's partials would keep its place from the next one's rows, so with many
 // items each CTA leaves a partial of its own and a third launch folds them all by the log-sum-exp rule (272 or 528 bytes a
 // partial, from L2).  Where all CTAs fit the GPU beside the prefix kernel's, they wait and fold at once: a launch less.
+#include <type_traits>
+
 #include "bt_common.cuh"
 #include "bt_device.h"
 #include "bt_kernels.h"
@@ -38,10 +40,13 @@ __device__ __forceinline__ uint4 ld_l2(const void* p)
     return r;
 }
 
-// 16 bytes global -> shared past L1
-__device__ __forceinline__ void copy_piece(uint32_t dst, const void* src, uint64_t policy)
+// 16 bytes each of K and V, global -> shared past L1: a lane's pieces of row U * (rows per pass of a lane group) from k, v on
+template <int HD, int U>
+__device__ __forceinline__ void copy_pieces(uint32_t slots, const char* k, const char* v, uint64_t policy)
 {
-    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+    constexpr int AT = U * RowGeo<HD>::RPW * HD * 2;
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0+%3], [%1+%4], 16, %2;" ::"r"(slots), "l"(k), "l"(policy), "n"(U * 1024), "n"(AT) : "memory");
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0+%3], [%1+%4], 16, %2;" ::"r"(slots), "l"(v), "l"(policy), "n"(U * 1024 + 512), "n"(AT) : "memory");
 }
 __device__ __forceinline__ uint4 lds128(uint32_t addr)
 {
@@ -86,28 +91,38 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
     // but its own copies has to be waited for; its slot u holds its piece of K row u * RPW + rg, then V's.  A pass is requested
     // as soon as the one before it is in registers.
     const uint32_t slots = smem_u32(stages) + warp * kStageBytes + lane * 16;
+    // A whole pass - the usual one - has no comparison and no address but the first row's.
     auto request = [&](int r0) {
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int r = r0 + u * RPW + rg;
-            if (r < end) {
-                copy_piece(slots + u * 1024, K + (size_t)r * HD, policy);
-                copy_piece(slots + u * 1024 + 512, V + (size_t)r * HD, policy);
+        if (r0 < end) {
+            const char* k = reinterpret_cast<const char*>(K + (size_t)(r0 + rg) * HD);
+            const char* v = reinterpret_cast<const char*>(V + (size_t)(r0 + rg) * HD);
+            const int left = end - r0 - rg;   // rows of this lane group's column that exist from row 0 on, RPW apart
+            if (r0 + PASS <= end) {
+                copy_pieces<HD, 0>(slots, k, v, policy);
+                copy_pieces<HD, 1>(slots, k, v, policy);
+                copy_pieces<HD, 2>(slots, k, v, policy);
+                copy_pieces<HD, 3>(slots, k, v, policy);
+            } else {
+                if (left > 0) copy_pieces<HD, 0>(slots, k, v, policy);
+                if (left > RPW) copy_pieces<HD, 1>(slots, k, v, policy);
+                if (left > 2 * RPW) copy_pieces<HD, 2>(slots, k, v, policy);
+                if (left > 3 * RPW) copy_pieces<HD, 3>(slots, k, v, policy);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    int r0 = first + warp * PASS;
-    request(r0);
-    for (; r0 < end; r0 += kWarps * PASS) {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    uint64_t q2[4], acc2[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        q2[i] = pack2(qf[2 * i], qf[2 * i + 1]);
+        acc2[i] = pack2(0.f, 0.f);
+    }
+    auto one_pass = [&](int r0, auto whole) {
         uint4 kr[kUnroll], vr[kUnroll];
-        const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const bool there = r0 + u * RPW + rg < end;
-            kr[u] = there ? lds128(slots + u * 1024) : zero;
-            vr[u] = there ? lds128(slots + u * 1024 + 512) : zero;
+            kr[u] = lds128(slots + u * 1024);
+            vr[u] = lds128(slots + u * 1024 + 512);
         }
         // the pieces must be in registers, not merely requested, before their slots are written again
 #pragma unroll
@@ -116,23 +131,36 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
         float s[kUnroll], mt = kNegInf;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const float d = row_sum<LPR>(dot8(qf, kr[u]));
-            s[u] = r0 + u * RPW + rg < end ? d : kNegInf;
+            s[u] = row_sum<LPR>(dot8_x2(q2, kr[u]));
+            if (!whole && r0 + u * RPW + rg >= end) {   // no such row: its slots hold anything
+                s[u] = kNegInf;
+                vr[u] = make_uint4(0, 0, 0, 0);
+            }
             mt = fmaxf(mt, s[u]);
         }
         const float mn = fmaxf(st.m, mt), m_use = mn == kNegInf ? 0.f : mn;   // this row group may have no row yet
         const float cf = ex2(st.m - m_use);
         st.l *= cf;
+        const uint64_t cf2 = pack2(cf, cf);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) st.acc[i] *= cf;
+        for (int i = 0; i < 4; ++i) acc2[i] = fmul2(acc2[i], cf2);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const float p = ex2(s[u] - m_use);
             st.l += p;
-            fma8(st.acc, p, vr[u]);
+            fma8_x2(acc2, p, vr[u]);
         }
         st.m = mn;
+    };
+    int r0 = first + warp * PASS;
+    request(r0);
+    for (; r0 < end; r0 += kWarps * PASS) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (r0 + PASS <= end) one_pass(r0, std::true_type());
+        else one_pass(r0, std::false_type());
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(acc2[i], st.acc[2 * i], st.acc[2 * i + 1]);
     merge_row_groups<LPR>(st);
     if (warp > 0 && rg == 0) {
         float* mine = sm_state[warp - 1];
