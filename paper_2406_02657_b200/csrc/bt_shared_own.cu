@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
             const float lse = st.l > 0.f ? st.m + log2f(st.l) : kNegInf;
             st.init();
             const float* all = a.parts + (size_t)bh * count * (HD + 4);
-            if (rg < a.n_pre) fold_partials<HD>(st, all + (size_t)rg * (HD + 4), (a.n_pre - rg + RPW - 1) / RPW, RPW, sub);
+            if (rg < a.n_pre) fold_partials<HD, 4>(st, all + (size_t)rg * (HD + 4), (a.n_pre - rg + RPW - 1) / RPW, RPW, sub);
             if (rg == RPW - 1) st.merge(lse, 1.f, o);
             merge_row_groups<LPR>(st);
             normalised(st, o);

@@ -11,15 +11,15 @@ namespace parts {
 
 
 // the lane's 8 dims of partials 0 .. count-1, `stride` of them apart
-template <int HD>
+template <int HD, int WIDE>
 __device__ __forceinline__ void fold_partials(SoftmaxState& st, const float* ws, int count, int stride, int sub)
 {
-    // four at a time, all requested before the first is used
-    for (int i0 = 0; i0 < count; i0 += 4) {
-        float lse[4];
-        float4 x[4], y[4];
+    // WIDE at a time, all requested before the first is used
+    for (int i0 = 0; i0 < count; i0 += WIDE) {
+        float lse[WIDE];
+        float4 x[WIDE], y[WIDE];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < WIDE; ++i) {
             const float* p = ws + (size_t)(i0 + i) * stride * (HD + 4);
             const bool there = i0 + i < count;
             lse[i] = there ? __ldcg(p + HD) : kNegInf;
@@ -30,7 +30,7 @@ __device__ __forceinline__ void fold_partials(SoftmaxState& st, const float* ws,
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < WIDE; ++i) {
             const float part[8] = {x[i].x, x[i].y, x[i].z, x[i].w, y[i].x, y[i].y, y[i].z, y[i].w};
             st.merge(lse[i], 1.f, part);
         }
@@ -66,7 +66,9 @@ __device__ __forceinline__ void join(const SharedDecodeArgs& a, int bh, int sub)
     SoftmaxState st;
     st.init();
     const int count = a.n_pre + a.splits;
-    fold_partials<HD>(st, a.parts + (size_t)bh * count * (HD + 4), count, 1, sub);
+    const float* ws = a.parts + (size_t)bh * count * (HD + 4);
+    if (count <= 4) fold_partials<HD, 4>(st, ws, count, 1, sub);
+    else fold_partials<HD, 8>(st, ws, count, 1, sub);
     float o[8];
     normalised(st, o);
     *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)bh * HD + sub * 8) = pack8(o);
