@@ -5,11 +5,12 @@
 // 4 x (256 / head_dim) rows and meet once, at the end, through shared memory.  The kernel starts while the prefix kernel
 // computes (see the wait there) and streams meanwhile, so it is built to fit beside one of that kernel's CTAs: 64 registers
 // a thread and 17 KB of shared memory leave room for four CTAs there and for eight on an SM of their own.  What bounds it
-// is bytes in flight, 4 KB a warp in single-buffered slots: two slots a warp and six CTAs ran no faster (134 against
-// 130 us at 512 sequences of up to 256 rows behind 8000 shared ones, 16 heads of 128; 32.3 against 30.2 us at 256 of up to
-// 128 rows behind 2041, heads of 64), and neither did a persistent form with requests running ahead (159 and 32.5 us: twelve
-// warps beside the prefix kernel cannot keep enough in flight) nor the ring of the plain decode calls (145 and 29.9 us,
-// its CTAs need an SM each, so the two kernels follow each other).
+// is bytes in flight, 4 KB a warp in single-buffered slots, and for items of a few dozen rows the instructions around
+// them (issue slots 64 % busy).  The whole call, at 512 sequences of up to 256 rows behind 8000 shared ones, 16 heads of 128,
+// and at 256 of up to 128 rows behind 2041, heads of 64: 125 and 28.4 us.  On the way there: two slots a warp and six CTAs an SM
+// 134 against 130 and 32.3 against 30.2 us; a persistent form with requests running ahead 159 and 32.5 us (twelve warps
+// beside the prefix kernel cannot keep enough in flight); the ring of the plain decode calls 145 and 29.9 us (its CTAs need an
+// SM each, so the two kernels follow each other).
 //
 // Join: a CTA that waited for the prefix's partials would keep its place from the next one's rows, so with many
 // items each CTA leaves a partial of its own and a third launch folds them all by the log-sum-exp rule (272 or 528 bytes a

@@ -2,19 +2,23 @@
 // is a dense product.  Per head the B queries of the batch form a [B x hd] matrix against the S prefix rows, so the
 // prefix is read once per 128 sequences instead of once per sequence, and scores and weighted sums run on the
 // 5th-generation tensor cores.  The result is a partial softmax state per (sequence, head, part of the prefix) -
-// normalised output and log2-sum-exp, fp32 - which the streaming kernel folds into the sequence's own rows.
+// normalised output and log2-sum-exp, fp32 - which is joined with those of the sequence's own rows (bt_shared_own.cu).
 //
 // One CTA per (head, part, tile of 128 sequences).  The part's 64-row key/value tiles alternate between two softmax
 // warpgroups, each with two score buffers and an output accumulator of its own in tensor memory; the two states meet
 // through shared memory at the end.  Roles:
 //   warps 0-3 / 4-7 : softmax over the even / odd tiles; a thread owns one query row (= one TMEM lane).  The scores
 //                     are read twice from tensor memory, 32 columns at a time (once for the maximum, once for the
-//                     exponentials), which keeps the kernel at 80 registers a thread, so that the streaming
-//                     kernel's CTAs fit beside it and both run at the same time.
+//                     exponentials), which keeps the kernel at 80 registers a thread, so that four CTAs of the
+//                     own-rows kernel fit beside it and both run at the same time.
 //   warps 8, 9      : tcgen05.mma issuers of the two warpgroups (S = Q K^T; O += P V with P read from tensor memory)
 //   warps 10, 11    : TMA producers of Q and K, and of V (separate rings: a K stage is free once its scores are done)
 // The probabilities are rounded to bf16 where they meet V (the row sum is taken in fp32 before that), as in the
 // prefill kernel.  All waits are bounded in wall time.
+//
+// What bounds it: with 2041 rows a chain of four tiles per warpgroup and the launch around it (12 us of the call's 28 at 256
+// sequences, 16 heads of 64); with 8000 rows of head_dim 128 the tensor pipe at 39 % and the softmax chain between its products
+// (52 us alone, 512 sequences; about 60 us beside the own rows' stream, which is what the call then takes: 125 us).
 #include <cuda.h>
 
 #include "bt_common.cuh"
@@ -36,8 +40,8 @@ constexpr int kMmaWarp = 8, kKWarp = 10, kVWarp = 11;
 constexpr int kThreads = 384;
 constexpr int kStages = 2;             // of K, and of V
 // Shared memory that lets one CTA on an SM, not two: they would take turns at the SM's tensor memory while other SMs have
-// none (calls back to back: 181 vs 157 us at 512 sequences and 8000 rows of head_dim 128), and leaves room for the
-// streaming kernel's CTA beside it.
+// none (calls back to back: 181 vs 145 us at 512 sequences and 8000 rows of head_dim 128, when the ring kernel streamed the own
+// rows), and leaves room for the own-rows kernel's CTAs beside it.
 constexpr int kSmemOnePerSm = 116 * 1024;
 constexpr uint32_t kTmemCols = 512;    // four score buffers of 64 columns, two outputs of head_dim columns
 constexpr uint32_t kSpinLimit = 1u << 26;
@@ -110,7 +114,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    // The next launch on the stream is the streaming kernel, which reads what earlier launches wrote without
+    // The next launch on the stream is the own-rows kernel, which reads what earlier launches wrote without
     // waiting for THIS one to end.  It may start once every CTA has passed this point, so the wait comes first:
     // everything before this launch is then complete and visible to both.
     pdl_wait();
@@ -385,7 +389,7 @@ static cudaError_t launch_t(const SharedDecodeArgs& a, cudaStream_t stream)
     e = raise_smem_limit_once(limit_raised, dev, shared_prefix_kernel<HD>, smem_bytes<HD>());
     if (e != cudaSuccess) return e;
     // an SM's split between L1 and shared memory cannot change while a CTA runs on it: take all of it, so that the
-    // streaming kernel's CTA still fits
+    // own-rows kernel's CTAs still fit
     static PerDeviceOnce carveout_set;
     e = carveout_set.once(dev, []() { return cudaFuncSetAttribute(shared_prefix_kernel<HD>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); });
     if (e != cudaSuccess) return e;
