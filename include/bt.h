@@ -289,10 +289,12 @@ bt_status bt_block_prefill_attn_window(const bt_config* cfg, const void* q, cons
  *   out[b,h,:] = softmax over the rows  { prefix rows 0 .. S-1 of head h }  then  { own rows 0 .. len[b]-1 of (b,h) }.
  * prefix: a block cache of ONE sequence, [n_layers][1][H][prefix_max][hd] with S = prefix->len[layer] - what
  * bt_block_kv_append, bt_block_qkv_project_append and the prefill calls fill under a config of batch 1 and max_blocks =
- * prefix_max.  It is only read.  Either part may be empty; both empty gives zeros and BT_DEV_EMPTY.
+ * prefix_max.  It is only read, and must not overlap the cache that a step appends to (BT_ERR_UNSUPPORTED where an array of
+ * theirs is the same).  Either part may be empty; both empty gives zeros and BT_DEV_EMPTY.
  * The prefix part is a dense product per head on the tensor cores (the softmax weights are rounded to bf16 where
  * they meet V, as in the prefill), the own part on the CUDA cores while the first one computes; two or three launches.  The step form
  * appends a row to the sequence's own cache first, exactly as bt_block_decode_step.
+ * After BT_DEV_TIMEOUT the affected outputs are undefined.
  * workspace: required, bt_workspace_bytes_shared bytes (0 on an invalid config), initialised by bt_workspace_init under the
  * same config; one call at a time.  Other arguments and errors as for bt_block_decode_attn / bt_block_decode_step.
  */
@@ -339,7 +341,7 @@ bt_status bt_block_decode_step_weights(const bt_config* cfg, bt_block_cache* cac
  *             source's (BT_ERR_UNSUPPORTED where they are the same); BT_ERR_CAPACITY if a sequence that is not cut,
  *             or n_keep rows, might not fit dst_max.
  * Rows and sums at or past the new length keep what they held.  workspace: in place bt_workspace_bytes bytes, initialised;
- * not used (may be NULL) with dst.  One launch.
+ * not used (may be NULL) with dst.  dev_status: no condition is raised (may be NULL).  One or two launches.
  */
 bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* weights, int layer, int n_keep,
                             int n_trigger, int n_sinks, int n_recent, bt_block_cache* dst, float* dst_weights, int dst_max,

@@ -124,7 +124,7 @@ bt_status validate_decode_attn_args(const bt_config* cfg, const bt_block_cache* 
 
 extern "C" {
 
-int bt_version(void) { return 200; }
+int bt_version(void) { return 300; }
 
 const char* bt_status_string(bt_status s)
 {
@@ -472,6 +472,8 @@ static bt_status decode_shared(const bt_config* cfg, const bt_block_cache* prefi
     if (st != BT_OK) return st;
     if (!workspace || workspace_bytes < bt_workspace_bytes_shared(cfg, prefix_max)) return BT_ERR_WORKSPACE;
     if (!block_cache_aligned(prefix) || !al16(workspace)) return BT_ERR_UNSUPPORTED;
+    // a step writes rows and lengths of the cache while the prefix is still being read
+    if (step && (prefix->k == cache->k || prefix->v == cache->v || prefix->len == cache->len)) return BT_ERR_UNSUPPORTED;
     const size_t prefix_layer = (size_t)cfg->heads * prefix_max * cfg->head_dim * 2;
     bt::SharedDecodeArgs a;
     fill_decode_args(a, cfg, cache, layer, q, k_new, v_new, out, workspace, shared_splits(cfg), dev_status);
@@ -580,7 +582,7 @@ bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* 
     if (!cache || !cache->k || !cache->v || !cache->len || !weights || !kept) return BT_ERR_NULL;
     if (dst && (!dst->k || !dst->v || !dst->len || !dst_weights)) return BT_ERR_NULL;
     if (n_keep < 1 || n_sinks < 0 || n_recent < 0 || n_trigger < 0 || n_sinks > n_keep || n_recent > n_keep - n_sinks) return BT_ERR_SHAPE;
-    if (n_trigger <= n_keep) n_trigger = n_keep + 1;
+    if (n_trigger <= n_keep) n_trigger = n_keep < 0x7fffffff ? n_keep + 1 : n_keep;   // (no cache is that long)
     if (dst) {
         if (dst_max < 1) return BT_ERR_SHAPE;
         // the longest sequence that is left whole has to fit, and so do the rows kept

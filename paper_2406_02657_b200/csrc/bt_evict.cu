@@ -206,6 +206,24 @@ struct Pair {
     int bh, b, n;
     bool cut;
 };
+// The CTA's pair.  One thread reads the length for all: in place it changes as soon as every pair of the sequence has been
+// counted in (settle_length), and a thread of its own CTA must not read it after that.
+__device__ __forceinline__ Pair pair_of_cta(const EvictArgs& a, int bh)
+{
+    __shared__ int rows;
+    Pair p;
+    p.bh = bh;
+    p.b = bh / a.H;
+    if (threadIdx.x == 0) {
+        const int n = a.len[p.b];
+        rows = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
+    }
+    __syncthreads();
+    p.n = rows;
+    p.cut = p.n >= a.trigger && p.n > a.n_keep;
+    return p;
+}
+// The same where nothing changes the length.
 __device__ __forceinline__ Pair pair_of(const EvictArgs& a, int bh)
 {
     Pair p;
@@ -289,7 +307,7 @@ __global__ void __launch_bounds__(kFusedThreads, 1024 / kFusedThreads) evict_fus
     __shared__ int32_t list[kFusedRows];
     pdl_launch_dependents();
     pdl_wait();
-    const Pair p = pair_of(a, blockIdx.x);
+    const Pair p = pair_of_cta(a, blockIdx.x);
     if (threadIdx.x == 0) settle_length(a, p);
     int32_t* kept = a.kept + (size_t)p.bh * a.n_keep;
     if (p.cut) {
@@ -310,7 +328,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a)
     __shared__ SelectSmem<THREADS, kSelectBits> sm;
     pdl_launch_dependents();
     pdl_wait();
-    const Pair p = pair_of(a, blockIdx.x);
+    const Pair p = pair_of_cta(a, blockIdx.x);
     if (threadIdx.x == 0) settle_length(a, p);
     int32_t* list = a.kept + (size_t)p.bh * a.n_keep;
     if (p.cut)

@@ -71,13 +71,6 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
     const uint4 qr = ld_l2(reinterpret_cast<const bf16*>(a.q) + (size_t)bh * HD + sub * 8);
     n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
     const bool step = a.k_new != nullptr, append = step && n < a.n_max;   // a full cache takes no row: flagged, attended as it is
-    // the length goes up once all of the sequence's CTAs have read the old one (the increment is computed from the value read)
-    int arrival = -1;
-    if (step && threadIdx.x == 0) {
-        int one;
-        asm volatile("and.b32 %0, %1, 0;\n\tadd.s32 %0, %0, 1;" : "=r"(one) : "r"(n));
-        arrival = atomicAdd(a.counters + (size_t)a.B * a.H + b, one);
-    }
     float qf[8];
     unpack8(qr, qf);
 #pragma unroll
@@ -174,6 +167,9 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
     }
     __syncthreads();
     if (warp == 0) {
+        // the length goes up once all of the sequence's CTAs - every warp of them: hence behind the barrier - have read the old one
+        int arrival = -1;
+        if (step && lane == 0) arrival = atomicAdd(a.counters + (size_t)a.B * a.H + b, 1);
         if (rg > 0) st.init();
         for (int w = rg; w < kWarps - 1; w += RPW) {   // row group rg joins warps rg + 1, rg + 1 + RPW, ...
             float a2[8];

@@ -62,6 +62,9 @@ def test_shared_refusals(bt):
     assert go(p=ref(mk(0x1008, 0x1000, 0x1000))) == bt.BT_ERR_UNSUPPORTED and go(p=ref(mk(0x1000, 0x1000, 0x1002))) == bt.BT_ERR_UNSUPPORTED
     assert step(ref(cfg), ref(pc), 100, ref(bc), 0, OK, None, OK, OK, OK, need, None, None) == bt.BT_ERR_NULL
     assert step(ref(cfg), ref(pc), 100, ref(bc), 0, OK, ODD, OK, OK, OK, need, None, None) == bt.BT_ERR_UNSUPPORTED
+    # the prefix a step reads must not be the cache it appends to
+    for same in (mk(0x1000, 0x2000, 0x2000), mk(0x2000, 0x1000, 0x2000), mk(0x2000, 0x2000, 0x1000)):
+        assert step(ref(cfg), ref(same), 100, ref(bc), 0, OK, OK, OK, OK, OK, need, None, None) == bt.BT_ERR_UNSUPPORTED
 
 
 def test_weights_refusals(bt):

@@ -237,7 +237,7 @@ def shared_case(bt, B, H, hd, cap, S, N, lens, splits=0, seed=9, layer=0, layers
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("cap,S", [(1, 1), (64, 0), (64, 1), (70, 63), (70, 64), (70, 65), (130, 128), (700, 129), (700, 513), (700, 700)])
 def test_shared_prefix(bt, hd, cap, S):
-    for B, H, splits in ((1, 1, 0), (3, 2, 0), (130, 3, 0), (5, 4, 3), (9, 16, 1)):
+    for B, H, splits in ((1, 1, 0), (3, 2, 0), (130, 3, 0), (5, 4, 3), (9, 16, 1), (40, 128 * 16 // hd, 0)):
         N = 70
         lens = [(b * 37) % (N + 1) for b in range(B)]
         cfg, cache, prefix, k, v, pk, pv = shared_case(bt, B, H, hd, cap, S, N, lens, splits)
@@ -301,6 +301,31 @@ def test_shared_prefix_at_size_with_back_to_back_calls(bt):
         ref, mass = both(lambda t: t), both(torch.abs)
         tol = (2.0 ** -8 + 2.0 ** -10) * mass * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs()
         assert ((x[l + 1].double() - ref).abs() <= tol).all(), l
+
+
+def test_shared_prefix_steps_at_size(bt):
+    """Many CTAs per sequence read its length and the last one raises it: over a whole cache of steps, lengths, rows and results
+    are those of the separate calls."""
+    B, H, hd, cap, S, N = 300, 16, 64, 256, 250, 40
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
+    fill = lambda i, shape: gen.normal_bf16_device(33, i, shape, device="cuda")   # noqa: E731
+    prefix = bt.BlockCache(bt.make_config(1, H, hd, 4, 1, cap, 1), k=fill(0, (1, 1, H, cap, hd)), v=fill(1, (1, 1, H, cap, hd)))
+    prefix.len.fill_(S)
+    one, two = bt.BlockCache(cfg), bt.BlockCache(cfg)
+    start = (torch.arange(B, dtype=torch.int32, device="cuda") % 4)[None]
+    one.len.copy_(start)
+    two.len.copy_(start)
+    ws, st = bt.alloc_workspace_shared(cfg, cap), status_word()
+    a, b = (torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for step in range(N - 4):
+        q, kn, vn = (fill(10 + 3 * step + i, (B, H, hd)) for i in range(3))
+        bt.bt_block_decode_step_shared(cfg, prefix, one, 0, q, kn, vn, a, ws, dev_status=st)
+        bt.bt_block_kv_append(cfg, two, 0, kn, vn, n_new=1, dev_status=st)
+        bt.bt_block_decode_attn_shared(cfg, prefix, two, 0, q, b, ws, dev_status=st)
+        assert torch.equal(one.len, two.len) and torch.equal(one.len, start + step + 1)
+        # the appended row joins the sum last instead of in its place: fp32 orders, then at most a step of bf16 (2^-7)
+        assert ((a.double() - b.double()).abs() <= 2.0 ** -7 * b.double().abs() + 1e-5).all(), step
+    assert torch.equal(one.k, two.k) and torch.equal(one.v, two.v) and st.item() == 0
 
 
 # ------------------------------------------------------------------------------------------------ summed weights
@@ -449,21 +474,27 @@ def test_evict_long_and_many(bt, into, B, H, N, n_keep):
     lens = torch.tensor([N - b % 7 for b in range(B)], dtype=torch.int32, device="cuda")
     cache.len[0].copy_(lens)
     sums = w.clone()
-    if into == "other":
-        dst, dsums = bt.BlockCache(bt.make_config(B, H, hd, 4, 1, n_keep, 1)), torch.zeros((1, B, H, n_keep), device="cuda")
-        kept = bt.bt_block_kv_evict(cfg, cache, sums, 0, n_keep, sinks, recent, dst=dst, dst_weights=dsums)
-    else:
-        dst, dsums = cache, sums
-        kept = bt.bt_block_kv_evict(cfg, cache, sums, 0, n_keep, sinks, recent, bt.alloc_workspace(cfg))
-    assert (dst.len == n_keep).all()
     j = torch.arange(N, device="cuda")
     n = lens.long()[:, None, None]
     rank = torch.where((j < sinks) | (j >= n - recent), float("inf"), w[0]).masked_fill(j >= n, float("-inf"))
     rows = rank.sort(dim=-1, descending=True, stable=True).indices[..., :n_keep].sort(-1).values
-    assert torch.equal(kept.long(), rows)
     at = rows[..., None].expand(-1, -1, -1, hd)
-    assert torch.equal(dst.k[0, :, :, :n_keep], k[0].gather(2, at)) and torch.equal(dst.v[0, :, :, :n_keep], v[0].gather(2, at))
-    assert torch.equal(dsums[0, :, :, :n_keep], w[0].gather(2, rows))
+    want_k, want_v, want_w = k[0].gather(2, at), v[0].gather(2, at), w[0].gather(2, rows)
+    ws = bt.alloc_workspace(cfg)
+    for _ in range(40 if B * H > 1000 else 3):   # many CTAs of a sequence read its length while the first ones are done with it
+        cache.k.copy_(k)
+        cache.v.copy_(v)
+        cache.len[0].copy_(lens)
+        sums.copy_(w)
+        if into == "other":
+            dst, dsums = bt.BlockCache(bt.make_config(B, H, hd, 4, 1, n_keep, 1)), torch.zeros((1, B, H, n_keep), device="cuda")
+            kept = bt.bt_block_kv_evict(cfg, cache, sums, 0, n_keep, sinks, recent, dst=dst, dst_weights=dsums)
+        else:
+            dst, dsums = cache, sums
+            kept = bt.bt_block_kv_evict(cfg, cache, sums, 0, n_keep, sinks, recent, ws)
+        assert (dst.len == n_keep).all() and torch.equal(kept.long(), rows)
+        assert torch.equal(dst.k[0, :, :, :n_keep], want_k) and torch.equal(dst.v[0, :, :, :n_keep], want_v)
+        assert torch.equal(dsums[0, :, :, :n_keep], want_w)
 
 
 # ------------------------------------------------------------------------------------------------ together
@@ -524,6 +555,42 @@ def test_generation_with_a_bounded_cache(bt):
             assert (np.abs(got - new)[:, :, :n] <= new_tol[:, :, :n]).all()
             assert (cache.len == n).all()
         assert evictions >= 3 and st.item() == 0
+
+
+@pytest.mark.parametrize("B,H,N,n_keep", [(2, 2, 2000, 900), (3, 1, 9000, 1500), (60, 16, 300, 100)])
+def test_evict_in_place_in_a_graph(bt, B, H, N, n_keep):
+    """Captured before it ever ran on these sizes, replayed on rows that change between replays (clusters of several CTAs in the
+    first two cases), equal to a stable selection each time."""
+    hd, sinks, recent = 64, 3, 11
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
+    cache, sums, ws = bt.BlockCache(cfg), torch.zeros((1, B, H, N), device="cuda"), bt.alloc_workspace(cfg)
+    kept = torch.empty((B, H, n_keep), dtype=torch.int32, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        bt.bt_block_kv_evict(cfg, cache, sums, 0, n_keep, sinks, recent, ws, kept=kept, stream=side)
+    for turn in range(4):
+        k, v = gen.normal_bf16_device(40 + turn, 0, (1, B, H, N, hd), device="cuda"), gen.normal_bf16_device(40 + turn, 1, (1, B, H, N, hd), device="cuda")
+        w = torch.rand((1, B, H, N), generator=torch.Generator("cuda").manual_seed(turn), device="cuda").pow_(4)
+        cache.k.copy_(k)
+        cache.v.copy_(v)
+        sums.copy_(w)
+        n = torch.full((1, B), N - turn, dtype=torch.int32, device="cuda")
+        n[0, 0] = n_keep if turn == 2 else N
+        cache.len.copy_(n)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph.replay()
+        torch.cuda.synchronize()
+        j, m = torch.arange(N, device="cuda"), n[0].long()[:, None, None]
+        rank = torch.where((j < sinks) | (j >= m - recent), float("inf"), w[0]).masked_fill(j >= m, float("-inf"))
+        rows = rank.sort(dim=-1, descending=True, stable=True).indices[..., :n_keep].sort(-1).values
+        cut = (m > n_keep).expand(-1, H, 1)
+        assert torch.equal(kept.long(), torch.where(cut, rows, -1)) and (cache.len == n_keep).all()
+        rows = torch.where(cut, rows, torch.arange(n_keep, device="cuda"))
+        at = rows[..., None].expand(-1, -1, -1, hd)
+        assert torch.equal(cache.k[0, :, :, :n_keep], k[0].gather(2, at)) and torch.equal(cache.v[0, :, :, :n_keep], v[0].gather(2, at))
+        assert torch.equal(cache.k[0, :, :, n_keep:], k[0, :, :, n_keep:]) and torch.equal(sums[0, :, :, :n_keep], w[0].gather(2, rows))
 
 
 def test_two_graphs_with_their_own_workspaces_on_two_streams(bt):
