@@ -2,12 +2,12 @@
 // over the shared prefix.
 //
 // Own rows: one CTA of four warps per (sequence, head, part of the row range); the warps take alternate passes of
-// 4 x (256 / head_dim) rows and meet once, at the end, through shared memory.  The kernel starts while the prefix kernel
+// 4 x (256 / head_dim) rows and meet once, at the end, through shared memory.  (Short caches: a warp each.)  The kernel starts while the prefix kernel
 // computes (see the wait there) and streams meanwhile, so it is built to fit beside one of that kernel's CTAs: 64 registers
 // a thread and 17 KB of shared memory leave room for four CTAs there and for eight on an SM of their own.  What bounds it
 // is bytes in flight, 4 KB a warp in single-buffered slots, and for items of a few dozen rows the instructions around
 // them (issue slots 64 % busy).  The whole call, at 512 sequences of up to 256 rows behind 8000 shared ones, 16 heads of 128,
-// and at 256 of up to 128 rows behind 2041, heads of 64: 125 and 28.4 us.  On the way there: two slots a warp and six CTAs an SM
+// and at 256 of up to 128 rows behind 2041, heads of 64: 127 and 27.3 us.  On the way there: two slots a warp and six CTAs an SM
 // 134 against 130 and 32.3 against 30.2 us; a persistent form with requests running ahead 159 and 32.5 us (twelve warps
 // beside the prefix kernel cannot keep enough in flight); the ring of the plain decode calls 145 and 29.9 us (its CTAs need an
 // SM each, so the two kernels follow each other).
@@ -56,15 +56,17 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr)
     return r;
 }
 
-template <int HD, bool JOIN>
+template <int HD, bool JOIN, int WPI>
 __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArgs a)
 {
-    constexpr int LPR = RowGeo<HD>::LPR, RPW = RowGeo<HD>::RPW, PASS = RPW * kUnroll;
+    constexpr int LPR = RowGeo<HD>::LPR, RPW = RowGeo<HD>::RPW, PASS = RPW * kUnroll, ITEMS = kWarps / WPI;
     __shared__ __align__(16) uint8_t stages[kWarps * kStageBytes];
-    __shared__ float sm_state[kWarps - 1][HD + 2];   // of warps 1 ..: acc, m, l
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % LPR, rg = lane / LPR;
-    const int bh = blockIdx.x / a.splits, sp = blockIdx.x - bh * a.splits, b = bh / a.H;
+    __shared__ float sm_state[kWarps - 1][HD + 2];   // WPI > 1: of the item's warps 1 ..: acc, m, l
+    const int warp_of_cta = threadIdx.x >> 5, warp = warp_of_cta % WPI;   // warp: of the item
+    const int lane = threadIdx.x & 31, sub = lane % LPR, rg = lane / LPR;
+    const int item = blockIdx.x * ITEMS + warp_of_cta / WPI, bh = item / a.splits, sp = item - bh * a.splits, b = bh / a.H;
     pdl_launch_dependents();
+    if (WPI == kWarps || bh < a.B * a.H) {
     uint64_t policy;   // the rows are read once
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     int n = __ldcg(a.len + b);
@@ -81,10 +83,10 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
     bf16* V = reinterpret_cast<bf16*>(a.v) + (size_t)bh * a.n_max * HD + sub * 8;
     const int per = a.splits == 1 ? n : (n + a.splits - 1) / a.splits;
     const int first = min(n, sp * per), end = min(n, first + per);
-    // Pass p of this warp: rows first + (warp + 4 p) * PASS ..  A lane copies the 16-byte pieces it will read itself, so nothing
+    // Pass p of this warp: rows first + (warp + p * WPI) * PASS ..  A lane copies the 16-byte pieces it will read itself, so nothing
     // but its own copies has to be waited for; its slot u holds its piece of K row u * RPW + rg, then V's.  A pass is requested
     // as soon as the one before it is in registers.
-    const uint32_t slots = smem_u32(stages) + warp * kStageBytes + lane * 16;
+    const uint32_t slots = smem_u32(stages) + warp_of_cta * kStageBytes + lane * 16;
     // A whole pass - the usual one - has no comparison and no address but the first row's.
     auto request = [&](int r0) {
         if (r0 < end) {
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
         // the pieces must be in registers, not merely requested, before their slots are written again
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) asm volatile("" ::"r"(kr[u].x), "r"(vr[u].x) : "memory");
-        request(r0 + kWarps * PASS);
+        request(r0 + WPI * PASS);
         float s[kUnroll], mt = kNegInf;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
     };
     int r0 = first + warp * PASS;
     request(r0);
-    for (; r0 < end; r0 += kWarps * PASS) {
+    for (; r0 < end; r0 += WPI * PASS) {
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         if (r0 + PASS <= end) one_pass(r0, std::true_type());
         else one_pass(r0, std::false_type());
@@ -156,26 +158,31 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
 #pragma unroll
     for (int i = 0; i < 4; ++i) unpack2(acc2[i], st.acc[2 * i], st.acc[2 * i + 1]);
     merge_row_groups<LPR>(st);
-    if (warp > 0 && rg == 0) {
-        float* mine = sm_state[warp - 1];
+    if constexpr (WPI > 1) {
+        static_assert(WPI == kWarps, "the barrier is the CTA's");
+        if (warp > 0 && rg == 0) {
+            float* mine = sm_state[warp - 1];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) mine[sub * 8 + i] = st.acc[i];
-        if (sub == 0) {
-            mine[HD] = st.m;
-            mine[HD + 1] = st.l;
+            for (int i = 0; i < 8; ++i) mine[sub * 8 + i] = st.acc[i];
+            if (sub == 0) {
+                mine[HD] = st.m;
+                mine[HD + 1] = st.l;
+            }
         }
+        __syncthreads();
     }
-    __syncthreads();
     if (warp == 0) {
-        // the length goes up once all of the sequence's CTAs - every warp of them: hence behind the barrier - have read the old one
+        // the length goes up once all of the sequence's items - every warp of them: hence behind the barrier - have read the old one
         int arrival = -1;
         if (step && lane == 0) arrival = atomicAdd(a.counters + (size_t)a.B * a.H + b, 1);
         if (rg > 0) st.init();
-        for (int w = rg; w < kWarps - 1; w += RPW) {   // row group rg joins warps rg + 1, rg + 1 + RPW, ...
-            float a2[8];
+        if constexpr (WPI > 1) {
+            for (int w = rg; w < kWarps - 1; w += RPW) {   // row group rg joins warps rg + 1, rg + 1 + RPW, ...
+                float a2[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a2[i] = sm_state[w][sub * 8 + i];
-            st.merge(sm_state[w][HD], sm_state[w][HD + 1], a2);
+                for (int i = 0; i < 8; ++i) a2[i] = sm_state[w][sub * 8 + i];
+                st.merge(sm_state[w][HD], sm_state[w][HD + 1], a2);
+            }
         }
         if (append && sp == a.splits - 1) {   // the new row: scored by row group 0 from the caller's buffer, stored into the cache
             const uint4 kn = ld_l2(reinterpret_cast<const bf16*>(a.k_new) + (size_t)bh * HD + sub * 8);
@@ -221,6 +228,7 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
             }
         }
     }
+    }
     // this grid's end has to imply the prefix kernel's; one waiting CTA is enough for that
     if (JOIN || blockIdx.x == gridDim.x - 1) pdl_wait();
 }
@@ -236,16 +244,17 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(SharedDecodeA
     if (bh < a.B * a.H) join<HD>(a, bh, sub);
 }
 
-template <int HD, bool JOIN>
+template <int HD, bool JOIN, int WPI>
 static cudaError_t launch_j(const SharedDecodeArgs& a, int dev, cudaStream_t stream)
 {
-    const long long bh = (long long)a.B * a.H, grid = bh * a.splits;
-    if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    constexpr int ITEMS = kWarps / WPI;
+    const long long bh = (long long)a.B * a.H, grid = (bh * a.splits + ITEMS - 1) / ITEMS;
+    if (grid * ITEMS > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
     // the same split between L1 and shared memory as the prefix kernel's, so that both fit an SM
     static PerDeviceOnce carveout_set;
-    cudaError_t e = carveout_set.once(dev, []() { return cudaFuncSetAttribute(shared_own_kernel<HD, JOIN>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); });
+    cudaError_t e = carveout_set.once(dev, []() { return cudaFuncSetAttribute(shared_own_kernel<HD, JOIN, WPI>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); });
     if (e != cudaSuccess) return e;
-    e = launch_pdl(shared_own_kernel<HD, JOIN>, dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
+    e = launch_pdl(shared_own_kernel<HD, JOIN, WPI>, dim3((unsigned)grid), dim3(kThreads), 0, stream, a);
     if (e != cudaSuccess || JOIN) return e;
     constexpr int PER = kJoinThreads / RowGeo<HD>::LPR;
     return launch_pdl(shared_join_kernel<HD>, dim3((unsigned)((bh + PER - 1) / PER)), dim3(kJoinThreads), 0, stream, a);
@@ -259,8 +268,12 @@ static cudaError_t launch_t(const SharedDecodeArgs& a, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     // few enough that all fit beside the prefix kernel's CTAs at once (four a SM): no CTA that waits keeps another one out
     // (11.2 against 13.4 us at 32 pairs; 33.1 against 31.8 us at 4096 pairs of 1 to 128 rows)
-    if (a.splits == 1 && (long long)a.B * a.H <= 4ll * sms) return launch_j<HD, true>(a, dev, stream);
-    return launch_j<HD, false>(a, dev, stream);
+    if (a.splits == 1 && (long long)a.B * a.H <= 4ll * sms) return launch_j<HD, true, kWarps>(a, dev, stream);
+    // a warp per item while it has at most eight passes (256 x 16 pairs of up to 32 rows behind 2041 shared ones: 19.8 against
+    // 24.3 us; 128 rows: 26.8 against 28.0; 256 rows: 38.8 against 35.1)
+    constexpr int kShortRows = 8 * RowGeo<HD>::RPW * kUnroll;
+    if (a.splits == 1 && a.n_max <= kShortRows) return launch_j<HD, false, 1>(a, dev, stream);
+    return launch_j<HD, false, kWarps>(a, dev, stream);
 }
 
 }  // namespace own

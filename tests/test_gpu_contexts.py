@@ -303,10 +303,11 @@ def test_shared_prefix_at_size_with_back_to_back_calls(bt):
         assert ((x[l + 1].double() - ref).abs() <= tol).all(), l
 
 
-def test_shared_prefix_steps_at_size(bt):
+@pytest.mark.parametrize("N", [40, 150])   # a warp per (sequence, head), and a CTA
+def test_shared_prefix_steps_at_size(bt, N):
     """Many CTAs per sequence read its length and the last one raises it: over a whole cache of steps, lengths, rows and results
     are those of the separate calls."""
-    B, H, hd, cap, S, N = 300, 16, 64, 256, 250, 40
+    B, H, hd, cap, S = 300, 16, 64, 256, 250
     cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
     fill = lambda i, shape: gen.normal_bf16_device(33, i, shape, device="cuda")   # noqa: E731
     prefix = bt.BlockCache(bt.make_config(1, H, hd, 4, 1, cap, 1), k=fill(0, (1, 1, H, cap, hd)), v=fill(1, (1, 1, H, cap, hd)))
@@ -317,7 +318,7 @@ def test_shared_prefix_steps_at_size(bt):
     two.len.copy_(start)
     ws, st = bt.alloc_workspace_shared(cfg, cap), status_word()
     a, b = (torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda") for _ in range(2))
-    for step in range(N - 4):
+    for step in range(36):
         q, kn, vn = (fill(10 + 3 * step + i, (B, H, hd)) for i in range(3))
         bt.bt_block_decode_step_shared(cfg, prefix, one, 0, q, kn, vn, a, ws, dev_status=st)
         bt.bt_block_kv_append(cfg, two, 0, kn, vn, n_new=1, dev_status=st)
