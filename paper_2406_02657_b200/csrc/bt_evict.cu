@@ -17,7 +17,7 @@
 //
 // Two shapes.  Many (sequence, head) pairs with short caches: a warp selects and moves a pair by itself, one launch, no
 // barriers.  Else a launch with a CTA per pair selects, and a second one moves with several CTAs per pair - in place, a
-// cluster of them that meets once per chunk.
+// cluster of them that meets once per chunk; into another cache, with few pairs, the first launch moves the last rows meanwhile.
 //
 // Bound by HBM: the kept rows are read and written once, the sums read once.
 #include "bt_common.cuh"
@@ -251,10 +251,10 @@ __device__ __forceinline__ void settle_length(const EvictArgs& a, const Pair& p)
     }
 }
 
-// Moves rows d0 .. d1 - 1 of the pair's result with a group of THREADS threads (this one is `tid`).  In place, group
-// `rank` of `ctas` takes every ctas-th chunk, and `meet` is their barrier.
+// Moves rows d0 .. d1 - 1 of the pair's result with a group of THREADS threads (this one is `tid`): row i comes from row list[i],
+// or without a list from row i + shift.  In place, group `rank` of `ctas` takes every ctas-th chunk, and `meet` is their barrier.
 template <int HD, bool IN_PLACE, int THREADS, class Meet>
-__device__ __forceinline__ void move_rows(const EvictArgs& a, const int32_t* list, int bh, bool cut, int d0, int d1, int rank, int ctas, int tid, Meet meet)
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const int32_t* list, int shift, int bh, int d0, int d1, int rank, int ctas, int tid, Meet meet)
 {
     using G = RowGeo<HD>;
     constexpr int ROWS = THREADS / G::LPR;      // rows one pass of the group covers
@@ -274,12 +274,12 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const int32_t* lis
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int i = c0 + u * ROWS + rg;
-            src[u] = i < d1 ? (cut ? list[i] : i) : -1;
+            src[u] = i < d1 ? (list != nullptr ? list[i] : i + shift) : -1;
             if (IN_PLACE && src[u] == i) src[u] = -1;   // already where it belongs
         }
         const int wi = c0 + tid;
         const bool has_w = tid < CHUNK && wi < d1;
-        const int wsrc = has_w ? (cut ? list[wi] : wi) : 0;
+        const int wsrc = has_w ? (list != nullptr ? list[wi] : wi + shift) : 0;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
             if (src[u] >= 0) {
@@ -318,17 +318,15 @@ __global__ void __launch_bounds__(kFusedThreads, 1024 / kFusedThreads) evict_fus
         for (int i = threadIdx.x; i < a.n_keep; i += kFusedThreads) kept[i] = -1;
         if (IN_PLACE) return;
     }
-    move_rows<HD, IN_PLACE, kFusedThreads>(a, list, p.bh, p.cut, 0, p.cut ? a.n_keep : min(p.n, a.dst_max), 0, 1, threadIdx.x, [] { __syncthreads(); });
+    move_rows<HD, IN_PLACE, kFusedThreads>(a, p.cut ? list : nullptr, 0, p.bh, 0, p.cut ? a.n_keep : min(p.n, a.dst_max), 0, 1, threadIdx.x, [] { __syncthreads(); });
 }
 
 // ---- few pairs or long caches: select, then move
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a)
+__device__ __forceinline__ void select_pair(const EvictArgs& a, int bh)
 {
     __shared__ SelectSmem<THREADS, kSelectBits> sm;
-    pdl_launch_dependents();
-    pdl_wait();
-    const Pair p = pair_of_cta(a, blockIdx.x);
+    const Pair p = pair_of_cta(a, bh);
     if (threadIdx.x == 0) settle_length(a, p);
     int32_t* list = a.kept + (size_t)p.bh * a.n_keep;
     if (p.cut)
@@ -337,10 +335,35 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a)
         for (int i = threadIdx.x; i < a.n_keep; i += THREADS) list[i] = -1;
 }
 
-// parts CTAs per pair; in place they are a cluster.  The list says whether the sequence was cut (in place its length has
+// At 46 registers a thread the moving launch's CTAs find room beside these before they have ended (in place, 64 pairs: 69 us;
+// at 61 registers 83 us).
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    select_pair<THREADS>(a, blockIdx.x);
+}
+
+// With one more CTA per pair that moves the pair's last rows meanwhile, which stay whatever the sums; into another cache only.
+template <int HD, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kSelectThreads ? 1 : 4) evict_select_move_kernel(EvictArgs a)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int pairs = (int)gridDim.x / 2;
+    if ((int)blockIdx.x < pairs) {
+        select_pair<THREADS>(a, blockIdx.x);
+    } else {
+        const Pair p = pair_of(a, blockIdx.x - pairs);
+        if (p.cut) move_rows<HD, false, THREADS>(a, nullptr, p.n - a.n_keep, p.bh, a.n_keep - a.n_recent, a.n_keep, 0, 1, threadIdx.x, [] {});
+    }
+}
+
+// parts CTAs per pair; in place they are a cluster.  The last `moved` rows of a cut sequence are there already.  The list says whether the sequence was cut (in place its length has
 // changed by now).
 template <int HD, bool IN_PLACE>
-__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a, int parts)
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a, int parts, int moved)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -349,13 +372,12 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a
     const bool cut = list[0] >= 0;
     if constexpr (IN_PLACE) {
         if (!cut) return;   // the whole cluster
-        move_rows<HD, true, kMoveThreads>(a, list, bh, true, 0, a.n_keep, part, parts, threadIdx.x, [] {
+        move_rows<HD, true, kMoveThreads>(a, list, 0, bh, 0, a.n_keep, part, parts, threadIdx.x, [] {
             asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         });
     } else {
-        const int total = cut ? a.n_keep : pair_of(a, bh).n;
-        const int rows = min(total, a.dst_max);
-        move_rows<HD, false, kMoveThreads>(a, list, bh, cut, (int)((long long)rows * part / parts), (int)((long long)rows * (part + 1) / parts), 0, 1, threadIdx.x, [] {});
+        const int rows = cut ? a.n_keep - moved : min(pair_of(a, bh).n, a.dst_max);
+        move_rows<HD, false, kMoveThreads>(a, cut ? list : nullptr, 0, bh, (int)((long long)rows * part / parts), (int)((long long)rows * (part + 1) / parts), 0, 1, threadIdx.x, [] {});
     }
 }
 
@@ -373,8 +395,13 @@ static cudaError_t launch_t(const EvictArgs& a, cudaStream_t stream)
         if (a.in_place) return launch_pdl(evict_fused_kernel<HD, true>, dim3((unsigned)pairs), dim3(kFusedThreads), 0, stream, a);
         return launch_pdl(evict_fused_kernel<HD, false>, dim3((unsigned)pairs), dim3(kFusedThreads), 0, stream, a);
     }
-    if (a.n_max <= kMoveThreads * kKeys) e = launch_pdl(evict_select_kernel<kMoveThreads>, dim3((unsigned)pairs), dim3(kMoveThreads), 0, stream, a);
-    else e = launch_pdl(evict_select_kernel<kSelectThreads>, dim3((unsigned)pairs), dim3(kSelectThreads), 0, stream, a);   // enough threads for one round
+    // Selecting leaves SMs idle where the pairs are few: they move the rows that stay in any case (60.6 -> 53.8 us at 64 pairs,
+    // 4096 of 16384 rows of head_dim 128 kept, 1024 of them the last ones)
+    const bool movers = !a.in_place && 2 * pairs <= sms && a.n_recent >= 256;
+    const bool small = a.n_max <= kMoveThreads * kKeys;   // enough threads for one round over the sums
+    const dim3 grid((unsigned)(movers ? 2 * pairs : pairs)), block(small ? kMoveThreads : kSelectThreads);
+    if (movers) e = launch_pdl(small ? evict_select_move_kernel<HD, kMoveThreads> : evict_select_move_kernel<HD, kSelectThreads>, grid, block, 0, stream, a);
+    else e = launch_pdl(small ? evict_select_kernel<kMoveThreads> : evict_select_kernel<kSelectThreads>, grid, block, 0, stream, a);
     if (e != cudaSuccess) return e;
     // four CTAs fit an SM; a part is at least one chunk
     constexpr int CHUNK = kMoveThreads / RowGeo<HD>::LPR * kUnroll;
@@ -384,7 +411,7 @@ static cudaError_t launch_t(const EvictArgs& a, cudaStream_t stream)
     if (parts > most) parts = most;
     if (!a.in_place) {
         if (pairs * parts > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-        return launch_pdl(evict_move_kernel<HD, false>, dim3((unsigned)(pairs * parts)), dim3(kMoveThreads), 0, stream, a, (int)parts);
+        return launch_pdl(evict_move_kernel<HD, false>, dim3((unsigned)(pairs * parts)), dim3(kMoveThreads), 0, stream, a, (int)parts, movers ? a.n_recent : 0);
     }
     int cluster = 1;
     while (cluster < kMaxCluster && cluster < parts) cluster *= 2;
@@ -400,7 +427,7 @@ static cudaError_t launch_t(const EvictArgs& a, cudaStream_t stream)
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, evict_move_kernel<HD, true>, a, cluster);
+    return cudaLaunchKernelEx(&cfg, evict_move_kernel<HD, true>, a, cluster, 0);
 }
 
 }  // namespace ev

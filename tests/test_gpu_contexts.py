@@ -498,6 +498,32 @@ def test_evict_long_and_many(bt, into, B, H, N, n_keep):
         assert torch.equal(dsums[0, :, :, :n_keep], want_w)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("N,n_keep,sinks,recent", [(3000, 1100, 4, 300), (3000, 700, 0, 700), (9000, 2500, 100, 1777), (6000, 5999, 1, 256)])
+def test_evict_into_another_cache_with_many_recent_rows(bt, hd, N, n_keep, sinks, recent):
+    """Few pairs: the last rows move while the others are selected.  Cut and uncut sequences side by side, second layer."""
+    B, H = 4, 2
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 2)
+    k, v = (gen.normal_bf16_device(50, i, (2, B, H, N, hd), device="cuda") for i in range(2))
+    w = torch.rand((2, B, H, N), generator=torch.Generator("cuda").manual_seed(5), device="cuda").pow_(4)
+    lens = torch.tensor([[0] * B, [N, n_keep, n_keep + 1, N // 2]], dtype=torch.int32, device="cuda")
+    cache = bt.BlockCache(cfg, k=k, v=v, length=lens)
+    dst, dw = bt.BlockCache(bt.make_config(B, H, hd, 4, 1, n_keep, 2)), torch.full((2, B, H, n_keep), -1.0, device="cuda")
+    kept = bt.bt_block_kv_evict(cfg, cache, w, 1, n_keep, sinks, recent, dst=dst, dst_weights=dw)
+    j, n = torch.arange(N, device="cuda"), lens[1].long()[:, None, None]
+    rank = torch.where((j < sinks) | (j >= n - recent), float("inf"), w[1]).masked_fill(j >= n, float("-inf"))
+    rows = rank.sort(dim=-1, descending=True, stable=True).indices[..., :n_keep].sort(-1).values
+    cut = (n > n_keep).expand(-1, H, 1)
+    assert torch.equal(kept.long(), torch.where(cut, rows, -1))
+    assert torch.equal(dst.len[1], lens[1].clamp(max=n_keep)) and not dst.len[0].any() and not dst.k[0].any()
+    for b in range(B):
+        m = min(int(lens[1, b]), n_keep)
+        for h in range(H):
+            r = rows[b, h] if cut[b, h, 0] else torch.arange(m, device="cuda")
+            assert torch.equal(dst.k[1, b, h, :m], k[1, b, h, r]) and torch.equal(dst.v[1, b, h, :m], v[1, b, h, r])
+            assert torch.equal(dw[1, b, h, :m], w[1, b, h, r]) and not dst.k[1, b, h, m:].any() and (dw[1, b, h, m:] == -1).all()
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def test_generation_with_a_bounded_cache(bt):
