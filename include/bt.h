@@ -332,7 +332,7 @@ bt_status bt_block_decode_step_weights(const bt_config* cfg, bt_block_cache* cac
  * the first n_sinks, the last n_recent, and of the rows between the n_keep - n_sinks - n_recent with the largest `weights`
  * (equal ones: the lowest index first; a NaN counts as lower than any number, -0 as 0).  They keep their
  * order and move, with their weights, to rows 0 .. n_keep-1; len[b] = n_keep.  The heads of a sequence choose
- * independently.  n_keep >= 1, 0 <= n_sinks + n_recent <= n_keep (else BT_ERR_SHAPE).
+ * independently.  1 <= n_keep <= 2^30, 0 <= n_sinks + n_recent <= n_keep (else BT_ERR_SHAPE).
  *   weights : float [n_layers][B][H][N_max], 16-byte aligned.
  *   kept    : int32 [B][H][n_keep], required: the old row of every new one, or -1 throughout for a sequence that was not cut.
  *   dst     : NULL = in place (dst_weights NULL, dst_max ignored).  Else another cache [n_layers][B][H][dst_max][hd] with

@@ -582,7 +582,8 @@ bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* 
     if (!cache || !cache->k || !cache->v || !cache->len || !weights || !kept) return BT_ERR_NULL;
     if (dst && (!dst->k || !dst->v || !dst->len || !dst_weights)) return BT_ERR_NULL;
     if (n_keep < 1 || n_sinks < 0 || n_recent < 0 || n_trigger < 0 || n_sinks > n_keep || n_recent > n_keep - n_sinks) return BT_ERR_SHAPE;
-    if (n_trigger <= n_keep) n_trigger = n_keep < 0x7fffffff ? n_keep + 1 : n_keep;   // (no cache is that long)
+    if (n_keep > 1 << 30) return BT_ERR_SHAPE;   // loops over the rows kept count past them by a CTA's threads
+    if (n_trigger <= n_keep) n_trigger = n_keep + 1;
     if (dst) {
         if (dst_max < 1) return BT_ERR_SHAPE;
         // the longest sequence that is left whole has to fit, and so do the rows kept

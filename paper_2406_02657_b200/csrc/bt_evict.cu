@@ -360,8 +360,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSelectThreads ? 1 : 4) ev
     }
 }
 
-// parts CTAs per pair; in place they are a cluster.  The last `moved` rows of a cut sequence are there already.  The list says whether the sequence was cut (in place its length has
-// changed by now).
+// parts CTAs per pair; in place they are a cluster.  The last `moved` rows of a cut sequence are there already.  The list says
+// whether the sequence was cut (in place its length has changed by now).
 template <int HD, bool IN_PLACE>
 __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(EvictArgs a, int parts, int moved)
 {

@@ -118,6 +118,12 @@ def test_evict_refusals(bt):
     assert go(dst=ref(other), dw=ODD, cap=64) == bt.BT_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("keep", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_evict_refuses_more_rows_than_it_can_count(bt, keep):
+    cfg, bc = bt.make_config(1, 1, 64, 4, 1, 64, 1), bt.binding.bt_block_cache(0x1000, 0x2000, 0x3000)
+    assert bt.lib().bt_block_kv_evict(ref(cfg), ref(bc), OK, 0, keep, 0, 0, 0, None, None, 0, OK, OK, 16, None, None) == bt.BT_ERR_SHAPE
+
+
 def test_definitions_agree_with_brute_force():
     rng = np.random.default_rng(0)
     q, K, V = rng.normal(size=16), rng.normal(size=(9, 16)), rng.normal(size=(9, 16))
