@@ -227,18 +227,19 @@ __device__ __forceinline__ int list_tile(const Item& it, int i)
     if constexpr (WINDOW) return i < it.ns ? i : i - it.ns + it.lo;
     return i;
 }
-// Step k of tile x as a step of the list, and whether tile A leaves that step of the list out.
+// Does tile A leave step i of the list out and tile B hand the stage back for it (none does so at the list's head)?
+template <bool WINDOW>
+__device__ __forceinline__ bool passed_by_a(const Item& it, int i)
+{
+    if constexpr (WINDOW) return it.skip_at > 0 && i >= it.skip_at && i < it.skip_at + it.skip_n;
+    return false;
+}
+// Step k of tile x as a step of the list.
 template <bool WINDOW>
 __device__ __forceinline__ int list_step(const Item& it, int x, int k)
 {
     if constexpr (WINDOW) return x == 0 && k >= it.skip_at ? k + it.skip_n : k;
     return k;
-}
-template <bool WINDOW>
-__device__ __forceinline__ bool skipped_by_a(const Item& it, int i)
-{
-    if constexpr (WINDOW) return i >= it.skip_at && i < it.skip_at + it.skip_n;
-    return false;
 }
 
 // One query row over its visible rows alone, by one warp, straight from global memory; the bf16 results go into the staged
@@ -398,8 +399,8 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
         // S_x(j) goes to score buffer j & 1 of the tile; S_x(j+2) overwrites the columns P_x(j) lived in: the
         // instructions of one thread execute in issue order and P_x(j) V(j) is issued before S_x(j+2).  The two
         // warps do not order their work against each other; the tensor pipe takes the instructions as they come.
-        // A key/value stage is handed back by two arrivals, one per tile (tile A arrives twice for the tiles that
-        // only it reads).  The whole warp walks the loop - control flow stays warp-uniform, every wait's outcome
+        // A key/value stage is handed back by two arrivals, one per tile (pass_over where a tile leaves it out).  The
+        // whole warp walks the loop - control flow stays warp-uniform, every wait's outcome
         // is agreed on by a vote - and one elected lane issues: a lone lane inside a divergent branch issues
         // tcgen05.mma slower than the tensor pipe runs them.
         {
@@ -420,8 +421,20 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                 const int qbuf = x ? qbuf_b(n_done) : qbuf_a(n_done);
                 const int steps = x ? it.nb : it.na - it.skip_n;
                 const uint32_t odd = WINDOW ? s_base & 1 : 0;   // score buffer of step 0
+                // A step of the list that this tile leaves out: waited for all the same - a warp that did not could meet the
+                // barrier two phases on, where the parity is that of the phase before - and handed back, but in the middle
+                // of the list, where tile B does that for A
+                auto pass_over = [&](int i, bool hand_back) {
+                    const uint32_t kc = kv_base + i, st = kc % kKvStages;
+                    ok = ok && wait_all(bar(B_KFULL + st), (kc / kKvStages) & 1);
+                    if (ok && hand_back && elect_one()) mbar_arrive(bar(B_KEMPTY + st));
+                    __syncwarp();
+                };
                 // S_x(j) = Q_x K_j^T, then the barriers that fire when it (and all before it) is done
                 auto issue_s = [&](int j) {
+                    // (this tile's last stage before the gap is not handed back yet, so no stage of the gap has been filled again)
+                    if (WINDOW && x == 0 && j == it.skip_at)
+                        for (int i = j; i < j + it.skip_n; ++i) pass_over(i, j == 0);
                     const uint32_t kc = kv_base + list_step<WINDOW>(it, x, j), st = kc % kKvStages;
                     ok = ok && wait_all(bar(B_KFULL + st), (kc / kKvStages) & 1);
                     if (ok && j == 0) {
@@ -468,8 +481,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                         mma_commit(bar(B_PVDONE + x));
                         // the stage (K_j and V_j) is free after its last reader
                         mma_commit(bar(B_KEMPTY + st));
-                        if (x == 0 && i >= it.nb) mma_commit(bar(B_KEMPTY + st));  // tile B does not read this one
-                        if (x == 1 && skipped_by_a<WINDOW>(it, i)) mma_commit(bar(B_KEMPTY + st));  // nor tile A this one
+                        if (x == 1 && passed_by_a<WINDOW>(it, i)) mbar_arrive(bar(B_KEMPTY + st));
                         if (j == steps - 1) mma_commit(bar(B_OFULL + x));
                     }
                     __syncwarp();
@@ -482,6 +494,8 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                         if (j + 2 < steps) issue_s(j + 2);
                     }
                 }
+                if (x == 1)
+                    for (int i = it.nb; i < it.na; ++i) pass_over(i, true);
                 kv_base += it.na;
                 if (WINDOW) s_base += steps;
             }

@@ -198,6 +198,34 @@ def test_window_prefill_many_items(bt, B, H, T, window, sinks):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("B,T,window,sinks", [(64, 600, 64, 4), (128, 100, 3, 0), (40, 1300, 300, 100), (96, 257, 300, 0)])
+def test_window_prefill_odd_tiles_many_items(bt, hd, B, T, window, sinks):
+    """An odd number of query tiles and many items per CTA: items of one query tile, whose key/value tiles the other issuing
+    warp leaves out, between items of two.  Three calls, the same bits, and within the tolerance of the test above."""
+    H = 16
+    cfg = bt.make_config(B, H, hd, 4, 1, T, 1)
+    q, k, v = (gen.normal_bf16_device(17, i, (B, H, T, hd), device="cuda") for i in range(3))
+    outs, st = [], status_word()
+    for _ in range(3):
+        outs.append(torch.full_like(q, 7.0))
+        bt.bt_block_prefill_attn_window(cfg, q, k, v, window, sinks, outs[-1], dev_status=st)
+    assert st.item() == 0 and torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    i = torch.arange(T, device="cuda")
+    seen = (i[None] <= i[:, None]) & ((i[None] > i[:, None] - window) | (i[None] < sinks))
+    for b in range(0, B, 3):
+        s = (q[b].double() @ k[b].double().transpose(1, 2) / hd ** 0.5).masked_fill(~seen, float("-inf"))
+        p = torch.softmax(s, -1)
+        ref, mass = p @ v[b].double(), p @ v[b].double().abs()
+        tol = (2.0 ** -8 + 2.0 ** -10) * mass * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs()
+        assert ((outs[0][b].double() - ref).abs() <= tol).all(), b
+    # all visible: the plain prefill's bits
+    whole = torch.empty_like(q)
+    bt.bt_block_prefill_attn(cfg, q, k, v, whole)
+    bt.bt_block_prefill_attn_window(cfg, q, k, v, T, 0, outs[0])
+    assert torch.equal(whole, outs[0])
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_window_prefill_rows_that_are_not_seen_may_hold_anything(bt, hd, bad):
     """A row of V (and one of K) that is not finite reaches the queries that see it and no other."""
