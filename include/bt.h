@@ -257,6 +257,11 @@ bt_status bt_block_prefill_attn(const bt_config* cfg, const void* q, const void*
  * its decoding is bound by reading that cache (appendix E.2).  These calls, which the paper has no counterpart for, bound
  * what is read or held: a window, a prefix held once for the batch, eviction.  They run over the same block cache.
  *
+ * Values that are not finite in a row that a query sees, here and in bt_block_decode_attn / bt_block_decode_step: a score that
+ * is NaN or plus infinity makes the query's whole output NaN, a NaN in V the dimension that holds it - however the rows
+ * are split and in whatever part they lie; a score of minus infinity is a weight of 0; where every score is minus infinity the
+ * output is zeros, as for no rows at all (but without BT_DEV_EMPTY).
+ *
  * Attention under a sliding window with sinks: of the n rows of a sequence the query of the newest block sees the first
  * min(sinks, n) and the last min(window, n) (a row that is both counts once):
  *   out[b,h,:] = sum_j softmax_j(scale * q[b,h,:] . K[b,h,j,:]) * V[b,h,j,:],  j < sinks or n - window <= j < n.

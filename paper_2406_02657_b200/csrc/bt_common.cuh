@@ -143,8 +143,14 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8])
     return r;
 }
 
+// What scores are taken relative to when m is their maximum so far: 2^(-inf - 0) is 0, 2^(-inf + inf) would be NaN.
+__device__ __forceinline__ float softmax_reference(float m) { return m == kNegInf ? 0.f : m; }
+// What turns a weighted sum into an output: no weight at all gives zeros, a NaN stays one.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
 // Running softmax state of one lane: maximum m (log2 domain), sum l of 2^(s-m), and the
-// 8 weighted-value accumulators the lane owns.
+// 8 weighted-value accumulators the lane owns.  m passes over NaN scores (fmaxf does); l does not, so a NaN among the scores
+// is in l and in the accumulators, whatever m says.
 struct SoftmaxState {
     float m, l, acc[8];
     __device__ __forceinline__ void init()
@@ -154,16 +160,25 @@ struct SoftmaxState {
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = 0.f;
     }
-    // fold another state (m2, l2, acc2) into this one
+    // fold another state (m2, l2, acc2) into this one; a state may be a finished part: (log2-sum-exp, 1, normalised output)
     __device__ __forceinline__ void merge(float m2, float l2, const float (&a2)[8])
     {
-        float mn = fmaxf(m, m2);
-        if (mn == kNegInf) return;  // both empty
-        float c1 = ex2(m - mn), c2 = ex2(m2 - mn);
+        const float mn = fmaxf(m, m2);
+        // without a maximum both sums are zero, or NaN and have to stay so: fold them like any others
+        const float m_use = softmax_reference(mn);
+        const float c1 = ex2(m - m_use), c2 = ex2(m2 - m_use);
         l = l * c1 + l2 * c2;
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = acc[i] * c1 + a2[i] * c2;
         m = mn;
+    }
+    // log2-sum-exp: minus infinity for no weight at all, NaN for a NaN score
+    __device__ __forceinline__ float lse() const { return l == 0.f ? kNegInf : m + log2f(l); }
+    __device__ __forceinline__ void normalised(float (&o)[8]) const
+    {
+        const float inv = inverse_sum(l);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = acc[i] * inv;
     }
 };
 

@@ -485,38 +485,35 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
                     }
                 }
                 keep_scores(s);
-                if (mt != kNegInf) {  // uniform within the LPR lanes of a row group
-                    const float mn = fmaxf(st.m, mt);
-                    const float cf = ex2(st.m - mn);
-                    st.l *= cf;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) st.acc[i] *= cf;
-#pragma unroll
-                    for (int u = 0; u < kUnroll; ++u) {
-                        if (u < ngroups) {
-                            const float p = ex2(s[u] - mn);   // 0 for the absent rows of the last group
-                            st.l += p;
-                            fma8(st.acc, p, vr[u]);
-                        }
-                    }
-                    st.m = mn;
-                }
-                continue;
-            }
-            if (mt != kNegInf) {  // uniform within the LPR lanes of a row group
-                const float mn = fmaxf(st.m, mt);
-                const float cf = ex2(st.m - mn);
+                const float mn = fmaxf(st.m, mt), m_use = softmax_reference(mn);
+                const float cf = ex2(st.m - m_use);
                 st.l *= cf;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) st.acc[i] *= cf;
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) {
-                    const float p = ex2(s[u] - mn);
-                    st.l += p;
-                    fma8(st.acc, p, vr[u]);
+                    if (u < ngroups) {
+                        const float p = ex2(s[u] - m_use);   // 0 for the absent rows of the last group
+                        st.l += p;
+                        fma8(st.acc, p, vr[u]);
+                    }
                 }
                 st.m = mn;
+                continue;
             }
+            // (never skipped for want of a maximum: a row group may have seen nothing but NaN scores, which mt passes over)
+            const float mn = fmaxf(st.m, mt), m_use = softmax_reference(mn);
+            const float cf = ex2(st.m - m_use);
+            st.l *= cf;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) st.acc[i] *= cf;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const float p = ex2(s[u] - m_use);
+                st.l += p;
+                fma8(st.acc, p, vr[u]);
+            }
+            st.m = mn;
         }
         if (!alive) {
             if constexpr (GROUP > 1) meet_group();   // nobody is left waiting
@@ -526,8 +523,8 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
             const float sn = row_sum<LPR>(dot8(qf, kn));
             new_score = sn;
             if (rg == 0) {
-                const float mn = fmaxf(st.m, sn);
-                const float cf = ex2(st.m - mn), pn = ex2(sn - mn);
+                const float mn = fmaxf(st.m, sn), m_use = softmax_reference(mn);
+                const float cf = ex2(st.m - m_use), pn = ex2(sn - m_use);
                 st.l = st.l * cf + pn;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) st.acc[i] *= cf;
@@ -552,9 +549,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
         };
         auto write_out = [&]() {  // lanes of row group 0: normalised bf16 output row
             float o[8];
-            const float inv = st.l > 0.f ? 1.f / st.l : 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = st.acc[i] * inv;
+            st.normalised(o);
             *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)w.bh * HD + sub * 8) = pack8(o);
         };
         if constexpr (GROUP > 1) {
@@ -610,13 +605,11 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
 
             if (rg == 0) {
                 float o[8];
-                const float inv = st.l > 0.f ? 1.f / st.l : 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = st.acc[i] * inv;
+                st.normalised(o);
                 float* ws = a.ws + ((size_t)w.bh * a.splits + w.sp) * (HD + 4);
                 *reinterpret_cast<float4*>(ws + sub * 8) = make_float4(o[0], o[1], o[2], o[3]);
                 *reinterpret_cast<float4*>(ws + sub * 8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
-                if (sub == 0) ws[HD] = st.l > 0.f ? st.m + log2f(st.l) : kNegInf;
+                if (sub == 0) ws[HD] = st.lse();
                 __threadfence();  // the partial is visible before this item counts itself in
             }
             __syncwarp();
@@ -634,7 +627,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
                     const float a2[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                     st.merge(lse, 1.f, a2);
                 }
-                    merge_row_groups();
+                merge_row_groups();
                 if (rg == 0) write_out();
                 add_weights();
                 if (lane == 0) a.counters[w.bh] = 0;

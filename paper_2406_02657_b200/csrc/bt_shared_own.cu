@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
             }
             mt = fmaxf(mt, s[u]);
         }
-        const float mn = fmaxf(st.m, mt), m_use = mn == kNegInf ? 0.f : mn;   // this row group may have no row yet
+        const float mn = fmaxf(st.m, mt), m_use = softmax_reference(mn);   // this row group may have no row yet
         const float cf = ex2(st.m - m_use);
         st.l *= cf;
         const uint64_t cf2 = pack2(cf, cf);
@@ -198,24 +198,24 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
         }
         merge_row_groups<LPR>(st);
         float o[8];
-        normalised(st, o);
+        st.normalised(o);
         const int count = a.n_pre + a.splits;
         if constexpr (JOIN) {   // splits == 1
             pdl_wait();         // the prefix's partials are complete and visible from here on
             // this item's own one is the last of them: row group rg folds partials rg, rg + RPW, ...
-            const float lse = st.l > 0.f ? st.m + log2f(st.l) : kNegInf;
+            const float lse = st.lse();
             st.init();
             const float* all = a.parts + (size_t)bh * count * (HD + 4);
             if (rg < a.n_pre) fold_partials<HD, 4>(st, all + (size_t)rg * (HD + 4), (a.n_pre - rg + RPW - 1) / RPW, RPW, sub);
             if (rg == RPW - 1) st.merge(lse, 1.f, o);
             merge_row_groups<LPR>(st);
-            normalised(st, o);
+            st.normalised(o);
             if (rg == 0) *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)bh * HD + sub * 8) = pack8(o);
         } else if (rg == 0) {
             float* mine = a.parts + ((size_t)bh * count + a.n_pre + sp) * (HD + 4);
             *reinterpret_cast<float4*>(mine + sub * 8) = make_float4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<float4*>(mine + sub * 8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
-            if (sub == 0) mine[HD] = st.l > 0.f ? st.m + log2f(st.l) : kNegInf;
+            if (sub == 0) mine[HD] = st.lse();
         }
         if (lane == 0) {
             if (bh == b * a.H && sp == 0) {

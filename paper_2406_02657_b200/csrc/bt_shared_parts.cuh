@@ -9,7 +9,6 @@
 namespace bt {
 namespace parts {
 
-
 // the lane's 8 dims of partials 0 .. count-1, `stride` of them apart
 template <int HD, int WIDE>
 __device__ __forceinline__ void fold_partials(SoftmaxState& st, const float* ws, int count, int stride, int sub)
@@ -32,16 +31,11 @@ __device__ __forceinline__ void fold_partials(SoftmaxState& st, const float* ws,
 #pragma unroll
         for (int i = 0; i < WIDE; ++i) {
             const float part[8] = {x[i].x, x[i].y, x[i].z, x[i].w, y[i].x, y[i].y, y[i].z, y[i].w};
-            st.merge(lse[i], 1.f, part);
+            // an empty part adds nothing.  (The branch also keeps the loads together: without it the compiler moves each to its
+            // use, and a call at 256 x 16 pairs takes 29.8 instead of 27.3 us.)
+            if (lse[i] != kNegInf) st.merge(lse[i], 1.f, part);
         }
     }
-}
-
-__device__ __forceinline__ void normalised(const SoftmaxState& st, float (&o)[8])
-{
-    const float inv = st.l > 0.f ? 1.f / st.l : 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = st.acc[i] * inv;
 }
 
 template <int LPR>
@@ -70,7 +64,7 @@ __device__ __forceinline__ void join(const SharedDecodeArgs& a, int bh, int sub)
     if (count <= 4) fold_partials<HD, 4>(st, ws, count, 1, sub);
     else fold_partials<HD, 8>(st, ws, count, 1, sub);
     float o[8];
-    normalised(st, o);
+    st.normalised(o);
     *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)bh * HD + sub * 8) = pack8(o);
 }
 

@@ -264,7 +264,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
                 }
                 l *= factor;
             }
-            const float m_use = m_ref == kNegInf ? 0.f : m_ref;
+            const float m_use = softmax_reference(m_ref);
 #pragma unroll
             for (int c = 0; c < BN; c += 32) {
                 float s[32];
@@ -333,7 +333,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
         const float m2 = ml[(1 - x) * 256 + row], l2 = ml[(1 - x) * 256 + 128 + row];
         const float m = fmaxf(m_ref, m2);
         const float f1 = m_ref == kNegInf ? 0.f : ex2(m_ref - m), f2 = m2 == kNegInf ? 0.f : ex2(m2 - m);
-        const float total = l * f1 + l2 * f2, inv = total > 0.f ? 1.f / total : 0.f;
+        const float total = l * f1 + l2 * f2, inv = inverse_sum(total);   // a NaN score is in l: the part becomes NaN, log2-sum-exp included
         const float g1 = f1 * inv, g2 = f2 * inv;
         const int b = qt * BM + row;
         float* dst = a.parts + (((size_t)(b < a.B ? b : 0) * a.H + h) * (a.n_pre + a.splits) + part) * (HD + 4);
@@ -355,7 +355,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_cons
                 }
             }
         }
-        if (x == 0 && b < a.B && ok) dst[HD] = total > 0.f ? m + log2f(total) : kNegInf;
+        if (x == 0 && b < a.B && ok) dst[HD] = total == 0.f ? kNegInf : m + log2f(total);
         tc_fence_before();
     }
 

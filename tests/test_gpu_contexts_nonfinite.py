@@ -1,0 +1,153 @@
+"""GPU tests of the operators for long and shared contexts on visible rows that are not finite: a NaN score, or one of plus infinity, makes the
+(sequence, head) that sees it NaN wherever the row lies and however the row range is cut; a score of minus infinity is a
+weight of zero; if nothing else is visible the output is zeros.  No other (sequence, head) notices."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import contexts as ctx
+from workloads import gen
+
+from test_gpu_contexts import f64, make_cache, rnd, shared_case
+from util import status_word, to_dev, to_f64
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF, NEG_INF = 0x7FC0, 0x7F80, 0xFF80
+
+
+@pytest.fixture(scope="module")
+def bt():
+    import paper_2406_02657_b200 as bt
+    assert torch.cuda.is_available()
+    return bt
+
+
+def attend(q, K, V, p_bf16=False):
+    """(out, tol, weights, relative tol on them) of one query over its visible rows, which may hold anything."""
+    hd = q.shape[0]
+    with np.errstate(invalid="ignore", over="ignore"):
+        s = K @ q
+    if np.isnan(s).any() or (s == np.inf).any():
+        return np.full(hd, np.nan), np.zeros(hd), np.full(len(s), np.nan), 0.0
+    some = s != -np.inf
+    out, p, tol, rel = ctx.attend(q, K[some], np.nan_to_num(V[some]), p_bf16=p_bf16)
+    out = np.where(np.isnan(V).any(0), np.nan, out)
+    weights = np.zeros(len(s))
+    weights[some] = p
+    return out, tol, weights, rel
+
+
+def check(got, ref, tol, what):
+    g = to_f64(got).reshape(ref.shape)
+    bad = np.isnan(ref)
+    assert np.isnan(g[bad]).all(), f"{what}: finite where the definition has a NaN, at {np.argwhere(bad & ~np.isnan(g))[:5].tolist()}"
+    assert np.isfinite(g[~bad]).all(), f"{what}: not finite at {np.argwhere(~bad & ~np.isfinite(g))[:5].tolist()}"
+    over = (np.abs(g - ref) - tol)[~bad]
+    assert (over <= 0).all(), f"{what}: {over.max():.3e} beyond the bound"
+
+
+def poison(k, v, q, at):
+    """One bad row per sequence, at[b]: in K of head 0 a NaN, in V of head 1 a NaN (dimension 5), in K of head 2 an infinity
+    (dimension 7: a score of plus or minus infinity by the sign of q there); head 3 stays clean."""
+    for b, j in enumerate(at):
+        k[b, 0, j, b % 8] = NAN
+        v[b, 1, j, 5] = NAN
+        k[b, 2, j, 7] = INF if b % 2 else NEG_INF
+
+
+def one_by_one(q, K, V, rows, p_bf16=False):
+    """attend() for every (sequence, head); rows(b, h) are its visible K and V."""
+    out, tol = np.zeros(q.shape), np.zeros(q.shape)
+    weights = {}
+    for b in range(q.shape[0]):
+        for h in range(q.shape[1]):
+            out[b, h], tol[b, h], *weights[b, h] = attend(q[b, h], *rows(b, h), p_bf16=p_bf16)
+    return out, tol, weights
+
+
+# whole chunks, chunk borders, the ragged end (where a row group holds one row), both ends
+AT = [0, 1, 31, 32, 63, 64, 130, 255, 256, 257, 259, 260]
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("splits", [0, 1, 2, 3, 7])
+@pytest.mark.parametrize("window,sinks", [(300, 0), (4, 3), (100, 33)])
+def test_window_decode_visible(bt, hd, splits, window, sinks):
+    B, H, N = len(AT), 4, 261
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    k, v, q = rnd(61, 1, (B, H, N, hd)), rnd(61, 2, (B, H, N, hd)), rnd(61, 3, (B, H, hd))
+    poison(k, v, q, AT)
+    cache = make_cache(bt, cfg, k, v, [N] * B)
+    out, st, ws = torch.zeros((B, H, hd), dtype=torch.bfloat16, device="cuda"), status_word(), bt.alloc_workspace(cfg)
+    bt.bt_block_decode_attn_window(cfg, cache, 0, to_dev(q), window, sinks, out, ws, dev_status=st)
+    K, V, seen = f64(k), f64(v), ctx.window_rows(N, window, sinks)
+    check(out, *one_by_one(f64(q), K, V, lambda b, h: (K[b, h, seen], V[b, h, seen]))[:2], f"window {window} sinks {sinks}")
+    assert st.item() == 0
+    if window > N:   # all rows: the plain call
+        bt.bt_block_decode_attn(cfg, cache, 0, to_dev(q), out, ws, dev_status=st)
+        check(out, *one_by_one(f64(q), K, V, lambda b, h: (K[b, h], V[b, h]))[:2], "plain")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("splits", [1, 4])
+@pytest.mark.parametrize("call", ["window", "weights", "shared"])
+def test_appended_row_visible(bt, hd, splits, call):
+    """The appended row is the bad one: alone, behind few rows, behind many."""
+    lens = [0, 1, 2, 3, 4, 31, 32, 33, 100, 129]
+    B, H, N = len(lens), 4, 130
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    k, v = rnd(62, 1, (B, H, N, hd)), rnd(62, 2, (B, H, N, hd))
+    cache = make_cache(bt, cfg, k, v, lens)
+    q, kn, vn = (rnd(62, 3 + i, (B, H, hd)) for i in range(3))
+    poison(kn[:, :, None], vn[:, :, None], q, [0] * B)
+    out, st = torch.zeros((B, H, hd), dtype=torch.bfloat16, device="cuda"), status_word()
+    for b, n in enumerate(lens):
+        k[b, :, n], v[b, :, n] = kn[b], vn[b]
+    K, V = f64(k), f64(v)
+    rows = lambda b, h: (K[b, h, :lens[b] + 1], V[b, h, :lens[b] + 1])   # noqa: E731
+    if call == "window":
+        bt.bt_block_decode_step_window(cfg, cache, 0, to_dev(q), to_dev(kn), to_dev(vn), N, 0, out, bt.alloc_workspace(cfg), dev_status=st)
+    elif call == "weights":
+        w = torch.zeros((1, B, H, N), device="cuda")
+        bt.bt_block_decode_step_weights(cfg, cache, 0, to_dev(q), to_dev(kn), to_dev(vn), out, w, w, bt.alloc_workspace_weights(cfg), dev_status=st)
+    else:
+        prefix = bt.BlockCache(bt.make_config(1, H, hd, 4, 1, 8, 1))
+        bt.bt_block_decode_step_shared(cfg, prefix, cache, 0, to_dev(q), to_dev(kn), to_dev(vn), out, bt.alloc_workspace_shared(cfg, 8), dev_status=st)
+    check(out, *one_by_one(f64(q), K, V, rows, p_bf16=call == "shared")[:2], call)
+    assert st.item() == 0 and cache.len[0].tolist() == [n + 1 for n in lens]
+
+
+# few pairs (the own rows' kernel joins), many (a launch of its own joins): a warp per pair, a CTA per pair, parts of own rows; one part of
+# the prefix and several
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("B,N,cap,splits", [(12, 70, 700, 0), (12, 70, 64, 0), (12, 261, 700, 3), (200, 60, 700, 0), (200, 60, 60, 0), (200, 140, 700, 0)])
+def test_shared_prefix_visible(bt, hd, B, N, cap, splits):
+    H, S = 4, cap - 1
+    lens = [N if b < 12 else (b * 37) % (N + 1) for b in range(B)]
+    lens[-1] = 0
+    q = rnd(63, 9, (B, H, hd))
+    # the bad row among the sequences' own
+    cfg, cache, prefix, k, v, pk, pv = shared_case(bt, B, H, hd, cap, S, N, lens, splits, seed=63)
+    at = [a % N for a in AT[:min(B, 12) - 1]]
+    poison(k, v, q, at)
+    cache = make_cache(bt, cfg, k, v, lens)
+    out, st, ws = torch.zeros((B, H, hd), dtype=torch.bfloat16, device="cuda"), status_word(), bt.alloc_workspace_shared(cfg, cap)
+    K, V, PK, PV, Q = f64(k), f64(v), f64(pk), f64(pv), f64(q)
+
+    def rows(b, h):
+        return np.concatenate([PK[h, :S], K[b, h, :lens[b]]]), np.concatenate([PV[h, :S], V[b, h, :lens[b]]])
+
+    bt.bt_block_decode_attn_shared(cfg, prefix, cache, 0, to_dev(q), out, ws, dev_status=st)
+    check(out, *one_by_one(Q, K, V, rows, p_bf16=True)[:2], "own rows")
+    # the bad row in the prefix, for all sequences
+    for j in sorted({0, 63, 64, 127, 128, 129, 300, S - 2, S - 1}):
+        if j >= S:
+            continue
+        bad_k, bad_v = pk[None].copy(), pv[None].copy()
+        poison(bad_k, bad_v, q, [j])
+        PK, PV = f64(bad_k[0]), f64(bad_v[0])
+        prefix = make_cache(bt, bt.make_config(1, H, hd, 4, 1, cap, 1), bad_k, bad_v, [S])
+        bt.bt_block_decode_attn_shared(cfg, prefix, cache, 0, to_dev(q), out, ws, dev_status=st)
+        check(out, *one_by_one(Q, K, V, rows, p_bf16=True)[:2], f"prefix row {j}")
+    assert st.item() == 0
