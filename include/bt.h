@@ -317,6 +317,8 @@ bt_status bt_block_decode_step_shared(const bt_config* cfg, const bt_block_cache
  *   weights_out[b,h,j] = weights_in[b,h,j] + softmax_j(scale * q[b,h,:] . K[b,h,j,:])     (fp32)
  * weights_in, weights_out: float [n_layers][B][H][N_max], 16-byte aligned; the same array for a running sum, or
  * weights_in = NULL to start the sums here (all zeros).  Entries at or past len[b] are neither read nor written.
+ * Where a visible score is NaN or plus infinity every weight of that (sequence, head) is NaN, and so are its sums from then on;
+ * where every score is minus infinity the sums stay as they are.
  * The step form appends a row first, as bt_block_decode_step; the sum of the appended row starts with its weight of
  * this step, whatever weights_in holds there.
  * workspace: bt_workspace_bytes_weights bytes, initialised by bt_workspace_init; it may be NULL for the attn form where

@@ -582,7 +582,8 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
         // kWeights: what turns the kept scores into weights - at once when this warp has them all, else for the second launch
         auto add_weights = [&]() {
             if constexpr (MODE == kWeights) {
-                const float lse = st.l > 0.f ? st.m + log2f(st.l) : kNegInf;
+                // where no row has any weight every score is -inf, and 2^(-inf - 0) adds nothing to its sum
+                const float lse = softmax_reference(st.lse());
                 if (a.smem_rows) {
                     __syncwarp();
                     add_row_weights(a, w, warp_scores, lse, new_score, lane);

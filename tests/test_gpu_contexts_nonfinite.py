@@ -151,3 +151,47 @@ def test_shared_prefix_visible(bt, hd, B, N, cap, splits):
         bt.bt_block_decode_attn_shared(cfg, prefix, cache, 0, to_dev(q), out, ws, dev_status=st)
         check(out, *one_by_one(Q, K, V, rows, p_bf16=True)[:2], f"prefix row {j}")
     assert st.item() == 0
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("step", [False, True])
+@pytest.mark.parametrize("N,splits", [(261, 1), (264, 1), (261, 4), (264, 7), (2051, 1)])   # sums by the same launch, and by a second one
+def test_sums_visible(bt, hd, step, N, splits):
+    """Sums grow by the definition's weights: NaN throughout where a score is NaN or plus infinity, nothing for a score of minus infinity, and
+    nothing at all where every score is.  With the step form the appended row is one of few scores that are finite, or is not either."""
+    lens = [260, 33, 260, 4, 1, 130, 255, 64, 31, 200, 260, 97]
+    B, H = len(lens), 6
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    k, v, q = rnd(64, 1, (B, H, N, hd)), rnd(64, 2, (B, H, N, hd)), rnd(64, 3, (B, H, hd))
+    poison(k, v, q, [min(a, n - 1) for a, n in zip(AT, lens)])
+    Q = f64(q)
+    for b in range(B):   # minus infinity: head 4 in every row, head 5 in the first half of them
+        for h, rows in ((4, slice(None)), (5, slice(0, lens[b] // 2))):
+            k[b, h, rows, 9] = NEG_INF if Q[b, h, 9] > 0 else INF
+    kn, vn = k[:, :, 0].copy(), rnd(64, 4, (B, H, hd))
+    kn[::2, 4] = rnd(64, 5, (B, H, hd))[::2, 4]
+    kn[:, 0], kn[:, 2] = rnd(64, 6, (B, H, hd))[:, 0], rnd(64, 7, (B, H, hd))[:, 2]
+    cache = make_cache(bt, cfg, k, v, lens)
+    old = np.random.default_rng(4).random((B, H, N)).astype(np.float32)
+    sums = torch.from_numpy(old)[None].cuda()
+    out, st, ws = torch.zeros((B, H, hd), dtype=torch.bfloat16, device="cuda"), status_word(), bt.alloc_workspace_weights(cfg)
+    n, base = list(lens), old.astype(np.float64)
+    if step:
+        bt.bt_block_decode_step_weights(cfg, cache, 0, to_dev(q), to_dev(kn), to_dev(vn), out, sums, sums, ws, dev_status=st)
+        for b in range(B):
+            k[b, :, n[b]], v[b, :, n[b]], base[b, :, n[b]] = kn[b], vn[b], 0.0
+            n[b] += 1
+    else:
+        bt.bt_block_decode_attn_weights(cfg, cache, 0, to_dev(q), out, sums, sums, ws, dev_status=st)
+    K, V = f64(k), f64(v)
+    ref, tol, weights = one_by_one(Q, K, V, lambda b, h: (K[b, h, :n[b]], V[b, h, :n[b]]))
+    check(out, ref, tol, "out")
+    got = sums[0].cpu().numpy()
+    for (b, h), (p, rel) in weights.items():
+        new, g = base[b, h, :n[b]] + p, got[b, h, :n[b]]
+        assert np.array_equal(np.isnan(g), np.isnan(new)), (b, h)
+        nothing = p == 0                                                      # bit for bit what was there
+        assert np.array_equal(g[nothing], base[b, h, :n[b]][nothing].astype(np.float32)), (b, h)
+        assert not (np.abs(g - new) > rel * p + ctx.STEP * np.abs(new) + 1e-30).any(), (b, h)
+        assert np.array_equal(got[b, h, n[b]:], old[b, h, n[b]:])
+    assert st.item() == 0
