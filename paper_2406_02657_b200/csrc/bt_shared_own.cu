@@ -120,9 +120,11 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
             kr[u] = lds128(slots + u * 1024);
             vr[u] = lds128(slots + u * 1024 + 512);
         }
-        // the pieces must be in registers, not merely requested, before their slots are written again
+        // The pieces have to be read before their slots are written again.  The empty statement keeps the compiler from moving a read
+        // down; what orders the reads before the asynchronous writes is the warp's barrier.
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) asm volatile("" ::"r"(kr[u].x), "r"(vr[u].x) : "memory");
+        __syncwarp();
         request(r0 + WPI * PASS);
         float s[kUnroll], mt = kNegInf;
 #pragma unroll
