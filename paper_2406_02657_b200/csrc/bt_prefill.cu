@@ -695,6 +695,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
             }
             if constexpr (WINDOW) {
                 uint32_t again = __ballot_sync(0xffffffffu, worst != 0.f && ok && qt * BM + row < p.T);   // NaN != 0
+                __syncwarp();   // a row staged by its own lane is written over by all of them: the vote does not order the two
                 while (again) {
                     const int who = __ffs(again) - 1, r = wq * 32 + who;
                     prefill_row_plain<HD>(p, it.bh, qt * BM + r, sQ + qbuf * Q_TILE_BYTES + r * 128, r, lane);
