@@ -66,18 +66,27 @@ __device__ __forceinline__ uint64_t global_ns()
 // for kernels whose threads wait on one another: *abort_flag is a shared-memory word that a thread sets
 // when its own wait runs out and that every waiting thread of the CTA watches, so that one failed wait
 // winds the whole CTA down.  Returns false when the limit ran out here or another thread gave up.
+// progress (optional): a shared-memory word that a thread with work of unforeseen length counts up; if it has changed since the
+// limit last ran out (or is not zero when it first does), the limit starts anew.
 __device__ __forceinline__ bool mbar_wait_walltime(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t spin_limit,
-                                                   uint64_t limit_ns)
+                                                   uint64_t limit_ns, volatile uint32_t* progress = nullptr)
 {
     if (mbar_test_wait(bar, parity)) return true;
     uint64_t t0 = 0;
+    uint32_t seen = 0;
     for (uint32_t it = 0; it < spin_limit; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((it & 63u) == 63u) {
             if (*abort_flag) return false;
             const uint64_t now = global_ns();
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > limit_ns) break;
+            if (t0 == 0) {
+                t0 = now;
+            } else if (now - t0 > limit_ns) {
+                if (progress == nullptr || *progress == seen) break;
+                seen = *progress;
+                t0 = now;
+                it = 0;
+            }
         }
     }
     *abort_flag = 1;

@@ -21,7 +21,8 @@
 //   warps 9, 10     : tcgen05.mma issuers of tile A and tile B (the whole warp walks the loop, an elected lane issues) -
 //                     S = Q K^T into tensor memory, O += P V with P read from tensor memory (the
 //                     probabilities never visit shared memory), each in the order PV(j) S(j+2)
-// All waits are bounded in wall time: one that runs out raises BT_DEV_TIMEOUT and the CTA winds down.
+// All waits are bounded in wall time: one that runs out raises BT_DEV_TIMEOUT and the CTA winds down.  (Time in which query rows
+// are worked out again, see below, does not count.)
 //
 // The windowed form (query t sees row j iff j <= t and (j > t - window or j < sinks)) is the same kernel compiled with
 // WINDOW: an item walks only the key/value tiles that hold a visible pair - those of the sinks, then those from the
@@ -56,10 +57,12 @@ constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s: far beyond any legitim
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 
 // Bounded wait: gives up after kWaitLimitNs of wall time (or kSpinLimit polls).  Returns false when
-// the limit ran out (BT_DEV_TIMEOUT is raised) or another thread of the CTA gave up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* dev_status)
+// the limit ran out (BT_DEV_TIMEOUT is raised) or another thread of the CTA gave up.  redone (windowed form): counts
+// while query rows are worked out again, which holds the other roles up for as long as it takes.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* dev_status,
+                                          volatile uint32_t* redone = nullptr)
 {
-    if (mbar_wait_walltime(bar, parity, abort_flag, kSpinLimit, kWaitLimitNs)) return true;
+    if (mbar_wait_walltime(bar, parity, abort_flag, kSpinLimit, kWaitLimitNs, redone)) return true;
     raise_status(dev_status, BT_DEV_TIMEOUT);
     return false;
 }
@@ -243,37 +246,75 @@ __device__ __forceinline__ int list_step(const Item& it, int x, int k)
 }
 
 // One query row over its visible rows alone, by one warp, straight from global memory; the bf16 results go into the staged
-// output row.  For the rows that the tiled product cannot answer: see the head of the file.
+// output row.  For the rows that the tiled product cannot answer: see the head of the file.  HD/8 lanes share a key/value row,
+// kRedoRows * 256/HD of them a pass (0.7 us, a round trip to L2; a row at a time, by 32 lanes, took 0.45 us a key); a pass in which
+// a score is NaN ends the row, which is NaN then.  *redone is counted up as it goes, so that the time this takes is nobody's
+// time-out.  At 2 x 16 heads of 64, 8191 positions, window 1024, a NaN that every query sees makes a call of 0.16 ms one of 10.1 ms
+// if it is in V and of 0.5 ms if it is in K.
+constexpr int kRedoRows = 4;
 template <int HD>
-__device__ __noinline__ void prefill_row_plain(const WindowParams& p, int bh, int t, uint32_t stage, int row, int lane)
+__device__ __noinline__ void prefill_row_plain(const WindowParams& p, int bh, int t, uint32_t stage, int row, int lane, uint32_t* redone)
 {
-    constexpr int PER = HD / 32;   // dims of a lane: PER * lane ..
-    const bf16* qr = p.q + ((size_t)bh * p.T + t) * HD + lane * PER;
-    const bf16* kr = p.k + (size_t)bh * p.kv_seq_stride * HD + lane * PER;
-    const bf16* vr = p.v + (size_t)bh * p.kv_seq_stride * HD + lane * PER;
-    float q[PER], acc[PER], m = kNegInf, l = 0.f;
-    for (int i = 0; i < PER; ++i) {
-        q[i] = __bfloat162float(qr[i]) * p.scale_log2;
-        acc[i] = 0.f;
+    constexpr int LPR = RowGeo<HD>::LPR, RPW = RowGeo<HD>::RPW, PASS = kRedoRows * RPW;
+    const int sub = lane % LPR, rg = lane / LPR;
+    const bf16* kr = p.k + (size_t)bh * p.kv_seq_stride * HD + sub * 8;
+    const bf16* vr = p.v + (size_t)bh * p.kv_seq_stride * HD + sub * 8;
+    float q[8];
+    unpack8(ld_plain(p.q + ((size_t)bh * p.T + t) * HD + sub * 8), q);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] *= p.scale_log2;
+    // visible row i is row i below ns and row i - ns + first from there on
+    const int first = t >= p.window ? t - p.window + 1 : 0, ns = min(p.sinks, first), n = ns + (t + 1 - first);
+    SoftmaxState st;
+    st.init();
+    for (int i0 = 0, pass = 0; i0 < n; i0 += PASS, ++pass) {
+        uint4 k[kRedoRows], v[kRedoRows];
+        float s[kRedoRows], mt = kNegInf;
+#pragma unroll
+        for (int u = 0; u < kRedoRows; ++u) {
+            const int i = i0 + u * RPW + rg;
+            k[u] = v[u] = make_uint4(0, 0, 0, 0);
+            if (i < n) {
+                const size_t at = (size_t)(i < ns ? i : i - ns + first) * HD;
+                k[u] = ld_plain(kr + at);
+                v[u] = ld_plain(vr + at);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kRedoRows; ++u) {
+            s[u] = row_sum<LPR>(dot8(q, k[u]));
+            if (i0 + u * RPW + rg >= n) s[u] = kNegInf;
+            if (s[u] == kNegInf) v[u] = make_uint4(0, 0, 0, 0);   // no weight: nothing of its value either
+            mt = fmaxf(mt, s[u]);
+        }
+        const float mn = fmaxf(st.m, mt), m_use = softmax_reference(mn), cf = ex2(st.m - m_use);
+        st.l *= cf;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) st.acc[i] *= cf;
+#pragma unroll
+        for (int u = 0; u < kRedoRows; ++u) {
+            const float pj = ex2(s[u] - m_use);
+            st.l += pj;
+            fma8(st.acc, pj, v[u]);
+        }
+        st.m = mn;
+        if (__any_sync(0xffffffffu, st.l != st.l)) break;
+        if (lane == 0 && (pass & 1023) == 1023) atomicAdd(redone, 1u);
     }
-    const int first = t >= p.window ? t - p.window + 1 : 0;
-    for (int j = 0; j <= t; ++j) {
-        if (j >= p.sinks && j < first) j = first;
-        float s = 0.f;
-        for (int i = 0; i < PER; ++i) s = fmaf(q[i], __bfloat162float(kr[(size_t)j * HD + i]), s);
-        s = row_sum<32>(s);
-        const float mn = s > m || s != s ? s : m;      // a NaN score makes the row NaN
-        const float cf = m == kNegInf ? 0.f : ex2(m - mn), pj = s == kNegInf ? 0.f : ex2(s - mn);
-        l = l * cf + pj;
-        if (s != kNegInf)
-            for (int i = 0; i < PER; ++i) acc[i] = acc[i] * cf + pj * __bfloat162float(vr[(size_t)j * HD + i]);
-        m = mn;
+    if (lane == 0) atomicAdd(redone, 1u);
+#pragma unroll
+    for (int off = LPR; off < 32; off <<= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, st.m, off), l2 = __shfl_xor_sync(0xffffffffu, st.l, off);
+        float a2[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a2[i] = __shfl_xor_sync(0xffffffffu, st.acc[i], off);
+        st.merge(m2, l2, a2);
     }
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-    for (int i = 0; i < PER; ++i) {
-        const int d = lane * PER + i;
-        const __nv_bfloat16_raw o = __float2bfloat16_rn(acc[i] * inv);
-        asm volatile("st.shared.b16 [%0], %1;" ::"r"(stage + (d >> 6) * kQBoxBytes + ((((d & 63) >> 3) ^ (row & 7)) << 4) + (d & 7) * 2), "h"(o.x) : "memory");
+    float o[8];
+    st.normalised(o);
+    if (rg == 0) {
+        const uint4 w = pack8(o);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + (sub >> 3) * kQBoxBytes + (((sub & 7) ^ (row & 7)) << 4)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
     }
 }
 
@@ -309,6 +350,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
     uint8_t* gen_tail = gen_base + (sBar - base);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen_tail + B_COUNT * 8);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_tail + B_COUNT * 8 + 8);
+    uint32_t* redone = WINDOW ? reinterpret_cast<uint32_t*>(gen_tail + B_COUNT * 8 + 12) : nullptr;
     auto bar = [&](int i) { return sBar + 8u * i; };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -317,6 +359,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
         for (int i = 0; i < B_COUNT; ++i)
             mbar_init(bar(i), (i >= B_PFULL && i < B_PFULL + 4) ? 128u : (i >= B_KEMPTY && i < B_KEMPTY + kKvStages) ? 2u : 1u);
         *abort_flag = 0;
+        if (WINDOW) *redone = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {  // this warp allocates the CTA's tensor-memory columns and frees them at the end
@@ -365,7 +408,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                 const long long item = walk_item(sched, wi);
                 const Item it = decode_item<WINDOW>(item, p);
                 auto load_q = [&](int buf, int qt) {
-                    ok = ok && mbar_wait(bar(B_QEMPTY + buf), (q_uses[buf] & 1) ^ 1, abort_flag, p.dev_status);
+                    ok = ok && mbar_wait(bar(B_QEMPTY + buf), (q_uses[buf] & 1) ^ 1, abort_flag, p.dev_status, redone);
                     if (!ok) return;
                     ++q_uses[buf];
                     mbar_expect_tx(bar(B_QFULL + buf), Q_TILE_BYTES);
@@ -375,7 +418,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                 auto load_kv = [&](int i) {
                     const int j = list_tile<WINDOW>(it, i);
                     const uint32_t st = kv_count % kKvStages, par = ((kv_count / kKvStages) & 1) ^ 1;
-                    ok = ok && mbar_wait(bar(B_KEMPTY + st), par, abort_flag, p.dev_status);
+                    ok = ok && mbar_wait(bar(B_KEMPTY + st), par, abort_flag, p.dev_status, redone);
                     if (!ok) return;
                     mbar_expect_tx(bar(B_KFULL + st), 2 * KV_TILE_BYTES);  // K and V of a stage arrive on one barrier
                     for (int bx = 0; bx < NB; ++bx)
@@ -406,7 +449,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
         {
             const int x = warp - kMmaWarp;
             auto wait_all = [&](uint32_t b, uint32_t parity) {
-                const bool r = mbar_wait(b, parity, abort_flag, p.dev_status);
+                const bool r = mbar_wait(b, parity, abort_flag, p.dev_status, redone);
                 return __all_sync(0xffffffffu, r) != 0;
             };
             uint32_t q_uses[4] = {0, 0, 0, 0};
@@ -520,7 +563,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
             for (int j = 0; j < n_kv; ++j, ++s_count) {
                 const uint32_t buf = s_count & 1;          // = j & 1 without a window: every tile takes an even number of steps
                 const uint32_t s_addr = lane_base + COL_S0 + (uint32_t)(x * 2 + buf) * BN;
-                ok = mbar_wait(bar(B_SFULL + x * 2 + buf), (s_count >> 1) & 1, abort_flag, p.dev_status);
+                ok = mbar_wait(bar(B_SFULL + x * 2 + buf), (s_count >> 1) & 1, abort_flag, p.dev_status, redone);
                 if (WINDOW) ok = __all_sync(0xffffffffu, ok) != 0;
                 if (!ok) break;
                 tc_fence_after();
@@ -593,7 +636,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                         // O still receives P(j-1) V(j-1): that product was issued when this thread's previous P tile
                         // was announced and is the (s_count - 1)-th completion on the tile's barrier.  (The product
                         // before it was complete before S(j) was announced, so the parity cannot be stale.)
-                        ok = mbar_wait(bar(B_PVDONE + x), (s_count - 1) & 1, abort_flag, p.dev_status);
+                        ok = mbar_wait(bar(B_PVDONE + x), (s_count - 1) & 1, abort_flag, p.dev_status, redone);
                         if (!__all_sync(0xffffffffu, ok)) {
                             ok = false;
                             break;
@@ -662,7 +705,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
             // From here to the named barrier below no thread leaves early: a thread whose wait ran out (ok ==
             // false; later waits then give up soon, the abort flag being up) still stages its row and meets the others, and the
             // barrier tells all 128 whether any of them failed, so that they give up at the same item.
-            if (ok) ok = mbar_wait(bar(B_OFULL + x), o_count & 1, abort_flag, p.dev_status);
+            if (ok) ok = mbar_wait(bar(B_OFULL + x), o_count & 1, abort_flag, p.dev_status, redone);
             ++o_count;
             tc_fence_after();
             const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -698,7 +741,7 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                 __syncwarp();   // a row staged by its own lane is written over by all of them: the vote does not order the two
                 while (again) {
                     const int who = __ffs(again) - 1, r = wq * 32 + who;
-                    prefill_row_plain<HD>(p, it.bh, qt * BM + r, sQ + qbuf * Q_TILE_BYTES + r * 128, r, lane);
+                    prefill_row_plain<HD>(p, it.bh, qt * BM + r, sQ + qbuf * Q_TILE_BYTES + r * 128, r, lane, redone);
                     again &= again - 1;
                 }
             }

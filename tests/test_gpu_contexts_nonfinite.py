@@ -195,3 +195,46 @@ def test_sums_visible(bt, hd, step, N, splits):
         assert not (np.abs(g - new) > rel * p + ctx.STEP * np.abs(new) + 1e-30).any(), (b, h)
         assert np.array_equal(got[b, h, n[b]:], old[b, h, n[b]:])
     assert st.item() == 0
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(400, 0), (50, 2), (70, 90)])
+@pytest.mark.parametrize("j", [0, 1, 63, 130, 299])
+def test_window_prefill_visible(bt, hd, window, sinks, j):
+    """Queries that see a bad row, and those that share a tile with it without seeing it."""
+    B, H, T = 2, 5, 300
+    cfg = bt.make_config(B, H, hd, 4, 1, T, 1)
+    q, k, v = (rnd(65, i, (B, H, T, hd)) for i in range(3))
+    poison(k, v, q, [j] * B)
+    q[:, 4, :, 9] &= 0x7FFF                   # head 4: every score is minus infinity
+    q[:, 4, :, 9] |= 0x3F80
+    k[:, 4, :, 9] = NEG_INF
+    out, st = torch.zeros((B, H, T, hd), dtype=torch.bfloat16, device="cuda"), status_word()
+    bt.bt_block_prefill_attn_window(cfg, to_dev(q), to_dev(k), to_dev(v), window, sinks, out, dev_status=st)
+    Q, K, V = f64(q), f64(k), f64(v)
+    ref, tol = np.zeros((B, H, T, hd)), np.zeros((B, H, T, hd))
+    for t in range(T):
+        seen = ctx.window_rows(t + 1, window, sinks)
+        for b in range(B):
+            for h in range(H):
+                ref[b, h, t], tol[b, h, t], *_ = attend(Q[b, h, t], K[b, h, seen], V[b, h, seen], p_bf16=True)
+    check(out, ref, tol, f"window {window} sinks {sinks} row {j}")
+    assert st.item() == 0
+
+
+def test_window_prefill_long_and_not_finite(bt):
+    """A value that every one of many queries sees: all rows of the head are worked out again over up to 131072 keys, for longer than the
+    kernel's waits last, and none of them runs out."""
+    H, hd, T = 2, 64, 131072
+    cfg = bt.make_config(1, H, hd, 4, 1, T, 1)
+    q, k, v = (gen.normal_bf16_device(66, i, (1, H, T, hd), device="cuda") for i in range(3))
+    clean, out, st = torch.empty_like(q), torch.full_like(q, 7.0), status_word()
+    bt.bt_block_prefill_attn_window(cfg, q, k, v, T, 0, clean, dev_status=st)
+    v[0, 0, 0, 3] = float("nan")
+    bt.bt_block_prefill_attn_window(cfg, q, k, v, T, 0, out, dev_status=st)
+    assert st.item() == 0
+    assert torch.isnan(out[0, 0, :, 3]).all() and torch.equal(out[0, 1], clean[0, 1])
+    others = [i for i in range(hd) if i != 3]
+    a, b = out[0, 0][:, others].double(), clean[0, 0][:, others].double()
+    # fp32 weights against bf16 ones: 2^-8 of the weighted |v|, which is below 6 everywhere, and a rounding of each result
+    assert ((a - b).abs() <= 2.0 ** -8 * 6 + 2.0 ** -7 * b.abs()).all()
