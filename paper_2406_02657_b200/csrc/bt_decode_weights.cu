@@ -20,7 +20,7 @@ __global__ void __launch_bounds__(kAddThreads) weights_add_kernel(WeightsDecodeA
     const int bh = blockIdx.x / pieces, r0 = (blockIdx.x - bh * pieces) * kAddRows;
     const int4 info = a.info[bh];   // lse, rows, appended row or -1
     const float lse = __int_as_float(info.x);
-    const int n = info.y;
+    const int n = min(info.y, a.n_max);   // an item that gave up (BT_DEV_TIMEOUT) has left whatever the workspace held
     if (r0 >= n) return;
     const size_t base = (size_t)bh * a.n_max;
     const int r = r0 + (int)threadIdx.x * 4;
