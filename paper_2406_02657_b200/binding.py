@@ -310,9 +310,14 @@ def _ws(workspace):
     return (_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
+def _i32(n):
+    """n as the C int that behaves like it: ctypes would take it modulo 2^32, and a window of 2^32 + 1 rows would be one of 1."""
+    return n if -2 ** 31 <= n < 2 ** 31 else 2 ** 31 - 1 if n > 0 else -2 ** 31
+
+
 def bt_block_decode_attn_window(cfg, cache: BlockCache, layer, q, window, sinks, out, workspace=None, dev_status=None, stream=None):
     """Decode attention over the first `sinks` and the last `window` rows of each sequence."""
-    _check(_lib.bt_block_decode_attn_window(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), window, sinks, _ptr(out),
+    _check(_lib.bt_block_decode_attn_window(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _i32(window), _i32(sinks), _ptr(out),
                                             *_ws(workspace), _ptr(dev_status), _stream(stream)), "bt_block_decode_attn_window")
 
 
@@ -320,7 +325,7 @@ def bt_block_decode_step_window(cfg, cache: BlockCache, layer, q, k_new, v_new, 
                                 stream=None):
     """Append the new block's row, then attend over the first `sinks` and the last `window` rows, in one launch."""
     _check(_lib.bt_block_decode_step_window(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(k_new), _ptr(v_new),
-                                            window, sinks, _ptr(out), *_ws(workspace), _ptr(dev_status), _stream(stream)),
+                                            _i32(window), _i32(sinks), _ptr(out), *_ws(workspace), _ptr(dev_status), _stream(stream)),
            "bt_block_decode_step_window")
 
 
@@ -328,8 +333,8 @@ def bt_block_prefill_attn_window(cfg, q, k, v, window, sinks, out, n_blocks=None
     """Prefill attention; position t sees rows j <= t with j > t - window or j < sinks."""
     n_blocks = q.shape[2] if n_blocks is None else n_blocks
     kv_seq_stride = n_blocks if kv_seq_stride is None else kv_seq_stride
-    _check(_lib.bt_block_prefill_attn_window(ctypes.byref(cfg), _ptr(q), _ptr(k), _ptr(v), n_blocks, kv_seq_stride, window, sinks,
-                                             _ptr(out), _ptr(dev_status), _stream(stream)), "bt_block_prefill_attn_window")
+    _check(_lib.bt_block_prefill_attn_window(ctypes.byref(cfg), _ptr(q), _ptr(k), _ptr(v), n_blocks, kv_seq_stride, _i32(window),
+                                             _i32(sinks), _ptr(out), _ptr(dev_status), _stream(stream)), "bt_block_prefill_attn_window")
 
 
 def bt_block_decode_attn_shared(cfg, prefix: BlockCache, cache: BlockCache, layer, q, out, workspace, dev_status=None, stream=None):
@@ -367,10 +372,10 @@ def bt_block_kv_evict(cfg, cache: BlockCache, weights, layer, n_keep, n_sinks, n
                       dst_weights=None, kept=None, dev_status=None, stream=None):
     """Cut every sequence of at least n_trigger rows to n_keep: the first n_sinks, the last n_recent and those with the largest
     sums; in place, or into the BlockCache `dst`.  Returns `kept` (allocated when not passed): int32 [B,H,n_keep]."""
-    if kept is None:
-        kept = torch.empty((cfg.batch, cfg.heads, max(n_keep, 1)), dtype=torch.int32, device=cache.k.device)
-    _check(_lib.bt_block_kv_evict(ctypes.byref(cfg), ctypes.byref(cache.c), _ptr(weights), layer, n_keep, n_trigger, n_sinks, n_recent,
-                                  None if dst is None else ctypes.byref(dst.c), _ptr(dst_weights),
+    if kept is None:   # (no memory for a call that will be refused)
+        kept = torch.empty((cfg.batch, cfg.heads, n_keep if 0 < n_keep <= 2 ** 30 else 1), dtype=torch.int32, device=cache.k.device)
+    _check(_lib.bt_block_kv_evict(ctypes.byref(cfg), ctypes.byref(cache.c), _ptr(weights), layer, _i32(n_keep), _i32(n_trigger),
+                                  _i32(n_sinks), _i32(n_recent), None if dst is None else ctypes.byref(dst.c), _ptr(dst_weights),
                                   0 if dst is None else dst.k.shape[3], _ptr(kept), *_ws(workspace), _ptr(dev_status),
                                   _stream(stream)), "bt_block_kv_evict")
     return kept

@@ -145,3 +145,16 @@ def test_definitions_agree_with_brute_force():
     assert ctx.evicted(sums, 10, 4, 0, 0) == [1, 6, 8, 9]
     assert ctx.evicted(sums, 10, 9, 0, 0) == [0, 1, 2, 3, 5, 6, 7, 8, 9]
     assert ctx.evicted(np.zeros(6, np.float32), 6, 3, 0, 1) == [0, 1, 5]
+
+
+@pytest.mark.parametrize("counts", [(2 ** 31 - 1, 0, 0), (2 ** 32 + 5, 1, 1), (5, 2 ** 32 + 1, 0), (5, 0, 2 ** 32), (-2 ** 32 + 5, 0, 0)])
+def test_evict_refuses_counts_that_no_int_holds(bt, counts):
+    """Through the binding, `kept` left to it: refused, not taken modulo 2^32 and not answered with an allocation of that many rows."""
+    import torch
+
+    cfg = bt.make_config(64, 16, 64, 4, 1, 8, 1)
+    cache = bt.BlockCache(cfg, device="cpu")
+    keep, sinks, recent = counts
+    with pytest.raises(bt.BtError) as e:
+        bt.bt_block_kv_evict(cfg, cache, torch.zeros(1, 64, 16, 8), 0, keep, sinks, recent, torch.zeros(1 << 16), stream=0)
+    assert e.value.code == bt.BT_ERR_SHAPE
