@@ -35,6 +35,14 @@ __device__ __forceinline__ uint4 ld_stream(const void* p)
 // Plain coherent 128-bit load (for memory this launch may also write).
 __device__ __forceinline__ uint4 ld_plain(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
+// 128-bit load from a shared-memory address.
+__device__ __forceinline__ uint4 lds128(uint32_t addr)
+{
+    uint4 r;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr));
+    return r;
+}
+
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -171,6 +179,20 @@ struct SoftmaxState {
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] = acc[i] * c1 + a2[i] * c2;
         m = mn;
+    }
+    // fold the states of the lanes LPR, 2 LPR, ... apart (the row groups of a warp) into one that all of them hold
+    template <int LPR>
+    __device__ __forceinline__ void merge_row_groups()
+    {
+#pragma unroll
+        for (int off = LPR; off < 32; off <<= 1) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, m, off);
+            const float l2 = __shfl_xor_sync(0xffffffffu, l, off);
+            float a2[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a2[i] = __shfl_xor_sync(0xffffffffu, acc[i], off);
+            merge(m2, l2, a2);
+        }
     }
     // log2-sum-exp: minus infinity for no weight at all, NaN for a NaN score
     __device__ __forceinline__ float lse() const { return l == 0.f ? kNegInf : m + log2f(l); }

@@ -104,12 +104,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
         ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "l"(policy)
         : "memory");
 }
-__device__ __forceinline__ uint4 lds128(uint32_t addr)
-{
-    uint4 r;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr));
-    return r;
-}
 
 // What one warp of a pair hands to the other: 8 accumulators a lane of row group 0, then maximum and sum.
 template <int HD>
@@ -535,18 +529,6 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
                 *reinterpret_cast<uint4*>(Vall + off) = vn;
             }
         }
-        // merge the RPW row groups of the warp
-        auto merge_row_groups = [&]() {
-#pragma unroll
-            for (int off = LPR; off < 32; off <<= 1) {
-                const float m2 = __shfl_xor_sync(0xffffffffu, st.m, off);
-                const float l2 = __shfl_xor_sync(0xffffffffu, st.l, off);
-                float a2[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) a2[i] = __shfl_xor_sync(0xffffffffu, st.acc[i], off);
-                st.merge(m2, l2, a2);
-            }
-        };
         auto write_out = [&]() {  // lanes of row group 0: normalised bf16 output row
             float o[8];
             st.normalised(o);
@@ -554,7 +536,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
         };
         if constexpr (GROUP > 1) {
             static_assert(GROUP == 2, "one state per group");
-            merge_row_groups();
+            st.merge_row_groups<LPR>();
             if (member > 0) {
                 if (rg == 0) {
 #pragma unroll
@@ -594,13 +576,13 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
             }
         };
         if (a.splits == 1) {
-            merge_row_groups();
+            st.merge_row_groups<LPR>();
             if (rg == 0) write_out();
             add_weights();
             if constexpr (MODE == kWeights)
                 if (w.new_row && !a.smem_rows && lane == 0) a.scores[(size_t)w.bh * a.n_max + w.n - 1] = new_score;
         } else {
-            merge_row_groups();
+            st.merge_row_groups<LPR>();
             if constexpr (MODE == kWeights)
                 if (w.new_row && lane == 0) a.scores[(size_t)w.bh * a.n_max + w.n - 1] = new_score;
 
@@ -628,7 +610,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
                     const float a2[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                     st.merge(lse, 1.f, a2);
                 }
-                merge_row_groups();
+                st.merge_row_groups<LPR>();
                 if (rg == 0) write_out();
                 add_weights();
                 if (lane == 0) a.counters[w.bh] = 0;

@@ -69,30 +69,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 
 using namespace tc;
 
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // Packed fp32 pairs (one instruction for two lanes' worth of work on sm_100).
-__device__ __forceinline__ uint64_t pack2(float lo, float hi)
-{
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
-    return d;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi)
-{
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t ffma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
 __device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b)
 {
     uint64_t d;
@@ -302,14 +279,7 @@ __device__ __noinline__ void prefill_row_plain(const WindowParams& p, int bh, in
         if (lane == 0 && (pass & 1023) == 1023) atomicAdd(redone, 1u);
     }
     if (lane == 0) atomicAdd(redone, 1u);
-#pragma unroll
-    for (int off = LPR; off < 32; off <<= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, st.m, off), l2 = __shfl_xor_sync(0xffffffffu, st.l, off);
-        float a2[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a2[i] = __shfl_xor_sync(0xffffffffu, st.acc[i], off);
-        st.merge(m2, l2, a2);
-    }
+    st.merge_row_groups<LPR>();
     float o[8];
     st.normalised(o);
     if (rg == 0) {
@@ -654,8 +624,9 @@ block_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_c
                     l *= factor;
                 }
                 // P = 2^(s*scale - m_ref) as bf16 pairs over the S columns (chunk c of P lands in columns
-                // 16c .. 16c+15; every S column is already in registers).  The row sum is taken in fp32
-                // before the rounding: the rounding errors of the terms average out in the normaliser.
+                // 16c .. 16c+15; every S column is already in registers): V is bf16, and one MMA takes operands of one
+                // type.  The row sum is taken in fp32 before the rounding (2^-8 of a weight at most): the rounding errors of
+                // the terms average out in the normaliser.
                 const float m_use = WINDOW && m_ref == kNegInf ? 0.f : m_ref;   // a row may see nothing of its first tiles
                 const uint64_t sc2 = pack2(p.scale_log2, p.scale_log2), nm2 = pack2(-m_use, -m_use);
                 uint64_t l2a = pack2(0.f, 0.f), l2b = l2a;

@@ -4,7 +4,8 @@
 // Own rows: one CTA of four warps per (sequence, head, part of the row range); the warps take alternate passes of
 // 4 x (256 / head_dim) rows and meet once, at the end, through shared memory.  (Short caches: a warp each.)  The kernel starts while the prefix kernel
 // computes (see the wait there) and streams meanwhile, so it is built to fit beside one of that kernel's CTAs: 64 registers
-// a thread and 17 KB of shared memory leave room for four CTAs there and for eight on an SM of their own.  What bounds it
+// a thread and 17 KB of shared memory leave room for four CTAs there and for eight on an SM of their own.  (At that limit every
+// form spills a little: 12 to 16 bytes a thread, 40 in the warp-per-pair form, around the pass loop.)  What bounds it
 // is bytes in flight, 4 KB a warp in single-buffered slots, and for items of a few dozen rows the instructions around
 // them (issue slots 64 % busy).  The whole call, at 512 sequences of up to 256 rows behind 8000 shared ones, 16 heads of 128,
 // and at 256 of up to 128 rows behind 2041, heads of 64: 127 and 27.3 us.  On the way there: two slots a warp and six CTAs an SM
@@ -49,12 +50,6 @@ __device__ __forceinline__ void copy_pieces(uint32_t slots, const char* k, const
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0+%3], [%1+%4], 16, %2;" ::"r"(slots), "l"(k), "l"(policy), "n"(U * 1024), "n"(AT) : "memory");
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0+%3], [%1+%4], 16, %2;" ::"r"(slots), "l"(v), "l"(policy), "n"(U * 1024 + 512), "n"(AT) : "memory");
 }
-__device__ __forceinline__ uint4 lds128(uint32_t addr)
-{
-    uint4 r;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr));
-    return r;
-}
 
 template <int HD, bool JOIN, int WPI>
 __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArgs a)
@@ -67,169 +62,169 @@ __global__ void __launch_bounds__(kThreads, 8) shared_own_kernel(SharedDecodeArg
     const int item = blockIdx.x * ITEMS + warp_of_cta / WPI, bh = item / a.splits, sp = item - bh * a.splits, b = bh / a.H;
     pdl_launch_dependents();
     if (WPI == kWarps || bh < a.B * a.H) {
-    uint64_t policy;   // the rows are read once
-    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-    int n = __ldcg(a.len + b);
-    const uint4 qr = ld_l2(reinterpret_cast<const bf16*>(a.q) + (size_t)bh * HD + sub * 8);
-    n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
-    const bool step = a.k_new != nullptr, append = step && n < a.n_max;   // a full cache takes no row: flagged, attended as it is
-    float qf[8];
-    unpack8(qr, qf);
+        uint64_t policy;   // the rows are read once
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        int n = __ldcg(a.len + b);
+        const uint4 qr = ld_l2(reinterpret_cast<const bf16*>(a.q) + (size_t)bh * HD + sub * 8);
+        n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
+        const bool step = a.k_new != nullptr, append = step && n < a.n_max;   // a full cache takes no row: flagged, attended as it is
+        float qf[8];
+        unpack8(qr, qf);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) qf[i] *= a.scale_log2;
-    SoftmaxState st;
-    st.init();
-    bf16* K = reinterpret_cast<bf16*>(a.k) + (size_t)bh * a.n_max * HD + sub * 8;
-    bf16* V = reinterpret_cast<bf16*>(a.v) + (size_t)bh * a.n_max * HD + sub * 8;
-    const int per = a.splits == 1 ? n : (n + a.splits - 1) / a.splits;
-    const int first = min(n, sp * per), end = min(n, first + per);
-    // Pass p of this warp: rows first + (warp + p * WPI) * PASS ..  A lane copies the 16-byte pieces it will read itself, so nothing
-    // but its own copies has to be waited for; its slot u holds its piece of K row u * RPW + rg, then V's.  A pass is requested
-    // as soon as the one before it is in registers.
-    const uint32_t slots = smem_u32(stages) + warp_of_cta * kStageBytes + lane * 16;
-    // A whole pass - the usual one - has no comparison and no address but the first row's.
-    auto request = [&](int r0) {
-        if (r0 < end) {
-            const char* k = reinterpret_cast<const char*>(K + (size_t)(r0 + rg) * HD);
-            const char* v = reinterpret_cast<const char*>(V + (size_t)(r0 + rg) * HD);
-            const int left = end - r0 - rg;   // rows of this lane group's column that exist from row 0 on, RPW apart
-            if (r0 + PASS <= end) {
-                copy_pieces<HD, 0>(slots, k, v, policy);
-                copy_pieces<HD, 1>(slots, k, v, policy);
-                copy_pieces<HD, 2>(slots, k, v, policy);
-                copy_pieces<HD, 3>(slots, k, v, policy);
-            } else {
-                if (left > 0) copy_pieces<HD, 0>(slots, k, v, policy);
-                if (left > RPW) copy_pieces<HD, 1>(slots, k, v, policy);
-                if (left > 2 * RPW) copy_pieces<HD, 2>(slots, k, v, policy);
-                if (left > 3 * RPW) copy_pieces<HD, 3>(slots, k, v, policy);
+        for (int i = 0; i < 8; ++i) qf[i] *= a.scale_log2;
+        SoftmaxState st;
+        st.init();
+        bf16* K = reinterpret_cast<bf16*>(a.k) + (size_t)bh * a.n_max * HD + sub * 8;
+        bf16* V = reinterpret_cast<bf16*>(a.v) + (size_t)bh * a.n_max * HD + sub * 8;
+        const int per = a.splits == 1 ? n : (n + a.splits - 1) / a.splits;
+        const int first = min(n, sp * per), end = min(n, first + per);
+        // Pass p of this warp: rows first + (warp + p * WPI) * PASS ..  A lane copies the 16-byte pieces it will read itself, so nothing
+        // but its own copies has to be waited for; its slot u holds its piece of K row u * RPW + rg, then V's.  A pass is requested
+        // as soon as the one before it is in registers.
+        const uint32_t slots = smem_u32(stages) + warp_of_cta * kStageBytes + lane * 16;
+        // A whole pass - the usual one - has no comparison and no address but the first row's.
+        auto request = [&](int r0) {
+            if (r0 < end) {
+                const char* k = reinterpret_cast<const char*>(K + (size_t)(r0 + rg) * HD);
+                const char* v = reinterpret_cast<const char*>(V + (size_t)(r0 + rg) * HD);
+                const int left = end - r0 - rg;   // rows of this lane group's column that exist from row 0 on, RPW apart
+                if (r0 + PASS <= end) {
+                    copy_pieces<HD, 0>(slots, k, v, policy);
+                    copy_pieces<HD, 1>(slots, k, v, policy);
+                    copy_pieces<HD, 2>(slots, k, v, policy);
+                    copy_pieces<HD, 3>(slots, k, v, policy);
+                } else {
+                    if (left > 0) copy_pieces<HD, 0>(slots, k, v, policy);
+                    if (left > RPW) copy_pieces<HD, 1>(slots, k, v, policy);
+                    if (left > 2 * RPW) copy_pieces<HD, 2>(slots, k, v, policy);
+                    if (left > 3 * RPW) copy_pieces<HD, 3>(slots, k, v, policy);
+                }
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        uint64_t q2[4], acc2[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            q2[i] = pack2(qf[2 * i], qf[2 * i + 1]);
+            acc2[i] = pack2(0.f, 0.f);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    uint64_t q2[4], acc2[4];
+        auto one_pass = [&](int r0, auto whole) {
+            uint4 kr[kUnroll], vr[kUnroll];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        q2[i] = pack2(qf[2 * i], qf[2 * i + 1]);
-        acc2[i] = pack2(0.f, 0.f);
-    }
-    auto one_pass = [&](int r0, auto whole) {
-        uint4 kr[kUnroll], vr[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            kr[u] = lds128(slots + u * 1024);
-            vr[u] = lds128(slots + u * 1024 + 512);
-        }
-        // The pieces have to be read before their slots are written again.  The empty statement keeps the compiler from moving a read
-        // down; what orders the reads before the asynchronous writes is the warp's barrier.
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) asm volatile("" ::"r"(kr[u].x), "r"(vr[u].x) : "memory");
-        __syncwarp();
-        request(r0 + WPI * PASS);
-        float s[kUnroll], mt = kNegInf;
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            s[u] = row_sum<LPR>(dot8_x2(q2, kr[u]));
-            if (!whole && r0 + u * RPW + rg >= end) {   // no such row: its slots hold anything
-                s[u] = kNegInf;
-                vr[u] = make_uint4(0, 0, 0, 0);
+            for (int u = 0; u < kUnroll; ++u) {
+                kr[u] = lds128(slots + u * 1024);
+                vr[u] = lds128(slots + u * 1024 + 512);
             }
-            mt = fmaxf(mt, s[u]);
-        }
-        const float mn = fmaxf(st.m, mt), m_use = softmax_reference(mn);   // this row group may have no row yet
-        const float cf = ex2(st.m - m_use);
-        st.l *= cf;
-        const uint64_t cf2 = pack2(cf, cf);
+            // The pieces have to be read before their slots are written again.  The empty statement keeps the compiler from moving a read
+            // down; what orders the reads before the asynchronous writes is the warp's barrier.
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc2[i] = fmul2(acc2[i], cf2);
+            for (int u = 0; u < kUnroll; ++u) asm volatile("" ::"r"(kr[u].x), "r"(vr[u].x) : "memory");
+            __syncwarp();
+            request(r0 + WPI * PASS);
+            float s[kUnroll], mt = kNegInf;
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const float p = ex2(s[u] - m_use);
-            st.l += p;
-            fma8_x2(acc2, p, vr[u]);
-        }
-        st.m = mn;
-    };
-    int r0 = first + warp * PASS;
-    request(r0);
-    for (; r0 < end; r0 += WPI * PASS) {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        if (r0 + PASS <= end) one_pass(r0, std::true_type());
-        else one_pass(r0, std::false_type());
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) unpack2(acc2[i], st.acc[2 * i], st.acc[2 * i + 1]);
-    merge_row_groups<LPR>(st);
-    if constexpr (WPI > 1) {
-        static_assert(WPI == kWarps, "the barrier is the CTA's");
-        if (warp > 0 && rg == 0) {
-            float* mine = sm_state[warp - 1];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) mine[sub * 8 + i] = st.acc[i];
-            if (sub == 0) {
-                mine[HD] = st.m;
-                mine[HD + 1] = st.l;
+            for (int u = 0; u < kUnroll; ++u) {
+                s[u] = row_sum<LPR>(dot8_x2(q2, kr[u]));
+                if (!whole && r0 + u * RPW + rg >= end) {   // no such row: its slots hold anything
+                    s[u] = kNegInf;
+                    vr[u] = make_uint4(0, 0, 0, 0);
+                }
+                mt = fmaxf(mt, s[u]);
             }
+            const float mn = fmaxf(st.m, mt), m_use = softmax_reference(mn);   // this row group may have no row yet
+            const float cf = ex2(st.m - m_use);
+            st.l *= cf;
+            const uint64_t cf2 = pack2(cf, cf);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc2[i] = fmul2(acc2[i], cf2);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const float p = ex2(s[u] - m_use);
+                st.l += p;
+                fma8_x2(acc2, p, vr[u]);
+            }
+            st.m = mn;
+        };
+        int r0 = first + warp * PASS;
+        request(r0);
+        for (; r0 < end; r0 += WPI * PASS) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (r0 + PASS <= end) one_pass(r0, std::true_type());
+            else one_pass(r0, std::false_type());
         }
-        __syncthreads();
-    }
-    if (warp == 0) {
-        // the length goes up once all of the sequence's items - every warp of them: hence behind the barrier - have read the old one
-        int arrival = -1;
-        if (step && lane == 0) arrival = atomicAdd(a.counters + (size_t)a.B * a.H + b, 1);
-        if (rg > 0) st.init();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack2(acc2[i], st.acc[2 * i], st.acc[2 * i + 1]);
+        st.merge_row_groups<LPR>();
         if constexpr (WPI > 1) {
-            for (int w = rg; w < kWarps - 1; w += RPW) {   // row group rg joins warps rg + 1, rg + 1 + RPW, ...
-                float a2[8];
+            static_assert(WPI == kWarps, "the barrier is the CTA's");
+            if (warp > 0 && rg == 0) {
+                float* mine = sm_state[warp - 1];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) a2[i] = sm_state[w][sub * 8 + i];
-                st.merge(sm_state[w][HD], sm_state[w][HD + 1], a2);
+                for (int i = 0; i < 8; ++i) mine[sub * 8 + i] = st.acc[i];
+                if (sub == 0) {
+                    mine[HD] = st.m;
+                    mine[HD + 1] = st.l;
+                }
             }
+            __syncthreads();
         }
-        if (append && sp == a.splits - 1) {   // the new row: scored by row group 0 from the caller's buffer, stored into the cache
-            const uint4 kn = ld_l2(reinterpret_cast<const bf16*>(a.k_new) + (size_t)bh * HD + sub * 8);
-            const uint4 vn = ld_l2(reinterpret_cast<const bf16*>(a.v_new) + (size_t)bh * HD + sub * 8);
-            const float sn = row_sum<LPR>(dot8(qf, kn));
-            if (rg == 0) {
-                float one_row[8];
-                unpack8(vn, one_row);
-                st.merge(sn, 1.f, one_row);
-                *reinterpret_cast<uint4*>(K + (size_t)n * HD) = kn;
-                *reinterpret_cast<uint4*>(V + (size_t)n * HD) = vn;
+        if (warp == 0) {
+            // the length goes up once all of the sequence's items - every warp of them: hence behind the barrier - have read the old one
+            int arrival = -1;
+            if (step && lane == 0) arrival = atomicAdd(a.counters + (size_t)a.B * a.H + b, 1);
+            if (rg > 0) st.init();
+            if constexpr (WPI > 1) {
+                for (int w = rg; w < kWarps - 1; w += RPW) {   // row group rg joins warps rg + 1, rg + 1 + RPW, ...
+                    float a2[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) a2[i] = sm_state[w][sub * 8 + i];
+                    st.merge(sm_state[w][HD], sm_state[w][HD + 1], a2);
+                }
             }
-        }
-        merge_row_groups<LPR>(st);
-        float o[8];
-        st.normalised(o);
-        const int count = a.n_pre + a.splits;
-        if constexpr (JOIN) {   // splits == 1
-            pdl_wait();         // the prefix's partials are complete and visible from here on
-            // this item's own one is the last of them: row group rg folds partials rg, rg + RPW, ...
-            const float lse = st.lse();
-            st.init();
-            const float* all = a.parts + (size_t)bh * count * (HD + 4);
-            if (rg < a.n_pre) fold_partials<HD, 4>(st, all + (size_t)rg * (HD + 4), (a.n_pre - rg + RPW - 1) / RPW, RPW, sub);
-            if (rg == RPW - 1) st.merge(lse, 1.f, o);
-            merge_row_groups<LPR>(st);
+            if (append && sp == a.splits - 1) {   // the new row: scored by row group 0 from the caller's buffer, stored into the cache
+                const uint4 kn = ld_l2(reinterpret_cast<const bf16*>(a.k_new) + (size_t)bh * HD + sub * 8);
+                const uint4 vn = ld_l2(reinterpret_cast<const bf16*>(a.v_new) + (size_t)bh * HD + sub * 8);
+                const float sn = row_sum<LPR>(dot8(qf, kn));
+                if (rg == 0) {
+                    float one_row[8];
+                    unpack8(vn, one_row);
+                    st.merge(sn, 1.f, one_row);
+                    *reinterpret_cast<uint4*>(K + (size_t)n * HD) = kn;
+                    *reinterpret_cast<uint4*>(V + (size_t)n * HD) = vn;
+                }
+            }
+            st.merge_row_groups<LPR>();
+            float o[8];
             st.normalised(o);
-            if (rg == 0) *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)bh * HD + sub * 8) = pack8(o);
-        } else if (rg == 0) {
-            float* mine = a.parts + ((size_t)bh * count + a.n_pre + sp) * (HD + 4);
-            *reinterpret_cast<float4*>(mine + sub * 8) = make_float4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<float4*>(mine + sub * 8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
-            if (sub == 0) mine[HD] = st.lse();
-        }
-        if (lane == 0) {
-            if (bh == b * a.H && sp == 0) {
-                if (n == 0 && !append && __ldcg(a.prefix_len) <= 0) raise_status(a.dev_status, BT_DEV_EMPTY);
-                if (step && !append) raise_status(a.dev_status, BT_DEV_OVERFLOW);
+            const int count = a.n_pre + a.splits;
+            if constexpr (JOIN) {   // splits == 1
+                pdl_wait();         // the prefix's partials are complete and visible from here on
+                // this item's own one is the last of them: row group rg folds partials rg, rg + RPW, ...
+                const float lse = st.lse();
+                st.init();
+                const float* all = a.parts + (size_t)bh * count * (HD + 4);
+                if (rg < a.n_pre) fold_partials<HD, 4>(st, all + (size_t)rg * (HD + 4), (a.n_pre - rg + RPW - 1) / RPW, RPW, sub);
+                if (rg == RPW - 1) st.merge(lse, 1.f, o);
+                st.merge_row_groups<LPR>();
+                st.normalised(o);
+                if (rg == 0) *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + (size_t)bh * HD + sub * 8) = pack8(o);
+            } else if (rg == 0) {
+                float* mine = a.parts + ((size_t)bh * count + a.n_pre + sp) * (HD + 4);
+                *reinterpret_cast<float4*>(mine + sub * 8) = make_float4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<float4*>(mine + sub * 8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
+                if (sub == 0) mine[HD] = st.lse();
             }
-            if (arrival == a.H * a.splits - 1) {
-                if (append) a.len[b] = n + 1;
-                a.counters[(size_t)a.B * a.H + b] = 0;
+            if (lane == 0) {
+                if (bh == b * a.H && sp == 0) {
+                    if (n == 0 && !append && __ldcg(a.prefix_len) <= 0) raise_status(a.dev_status, BT_DEV_EMPTY);
+                    if (step && !append) raise_status(a.dev_status, BT_DEV_OVERFLOW);
+                }
+                if (arrival == a.H * a.splits - 1) {
+                    if (append) a.len[b] = n + 1;
+                    a.counters[(size_t)a.B * a.H + b] = 0;
+                }
             }
         }
-    }
     }
     // this grid's end has to imply the prefix kernel's; one waiting CTA is enough for that
     if (JOIN || blockIdx.x == gridDim.x - 1) pdl_wait();

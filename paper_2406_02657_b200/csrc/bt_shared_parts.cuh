@@ -38,21 +38,6 @@ __device__ __forceinline__ void fold_partials(SoftmaxState& st, const float* ws,
     }
 }
 
-template <int LPR>
-__device__ __forceinline__ void merge_row_groups(SoftmaxState& st)
-{
-#pragma unroll
-    for (int off = LPR; off < 32; off <<= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, st.m, off);
-        const float l2 = __shfl_xor_sync(0xffffffffu, st.l, off);
-        float a2[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a2[i] = __shfl_xor_sync(0xffffffffu, st.acc[i], off);
-        st.merge(m2, l2, a2);
-    }
-}
-
-
 // The lane's 8 dims of the joined result of one (sequence, head).
 template <int HD>
 __device__ __forceinline__ void join(const SharedDecodeArgs& a, int bh, int sub)
