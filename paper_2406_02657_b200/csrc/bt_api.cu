@@ -507,6 +507,14 @@ bt_status bt_block_decode_step_shared(const bt_config* cfg, const bt_block_cache
 // Ways the row range is split when weights are summed.  Where the plain calls split, this one's workspace has room for
 // as many parts as fill the kernel's seven warps on each of 148 SMs (86.8 us at 4 x 16 heads of 16384 rows, head_dim 128, in 16
 // parts; 91.5 us in the plain calls' 8, two warps on each), each of at least 128 rows.
+//   Short caches of few pairs are cut like the plain calls' too, and then pay a second launch, although a single one with the
+// scores in shared memory is shorter up to 128 rows of head_dim 64 or 64 rows of 128.  Replayed back to back from a graph, us, as cut here / in one piece
+// (decode_splits = 1):
+//     rows:                    32          64          128         256         512
+//     32 pairs, head_dim 64    7.0 / 3.4   7.0 / 4.1   7.3 / 5.3   7.5 / 8.1   8.2 / 13.9
+//     32 pairs, head_dim 128   7.7 / 4.0   7.8 / 5.4   7.8 / 8.1   8.1 / 14.1  9.8 / 25.8
+//     256 pairs, head_dim 64   7.8 / 3.8   7.7 / 4.4   8.0 / 5.6   9.1 / 8.4   10.2 / 14.5
+//     256 pairs, head_dim 128  8.4 / 4.3   8.6 / 5.6   9.1 / 8.5   11.3 / 14.7 14.3 / 26.5
 static int weights_splits(const bt_config* cfg)
 {
     const int base = choose_splits(cfg);

@@ -1,23 +1,24 @@
 // bt_block_kv_evict: per (sequence, head), keep the first rows, the last rows and those with the largest summed
 // attention weights, in their order, and move them together.
 //
-// Selection works on order-preserving 32-bit keys in registers and finds the smallest key that stays.  Ties go to the lowest
-// index, so the result does not depend on the order of any atomic.
-//   A warp alone (select_rows_warp, up to 1024 rows): bisection, one bit a step from the top, each step 32 compares and
-//   a warp reduction; it ends as soon as the count is the number wanted, long before the last bit if sums are distinct.
-//   A CTA (select_rows): a radix select over digits of 12, 10 and 10 bits.  The first digit holds the exponent and three
-//   bits more: real sums crowd into few exponents, and with an 8-bit digit the lanes of a warp met in the same bins (35 us
-//   for 16384 rows; bisection with a barrier per step took as long).  Counts per warp and register,
-//   scanned, then place every row.
+// Selection (select_rows, by one CTA) works on order-preserving 32-bit keys in registers and finds the smallest key that
+// stays.  Ties go to the lowest index, so the result does not depend on the order of any atomic.  A histogram of the keys' first
+// digit finds the bin that the smallest key lies in.  The digit is 12 bits (10 in the fused kernel, whose shared memory is smaller), which holds
+// the exponent and some mantissa: real sums crowd into few exponents, and with an 8-bit digit the lanes of a warp met in the same
+// bins (35 us for 16384 rows; bisection with a barrier per step took as long).  If no more keys fell into that bin than the CTA has
+// threads - the usual case - they are gathered, one per thread, and the rest goes bit by bit, a counting barrier each, until the
+// count is the number wanted.  Else (many equal or close sums) the next digit of the keys in the bin is taken the same way, down to
+// the last bits.  Counts per thread, scanned, then place every row.
 //
 // Moving: rows travel in 16-byte pieces through registers.  Into another cache all pieces are independent.  In place, row
 // i of the result comes from row list[i] >= i, and list grows: a chunk is read, its readers meet, and only then is it
 // written.  What a chunk writes (rows <= its own sources) is below every source of a later chunk, so one barrier per
 // chunk is enough.
 //
-// Two shapes.  Many (sequence, head) pairs with short caches: a warp selects and moves a pair by itself, one launch, no
-// barriers.  Else a launch with a CTA per pair selects, and a second one moves with several CTAs per pair - in place, a
-// cluster of them that meets once per chunk; into another cache, with few pairs, the first launch moves the last rows meanwhile.
+// Two shapes.  Many (sequence, head) pairs with short caches: a CTA of 128 threads selects and moves a pair, one launch
+// (evict_fused_kernel).  Else a launch with a CTA per pair selects, and a second one moves with several CTAs per pair - in place, a
+// cluster of them that meets once per chunk.  Into another cache, with few pairs, the first launch has a second CTA per pair that
+// moves the last rows meanwhile (evict_select_move_kernel).
 //
 // Bound by HBM: the kept rows are read and written once, the sums read once.
 #include "bt_common.cuh"
@@ -335,7 +336,7 @@ __device__ __forceinline__ void select_pair(const EvictArgs& a, int bh)
         for (int i = threadIdx.x; i < a.n_keep; i += THREADS) list[i] = -1;
 }
 
-// At 46 registers a thread the moving launch's CTAs find room beside these before they have ended (in place, 64 pairs: 69 us;
+// At 47 or 48 registers a thread the moving launch's CTAs find room beside these before they have ended (in place, 64 pairs: 69 us;
 // at 61 registers 83 us).
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a)
