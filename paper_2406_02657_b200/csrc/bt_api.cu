@@ -505,8 +505,8 @@ bt_status bt_block_decode_step_shared(const bt_config* cfg, const bt_block_cache
 }
 
 // Ways the row range is split when weights are summed.  Where the plain calls split, this one's workspace has room for
-// as many parts as fill the kernel's seven warps on each of 148 SMs (86.8 us at 4 x 16 heads of 16384 rows, head_dim 128, in 16
-// parts; 91.5 us in the plain calls' 8, two warps on each), each of at least 128 rows.
+// as many parts as fill the kernel's seven warps on each of 148 SMs (84.6 us at 4 x 16 heads of 12001 to 16384 rows, head_dim 128, in 16
+// parts; in the plain calls' 8, two warps on each, it was 91.5 when this was 86.8), each of at least 128 rows.
 //   Short caches of few pairs are cut like the plain calls' too, and then pay a second launch, although a single one with the
 // scores in shared memory is shorter up to 128 rows of head_dim 64 or 64 rows of 128.  Replayed back to back from a graph, us, as cut here / in one piece
 // (decode_splits = 1):

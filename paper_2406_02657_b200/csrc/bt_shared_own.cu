@@ -8,7 +8,7 @@
 // form spills a little: 12 to 16 bytes a thread, 40 in the warp-per-pair form, around the pass loop.)  What bounds it
 // is bytes in flight, 4 KB a warp in single-buffered slots, and for items of a few dozen rows the instructions around
 // them (issue slots 64 % busy).  The whole call, at 512 sequences of up to 256 rows behind 8000 shared ones, 16 heads of 128,
-// and at 256 of up to 128 rows behind 2041, heads of 64: 127 and 27.3 us.  On the way there: two slots a warp and six CTAs an SM
+// and at 256 of up to 128 rows behind 2041, heads of 64: 127 and 26.9 us.  On the way there: two slots a warp and six CTAs an SM
 // 134 against 130 and 32.3 against 30.2 us; a persistent form with requests running ahead 159 and 32.5 us (twelve warps
 // beside the prefix kernel cannot keep enough in flight); the ring of the plain decode calls 145 and 29.9 us (its CTAs need an
 // SM each, so the two kernels follow each other).

@@ -21,7 +21,7 @@
 //
 // What bounds it: with 2041 rows a chain of four tiles per warpgroup and the launch around it (12 us of the call's 27 at 256
 // sequences, 16 heads of 64); with 8000 rows of head_dim 128 the tensor pipe at 39 % and the softmax chain between its products
-// (52 us alone, 512 sequences; about 60 us beside the own rows' stream, which is what the call then takes: 125 us).
+// (52 us alone, 512 sequences; about 60 us beside the own rows' stream; that stream is what the call's 127 us are).
 #include <cuda.h>
 
 #include "bt_common.cuh"
