@@ -865,7 +865,11 @@ static cudaError_t launch_t(const PrefillArgs& a, int window, int sinks, uint32_
     // one persistent CTA per SM
     long long grid = p.n_items < sms ? p.n_items : sms;
     static thread_local Schedule sc;  // 8 KB: passed to the kernel by value
-    cached_schedule(&sc, slabs, p.n_qtiles, p.n_classes, (int)grid, HD, a.T, WINDOW ? window : 0, WINDOW ? sinks : 0);
+    try {
+        cached_schedule(&sc, slabs, p.n_qtiles, p.n_classes, (int)grid, HD, a.T, WINDOW ? window : 0, WINDOW ? sinks : 0);
+    } catch (...) {   // no host memory for a table: the round robin needs none, and nothing may be thrown through the C interface
+        sc.use_table = 0;
+    }
     if (!sc.use_table) {
         // no table: a grid size coprime to the number of classes makes every CTA cycle through all classes
         // (heavy and light items alike)
