@@ -441,7 +441,8 @@ __global__ void __launch_bounds__(kMaxThreads, 1) block_decode_ring_kernel(ArgsO
             };
             auto refill = [&]() {
                 ++consumed;
-                // the loaded values must be in registers, not merely requested, before the stage is overwritten
+                // The stage has to be read before it is written again.  The empty statement keeps the compiler from moving a read
+                // down; what orders the lanes' reads before the copy that lane 0 requests is the warp's barrier.
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) asm volatile("" ::"r"(kr[u].x), "r"(vr[u].x) : "memory");
                 __syncwarp();
