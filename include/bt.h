@@ -357,6 +357,61 @@ bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* 
                             int32_t* kept, void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream);
 
 /*
+ * ---- The block cache in 4 bits.  The paper keeps K and V as they are computed; decoding is bound by reading them (appendix
+ * E.2).  Held in 4 bits a row takes 1.125 hd bytes instead of 4 hd.
+ *
+ * What a row is held as: for every 32 dimensions a step s = bf16(max|x| / 7) and codes u = round(x / s), halves away from zero
+ * (-7 <= u <= 7); its value is s u.  Where s would be below 2^-126 the 32 values are held as zeros; where one of them is
+ * not finite all 32 are held as NaN.
+ *   kv  : uint8 [n_layers][B][H][ceil(N_max / 16)][hd / 64][BT_KV4_TILE_BYTES], 16-byte aligned; the last 16 rows may be there in
+ *         part only, and their tiles are whole nevertheless.  A tile holds 16 rows x 64 dimensions of K and V:
+ *           bytes    0 ..  511  K codes, 32 bytes a row: u + 8, dimension 2i in the low half of byte i, 2i + 1 in the high half
+ *           bytes  512 .. 1023  V codes
+ *           bytes 1024 .. 1087  K steps, two bf16 a row
+ *           bytes 1088 .. 1151  V steps
+ *   len : int32 [n_layers][B]
+ * It needs no initialisation but the lengths.  N_max is at most 2^30 for these calls (else BT_ERR_UNSUPPORTED).
+ */
+#define BT_KV4_TILE_BYTES 1152
+typedef struct bt_block_cache_kv4 {
+    void* kv;
+    int32_t* len;
+} bt_block_cache_kv4;
+
+/*
+ * Rows quantised as they are written: k_new, v_new bf16, slab (b,h) src_stride rows after the one before it (n_new for packed
+ * [B][H][n_new][hd]; N_max to take the first rows of a bf16 block cache, whose kv_seq_stride that is), src_stride >= n_new.
+ * Otherwise as bt_block_kv_append, but that with reset_first != 0 every sequence starts anew: the rows become rows
+ * 0 .. n_new-1 and len[b] = n_new, whatever it was.  One launch (two for many rows without reset_first).
+ */
+bt_status bt_block_kv4_append(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* k_new, const void* v_new,
+                              int n_new, int64_t src_stride, int reset_first, uint32_t* dev_status, void* stream);
+
+/*
+ * Rows read back: rows first .. first+n_rows-1 of every (sequence, head), as far as they are below len[b], go to rows 0 .. of
+ * k_out, v_out (bf16, slabs dst_stride >= n_rows rows apart), s u rounded to bf16.  Rows of k_out, v_out for which there is no row in the
+ * cache are left as they are.  first >= 0, n_rows >= 1 (else BT_ERR_SHAPE), first + n_rows <= N_max (else BT_ERR_CAPACITY).
+ */
+bt_status bt_block_kv4_read(const bt_config* cfg, const bt_block_cache_kv4* cache, int layer, int first, int n_rows, void* k_out,
+                            void* v_out, int64_t dst_stride, void* stream);
+
+/*
+ * bt_block_decode_attn and bt_block_decode_step over the 4-bit cache: K and V are the values s u, in fp32 arithmetic; the weights
+ * meet V as sums of two bf16 (2^-17 of a weight off at most).  The step quantises the new row, stores it and attends over it as it is
+ * stored: it gives what bt_block_kv4_append and bt_block_decode_attn_kv4 give.
+ * Values that are not finite: as for the contexts calls above, where a NaN in V is in all 32 dimensions of its step, and a score is
+ * NaN where the query holds an infinity and the row a code of 0 in that dimension.
+ * workspace: required, bt_workspace_bytes_kv4 bytes (0 on an invalid config), initialised by bt_workspace_init under the same
+ * config; one call at a time.  Other arguments and errors as for bt_block_decode_attn / bt_block_decode_step.
+ */
+size_t bt_workspace_bytes_kv4(const bt_config* cfg);
+bt_status bt_block_decode_attn_kv4(const bt_config* cfg, const bt_block_cache_kv4* cache, int layer, const void* q, void* out,
+                                   void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream);
+bt_status bt_block_decode_step_kv4(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* q, const void* k_new,
+                                   const void* v_new, void* out, void* workspace, size_t workspace_bytes, uint32_t* dev_status,
+                                   void* stream);
+
+/*
  * One block-decoder decode step of one layer driven from HOST buffers (bt_block_decode_step with
  * the copies around it, section 2.3): q_host, k_new_host,
  * v_new_host [B][H][hd] bf16 are copied to the caller's device staging buffers q_dev, k_dev,
@@ -410,6 +465,42 @@ bt_status bt_block_qkv_project_append(const bt_config* cfg, bt_block_cache* cach
 bt_status bt_local_qkv_project_append(const bt_config* cfg, bt_local_cache* cache, int layer, const void* x,
                                       int n_rows, const void* w_qkv, const void* bias, int reset_first,
                                       const uint8_t* reset_mask, void* q_out, uint32_t* dev_status, void* stream);
+
+/*
+ * bt_block_qkv_project_append into the 4-bit cache: K and V, rounded to bf16, are quantised by the product's epilogue, and the cache
+ * holds what bt_block_kv4_append would have made of them.
+ */
+bt_status bt_block_qkv_project_append_kv4(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* x, int n_rows,
+                                          const void* w_qkv, const void* bias, void* q_out, uint32_t* dev_status, void* stream);
+
+/*
+ * ---- The same linear maps in 8-bit integers, with a step for each token and each output feature.
+ *
+ * Rows quantised: x bf16 [n_rows][n_cols] (activations: a row per token; weights: a row per output feature), for each row
+ *   steps[r] = bf16(max|x[r]| / 127) (fp32),  x8[r][c] = round(x[r][c] / steps[r]), halves away from zero (int8, -127 .. 127).
+ * A step that would be below 2^-126 is 0, and its codes 0; a row with a value that is not finite has a NaN step and codes of 0.
+ * x, x8 16-byte aligned, n_cols a multiple of 16 up to 2048 (else BT_ERR_UNSUPPORTED), n_rows and n_cols >= 1 (else BT_ERR_SHAPE).
+ */
+bt_status bt_rows_quantize_i8(const void* x, int64_t n_rows, int n_cols, void* x8, float* steps, void* stream);
+
+/*
+ * bt_prefix_project, bt_block_qkv_project_append, bt_local_qkv_project_append and bt_block_qkv_project_append_kv4 with x and w as
+ * int8 (x8: [rows][D]; w8: [features][D]; any of -128 .. 127) and their steps (x_steps fp32 [rows], w_steps fp32 [features], both
+ * required and 16-byte aligned):
+ *   y[m][n] = (sum_k x8[m][k] w8[n][k]) * (x_steps[m] * w_steps[n]) + bias[n],
+ * the sum exact, the rest in fp32, then rounded to bf16.  bias: bf16 or NULL.  Everything else is as for those calls.
+ */
+bt_status bt_prefix_project_i8(const bt_config* cfg, const void* ctx8, const float* ctx_steps, const void* w8, const float* w_steps,
+                               const void* bias, void* prefix_out, uint32_t* dev_status, void* stream);
+bt_status bt_block_qkv_project_append_i8(const bt_config* cfg, bt_block_cache* cache, int layer, const void* x8, const float* x_steps,
+                                         int n_rows, const void* w8, const float* w_steps, const void* bias, void* q_out,
+                                         uint32_t* dev_status, void* stream);
+bt_status bt_local_qkv_project_append_i8(const bt_config* cfg, bt_local_cache* cache, int layer, const void* x8, const float* x_steps,
+                                         int n_rows, const void* w8, const float* w_steps, const void* bias, int reset_first,
+                                         const uint8_t* reset_mask, void* q_out, uint32_t* dev_status, void* stream);
+bt_status bt_block_qkv_project_append_i8_kv4(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* x8,
+                                             const float* x_steps, int n_rows, const void* w8, const float* w_steps, const void* bias,
+                                             void* q_out, uint32_t* dev_status, void* stream);
 
 /*
  * Self-test of the bounded waits (test support; the paper has no counterpart).  Every wait inside the

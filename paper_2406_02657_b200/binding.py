@@ -26,6 +26,9 @@ EXPORTS = [
     "bt_workspace_bytes_shared", "bt_workspace_bytes_weights", "bt_block_decode_attn_window", "bt_block_decode_step_window",
     "bt_block_prefill_attn_window", "bt_block_decode_attn_shared", "bt_block_decode_step_shared",
     "bt_block_decode_attn_weights", "bt_block_decode_step_weights", "bt_block_kv_evict",
+    "bt_workspace_bytes_kv4", "bt_block_kv4_append", "bt_block_kv4_read", "bt_block_decode_attn_kv4", "bt_block_decode_step_kv4",
+    "bt_block_qkv_project_append_kv4", "bt_rows_quantize_i8", "bt_prefix_project_i8", "bt_block_qkv_project_append_i8",
+    "bt_local_qkv_project_append_i8", "bt_block_qkv_project_append_i8_kv4",
 ]
 
 
@@ -41,6 +44,10 @@ class bt_block_cache(ctypes.Structure):
 
 
 class bt_local_cache(ctypes.Structure):
+    _fields_ = [("kv", ctypes.c_void_p), ("len", ctypes.c_void_p)]
+
+
+class bt_block_cache_kv4(ctypes.Structure):
     _fields_ = [("kv", ctypes.c_void_p), ("len", ctypes.c_void_p)]
 
 
@@ -91,9 +98,21 @@ def _load() -> ctypes.CDLL:
     lib.bt_block_decode_attn_weights.argtypes = [cfgp, cachep, i32, vp, vp, vp, vp, vp, u64, vp, vp]
     lib.bt_block_decode_step_weights.argtypes = [cfgp, cachep, i32, vp, vp, vp, vp, vp, vp, vp, u64, vp, vp]
     lib.bt_block_kv_evict.argtypes = [cfgp, cachep, vp, i32, i32, i32, i32, i32, cachep, vp, i32, vp, vp, u64, vp, vp]
+    kv4p, localp, i64 = ctypes.POINTER(bt_block_cache_kv4), ctypes.POINTER(bt_local_cache), ctypes.c_int64
+    lib.bt_workspace_bytes_kv4.argtypes = [cfgp]
+    lib.bt_block_kv4_append.argtypes = [cfgp, kv4p, i32, vp, vp, i32, i64, i32, vp, vp]
+    lib.bt_block_kv4_read.argtypes = [cfgp, kv4p, i32, i32, i32, vp, vp, i64, vp]
+    lib.bt_block_decode_attn_kv4.argtypes = [cfgp, kv4p, i32, vp, vp, vp, u64, vp, vp]
+    lib.bt_block_decode_step_kv4.argtypes = [cfgp, kv4p, i32, vp, vp, vp, vp, vp, u64, vp, vp]
+    lib.bt_block_qkv_project_append_kv4.argtypes = [cfgp, kv4p, i32, vp, i32, vp, vp, vp, vp, vp]
+    lib.bt_rows_quantize_i8.argtypes = [vp, i64, i32, vp, vp, vp]
+    lib.bt_prefix_project_i8.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.bt_block_qkv_project_append_i8.argtypes = [cfgp, cachep, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.bt_local_qkv_project_append_i8.argtypes = [cfgp, localp, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.bt_block_qkv_project_append_i8_kv4.argtypes = [cfgp, kv4p, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     for name in EXPORTS[4:]:
         getattr(lib, name).restype = ctypes.c_int
-    for name in ("bt_workspace_bytes_shared", "bt_workspace_bytes_weights"):
+    for name in ("bt_workspace_bytes_shared", "bt_workspace_bytes_weights", "bt_workspace_bytes_kv4"):
         getattr(lib, name).restype = ctypes.c_size_t
     return lib
 
@@ -160,6 +179,20 @@ class LocalCache:
                               device=device)
         self.len = torch.zeros((cfg.n_layers, cfg.batch), dtype=torch.int32, device=device)
         self.c = bt_local_cache(self.kv.data_ptr(), self.len.data_ptr())
+
+
+KV4_TILE_ROWS, KV4_TILE_BYTES = 16, 1152
+
+
+class BlockCacheKV4:
+    """Caller-owned block KV cache in 4 bits: kv uint8 [layers,B,H,ceil(N_max/16),hd/64,1152], len int32 [layers,B]."""
+
+    def __init__(self, cfg: bt_config, device="cuda", kv=None, length=None):
+        shape = (cfg.n_layers, cfg.batch, cfg.heads, -(-cfg.max_blocks // KV4_TILE_ROWS), cfg.head_dim // 64, KV4_TILE_BYTES)
+        self.kv = torch.zeros(shape, dtype=torch.uint8, device=device) if kv is None else kv
+        self.len = torch.zeros((cfg.n_layers, cfg.batch), dtype=torch.int32, device=device) if length is None else length
+        assert self.kv.shape == shape and self.kv.is_contiguous() and self.len.is_contiguous()
+        self.c = bt_block_cache_kv4(self.kv.data_ptr(), self.len.data_ptr())
 
 
 def bt_version() -> int:
@@ -379,6 +412,92 @@ def bt_block_kv_evict(cfg, cache: BlockCache, weights, layer, n_keep, n_sinks, n
                                   0 if dst is None else dst.k.shape[3], _ptr(kept), *_ws(workspace), _ptr(dev_status),
                                   _stream(stream)), "bt_block_kv_evict")
     return kept
+
+
+def bt_workspace_bytes_kv4(cfg) -> int:
+    return _lib.bt_workspace_bytes_kv4(ctypes.byref(cfg))
+
+
+def alloc_workspace_kv4(cfg, device="cuda"):
+    """A workspace for the decode calls over the 4-bit cache, initialised and ready."""
+    return _alloc_initialised(cfg, bt_workspace_bytes_kv4(cfg), device)
+
+
+def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=None, src_stride=None, reset_first=False, dev_status=None,
+                        stream=None):
+    """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
+    slabs of k_new, v_new (a bf16 block cache has N_max)."""
+    n_new = k_new.shape[2] if n_new is None else n_new
+    src_stride = k_new.shape[2] if src_stride is None else src_stride
+    _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(k_new), _ptr(v_new), _i32(n_new), src_stride,
+                                    1 if reset_first else 0, _ptr(dev_status), _stream(stream)), "bt_block_kv4_append")
+
+
+def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
+    """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
+    n_rows = k_out.shape[2] if n_rows is None else n_rows
+    dst_stride = k_out.shape[2] if dst_stride is None else dst_stride
+    _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _i32(first), _i32(n_rows), _ptr(k_out), _ptr(v_out),
+                                  dst_stride, _stream(stream)), "bt_block_kv4_read")
+
+
+def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace, dev_status=None, stream=None):
+    """Decode attention over the 4-bit cache."""
+    _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(out), *_ws(workspace),
+                                         _ptr(dev_status), _stream(stream)), "bt_block_decode_attn_kv4")
+
+
+def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, out, workspace, dev_status=None, stream=None):
+    """Quantise and append the new block's row, then attend over the 4-bit cache including it, in one launch."""
+    _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                         *_ws(workspace), _ptr(dev_status), _stream(stream)), "bt_block_decode_step_kv4")
+
+
+def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, bias, q_out, n_rows=None, dev_status=None, stream=None):
+    """bt_block_qkv_project_append into the 4-bit cache."""
+    n_rows = x.shape[1] if n_rows is None else n_rows
+    _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x), _i32(n_rows), _ptr(w_qkv), _ptr(bias),
+                                                _ptr(q_out), _ptr(dev_status), _stream(stream)), "bt_block_qkv_project_append_kv4")
+
+
+def bt_rows_quantize_i8(x, x8, steps, stream=None):
+    """Rows of x bf16 [..., n_cols] -> int8 of the same shape and fp32 steps [...]."""
+    n_cols = x.shape[-1]
+    _check(_lib.bt_rows_quantize_i8(_ptr(x), x.numel() // max(n_cols, 1), _i32(n_cols), _ptr(x8), _ptr(steps), _stream(stream)),
+           "bt_rows_quantize_i8")
+
+
+def bt_prefix_project_i8(cfg, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status=None, stream=None):
+    """bt_prefix_project of 8-bit operands and their steps."""
+    _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), _ptr(ctx8), _ptr(ctx_steps), _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(prefix_out),
+                                     _ptr(dev_status), _stream(stream)), "bt_prefix_project_i8")
+
+
+def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
+                                   stream=None):
+    """bt_block_qkv_project_append of 8-bit operands and their steps."""
+    n_rows = x8.shape[1] if n_rows is None else n_rows
+    _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
+                                               _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream(stream)),
+           "bt_block_qkv_project_append_i8")
+
+
+def bt_local_qkv_project_append_i8(cfg, cache: LocalCache, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, reset_first=False,
+                                   reset_mask=None, dev_status=None, stream=None):
+    """bt_local_qkv_project_append of 8-bit operands and their steps."""
+    n_rows = x8.shape[1] if n_rows is None else n_rows
+    _check(_lib.bt_local_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
+                                               _ptr(w_steps), _ptr(bias), 1 if reset_first else 0, _ptr(reset_mask), _ptr(q_out),
+                                               _ptr(dev_status), _stream(stream)), "bt_local_qkv_project_append_i8")
+
+
+def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
+                                       stream=None):
+    """bt_block_qkv_project_append of 8-bit operands and their steps into the 4-bit cache."""
+    n_rows = x8.shape[1] if n_rows is None else n_rows
+    _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows),
+                                                   _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream(stream)),
+           "bt_block_qkv_project_append_i8_kv4")
 
 
 def bt_block_decode_step_host(cfg, cache: BlockCache, layer, q_host, k_new_host, v_new_host, out_host, q_dev, k_dev,

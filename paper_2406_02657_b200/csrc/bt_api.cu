@@ -644,93 +644,305 @@ bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* 
     return cuda_status(bt::launch_block_kv_evict(a, (cudaStream_t)stream));
 }
 
+// ---- the block cache in 4 bits
+
+static bt_status check_kv4(const bt_config* cfg, const bt_block_cache_kv4* cache, int layer)
+{
+    bt_status st = check_config(cfg, layer);
+    if (st != BT_OK) return st;
+    if (!cache || !cache->kv || !cache->len) return BT_ERR_NULL;
+    if (cfg->max_blocks > 1 << 30) return BT_ERR_UNSUPPORTED;   // rows are counted past the end by a chunk
+    return BT_OK;
+}
+static bool kv4_aligned(const bt_block_cache_kv4* c) { return al16(c->kv) && al4(c->len); }
+static size_t kv4_slab_bytes(const bt_config* c) { return (size_t)((c->max_blocks + 15) / 16) * (c->head_dim / 64) * BT_KV4_TILE_BYTES; }
+static char* kv4_layer(const bt_config* c, const bt_block_cache_kv4* cache, int layer)
+{
+    return (char*)cache->kv + kv4_slab_bytes(c) * c->batch * c->heads * layer;
+}
+
+static void fill_kv4_args(bt::Kv4Args& a, const bt_config* cfg, const bt_block_cache_kv4* cache, int layer, const void* k, const void* v,
+                          int64_t stride, int n_rows, uint32_t* dev_status)
+{
+    a.k = const_cast<void*>(k);
+    a.v = const_cast<void*>(v);
+    a.stride = stride;
+    a.kv = kv4_layer(cfg, cache, layer);
+    a.slab_bytes = (int64_t)kv4_slab_bytes(cfg);
+    a.len = cache->len + (size_t)layer * cfg->batch;
+    a.dev_status = dev_status;
+    a.B = cfg->batch;
+    a.H = cfg->heads;
+    a.hd = cfg->head_dim;
+    a.cap = cfg->max_blocks;
+    a.n_rows = n_rows;
+    a.first = 0;
+    a.reset = 0;
+}
+
+bt_status bt_block_kv4_append(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* k_new, const void* v_new, int n_new,
+                              int64_t src_stride, int reset_first, uint32_t* dev_status, void* stream)
+{
+    bt_status st = check_kv4(cfg, cache, layer);
+    if (st != BT_OK) return st;
+    if (!k_new || !v_new) return BT_ERR_NULL;
+    if (n_new <= 0 || src_stride < n_new) return BT_ERR_SHAPE;
+    if (n_new > cfg->max_blocks) return BT_ERR_CAPACITY;
+    if (!kv4_aligned(cache) || !al16(k_new) || !al16(v_new) || !al4(dev_status)) return BT_ERR_UNSUPPORTED;
+    bt::Kv4Args a;
+    fill_kv4_args(a, cfg, cache, layer, k_new, v_new, src_stride, n_new, dev_status);
+    a.reset = reset_first ? 1 : 0;
+    return cuda_status(bt::launch_kv4_append(a, (cudaStream_t)stream));
+}
+
+bt_status bt_block_kv4_read(const bt_config* cfg, const bt_block_cache_kv4* cache, int layer, int first, int n_rows, void* k_out, void* v_out,
+                            int64_t dst_stride, void* stream)
+{
+    bt_status st = check_kv4(cfg, cache, layer);
+    if (st != BT_OK) return st;
+    if (!k_out || !v_out) return BT_ERR_NULL;
+    if (first < 0 || n_rows <= 0 || dst_stride < n_rows) return BT_ERR_SHAPE;
+    if (n_rows > cfg->max_blocks - first) return BT_ERR_CAPACITY;
+    if (!kv4_aligned(cache) || !al16(k_out) || !al16(v_out)) return BT_ERR_UNSUPPORTED;
+    bt::Kv4Args a;
+    fill_kv4_args(a, cfg, cache, layer, k_out, v_out, dst_stride, n_rows, nullptr);
+    a.first = first;
+    return cuda_status(bt::launch_kv4_read(a, (cudaStream_t)stream));
+}
+
+// Ways the row range of a (sequence, head) is cut: enough parts for eight warps on each of 148 SMs, each of at least 128 rows.
+static int kv4_splits(const bt_config* cfg)
+{
+    if (cfg->decode_splits > 0) return cfg->decode_splits;
+    long long s = 8 * 148 / ((long long)cfg->batch * cfg->heads);
+    const long long most = cfg->max_blocks / 128;
+    if (s > most) s = most;
+    if (s > 64) s = 64;
+    return s < 1 ? 1 : (int)s;
+}
+
+size_t bt_workspace_bytes_kv4(const bt_config* cfg)
+{
+    if (check_config(cfg, 0) != BT_OK) return 0;
+    const int s = kv4_splits(cfg);
+    return align16(bt_workspace_bytes(cfg)) + (s <= 1 ? 0 : (size_t)s * cfg->batch * cfg->heads * (cfg->head_dim + 4) * sizeof(float));
+}
+
+static bt_status decode_kv4(const bt_config* cfg, const bt_block_cache_kv4* cache, int layer, const void* q, const void* k_new, const void* v_new,
+                            bool step, void* out, void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    bt_status st = check_kv4(cfg, cache, layer);
+    if (st != BT_OK) return st;
+    if (!q || !out || (step && (!k_new || !v_new))) return BT_ERR_NULL;
+    if (!workspace || workspace_bytes < bt_workspace_bytes_kv4(cfg)) return BT_ERR_WORKSPACE;
+    if (!kv4_aligned(cache) || !al16(q) || !al16(out) || !al16(k_new) || !al16(v_new) || !al16(workspace) || !al4(dev_status)) return BT_ERR_UNSUPPORTED;
+    bt::Kv4DecodeArgs a = {};
+    a.q = q;
+    a.kv = kv4_layer(cfg, cache, layer);
+    a.slab_bytes = (int64_t)kv4_slab_bytes(cfg);
+    a.len = cache->len + (size_t)layer * cfg->batch;
+    a.out = out;
+    a.ws = (float*)((char*)workspace + align16(bt_workspace_bytes(cfg)));
+    a.counters = (int32_t*)((char*)workspace + partial_bytes(cfg));
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.dev_status = dev_status;
+    a.B = cfg->batch;
+    a.H = cfg->heads;
+    a.hd = cfg->head_dim;
+    a.n_max = cfg->max_blocks;
+    a.splits = kv4_splits(cfg);
+    a.scale_log2 = scale_log2(cfg);
+    return cuda_status(bt::launch_block_decode_kv4(a, (cudaStream_t)stream));
+}
+
+bt_status bt_block_decode_attn_kv4(const bt_config* cfg, const bt_block_cache_kv4* cache, int layer, const void* q, void* out, void* workspace,
+                                   size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    return decode_kv4(cfg, cache, layer, q, nullptr, nullptr, false, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+bt_status bt_block_decode_step_kv4(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* q, const void* k_new, const void* v_new,
+                                   void* out, void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream)
+{
+    return decode_kv4(cfg, cache, layer, q, k_new, v_new, true, out, workspace, workspace_bytes, dev_status, stream);
+}
+
 // ---- the linear maps either side of the attention path
 
-static bt_status project_common(const bt_config* cfg, const void* x, const void* w, const void* bias, const void* out,
-                                const uint32_t* dev_status)
+// What is multiplied: bf16 x and w, or 8-bit integers with their steps.
+struct Operands {
+    const void* x;
+    const void* w;
+    const void* bias;
+    bool int8;
+    const float* x_steps;
+    const float* w_steps;
+};
+
+static bt_status project_common(const bt_config* cfg, const Operands& op, const void* out, const uint32_t* dev_status)
 {
-    if (!x || !w || !out) return BT_ERR_NULL;
-    if (!al16(x) || !al16(w) || !al16(bias) || !al16(out) || !al4(dev_status)) return BT_ERR_UNSUPPORTED;
+    if (!op.x || !op.w || !out || (op.int8 && (!op.x_steps || !op.w_steps))) return BT_ERR_NULL;
+    if (!al16(op.x) || !al16(op.w) || !al16(op.bias) || !al16(op.x_steps) || !al16(op.w_steps) || !al16(out) || !al4(dev_status))
+        return BT_ERR_UNSUPPORTED;
     if ((long long)cfg->heads * cfg->head_dim > (1 << 20)) return BT_ERR_UNSUPPORTED;
     return BT_OK;
 }
 
-bt_status bt_prefix_project(const bt_config* cfg, const void* ctx, const void* w_prefix, const void* bias, void* prefix_out,
-                            uint32_t* dev_status, void* stream)
+static void fill_project_args(bt::ProjectArgs& a, const Operands& op, void* out, uint32_t* dev_status)
+{
+    a.x = op.x;
+    a.w = op.w;
+    a.bias = op.bias;
+    a.x_steps = op.x_steps;
+    a.w_steps = op.w_steps;
+    a.out = out;
+    a.dev_status = dev_status;
+}
+
+static bt_status prefix_project(const bt_config* cfg, const Operands& op, void* prefix_out, uint32_t* dev_status, void* stream)
 {
     bt_status st = check_config(cfg, 0);
     if (st != BT_OK) return st;
-    st = project_common(cfg, ctx, w_prefix, bias, prefix_out, dev_status);
+    st = project_common(cfg, op, prefix_out, dev_status);
     if (st != BT_OK) return st;
     const long long D = (long long)cfg->heads * cfg->head_dim;
     if (D * cfg->prefix_len > 0x7fffffffLL) return BT_ERR_UNSUPPORTED;
     bt::ProjectArgs a = {};
-    a.x = ctx;
-    a.w = w_prefix;
-    a.bias = bias;
-    a.out = prefix_out;
+    fill_project_args(a, op, prefix_out, dev_status);
     a.M = cfg->batch;
     a.K = (int)D;
     a.N = (int)(D * cfg->prefix_len);
     a.mode = bt::kProjectPlain;
-    a.dev_status = dev_status;
     if (!bt::project_supported(a)) return BT_ERR_UNSUPPORTED;
     return cuda_status(bt::launch_project(a, (cudaStream_t)stream));
 }
 
-static bt_status qkv_project(const bt_config* cfg, const bt::CacheView& view, const void* x, int n_rows, const void* w_qkv,
-                             const void* bias, int reset_first, const uint8_t* reset_mask, void* q_out, uint32_t* dev_status,
-                             void* stream)
+static bt_status qkv_project(const bt_config* cfg, int mode, const bt::CacheView& view, const Operands& op, int n_rows, int reset_first,
+                             const uint8_t* reset_mask, void* q_out, uint32_t* dev_status, void* stream)
 {
     const long long D = (long long)cfg->heads * cfg->head_dim;
     if ((long long)cfg->batch * n_rows > 0x7fffffffLL / 2 || 3 * D > 0x7fffffffLL) return BT_ERR_UNSUPPORTED;
     bt::ProjectArgs a = {};
-    a.x = x;
-    a.w = w_qkv;
-    a.bias = bias;
-    a.out = q_out;
+    fill_project_args(a, op, q_out, dev_status);
     a.M = cfg->batch * n_rows;
     a.K = (int)D;
     a.N = (int)(3 * D);
-    a.mode = bt::kProjectQkv;
+    a.mode = mode;
     a.cache = view;
     a.n_rows = n_rows;
     a.H = cfg->heads;
     a.hd = cfg->head_dim;
     a.reset_first = reset_first ? 1 : 0;
     a.reset_mask = reset_mask;
-    a.dev_status = dev_status;
     if (!bt::project_supported(a)) return BT_ERR_UNSUPPORTED;
     return cuda_status(bt::launch_project(a, (cudaStream_t)stream));
+}
+
+static bt_status block_qkv_project(const bt_config* cfg, const bt_block_cache* cache, int layer, const Operands& op, int n_rows, void* q_out,
+                                   uint32_t* dev_status, void* stream)
+{
+    bt_status st = check_config(cfg, layer);
+    if (st != BT_OK) return st;
+    if (!cache || !cache->k || !cache->v || !cache->len) return BT_ERR_NULL;
+    st = project_common(cfg, op, q_out, dev_status);
+    if (st != BT_OK) return st;
+    if (n_rows <= 0) return BT_ERR_SHAPE;
+    if (n_rows > cfg->max_blocks) return BT_ERR_CAPACITY;
+    if (!block_cache_aligned(cache)) return BT_ERR_UNSUPPORTED;
+    return qkv_project(cfg, bt::kProjectQkv, block_view(cfg, cache, layer), op, n_rows, 0, nullptr, q_out, dev_status, stream);
+}
+
+static bt_status local_qkv_project(const bt_config* cfg, const bt_local_cache* cache, int layer, const Operands& op, int n_rows, int reset_first,
+                                   const uint8_t* reset_mask, void* q_out, uint32_t* dev_status, void* stream)
+{
+    bt_status st = check_config(cfg, layer);
+    if (st != BT_OK) return st;
+    if (!cache || !cache->kv || !cache->len) return BT_ERR_NULL;
+    st = project_common(cfg, op, q_out, dev_status);
+    if (st != BT_OK) return st;
+    if (n_rows <= 0) return BT_ERR_SHAPE;
+    if (n_rows > local_cap(cfg)) return BT_ERR_CAPACITY;
+    if (!local_cache_aligned(cache)) return BT_ERR_UNSUPPORTED;
+    return qkv_project(cfg, bt::kProjectQkv, local_view(cfg, cache, layer), op, n_rows, reset_first, reset_mask, q_out, dev_status, stream);
+}
+
+static bt_status kv4_qkv_project(const bt_config* cfg, const bt_block_cache_kv4* cache, int layer, const Operands& op, int n_rows, void* q_out,
+                                 uint32_t* dev_status, void* stream)
+{
+    bt_status st = check_kv4(cfg, cache, layer);
+    if (st != BT_OK) return st;
+    st = project_common(cfg, op, q_out, dev_status);
+    if (st != BT_OK) return st;
+    if (n_rows <= 0) return BT_ERR_SHAPE;
+    if (n_rows > cfg->max_blocks) return BT_ERR_CAPACITY;
+    if (!kv4_aligned(cache)) return BT_ERR_UNSUPPORTED;
+    bt::CacheView v = {};
+    v.k = kv4_layer(cfg, cache, layer);
+    v.len = cache->len + (size_t)layer * cfg->batch;
+    v.slab_stride = (int64_t)kv4_slab_bytes(cfg);
+    v.cap = cfg->max_blocks;
+    return qkv_project(cfg, bt::kProjectQkvKv4, v, op, n_rows, 0, nullptr, q_out, dev_status, stream);
+}
+
+bt_status bt_prefix_project(const bt_config* cfg, const void* ctx, const void* w_prefix, const void* bias, void* prefix_out,
+                            uint32_t* dev_status, void* stream)
+{
+    return prefix_project(cfg, {ctx, w_prefix, bias, false, nullptr, nullptr}, prefix_out, dev_status, stream);
 }
 
 bt_status bt_block_qkv_project_append(const bt_config* cfg, bt_block_cache* cache, int layer, const void* x, int n_rows,
                                       const void* w_qkv, const void* bias, void* q_out, uint32_t* dev_status, void* stream)
 {
-    bt_status st = check_config(cfg, layer);
-    if (st != BT_OK) return st;
-    if (!cache || !cache->k || !cache->v || !cache->len) return BT_ERR_NULL;
-    st = project_common(cfg, x, w_qkv, bias, q_out, dev_status);
-    if (st != BT_OK) return st;
-    if (n_rows <= 0) return BT_ERR_SHAPE;
-    if (n_rows > cfg->max_blocks) return BT_ERR_CAPACITY;
-    if (!block_cache_aligned(cache)) return BT_ERR_UNSUPPORTED;
-    return qkv_project(cfg, block_view(cfg, cache, layer), x, n_rows, w_qkv, bias, 0, nullptr, q_out, dev_status, stream);
+    return block_qkv_project(cfg, cache, layer, {x, w_qkv, bias, false, nullptr, nullptr}, n_rows, q_out, dev_status, stream);
 }
 
 bt_status bt_local_qkv_project_append(const bt_config* cfg, bt_local_cache* cache, int layer, const void* x, int n_rows,
                                       const void* w_qkv, const void* bias, int reset_first, const uint8_t* reset_mask,
                                       void* q_out, uint32_t* dev_status, void* stream)
 {
-    bt_status st = check_config(cfg, layer);
-    if (st != BT_OK) return st;
-    if (!cache || !cache->kv || !cache->len) return BT_ERR_NULL;
-    st = project_common(cfg, x, w_qkv, bias, q_out, dev_status);
-    if (st != BT_OK) return st;
-    if (n_rows <= 0) return BT_ERR_SHAPE;
-    if (n_rows > local_cap(cfg)) return BT_ERR_CAPACITY;
-    if (!local_cache_aligned(cache)) return BT_ERR_UNSUPPORTED;
-    return qkv_project(cfg, local_view(cfg, cache, layer), x, n_rows, w_qkv, bias, reset_first, reset_mask, q_out, dev_status, stream);
+    return local_qkv_project(cfg, cache, layer, {x, w_qkv, bias, false, nullptr, nullptr}, n_rows, reset_first, reset_mask, q_out, dev_status,
+                             stream);
+}
+
+bt_status bt_block_qkv_project_append_kv4(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* x, int n_rows,
+                                          const void* w_qkv, const void* bias, void* q_out, uint32_t* dev_status, void* stream)
+{
+    return kv4_qkv_project(cfg, cache, layer, {x, w_qkv, bias, false, nullptr, nullptr}, n_rows, q_out, dev_status, stream);
+}
+
+bt_status bt_rows_quantize_i8(const void* x, int64_t n_rows, int n_cols, void* x8, float* steps, void* stream)
+{
+    if (!x || !x8 || !steps) return BT_ERR_NULL;
+    if (n_rows <= 0 || n_cols <= 0) return BT_ERR_SHAPE;
+    if (n_cols % 16 != 0 || n_cols > bt::kQuantizeCols || n_rows > 0x7fffffffLL || !al16(x) || !al16(x8) || !al4(steps)) return BT_ERR_UNSUPPORTED;
+    return cuda_status(bt::launch_rows_quantize(x, n_rows, n_cols, x8, steps, (cudaStream_t)stream));
+}
+
+bt_status bt_prefix_project_i8(const bt_config* cfg, const void* ctx8, const float* ctx_steps, const void* w8, const float* w_steps,
+                               const void* bias, void* prefix_out, uint32_t* dev_status, void* stream)
+{
+    return prefix_project(cfg, {ctx8, w8, bias, true, ctx_steps, w_steps}, prefix_out, dev_status, stream);
+}
+
+bt_status bt_block_qkv_project_append_i8(const bt_config* cfg, bt_block_cache* cache, int layer, const void* x8, const float* x_steps, int n_rows,
+                                         const void* w8, const float* w_steps, const void* bias, void* q_out, uint32_t* dev_status, void* stream)
+{
+    return block_qkv_project(cfg, cache, layer, {x8, w8, bias, true, x_steps, w_steps}, n_rows, q_out, dev_status, stream);
+}
+
+bt_status bt_local_qkv_project_append_i8(const bt_config* cfg, bt_local_cache* cache, int layer, const void* x8, const float* x_steps, int n_rows,
+                                         const void* w8, const float* w_steps, const void* bias, int reset_first, const uint8_t* reset_mask,
+                                         void* q_out, uint32_t* dev_status, void* stream)
+{
+    return local_qkv_project(cfg, cache, layer, {x8, w8, bias, true, x_steps, w_steps}, n_rows, reset_first, reset_mask, q_out, dev_status, stream);
+}
+
+bt_status bt_block_qkv_project_append_i8_kv4(const bt_config* cfg, bt_block_cache_kv4* cache, int layer, const void* x8, const float* x_steps,
+                                             int n_rows, const void* w8, const float* w_steps, const void* bias, void* q_out,
+                                             uint32_t* dev_status, void* stream)
+{
+    return kv4_qkv_project(cfg, cache, layer, {x8, w8, bias, true, x_steps, w_steps}, n_rows, q_out, dev_status, stream);
 }
 
 bt_status bt_selftest_bounded_wait(uint32_t* report, uint32_t* dev_status, void* stream)

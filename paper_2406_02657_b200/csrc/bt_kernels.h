@@ -118,6 +118,30 @@ struct EvictArgs {
 };
 cudaError_t launch_block_kv_evict(const EvictArgs& a, cudaStream_t stream);
 
+// Rows written into a layer of the 4-bit block cache, or read back from it.
+struct Kv4Args {
+    void* k;             // bf16 rows of the caller: slab s at k + s * stride * hd; the source of an append, where a read goes
+    void* v;
+    int64_t stride;      // rows between slabs
+    void* kv;            // layer base of the cache
+    int64_t slab_bytes;
+    int32_t* len;        // [B]
+    uint32_t* dev_status;
+    int B, H, hd, cap;
+    int n_rows;
+    int first;           // read: cache row that goes to row 0
+    int reset;           // append: the rows become rows 0 .. n_rows - 1 of every sequence
+};
+cudaError_t launch_kv4_append(const Kv4Args& a, cudaStream_t stream);
+cudaError_t launch_kv4_read(const Kv4Args& a, cudaStream_t stream);
+
+// Decode attention over the 4-bit block cache (k and v of the base are unused; counters are always needed).
+struct Kv4DecodeArgs : DecodeArgs {
+    void* kv;            // layer base
+    int64_t slab_bytes;
+};
+cudaError_t launch_block_decode_kv4(const Kv4DecodeArgs& a, cudaStream_t stream);
+
 struct TokenArgs {
     void* kv;            // layer base, [B][H][C][2][hd]
     int32_t* len;        // [B]
@@ -150,23 +174,31 @@ cudaError_t launch_block_prefill_tc(const PrefillArgs& a, uint32_t* dev_status, 
 cudaError_t launch_block_prefill_window(const PrefillArgs& a, int window, int sinks, uint32_t* dev_status, cudaStream_t stream);
 
 
+// Rows of bf16 to 8 bits, a step for each row; cols a multiple of 16, at most kQuantizeCols.
+constexpr int kQuantizeCols = 2048;
+cudaError_t launch_rows_quantize(const void* x, long long rows, int cols, void* x8, float* steps, cudaStream_t stream);
+
 // y = W x + b on the tensor cores.  x [M][K], w [N][K] (row o = weights of output feature o), bias [N] or
-// NULL, all bf16; fp32 accumulation, bf16 results.
+// NULL, all bf16; fp32 accumulation, bf16 results.  With steps (x_steps, w_steps not NULL) x and w are 8-bit integers:
+// y[m][n] = x_steps[m] w_steps[n] (sum of products, exact in 32 bits) + b[n].
 //   kProjectPlain : out [M][N]
 //   kProjectQkv   : M = B * n_rows rows (sequence b, row i), N = 3 * H * hd output features ordered Q, K, V,
 //                   each (h, d): Q -> out [B][H][n_rows][hd]; K, V -> rows len_old[b] + i of `cache`
 //                   (len_old = 0 where the reset applies); a sequence without room for n_rows rows keeps
 //                   its cache.  A second launch then advances the lengths (and flags those sequences).
-enum { kProjectPlain = 0, kProjectQkv = 1 };
+//   kProjectQkvKv4: the same into the 4-bit block cache: cache.k is its layer base, cache.slab_stride its slabs' bytes.
+enum { kProjectPlain = 0, kProjectQkv = 1, kProjectQkvKv4 = 2 };
 struct ProjectArgs {
     const void* x;
     const void* w;
     const void* bias;
+    const float* x_steps;     // 8-bit x and w; else NULL
+    const float* w_steps;
     void* out;
     int M, N, K;
     int mode;
-    CacheView cache;          // kProjectQkv
-    int n_rows, H, hd;        // kProjectQkv
+    CacheView cache;          // the QKV forms
+    int n_rows, H, hd;        // the QKV forms
     int reset_first;
     const uint8_t* reset_mask;
     uint32_t* dev_status;

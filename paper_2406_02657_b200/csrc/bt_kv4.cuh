@@ -1,0 +1,99 @@
+// The 4-bit form of the block cache, shared by the kernels that write and read it.  Internal to the library.
+//
+// For every row and every 32 dimensions ("group") a step s = bf16(max|x| / 7) and codes u = round(x / s), halves away from
+// zero, so -7 <= u <= 7; the value held is s u.  A step that would be below 2^-126 is 0 (the group is held as zeros), a group
+// with a value that is not finite has the step NaN.
+//   Rounding.  x and s have 8 significant bits each, x = X 2^a, s = S 2^b, so x / s - (k + 1/2) is a whole number over 2 S 2^j:
+// either zero or at least 2^-12 of the quotient (2^-16 for the 127 steps of the 8-bit rows).  The product with
+// (1 + 2^-19) / s, off by 2^-22 at most, therefore rounds every quotient as the exact one would be, and a quotient that is a
+// half exactly away from zero, without a division for each value.
+//
+// A tile is 16 rows of 64 dimensions of K and of V, 1152 contiguous bytes (nine 128-byte lines, so a range of rows is one
+// bulk copy):
+//   bytes    0 ..  511   K codes, 32 bytes a row: dimension 2i in the low half of byte i, 2i+1 in the high half, as u + 8
+//   bytes  512 .. 1023   V codes
+//   bytes 1024 .. 1087   K steps, two bf16 a row
+//   bytes 1088 .. 1151   V steps
+// A (sequence, head) slab is [ceil(N_max / 16)][hd / 64] tiles.
+#pragma once
+
+#include "bt_common.cuh"
+
+namespace bt {
+namespace kv4 {
+
+constexpr int kTileRows = 16;
+constexpr int kTileBytes = 1152;
+constexpr int kPartBytes = 512;       // K codes, V codes
+constexpr int kStepsAt = 1024;        // K steps; V steps 64 bytes later
+constexpr uint32_t kZeroCodes = 0x88888888u;
+constexpr float kRoundUpHalves = 1.0f + 1.0f / 524288.0f;   // 1 + 2^-19
+constexpr float kLeastStep = 1.17549435e-38f;               // 2^-126
+
+__host__ __device__ __forceinline__ int64_t slab_bytes(int cap, int hd)
+{
+    return (int64_t)((cap + kTileRows - 1) / kTileRows) * (hd / 64) * kTileBytes;
+}
+
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// Magnitudes of bf16 values compare like their bits, infinities and NaN above all numbers.
+__device__ __forceinline__ uint32_t magnitude_max8(const uint4& r)
+{
+    const uint32_t m = 0x7fff7fffu;
+    return max_u16x2(max_u16x2(r.x & m, r.y & m), max_u16x2(r.z & m, r.w & m));
+}
+
+// Step of a group and what its values are multiplied with to get codes; `packed` holds magnitudes in both halves.
+struct Step {
+    uint32_t bits;   // bf16
+    float inv;
+    bool finite;
+};
+template <int MOST>
+__device__ __forceinline__ Step step_of_group(uint32_t packed)
+{
+    const uint32_t mag = max(packed & 0xffffu, packed >> 16);
+    Step st;
+    st.finite = mag < 0x7f80u;
+    const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(mag << 16), (float)MOST)));
+    const bool some = st.finite && s >= kLeastStep;
+    st.bits = !st.finite ? 0x7fffu : some ? __float_as_uint(s) >> 16 : 0u;
+    st.inv = some ? __frcp_rn(s) * kRoundUpHalves : 0.f;
+    return st;
+}
+
+// 8 values -> 8 codes of four bits.  Adding 1.5 * 2^23 (+ 8) leaves the whole number nearest in the low bits.
+__device__ __forceinline__ uint32_t codes8(const uint4& r, const Step& st)
+{
+    constexpr float kWhole = 12582912.0f + 8.0f;
+    float f[8];
+    unpack8(r, f);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w |= (__float_as_uint(fmaf(f[i], st.inv, kWhole)) & 15u) << (4 * i);
+    return st.finite ? w : kZeroCodes;
+}
+
+// Four lanes hold a group (8 values each): its step, on all four of them.
+__device__ __forceinline__ Step step_of_lanes(const uint4& r)
+{
+    uint32_t m = magnitude_max8(r);
+    m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    return step_of_group<7>(m);
+}
+
+// 8 codes -> values
+__device__ __forceinline__ void values8(uint32_t codes, float step, float (&f)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = step * (float)((int)((codes >> (4 * i)) & 15u) - 8);
+}
+
+}  // namespace kv4
+}  // namespace bt

@@ -27,11 +27,19 @@
 // memory and accumulate each CTA's 128 rows in that CTA's tensor memory; commits are multicast to both CTAs'
 // barriers; each CTA drains its own accumulator and reports to the leader.  Per CTA this moves a third less
 // operand data from L2 into shared memory for the same products.
+//
+// 8-bit operands (kInt8: a step per row of x and per output feature) run through the same stages and tiles: 128 bytes of a row are
+// 128 values of K instead of 64, an instruction takes 32 of them, and the sums are whole numbers (at most 2048 * 128 * 128 = 2^25,
+// so 32 bits hold them), which the epilogue multiplies with both steps.
+//
+// With the 4-bit block cache as the target (kProjectQkvKv4) the epilogue thread that holds 64 values of a K or V row, rounded to bf16
+// as they would be cached, quantises them (two groups of 32) and stores codes and steps itself: 32 + 4 bytes instead of 128.
 #include <cuda.h>
 
 #include "bt_common.cuh"
 #include "bt_device.h"
 #include "bt_kernels.h"
+#include "bt_kv4.cuh"
 #include "bt_mbarrier.cuh"
 #include "bt_tcgen05.cuh"
 #include "bt_tensor_map.h"
@@ -42,10 +50,10 @@ namespace proj {
 using namespace tc;
 
 constexpr int BM = 128;                  // rows of x per tile (= tensor-memory lanes)
-constexpr int BK = 64;                   // K elements per stage: one 128-byte swizzle atom
+constexpr int kRowBytes = 128;           // bytes of K per stage and row: one swizzle atom (64 bf16, 128 8-bit values)
 constexpr int kEpilogueWarps = 8, kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 320;
-constexpr uint32_t kABytes = BM * BK * 2;
+constexpr uint32_t kABytes = BM * kRowBytes;
 constexpr uint32_t kSpinLimit = 1u << 26;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s: far beyond any legitimate wait
 constexpr uint32_t kPatchBytes = 32 * 128;         // per epilogue warp: 32 rows x 64 bf16
@@ -54,7 +62,7 @@ constexpr uint32_t kPeerBitMask = 0xFEFFFFFFu;   // clears the bit that tells th
 
 template <int BN, int kCtas>
 struct Cfg {
-    static constexpr uint32_t kBBytes = (BN / kCtas) * BK * 2;   // a CTA of a pair holds half of the W tile
+    static constexpr uint32_t kBBytes = (BN / kCtas) * kRowBytes;   // a CTA of a pair holds half of the W tile
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = kStageBytes == 48 * 1024 ? 4 : (kStageBytes == 32 * 1024 ? 6 : 8);
     static constexpr uint32_t kTmemCols = 2 * BN;   // two accumulators
@@ -125,6 +133,16 @@ __device__ __forceinline__ void mma_bf16_pair(uint32_t tmem_d, uint64_t adesc, u
         ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(z)
         : "memory");
 }
+__device__ __forceinline__ void mma_s8_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    const uint32_t z = 0;   // no output lane disabled
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(z)
+        : "memory");
+}
 // arrives, once the MMAs issued so far are done, on the barrier at this address in both CTAs of the pair
 __device__ __forceinline__ void mma_commit_pair(uint32_t bar)
 {
@@ -146,13 +164,39 @@ __device__ __forceinline__ uint32_t cluster_cta_rank()
     return r;
 }
 
-template <int BN, int kCtas>
+// 64 bf16 values of a K (part 0) or V (part 1) row, in w[0..31]: quantised and stored into the 4-bit cache by one thread.
+__device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (&w)[64], size_t slab, int row, int plane, int part)
+{
+    uint8_t* tile = reinterpret_cast<uint8_t*>(a.cache.k) + slab * a.cache.slab_stride +
+                    (size_t)(row / kv4::kTileRows * (a.hd / 64) + plane) * kv4::kTileBytes;
+    const int at = row % kv4::kTileRows;
+    uint32_t steps = 0;
+#pragma unroll
+    for (int grp = 0; grp < 2; ++grp) {
+        uint4 x[4];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t* v = w + grp * 16 + i * 4;
+            x[i] = make_uint4(v[0], v[1], v[2], v[3]);
+            m = kv4::max_u16x2(m, kv4::magnitude_max8(x[i]));
+        }
+        const kv4::Step st = kv4::step_of_group<7>(m);
+        const uint4 codes = make_uint4(kv4::codes8(x[0], st), kv4::codes8(x[1], st), kv4::codes8(x[2], st), kv4::codes8(x[3], st));
+        *reinterpret_cast<uint4*>(tile + part * kv4::kPartBytes + at * 32 + grp * 16) = codes;
+        steps |= st.bits << (16 * grp);
+    }
+    *reinterpret_cast<uint32_t*>(tile + kv4::kStepsAt + part * 64 + at * 4) = steps;
+}
+
+template <int BN, int kCtas, bool kInt8>
 __global__ void __launch_bounds__(kThreads, 1)
 project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, Params p)
 {
     using C = Cfg<BN, kCtas>;
     constexpr int S = C::kStages;
-    constexpr uint32_t IDESC = make_idesc(BM * kCtas, BN, false);
+    constexpr uint32_t IDESC = kInt8 ? make_idesc_s8(BM * kCtas, BN) : make_idesc(BM * kCtas, BN, false);
+    constexpr int BK = kInt8 ? kRowBytes : kRowBytes / 2;   // elements of K per stage
     const ProjectArgs& a = p.a;
     // a pair of CTAs works on one tile of 256 rows: `rank` is this CTA's half, `unit` numbers the pairs
     const uint32_t rank = kCtas == 2 ? cluster_cta_rank() : 0u;
@@ -256,19 +300,19 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     ok = wait_all(full(s), (it / S) & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    // descriptor low words: address in 16-byte units plus the leading-dimension field; 16 elements
-                    // of K are 32 bytes inside a swizzled 128-byte row
+                    // descriptor low words: address in 16-byte units plus the leading-dimension field; an instruction takes
+                    // 32 bytes of K inside a swizzled 128-byte row
                     const uint32_t a0 = base + s * C::kStageBytes, b0 = a0 + kABytes;
                     const uint32_t alo = (a0 >> 4) | (1u << 16), blo = (b0 >> 4) | (1u << 16);
                     if (elect_one()) {
 #pragma unroll
-                        for (int kk = 0; kk < BK / 16; ++kk) {
-                            if constexpr (kCtas == 1)
-                                mma_bf16(tmem + acc * BN, desc_words(alo + kk * 2, kDescHiSw128), desc_words(blo + kk * 2, kDescHiSw128), IDESC,
-                                         (kb > 0 || kk > 0) ? 1u : 0u);
-                            else
-                                mma_bf16_pair(tmem + acc * BN, desc_words(alo + kk * 2, kDescHiSw128), desc_words(blo + kk * 2, kDescHiSw128), IDESC,
-                                              (kb > 0 || kk > 0) ? 1u : 0u);
+                        for (int kk = 0; kk < kRowBytes / 32; ++kk) {
+                            const uint64_t da = desc_words(alo + kk * 2, kDescHiSw128), db = desc_words(blo + kk * 2, kDescHiSw128);
+                            const uint32_t more = (kb > 0 || kk > 0) ? 1u : 0u;
+                            if constexpr (kInt8 && kCtas == 1) mma_s8(tmem + acc * BN, da, db, IDESC, more);
+                            else if constexpr (kInt8) mma_s8_pair(tmem + acc * BN, da, db, IDESC, more);
+                            else if constexpr (kCtas == 1) mma_bf16(tmem + acc * BN, da, db, IDESC, more);
+                            else mma_bf16_pair(tmem + acc * BN, da, db, IDESC, more);
                         }
                         if constexpr (kCtas == 1) mma_commit(empty(s));
                         else mma_commit_pair(empty(s));
@@ -310,6 +354,9 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     if (len_old >= 0 && len_old + a.n_rows <= a.cache.cap) row_rc = len_old + row_i;  // else: no room, K and V are dropped
                 }
             }
+            float x_step = 0.f;
+            if constexpr (kInt8)
+                if (m < a.M) x_step = a.x_steps[m];
             ok = wait(acc_full(acc), (t >> 1) & 1, abort_flag, a.dev_status);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -324,13 +371,35 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 tmem_wait_ld();
                 tmem_ld_fence32(r);
                 tmem_ld_fence32(r + 32);
-                // + bias, -> bf16, into the patch: row `lane`, 16-byte piece q8 at (q8 ^ (lane & 7))
+                // Where the piece goes.  head_dim is a multiple of 64 and so is col0: the 64 columns lie inside one
+                // head of one of Q, K, V, so everything but the row is the same for the whole warp.
+                int part = 0, piece_h = 0, piece_d = 0;            // part 0: Q, 1: K, 2: V
+                if (a.mode != kProjectPlain) {
+                    part = col0 / D;
+                    const int cc = col0 - part * D;
+                    piece_h = cc / a.hd;
+                    piece_d = cc - piece_h * a.hd;
+                }
+                // + bias, -> bf16, into the patch: row `lane`, 16-byte piece q8 at (q8 ^ (lane & 7)) - or, bound for the 4-bit
+                // cache, back into registers
+                const bool to_kv4 = a.mode == kProjectQkvKv4 && part != 0;
 #pragma unroll
                 for (int q8 = 0; q8 < 8; ++q8) {
                     float f[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r[q8 * 8 + i]);
                     const int col = col0 + q8 * 8;
+                    if constexpr (kInt8) {
+                        float4 s0 = make_float4(0.f, 0.f, 0.f, 0.f), s1 = s0;
+                        if (col < a.N) {
+                            s0 = *reinterpret_cast<const float4*>(a.w_steps + col);
+                            s1 = *reinterpret_cast<const float4*>(a.w_steps + col + 4);
+                        }
+                        const float ws[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = (float)(int)r[q8 * 8 + i] * (x_step * ws[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r[q8 * 8 + i]);
+                    }
                     if (bias != nullptr && col < a.N) {
                         float bf[8];
                         unpack8(*reinterpret_cast<const uint4*>(bias + col), bf);
@@ -338,21 +407,25 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                         for (int i = 0; i < 8; ++i) f[i] += bf[i];
                     }
                     const uint4 w = pack8(f);
+                    if (to_kv4) {
+                        r[q8 * 4] = w.x;
+                        r[q8 * 4 + 1] = w.y;
+                        r[q8 * 4 + 2] = w.z;
+                        r[q8 * 4 + 3] = w.w;
+                        continue;
+                    }
                     const uint32_t dst = patch + lane * 128 + ((q8 ^ (lane & 7)) << 4);
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
                 }
+                if (to_kv4) {
+                    if (row_rc >= 0) store_kv4(a, r, (size_t)row_b * a.H + piece_h, row_rc, piece_d / 64, part - 1);
+                    continue;
+                }
                 __syncwarp();
-                // Where the piece goes.  head_dim is a multiple of 64 and so is col0: the 64 columns lie inside one
-                // head of one of Q, K, V, so everything but the row is the same for the whole warp.
                 bf16* piece_base = reinterpret_cast<bf16*>(a.out);
                 size_t slab_elems = 0, row_elems = 0;     // element strides: per (sequence, head) slab, per row
-                int piece_h = 0, piece_d = 0;
-                bool to_cache = false;
-                if (a.mode == kProjectQkv) {
-                    const int part = col0 / D, cc = col0 - part * D;   // 0: Q, 1: K, 2: V
-                    piece_h = cc / a.hd;
-                    piece_d = cc - piece_h * a.hd;
-                    to_cache = part != 0;
+                const bool to_cache = part != 0;
+                if (a.mode != kProjectPlain) {
                     if (to_cache) {
                         piece_base = reinterpret_cast<bf16*>(part == 1 ? a.cache.k : a.cache.v);
                         slab_elems = (size_t)a.cache.slab_stride;
@@ -413,15 +486,19 @@ __global__ void project_len_advance_kernel(int32_t* len, int B, int n, int cap, 
     if (b < B) advance_len(len, b, n, cap, reset_first, reset_mask, dev_status);
 }
 
-template <int BN, int kCtas>
+template <int BN, int kCtas, bool kInt8>
 static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_t stream)
 {
     using C = Cfg<BN, kCtas>;
     static PerDeviceOnce limit_raised;
-    cudaError_t e = raise_smem_limit_once(limit_raised, dev, project_tc_kernel<BN, kCtas>, C::kSmemBytes);
+    cudaError_t e = raise_smem_limit_once(limit_raised, dev, project_tc_kernel<BN, kCtas, kInt8>, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     CUtensorMap mx, mw;
-    if (!make_slab_map(&mx, a.x, a.K, a.M, a.M, 1, BM) || !make_slab_map(&mw, a.w, a.K, a.N, a.N, 1, BN / kCtas)) return cudaErrorInvalidValue;
+    if constexpr (kInt8) {
+        if (!make_byte_map(&mx, a.x, a.K, a.M, BM) || !make_byte_map(&mw, a.w, a.K, a.N, BN / kCtas)) return cudaErrorInvalidValue;
+    } else {
+        if (!make_slab_map(&mx, a.x, a.K, a.M, a.M, 1, BM) || !make_slab_map(&mw, a.w, a.K, a.N, a.N, 1, BN / kCtas)) return cudaErrorInvalidValue;
+    }
     Params p;
     p.a = a;
     p.tiles_m = (a.M + BM * kCtas - 1) / (BM * kCtas);
@@ -444,12 +521,19 @@ static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = kCtas == 2 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, project_tc_kernel<BN, kCtas>, mx, mw, p);
+    return cudaLaunchKernelEx(&cfg, project_tc_kernel<BN, kCtas, kInt8>, mx, mw, p);
+}
+
+template <int BN, int kCtas>
+static cudaError_t launch_type(const ProjectArgs& a, int dev, int sms, cudaStream_t stream)
+{
+    return a.x_steps ? launch_bn<BN, kCtas, true>(a, dev, sms, stream) : launch_bn<BN, kCtas, false>(a, dev, sms, stream);
 }
 
 }  // namespace proj
 
-bool project_supported(const ProjectArgs& a) { return a.K % 8 == 0 && a.N % 8 == 0 && tensor_map_encode_fn() != nullptr; }
+// rows are copied in 16-byte pieces
+bool project_supported(const ProjectArgs& a) { return a.K % (a.x_steps ? 16 : 8) == 0 && a.N % 8 == 0 && tensor_map_encode_fn() != nullptr; }
 
 cudaError_t launch_project(const ProjectArgs& a, cudaStream_t stream)
 {
@@ -481,10 +565,10 @@ cudaError_t launch_project(const ProjectArgs& a, cudaStream_t stream)
         }
     }
     switch (best) {
-        case 0: e = proj::launch_bn<256, 2>(a, dev, sms, stream); break;
-        case 1: e = proj::launch_bn<256, 1>(a, dev, sms, stream); break;
-        case 2: e = proj::launch_bn<128, 1>(a, dev, sms, stream); break;
-        default: e = proj::launch_bn<64, 1>(a, dev, sms, stream); break;
+        case 0: e = proj::launch_type<256, 2>(a, dev, sms, stream); break;
+        case 1: e = proj::launch_type<256, 1>(a, dev, sms, stream); break;
+        case 2: e = proj::launch_type<128, 1>(a, dev, sms, stream); break;
+        default: e = proj::launch_type<64, 1>(a, dev, sms, stream); break;
     }
     if (e != cudaSuccess || a.mode == kProjectPlain) return e;
     const int B = a.M / a.n_rows;

@@ -43,4 +43,17 @@ inline bool make_slab_map(CUtensorMap* m, const void* ptr, int hd, long long row
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// [rows][cols] bytes; box = 128 bytes x box_rows rows, 128-byte swizzle; what lies outside reads as zeros.
+inline bool make_byte_map(CUtensorMap* m, const void* ptr, long long cols, long long rows, int box_rows)
+{
+    TensorMapEncodeFn fn = tensor_map_encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 1};
+    cuuint64_t strides[2] = {(cuuint64_t)cols, (cuuint64_t)rows * cols};
+    cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace bt
