@@ -364,11 +364,11 @@ bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* 
  * (-7 <= u <= 7); its value is s u.  Where s would be below 2^-126 the 32 values are held as zeros; where one of them is
  * not finite all 32 are held as NaN.
  *   kv  : uint8 [n_layers][B][H][ceil(N_max / 16)][hd / 64][BT_KV4_TILE_BYTES], 16-byte aligned; the last 16 rows may be there in
- *         part only, and their tiles are whole nevertheless.  A tile holds 16 rows x 64 dimensions of K and V:
- *           bytes    0 ..  511  K codes, 32 bytes a row: u + 8, dimension 2i in the low half of byte i, 2i + 1 in the high half
- *           bytes  512 .. 1023  V codes
- *           bytes 1024 .. 1087  K steps, two bf16 a row
- *           bytes 1088 .. 1151  V steps
+ *         part only, and their tiles are whole nevertheless.  A tile holds 16 rows x 64 dimensions of K and V, two codes a byte as
+ *         u + 8 (dimension 2i in the low half, 2i + 1 in the high half); byte i of row r of the tile lies at
+ *           K: (r/2) * 64 + (i/8) * 16 + (r%2) * 8 + i%8
+ *           V: 512 + (r/4) * 128 + ((i/4) ^ (2 * (r/4))) * 16 + (i%4) * 4 + r%4
+ *         and behind the codes the steps, two bf16 a row: bytes 1024 .. 1087 K, 1088 .. 1151 V.
  *   len : int32 [n_layers][B]
  * It needs no initialisation but the lengths.  N_max is at most 2^30 for these calls (else BT_ERR_UNSUPPORTED).
  */
@@ -396,11 +396,12 @@ bt_status bt_block_kv4_read(const bt_config* cfg, const bt_block_cache_kv4* cach
                             void* v_out, int64_t dst_stride, void* stream);
 
 /*
- * bt_block_decode_attn and bt_block_decode_step over the 4-bit cache: K and V are the values s u, in fp32 arithmetic; the weights
- * meet V as sums of two bf16 (2^-17 of a weight off at most).  The step quantises the new row, stores it and attends over it as it is
- * stored: it gives what bt_block_kv4_append and bt_block_decode_attn_kv4 give.
- * Values that are not finite: as for the contexts calls above, where a NaN in V is in all 32 dimensions of its step, and a score is
- * NaN where the query holds an infinity and the row a code of 0 in that dimension.
+ * bt_block_decode_attn and bt_block_decode_step over the 4-bit cache: K and V are the values s u.  The query is rounded to whole
+ * numbers (2^-18 of its largest value per dimension at most), weights times steps of V likewise (2^-28 of the largest at most); sums
+ * of products are exact, the rest is fp32.  The step quantises the new row, stores it and attends over it as it is stored: it gives what
+ * bt_block_kv4_append and bt_block_decode_attn_kv4 give.
+ * Values that are not finite: as for the contexts calls above, where a NaN in V is in all 32 dimensions of its step; a query that
+ * holds a NaN or an infinity gives NaN.
  * workspace: required, bt_workspace_bytes_kv4 bytes (0 on an invalid config), initialised by bt_workspace_init under the same
  * config; one call at a time.  Other arguments and errors as for bt_block_decode_attn / bt_block_decode_step.
  */

@@ -51,10 +51,20 @@ def step_bits(steps):
     return np.where(np.isnan(steps), 0x7FFF, bits).astype(np.uint16)
 
 
+def k_byte(row, pair):
+    """Where the codes of dimensions 2 pair, 2 pair + 1 of K of a row lie in a tile (row, pair within it)."""
+    return row // 2 * 64 + pair // 8 * 16 + row % 2 * 8 + pair % 8
+
+
+def v_byte(row, pair):
+    quad, unit, word = row // 4, pair // 4, pair % 4
+    return 512 + quad * 128 + (unit ^ 2 * quad) * 16 + word * 4 + row % 4
+
+
 def write_tiles(tiles, row0, k, v):
     """Rows k, v [n, hd] (float64) written into the tiles [ceil(N/16), hd/64, 1152] of one (sequence, head), from row0 on."""
     hd = k.shape[1]
-    for part, x in enumerate((k, v)):
+    for part, (x, byte) in enumerate(((k, k_byte), (v, v_byte))):
         codes, steps = kv4(x)
         nib = (codes + 8).astype(np.uint8)
         nib = nib[:, 0::2] | (nib[:, 1::2] << 4)
@@ -62,18 +72,25 @@ def write_tiles(tiles, row0, k, v):
         for i in range(x.shape[0]):
             t, r = divmod(row0 + i, TILE_ROWS)
             for p in range(hd // 64):
-                tiles[t, p, part * 512 + r * 32: part * 512 + r * 32 + 32] = nib[i, p * 32: p * 32 + 32]
+                tiles[t, p, [byte(r, j) for j in range(32)]] = nib[i, p * 32: p * 32 + 32]
                 at = 1024 + part * 64 + r * 4
                 tiles[t, p, at: at + 4] = bits[i, 2 * p: 2 * p + 2].view(np.uint8)
 
 
 def decode(q, K, V, n):
-    """q [B,H,hd], K, V [B,H,N,hd] as held, n [B]: (out, tol).  The weights meet V as the sum of two bf16."""
+    """q [B,H,hd], K, V [B,H,N,hd] as held, n [B]: (out, tol).  Beside what contexts.attend allows: the query is rounded to whole
+    numbers, by 2^-18 of its largest value at most (a score error of e moves a weight by a factor within exp(+-e), in numerator and
+    denominator), the weights times the steps of V are, by 2^-28 of the largest step at most where the largest weight counts one,
+    for a code of up to 7."""
     out, tol = np.zeros(q.shape), np.zeros(q.shape)
     for b in range(q.shape[0]):
         for h in range(q.shape[1]):
-            o, p, e, _ = ctx.attend(q[b, h], K[b, h, :n[b]], V[b, h, :n[b]])
-            out[b, h], tol[b, h] = o, e + ctx.BF16 ** 2 * (p @ np.abs(V[b, h, :n[b]]) if n[b] else 0.0)
+            k, v = K[b, h, :n[b]], V[b, h, :n[b]]
+            o, p, e, _ = ctx.attend(q[b, h], k, v)
+            if n[b]:
+                score = np.abs(k).sum(1).max() * np.abs(q[b, h]).max() * 2.0 ** -18 / np.sqrt(q.shape[2])
+                e += 2 * score * (p @ np.abs(v)) + n[b] * 2.0 ** -28 * 1.01 * np.abs(v).max()
+            out[b, h], tol[b, h] = o, e
     return out, tol
 
 

@@ -9,9 +9,13 @@
 // half exactly away from zero, without a division for each value.
 //
 // A tile is 16 rows of 64 dimensions of K and of V, 1152 contiguous bytes (nine 128-byte lines, so a range of rows is one
-// bulk copy):
-//   bytes    0 ..  511   K codes, 32 bytes a row: dimension 2i in the low half of byte i, 2i+1 in the high half, as u + 8
-//   bytes  512 .. 1023   V codes
+// bulk copy).  A byte holds dimension 2i in its low half and 2i + 1 in its high half, as u + 8 (1 .. 15): such a number in a byte of its
+// own is also an 8-bit float with four exponent bits, of value (u + 8) 2^-9, so that the attention feeds codes to the tensor cores
+// after one mask (low halves) or a shift and a mask (high halves) for four of them.  Bytes lie where the attention's matrix
+// fragments want them:
+//   bytes    0 ..  511   K: two rows together, 16 dimensions of the even row, the same of the odd one, and so on
+//   bytes  512 .. 1023   V: four rows together, their bytes of two dimensions side by side; the eight 16-byte units of a row quad q (eight
+//                        dimensions each) in the order unit ^ 2q, which spreads the four quads over the shared-memory banks
 //   bytes 1024 .. 1087   K steps, two bf16 a row
 //   bytes 1088 .. 1151   V steps
 // A (sequence, head) slab is [ceil(N_max / 16)][hd / 64] tiles.
@@ -33,6 +37,19 @@ constexpr float kLeastStep = 1.17549435e-38f;               // 2^-126
 __host__ __device__ __forceinline__ int64_t slab_bytes(int cap, int hd)
 {
     return (int64_t)((cap + kTileRows - 1) / kTileRows) * (hd / 64) * kTileBytes;
+}
+
+// where the codes of dimensions 8 j .. 8 j + 7 (four bytes) of a row lie: four bytes of K in a word, four of V a word apart
+__device__ __forceinline__ int k_codes_at(int row, int j) { return (row >> 1) * 64 + (j >> 1) * 16 + (row & 1) * 8 + (j & 1) * 4; }
+__device__ __forceinline__ int v_unit_at(int quad, int j) { return kPartBytes + quad * 128 + (j ^ (2 * quad)) * 16; }
+__device__ __forceinline__ int v_codes_at(int row, int j) { return v_unit_at(row >> 2, j) + (row & 3); }
+
+// four words of four bytes each, transposed: the codes of four rows to and from the bytes of a V unit
+__device__ __forceinline__ uint4 transpose4x4(const uint4& r)
+{
+    const uint32_t a = __byte_perm(r.x, r.y, 0x5140), b = __byte_perm(r.z, r.w, 0x5140);   // bytes 0 and 1 of two rows
+    const uint32_t c = __byte_perm(r.x, r.y, 0x7362), d = __byte_perm(r.z, r.w, 0x7362);   // bytes 2 and 3
+    return make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), __byte_perm(c, d, 0x5410), __byte_perm(c, d, 0x7632));
 }
 
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)

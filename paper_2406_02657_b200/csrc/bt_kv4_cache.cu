@@ -2,8 +2,8 @@
 // of the bytes).  Both are bound by memory: 4 hd bytes of bf16 and 1.125 hd bytes of codes and steps a row.
 //
 // One warp takes a tile (16 rows x 64 dimensions of K and V).  Eight lanes hold a row's 64 dimensions, 16 bytes each, and a group
-// of eight lanes takes four consecutive rows, so that a lane group ends up with the steps of four rows and writes them in one
-// 16-byte store; the eight loads (K and V of four rows) are all in flight before the first is used.
+// of eight lanes takes four consecutive rows, so that a lane group ends up with the steps of four rows and a lane with a unit of V codes,
+// and writes either in one 16-byte store; the eight loads (K and V of four rows) are all in flight before the first is used.
 #include "bt_device.h"
 #include "bt_kernels.h"
 #include "bt_kv4.cuh"
@@ -49,19 +49,33 @@ __device__ __forceinline__ void write_tile(const Kv4Args& a, const Item& it, int
         }
     }
     uint8_t* dst = reinterpret_cast<uint8_t*>(a.kv) + (size_t)it.slab * a.slab_bytes + (size_t)(tile * (a.hd / 64) + it.plane) * kTileBytes;
+    const bool all = there[0] && there[3];
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
-        uint32_t steps[4];
+        uint32_t steps[4], codes[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4& x = part == 0 ? k[i] : v[i];
             const Step st = step_of_lanes(x);
-            if (there[i]) *reinterpret_cast<uint32_t*>(dst + part * kPartBytes + (g * 4 + i) * 32 + sub * 4) = codes8(x, st);
+            codes[i] = codes8(x, st);
             steps[i] = st.bits | __shfl_down_sync(0xffffffffu, st.bits, 4) << 16;   // both groups' (lanes 0 of eight)
+        }
+        if (part == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (there[i]) *reinterpret_cast<uint32_t*>(dst + k_codes_at(g * 4 + i, sub)) = codes[i];
+        } else if (all) {
+            *reinterpret_cast<uint4*>(dst + v_unit_at(g, sub)) = transpose4x4(make_uint4(codes[0], codes[1], codes[2], codes[3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (there[i])
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) dst[v_codes_at(g * 4 + i, sub) + 4 * j] = (uint8_t)(codes[i] >> (8 * j));
         }
         if (sub == 0) {
             uint32_t* at = reinterpret_cast<uint32_t*>(dst + kStepsAt + part * 64) + g * 4;
-            if (there[0] && there[3]) {
+            if (all) {
                 *reinterpret_cast<uint4*>(at) = make_uint4(steps[0], steps[1], steps[2], steps[3]);
             } else {
 #pragma unroll
@@ -133,15 +147,22 @@ __global__ void __launch_bounds__(kThreads) kv4_read_kernel(Kv4Args a, int tiles
     if (row0 >= end) return;
     const int g = lane >> 3, sub = lane & 7;
     const uint8_t* src = reinterpret_cast<const uint8_t*>(a.kv) + (size_t)it.slab * a.slab_bytes + (size_t)(tile * planes + it.plane) * kTileBytes;
-    uint32_t codes[2][4];
-    uint32_t steps[2][4];
+    uint32_t codes[2][4], steps[2][4];
 #pragma unroll
-    for (int part = 0; part < 2; ++part)
+    for (int j = 0; j < 4; ++j) codes[0][j] = *reinterpret_cast<const uint32_t*>(src + k_codes_at(g * 4 + j, sub));
+    const uint4 unit = transpose4x4(*reinterpret_cast<const uint4*>(src + v_unit_at(g, sub)));
+    codes[1][0] = unit.x;
+    codes[1][1] = unit.y;
+    codes[1][2] = unit.z;
+    codes[1][3] = unit.w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            codes[part][j] = *reinterpret_cast<const uint32_t*>(src + part * kPartBytes + (g * 4 + j) * 32 + sub * 4);
-            steps[part][j] = *reinterpret_cast<const uint32_t*>(src + kStepsAt + part * 64 + (g * 4 + j) * 4);
-        }
+    for (int part = 0; part < 2; ++part) {
+        const uint4 four = *reinterpret_cast<const uint4*>(src + kStepsAt + part * 64 + g * 16);
+        steps[part][0] = four.x;
+        steps[part][1] = four.y;
+        steps[part][2] = four.z;
+        steps[part][3] = four.w;
+    }
     const size_t dst0 = ((size_t)it.slab * a.stride) * a.hd + it.plane * 64 + sub * 8;
 #pragma unroll
     for (int part = 0; part < 2; ++part) {

@@ -2,19 +2,21 @@
 //
 // With (s, u) the step and code of K, (t, w) those of V, g(d) the group of 32 dimensions that d lies in:
 //   score_j = scale * sum_g s_jg sum_{d in g} q_d u_jd,     out_d = sum_j (p_j t_jg(d)) w_jd / sum_j p_j.
-// Codes are small whole numbers, exact in bf16, and steps can be taken out of both sums, so the inner sums are products of bf16
-// matrices.  What bounds the kernel is the 1.125 hd bytes a row of the cache, 3.6 times fewer than of the bf16 one, and next to
-// it the instructions: a value that is unpacked to fp32 and multiplied on its own costs three issue slots or more, and the slots
-// of 148 SMs then last for 6.7 TB/s at best.  Unpacked in pairs to bf16 (a shift, a masked or, a subtraction of two: 1.4 slots a
-// value) and multiplied by warp-level m16n8k16 instructions it is less than half.
-//
-//   scores:  A = codes of 16 rows x 16 dimensions; B = the query, each of its columns with the values of one group only and zeros
-//            elsewhere, so that a column of the result is the sum of one group.  Columns alternate between the two groups of
-//            64 dimensions, so that all four lanes that share a row hold its sums; lane c of them goes on with tile c of a chunk.
-//   output:  A = codes of V transposed, 16 dimensions x 16 rows (a word of eight codes from each of four rows a lane); B = the
-//            weights p t of a group, as two bf16 columns, the rounded weight and what the rounding left (2^-17 of the weight in
-//            all; one column alone would cost 2^-9, and the columns are there).
-// Subtracting the offset of the unpacked codes pairwise, not from the sums, keeps the products as small as they are.
+// What bounds the kernel is the 1.125 hd bytes a row of the cache, 3.6 times fewer than of the bf16 one, and next to it the
+// instructions: at 6.5 TB/s a scheduler has 800 cycles for 64 rows of 64 dimensions (8192 values), so a value may not be unpacked to
+// fp32 and multiplied on its own (three slots or more).  Codes stay whole numbers here: one mask gives the codes u + 8 of four even dimensions as
+// bytes, another those of four odd ones as 16 (u + 8), and warp-level m16n8k32 integer instructions multiply them (8 cycles each, half of
+// what 16-bit floats would take; unpacking to those also takes seven integer instructions for eight values instead of two).
+// The other operand becomes whole numbers cut into bytes, and the sums are exact:
+//   scores:  A = codes of 16 rows x 32 dimensions; B = the query, times a power of two that brings its largest value to 2^21 .. 2^22 (odd
+//            dimensions to 2^17 .. 2^18: half a step of the rounding is 2^-18 of the largest value at most), as three signed bytes.  One byte of
+//            all of them after the other is multiplied into the same sums, which are shifted in between.  A column has the values of one
+//            group only and zeros elsewhere; columns alternate between the two groups of 64 dimensions, so that all four lanes that share
+//            a row hold its two sums, and lane c of them goes on with tile c of a chunk.
+//   output:  A = codes of V transposed, 16 dimensions x 32 rows; B = the weights p t of a group as whole numbers of 32 bits, relative to
+//            2^28 .. 2^32 for the largest (so that the rounding, 2^-29 of the largest, does not add up over a million rows), a byte in each of four
+//            columns (2 groups x 4 bytes).  Sums are kept as 32-bit whole numbers until what they are relative to changes.
+// Products of the same bytes with rows of eights give what the offsets of the codes of V add; for K a sum over the query does.
 //
 // As in the streaming kernel of the bf16 cache: one persistent CTA per SM, every warp on its own with a ring of chunks (64 rows,
 // one bulk copy: tiles hold K and V), work items (sequence, head, part of the rows), partial results joined by the part that ends
@@ -36,9 +38,9 @@ struct Geo {
     static constexpr int PLANES = HD / 64;
     static constexpr int TILE = PLANES * kTileBytes;
     static constexpr int STAGE = kChunkTiles * TILE;
-    static constexpr int COLS = 4 * PLANES;                       // weights: (group, rounded or rest)
-    static constexpr int WEIGHT_TILE = (COLS * 8 + 8) * 4;        // 8 row pairs a column; 8 words apart from a multiple of 32 banks
-    static constexpr int WEIGHTS = kChunkTiles * WEIGHT_TILE;
+    static constexpr int WEIGHT_TILE = 8 * kTileRows + 16;        // 8 columns (group, byte) of 16 rows; 16 more spread the tiles over the banks
+    static constexpr int WEIGHT_PLANE = kChunkTiles * WEIGHT_TILE;
+    static constexpr int WEIGHTS = PLANES * WEIGHT_PLANE;
 };
 template <int HD>
 constexpr int smem_bytes(int warps, int stages) { return warps * (stages * (Geo<HD>::STAGE + 8) + Geo<HD>::WEIGHTS); }
@@ -55,20 +57,53 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
 }
 __device__ __forceinline__ void sts32(uint32_t addr, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(x) : "memory"); }
 
-// Codes R and R + 4 of a word as a pair of bf16: 128 + (u + 8) is a bf16 with the code in its low bits, and 136 less is exact.
-template <int R>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w)
+__device__ __forceinline__ void sts16(uint32_t addr, uint32_t x) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"((uint16_t)x) : "memory"); }
+
+// four codes of a word as bytes: u + 8 of the even dimensions, 16 (u + 8) of the odd ones
+__device__ __forceinline__ uint32_t even_codes(uint32_t w) { return w & 0x0f0f0f0fu; }
+__device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return w & 0xf0f0f0f0u; }
+// D (16 x 8, 32-bit whole numbers) += A (16 x 32, unsigned bytes) B (32 x 8, signed or unsigned bytes)
+__device__ __forceinline__ void mma_signed(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    uint32_t x = ((w >> (4 * R)) & 0x000f000fu) | 0x43004300u, d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(0x43084308u));
-    return d;
-}
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_signed_new(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(0));
+}
+__device__ __forceinline__ void mma_unsigned(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 2^(TO - e) for a largest magnitude 2^e <= x < 2^(e + 1) of what is multiplied with it, as far as that is a normal number
+template <int TO>
+__device__ __forceinline__ float power_to(float x)
+{
+    const int e = (int)(__float_as_uint(x) >> 23) & 255;                       // 127 + e
+    return __uint_as_float((uint32_t)(254 + TO - max(e, 1 + TO)) << 23);        // exponent field 127 + TO - e, at most 253
+}
+__device__ __forceinline__ float inverse_power(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
+__device__ __forceinline__ uint32_t whole(float x)
+{
+    uint32_t w;
+    asm("cvt.rni.u32.f32 %0, %1;" : "=r"(w) : "f"(x));
+    return w;
+}
+// byte B of four words
+template <int B>
+__device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4])
+{
+    return __byte_perm(__byte_perm(w[0], w[1], B | (4 + B) << 4), __byte_perm(w[2], w[3], B | (4 + B) << 4), 0x5410);
+}
+constexpr int kChunksPerSum = 512;       // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
+constexpr float kHeadroom = 4.f;         // how far (log2) scores may exceed what weights are relative to before that changes
+constexpr int kWeightTo = 27;            // the largest step of V to 2^27 .. 2^28, weights up to 2^4 times that
 // the largest of a warp's values that are numbers
 __device__ __forceinline__ float warp_max(float x)
 {
@@ -76,12 +111,6 @@ __device__ __forceinline__ float warp_max(float x)
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
     return m;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-
 // Rows r0 .. r1 - 1 of a work item; n counts the new row, which is row n - 1 and lies here when new_row is set.
 struct Work {
     int bh, sp, b, n, r0, r1;
@@ -207,27 +236,79 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
         }
         // Query fragments: lane c holds dimensions 16 c .. 16 c + 15 of a plane, in the order of the codes of two words; in the
         // columns of the other group it holds zeros.
-        uint32_t qf[PLANES][2][4];
-        const uint32_t own_group = (g & 1) == (c >> 1) ? 0xffffffffu : 0u;
+        uint32_t qf[PLANES][2][3][2];      // word, byte (highest first), even | odd dimensions
+        int q_off[PLANES][2];              // what the eights of a group's codes add to its sum
+        float q_unit;                      // what a sum has to be multiplied with
+        {
+            uint32_t top = 0;
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p)
+            for (int p = 0; p < PLANES; ++p) top = max_u16x2(top, max_u16x2(magnitude_max8(q_next[p][0]), magnitude_max8(q_next[p][1])));
+            top = max(top & 0xffffu, top >> 16);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const float to = power_to<21>(__uint_as_float(top << 16));
+            // a query with a value that is not finite gives NaN throughout
+            q_unit = top < 0x7f80u ? inverse_power(to) : __uint_as_float(0x7fffffffu);
+            const uint32_t own_group = (g & 1) == (c >> 1) ? 0xffffffffu : 0u;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint4 x = q_next[p][i];
-                qf[p][i][0] = __byte_perm(x.x, x.z, 0x5410) & own_group;
-                qf[p][i][1] = __byte_perm(x.x, x.z, 0x7632) & own_group;
-                qf[p][i][2] = __byte_perm(x.y, x.w, 0x5410) & own_group;
-                qf[p][i][3] = __byte_perm(x.y, x.w, 0x7632) & own_group;
+            for (int p = 0; p < PLANES; ++p) {
+                int sum = 0;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float f[8];
+                    unpack8(q_next[p][i], f);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int n = __float2int_rn(f[2 * j + h] * (h ? to * 0.0625f : to));
+                            sum += n * (h ? 128 : 8);
+                            x[j] = (uint32_t)n + 0x00808080u;    // bytes 0 .. 255 for digits -128 .. 127
+                        }
+                        qf[p][i][0][h] = (gather_byte<2>(x) ^ 0x80808080u) & own_group;
+                        qf[p][i][1][h] = (gather_byte<1>(x) ^ 0x80808080u) & own_group;
+                        qf[p][i][2][h] = (gather_byte<0>(x) ^ 0x80808080u) & own_group;
+                    }
+                }
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);      // the two lanes of a group
+                const int other = __shfl_xor_sync(0xffffffffu, sum, 2);
+                q_off[p][0] = c < 2 ? sum : other;
+                q_off[p][1] = c < 2 ? other : sum;
             }
+        }
         if (cn.item < n_items) fetch_q(cn.bh);
-        float m = kNegInf, l = 0.f;
-        float o[PLANES][4][4];
+        float m = kNegInf, l = 0.f;                // what scores are relative to, the sum of 2^(score - m)
+        float t_most = 0.f, t_to = power_to<kWeightTo>(0.f);   // the largest step of V so far and the power of two for it
+        float o[PLANES][4][2], bad[PLANES][2];     // even | odd dimension; not a number once a step of V was none
+        int sums[PLANES][4][4], eights[PLANES][4], pending = 0;
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p)
+        for (int p = 0; p < PLANES; ++p) {
+            bad[p][0] = bad[p][1] = 0.f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r) {
+                o[p][r][0] = o[p][r][1] = 0.f;
+                eights[p][r] = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[p][r][i] = 0.f;
+                for (int i = 0; i < 4; ++i) sums[p][r][i] = 0;
+            }
+        }
+        // the whole-number sums of bytes b and b + 1 of the weights into the outputs (lanes with odd c: bytes 2 and 3, 2^16 times as much in the end)
+        auto flush = [&]() {
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    o[p][r][0] += fmaf(256.f, (float)(sums[p][r][1] - eights[p][1]), (float)(sums[p][r][0] - eights[p][0]));
+                    o[p][r][1] += fmaf(256.f, (float)(sums[p][r][3] - eights[p][3]), (float)(sums[p][r][2] - eights[p][2]));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sums[p][r][i] = 0;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) eights[p][i] = 0;
+            }
+            pending = 0;
+        };
 
         for (int row = w.r0; row < w.r1; row += kChunkRows) {
             const uint32_t sidx = consumed % STAGES;
@@ -245,104 +326,137 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
                 const Step sg = step_of_lanes(x);
                 const uint32_t codes = codes8(x, sg);
                 if (lane < 2 * LPR) {
-                    const int r = w.n - 1 - row;
+                    const int r = w.n - 1 - row, in_tile = r % kTileRows, j = piece & 7;
                     const uint32_t tile = (uint32_t)(r / kTileRows) * G::TILE + (piece / 8) * kTileBytes;
-                    const uint32_t code_at = tile + part * kPartBytes + (r % kTileRows) * 32 + (piece & 7) * 4;
-                    const uint32_t step_at = tile + kStepsAt + part * 64 + (r % kTileRows) * 4 + ((piece >> 2) & 1) * 2;
+                    const uint32_t step_at = tile + kStepsAt + part * 64 + in_tile * 4 + (j >> 2) * 2;
                     uint8_t* copy = ring_ptr + sidx * G::STAGE;
                     uint8_t* held = kv + (size_t)w.bh * a.slab_bytes + (size_t)(row / kTileRows) * G::TILE;
-                    *reinterpret_cast<uint32_t*>(copy + code_at) = codes;
-                    *reinterpret_cast<uint32_t*>(held + code_at) = codes;
-                    if ((piece & 3) == 0) {
+                    if (part == 0) {
+                        const uint32_t at = tile + k_codes_at(in_tile, j);
+                        *reinterpret_cast<uint32_t*>(copy + at) = codes;
+                        *reinterpret_cast<uint32_t*>(held + at) = codes;
+                    } else {
+                        const uint32_t at = tile + v_codes_at(in_tile, j);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) copy[at + 4 * i] = held[at + 4 * i] = (uint8_t)(codes >> (8 * i));
+                    }
+                    if ((j & 3) == 0) {
                         *reinterpret_cast<uint16_t*>(copy + step_at) = (uint16_t)sg.bits;
                         *reinterpret_cast<uint16_t*>(held + step_at) = (uint16_t)sg.bits;
                     }
                 }
                 __syncwarp();
             }
-            // ---- scores of rows 16 c + g and 16 c + g + 8 of the chunk, in this lane
+            // ---- scores of rows 16 c + 2 g and 16 c + 2 g + 1 of the chunk, in this lane
             float s0 = 0.f, s1 = 0.f;
+            const uint32_t own_tile = st + c * G::TILE + g * 8;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
-                float acc[kChunkTiles][4];
+                int acc[kChunkTiles][4];
 #pragma unroll
                 for (int t = 0; t < kChunkTiles; ++t) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t][i] = 0.f;
                     if (t < ntiles) {
-                        const uint32_t at = st + t * G::TILE + p * kTileBytes + g * 32 + c * 8;
-                        uint32_t x[2], y[2];
-                        lds64(at, x[0], x[1]);
-                        lds64(at + 8 * 32, y[0], y[1]);
+                        const uint4 x = lds128(st + t * G::TILE + p * kTileBytes + lane * 16);   // two words of the even row, two of the odd
+                        const uint32_t a0 = even_codes(x.x), a1 = even_codes(x.z), a2 = odd_codes(x.x), a3 = odd_codes(x.z);
+                        const uint32_t b0 = even_codes(x.y), b1 = even_codes(x.w), b2 = odd_codes(x.y), b3 = odd_codes(x.w);
+                        mma_signed_new(acc[t], a0, a1, a2, a3, qf[p][0][0][0], qf[p][0][0][1]);
+                        mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][0][0], qf[p][1][0][1]);
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            mma(acc[t], code_pair<0>(x[i]), code_pair<0>(y[i]), code_pair<1>(x[i]), code_pair<1>(y[i]), qf[p][i][0], qf[p][i][1]);
-                            mma(acc[t], code_pair<2>(x[i]), code_pair<2>(y[i]), code_pair<3>(x[i]), code_pair<3>(y[i]), qf[p][i][2], qf[p][i][3]);
+                        for (int byte = 1; byte < 3; ++byte) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[t][i] *= 256;
+                            mma_signed(acc[t], a0, a1, a2, a3, qf[p][0][byte][0], qf[p][0][byte][1]);
+                            mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][byte][0], qf[p][1][byte][1]);
                         }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][i] = 0;
                     }
                 }
                 float mine[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float lo = c & 1 ? acc[1][i] : acc[0][i], hi = c & 1 ? acc[3][i] : acc[2][i];
-                    mine[i] = c & 2 ? hi : lo;
+                    const int lo = c & 1 ? acc[1][i] : acc[0][i], hi = c & 1 ? acc[3][i] : acc[2][i];
+                    mine[i] = (float)((c & 2 ? hi : lo) - q_off[p][i & 1]);
                 }
-                const uint32_t steps = st + c * G::TILE + p * kTileBytes + kStepsAt + g * 4;
-                const uint32_t k0 = lds32(steps), k1 = lds32(steps + 8 * 4);
+                uint32_t k0, k1;
+                lds64(own_tile + p * kTileBytes + kStepsAt, k0, k1);
                 s0 = fmaf(mine[1], bf_hi(k0), fmaf(mine[0], bf_lo(k0), s0));
                 s1 = fmaf(mine[3], bf_hi(k1), fmaf(mine[2], bf_lo(k1), s1));
             }
-            const bool in0 = 16 * c + g < nvalid, in1 = 16 * c + g + 8 < nvalid;
-            s0 = in0 ? s0 * a.scale_log2 : kNegInf;
-            s1 = in1 ? s1 * a.scale_log2 : kNegInf;
+            const bool in0 = 16 * c + 2 * g < nvalid, in1 = 16 * c + 2 * g + 1 < nvalid;
+            s0 = in0 ? s0 * q_unit * a.scale_log2 : kNegInf;
+            s1 = in1 ? s1 * q_unit * a.scale_log2 : kNegInf;
+            // steps of V of the two rows; a row that is not there has no weight whatever its step is
+            float t0[PLANES][2], t1[PLANES][2], most = t_most;
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+                uint32_t v0, v1;
+                lds64(own_tile + p * kTileBytes + kStepsAt + 64, v0, v1);
+                v0 = in0 ? v0 : 0u;
+                v1 = in1 ? v1 : 0u;
+                t0[p][0] = bf_lo(v0);
+                t0[p][1] = bf_hi(v0);
+                t1[p][0] = bf_lo(v1);
+                t1[p][1] = bf_hi(v1);
+                most = fmaxf(most, fmaxf(fmaxf(t0[p][0], t0[p][1]), fmaxf(t1[p][0], t1[p][1])));
+                bad[p][0] = fmaf(0.f, t0[p][0], fmaf(0.f, t1[p][0], bad[p][0]));
+                bad[p][1] = fmaf(0.f, t0[p][1], fmaf(0.f, t1[p][1], bad[p][1]));
+            }
             const float mn = fmaxf(m, warp_max(fmaxf(s0, s1)));
-            const float m_use = softmax_reference(mn);
-            if (mn > m) {   // warp-uniform; where the maximum stays the factor is one
-                const float cf = ex2(m - m_use);
+            t_most = warp_max(most);
+            const float to = power_to<kWeightTo>(t_most);
+            // What weights are relative to changes (for all of the warp) when a score would leave the headroom or a step of V the range.
+            const bool grown = mn > m + kHeadroom || (m == kNegInf && mn > m);
+            if (grown || to != t_to || pending == kChunksPerSum) {
+                if (pending > 0) flush();
+                const float m2 = grown ? mn : m, cf = ex2(m - softmax_reference(m2));
                 l *= cf;
+                const float co = cf * (to * inverse_power(t_to));
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[p][r][i] *= cf;
-                m = mn;
+                    for (int r = 0; r < 4; ++r) {
+                        o[p][r][0] *= co;
+                        o[p][r][1] *= co;
+                    }
+                m = m2;
+                t_to = to;
             }
+            ++pending;
+            const float m_use = softmax_reference(m);
             const float p0 = ex2(s0 - m_use), p1 = ex2(s1 - m_use);
             l += p0 + p1;
-            // ---- weights of the two rows, a pair of them a word: column 2 (group) the rounded ones, column 2 (group) + 1 the rest
+            // ---- weights of the two rows: column 4 (group) + byte of a plane
+            const float w0 = p0 * t_to, w1 = p1 * t_to;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
-                const uint32_t steps = st + c * G::TILE + p * kTileBytes + kStepsAt + 64 + g * 4;
-                const uint32_t v0 = lds32(steps), v1 = lds32(steps + 8 * 4);
 #pragma unroll
                 for (int gl = 0; gl < 2; ++gl) {
-                    const float w0 = in0 ? p0 * (gl ? bf_hi(v0) : bf_lo(v0)) : 0.f;
-                    const float w1 = in1 ? p1 * (gl ? bf_hi(v1) : bf_lo(v1)) : 0.f;
-                    const uint32_t near = pack_bf16(w0, w1);
-                    const uint32_t rest = pack_bf16(w0 - bf_lo(near), w1 - bf_hi(near));
-                    const uint32_t at = wbuf + c * G::WEIGHT_TILE + (2 * (2 * p + gl)) * 32 + ((g & 3) * 2 + (g >> 2)) * 4;
-                    sts32(at, near);
-                    sts32(at + 32, rest);
+                    const uint32_t at = wbuf + p * G::WEIGHT_PLANE + c * G::WEIGHT_TILE + gl * (4 * kTileRows) + 2 * g;
+                    const uint32_t x = whole(w0 * t0[p][gl]), y = whole(w1 * t1[p][gl]);
+                    sts16(at, __byte_perm(x, y, 0x0040));
+                    sts16(at + kTileRows, __byte_perm(x, y, 0x0051));
+                    sts16(at + 2 * kTileRows, __byte_perm(x, y, 0x0062));
+                    sts16(at + 3 * kTileRows, __byte_perm(x, y, 0x0073));
                 }
             }
             __syncwarp();
-            // ---- weighted codes of V: rows c, c + 8 | c + 4, c + 12 of a tile are this lane's pairs
+            // ---- weighted codes of V: rows 4 c .. 4 c + 3 of two tiles are this lane's
 #pragma unroll
-            for (int t = 0; t < kChunkTiles; ++t) {
-                if (t < ntiles) {
-                    uint32_t b0, b1;
-                    lds64(wbuf + t * G::WEIGHT_TILE + (g % G::COLS) * 32 + c * 8, b0, b1);
+            for (int t = 0; t < kChunkTiles; t += 2) {
+                if (t < ntiles) {   // (codes of a second tile that is not there meet weights of zero)
 #pragma unroll
                     for (int p = 0; p < PLANES; ++p) {
-                        const uint32_t at = st + t * G::TILE + p * kTileBytes + kPartBytes + c * 32 + g * 4;
-                        const uint32_t x0 = lds32(at), x1 = lds32(at + 4 * 32), x2 = lds32(at + 8 * 32), x3 = lds32(at + 12 * 32);
-                        const uint32_t l02 = __byte_perm(x0, x2, 0x5410), h02 = __byte_perm(x0, x2, 0x7632);
-                        const uint32_t l13 = __byte_perm(x1, x3, 0x5410), h13 = __byte_perm(x1, x3, 0x7632);
-                        mma(o[p][0], code_pair<0>(l02), code_pair<0>(h02), code_pair<0>(l13), code_pair<0>(h13), b0, b1);
-                        mma(o[p][1], code_pair<1>(l02), code_pair<1>(h02), code_pair<1>(l13), code_pair<1>(h13), b0, b1);
-                        mma(o[p][2], code_pair<2>(l02), code_pair<2>(h02), code_pair<2>(l13), code_pair<2>(h13), b0, b1);
-                        mma(o[p][3], code_pair<3>(l02), code_pair<3>(h02), code_pair<3>(l13), code_pair<3>(h13), b0, b1);
+                        const uint32_t wt = wbuf + p * G::WEIGHT_PLANE + t * G::WEIGHT_TILE + lane * 4;
+                        const uint32_t b0 = lds32(wt), b1 = lds32(wt + G::WEIGHT_TILE);
+                        const uint32_t at = st + t * G::TILE + p * kTileBytes + kPartBytes + c * 128 + ((g ^ (2 * c)) << 4);
+                        const uint4 x = lds128(at), y = lds128(at + G::TILE);
+                        mma_unsigned(sums[p][0], even_codes(x.x), odd_codes(x.x), even_codes(y.x), odd_codes(y.x), b0, b1);
+                        mma_unsigned(sums[p][1], even_codes(x.y), odd_codes(x.y), even_codes(y.y), odd_codes(y.y), b0, b1);
+                        mma_unsigned(sums[p][2], even_codes(x.z), odd_codes(x.z), even_codes(y.z), odd_codes(y.z), b0, b1);
+                        mma_unsigned(sums[p][3], even_codes(x.w), odd_codes(x.w), even_codes(y.w), odd_codes(y.w), b0, b1);
+                        mma_unsigned(eights[p], 0x08080808u, 0x80808080u, 0x08080808u, 0x80808080u, b0, b1);
                     }
                 }
             }
@@ -356,16 +470,22 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
         if (!alive) break;
 #pragma unroll
         for (int off = 16; off >= 1; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-        // Lane (g, c) holds dimensions 8 g .. 8 g + 7 of a plane under the weights of group c: the ones that count where that is
-        // their group.  Rounded weights and rests are added up here.
-        auto own_piece = [&](int p) { return c == 2 * p + (g >> 2); };
+        flush();
+        // Lane (g, c) holds dimensions 8 g .. 8 g + 7 of a plane under two bytes of the weights of group c >> 1: the low ones in lanes of even c,
+        // the high ones in those of odd c.  They count where that is the dimensions' group, and are added up here.
+        const bool own_piece = c == 2 * (g >> 2);
+        const float high = c & 1 ? 65536.f : 1.f;
+        const float unit = inverse_power(t_to) * inverse_sum(l);
         auto piece = [&](int p, float (&f)[8]) {
-            const float inv = inverse_sum(l);
+            const bool bad0 = __any_sync(0xffffffffu, bad[p][0] != 0.f), bad1 = __any_sync(0xffffffffu, bad[p][1] != 0.f);
+            const float u = (g < 4 ? bad0 : bad1) ? __uint_as_float(0x7fffffffu) : unit;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                f[r] = (o[p][r][0] + o[p][r][1]) * inv;
-                f[r + 4] = (o[p][r][2] + o[p][r][3]) * inv;
+                f[2 * r] = o[p][r][0] * high;
+                f[2 * r + 1] = o[p][r][1] * (high * 0.0625f);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = (f[i] + __shfl_xor_sync(0xffffffffu, f[i], 1)) * u;
         };
         bf16* const out = reinterpret_cast<bf16*>(a.out) + (size_t)w.bh * HD;
         if (a.splits == 1) {
@@ -373,7 +493,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
             for (int p = 0; p < PLANES; ++p) {
                 float f[8];
                 piece(p, f);
-                if (own_piece(p)) *reinterpret_cast<uint4*>(out + p * 64 + g * 8) = pack8(f);
+                if (own_piece) *reinterpret_cast<uint4*>(out + p * 64 + g * 8) = pack8(f);
             }
         } else {
             float* ws = a.ws + ((size_t)w.bh * a.splits + w.sp) * (HD + 4);
@@ -381,7 +501,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
             for (int p = 0; p < PLANES; ++p) {
                 float f[8];
                 piece(p, f);
-                if (own_piece(p)) {
+                if (own_piece) {
                     *reinterpret_cast<float4*>(ws + p * 64 + g * 8) = make_float4(f[0], f[1], f[2], f[3]);
                     *reinterpret_cast<float4*>(ws + p * 64 + g * 8 + 4) = make_float4(f[4], f[5], f[6], f[7]);
                 }

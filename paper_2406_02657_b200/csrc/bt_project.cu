@@ -182,9 +182,19 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
             m = kv4::max_u16x2(m, kv4::magnitude_max8(x[i]));
         }
         const kv4::Step st = kv4::step_of_group<7>(m);
-        const uint4 codes = make_uint4(kv4::codes8(x[0], st), kv4::codes8(x[1], st), kv4::codes8(x[2], st), kv4::codes8(x[3], st));
-        *reinterpret_cast<uint4*>(tile + part * kv4::kPartBytes + at * 32 + grp * 16) = codes;
         steps |= st.bits << (16 * grp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = grp * 4 + i;
+            const uint32_t codes = kv4::codes8(x[i], st);
+            if (part == 0) {
+                *reinterpret_cast<uint32_t*>(tile + kv4::k_codes_at(at, j)) = codes;
+            } else {
+                uint8_t* bytes = tile + kv4::v_codes_at(at, j);   // a byte for each pair of dimensions: the row's neighbours lie between
+#pragma unroll
+                for (int q = 0; q < 4; ++q) bytes[4 * q] = (uint8_t)(codes >> (8 * q));
+            }
+        }
     }
     *reinterpret_cast<uint32_t*>(tile + kv4::kStepsAt + part * 64 + at * 4) = steps;
 }

@@ -172,7 +172,10 @@ def test_tiles_hold_the_rows():
         for r in (0, 15, 16, 19):
             for d in (0, 1, 31, 32, 63, 64, 127):
                 tile, p = tiles[r // 16, d // 64], d % 64
-                byte = tile[part * 512 + (r % 16) * 32 + p // 2]
+                i = p // 2                                       # the layout again, written out
+                at = (r % 16 // 2) * 64 + (i // 8) * 16 + (r % 2) * 8 + i % 8 if part == 0 else \
+                    512 + (r % 16 // 4) * 128 + ((i // 4) ^ (2 * (r % 16 // 4))) * 16 + (i % 4) * 4 + r % 4
+                byte = tile[at]
                 code = int(byte >> 4 if p % 2 else byte & 15) - 8
                 at = 1024 + part * 64 + (r % 16) * 4 + (p // 32) * 2
                 step = gen.bf16_bits_to_f32(tile[at:at + 2].view(np.uint16))[0]
