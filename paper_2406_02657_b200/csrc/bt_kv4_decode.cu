@@ -65,19 +65,19 @@ __device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return w & 0xf0f0f0f
 // D (16 x 8, 32-bit whole numbers) += A (16 x 32, unsigned bytes) B (32 x 8, signed or unsigned bytes)
 __device__ __forceinline__ void mma_signed(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_signed_new(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
                  : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(0));
 }
 __device__ __forceinline__ void mma_unsigned(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -116,13 +116,12 @@ struct Work {
     int bh, sp, b, n, r0, r1;
     bool new_row, overflow;
 };
-__device__ __forceinline__ Work work_at(const Cursor& c, const Kv4DecodeArgs& a)
+__device__ __forceinline__ Work work_of(const Cursor& c, const Kv4DecodeArgs& a, int n)   // n: the sequence's length
 {
     Work w;
     w.bh = c.bh;
     w.sp = c.sp;
     w.b = c.b;
-    int n = a.len[w.b];
     n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
     const bool append = a.k_new != nullptr && n < a.n_max;   // a full cache takes no row: flagged, attended as it is
     w.overflow = a.k_new != nullptr && !append;
@@ -136,6 +135,7 @@ __device__ __forceinline__ Work work_at(const Cursor& c, const Kv4DecodeArgs& a)
     w.new_row = append && w.r1 == n && w.r0 < n;
     return w;
 }
+__device__ __forceinline__ Work work_at(const Cursor& c, const Kv4DecodeArgs& a) { return work_of(c, a, a.len[c.b]); }
 
 template <int HD, int STAGES, int MAX_WARPS>
 __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4DecodeArgs a)
@@ -164,12 +164,20 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
     const int stride = n_warps * gridDim.x;
     const int first = warp * gridDim.x + blockIdx.x;   // neighbouring items go to different SMs
     uint8_t* const kv = reinterpret_cast<uint8_t*>(a.kv);
-    pdl_wait();
-
-    // ---- producer cursor (kept by every lane, acted on by lane 0): next chunk to request
     const ring::Step step = ring::step_of(stride, a);
     Cursor pc = ring::cursor_at(first < n_items ? first : 0, a);
     pc.item = first;
+    // While the kernel before this one drains, have the chunks that this warp will request first brought into L2: which those are comes
+    // from a look at the length that may be out of date (read past L1), so it is a hint and decides nothing.
+    if (first < n_items && lane == 0) {
+        const Work h = work_of(pc, a, __ldcg(a.len + pc.b));
+        const uint32_t bytes = (uint32_t)((min(STAGES * kChunkRows, h.r1 - h.r0) + kTileRows - 1) / kTileRows) * G::TILE;
+        if (bytes > 0)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(kv + (size_t)h.bh * a.slab_bytes + (size_t)(h.r0 / kTileRows) * G::TILE), "r"(bytes) : "memory");
+    }
+    pdl_wait();
+
+    // ---- producer cursor (kept by every lane, acted on by lane 0): next chunk to request
     int p_row = 0;
     Work pw = {};
     auto p_seek = [&]() {   // move to the next item that has rows
@@ -318,7 +326,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
                 break;
             }
             const uint32_t st = ring0 + sidx * G::STAGE;
-            const int nvalid = min(kChunkRows, w.r1 - row), ntiles = (nvalid + kTileRows - 1) / kTileRows;
+            const int nvalid = min(kChunkRows, w.r1 - row);
             if (w.new_row && row + kChunkRows >= w.r1) {
                 // the new row, eight values a lane: lanes 0 .. LPR - 1 K, the next V (at head_dim 64 the upper half repeats them)
                 const int part = (lane / LPR) & 1, piece = lane % LPR;
@@ -353,24 +361,21 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
                 int acc[kChunkTiles][4];
+                // (Tiles that the chunk has not are multiplied all the same: what a stage holds there is whole numbers too, and their scores
+                // are set aside below.  Without branches the tiles' instructions interleave.)
 #pragma unroll
                 for (int t = 0; t < kChunkTiles; ++t) {
-                    if (t < ntiles) {
-                        const uint4 x = lds128(st + t * G::TILE + p * kTileBytes + lane * 16);   // two words of the even row, two of the odd
-                        const uint32_t a0 = even_codes(x.x), a1 = even_codes(x.z), a2 = odd_codes(x.x), a3 = odd_codes(x.z);
-                        const uint32_t b0 = even_codes(x.y), b1 = even_codes(x.w), b2 = odd_codes(x.y), b3 = odd_codes(x.w);
-                        mma_signed_new(acc[t], a0, a1, a2, a3, qf[p][0][0][0], qf[p][0][0][1]);
-                        mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][0][0], qf[p][1][0][1]);
+                    const uint4 x = lds128(st + t * G::TILE + p * kTileBytes + lane * 16);   // two words of the even row, two of the odd
+                    const uint32_t a0 = even_codes(x.x), a1 = even_codes(x.z), a2 = odd_codes(x.x), a3 = odd_codes(x.z);
+                    const uint32_t b0 = even_codes(x.y), b1 = even_codes(x.w), b2 = odd_codes(x.y), b3 = odd_codes(x.w);
+                    mma_signed_new(acc[t], a0, a1, a2, a3, qf[p][0][0][0], qf[p][0][0][1]);
+                    mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][0][0], qf[p][1][0][1]);
 #pragma unroll
-                        for (int byte = 1; byte < 3; ++byte) {
+                    for (int byte = 1; byte < 3; ++byte) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[t][i] *= 256;
-                            mma_signed(acc[t], a0, a1, a2, a3, qf[p][0][byte][0], qf[p][0][byte][1]);
-                            mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][byte][0], qf[p][1][byte][1]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[t][i] = 0;
+                        for (int i = 0; i < 4; ++i) acc[t][i] *= 256;
+                        mma_signed(acc[t], a0, a1, a2, a3, qf[p][0][byte][0], qf[p][0][byte][1]);
+                        mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][byte][0], qf[p][1][byte][1]);
                     }
                 }
                 float mine[4];
@@ -444,20 +449,18 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
             __syncwarp();
             // ---- weighted codes of V: rows 4 c .. 4 c + 3 of two tiles are this lane's
 #pragma unroll
-            for (int t = 0; t < kChunkTiles; t += 2) {
-                if (t < ntiles) {   // (codes of a second tile that is not there meet weights of zero)
+            for (int t = 0; t < kChunkTiles; t += 2) {   // (rows that are not there have weights of zero)
 #pragma unroll
-                    for (int p = 0; p < PLANES; ++p) {
-                        const uint32_t wt = wbuf + p * G::WEIGHT_PLANE + t * G::WEIGHT_TILE + lane * 4;
-                        const uint32_t b0 = lds32(wt), b1 = lds32(wt + G::WEIGHT_TILE);
-                        const uint32_t at = st + t * G::TILE + p * kTileBytes + kPartBytes + c * 128 + ((g ^ (2 * c)) << 4);
-                        const uint4 x = lds128(at), y = lds128(at + G::TILE);
-                        mma_unsigned(sums[p][0], even_codes(x.x), odd_codes(x.x), even_codes(y.x), odd_codes(y.x), b0, b1);
-                        mma_unsigned(sums[p][1], even_codes(x.y), odd_codes(x.y), even_codes(y.y), odd_codes(y.y), b0, b1);
-                        mma_unsigned(sums[p][2], even_codes(x.z), odd_codes(x.z), even_codes(y.z), odd_codes(y.z), b0, b1);
-                        mma_unsigned(sums[p][3], even_codes(x.w), odd_codes(x.w), even_codes(y.w), odd_codes(y.w), b0, b1);
-                        mma_unsigned(eights[p], 0x08080808u, 0x80808080u, 0x08080808u, 0x80808080u, b0, b1);
-                    }
+                for (int p = 0; p < PLANES; ++p) {
+                    const uint32_t wt = wbuf + p * G::WEIGHT_PLANE + t * G::WEIGHT_TILE + lane * 4;
+                    const uint32_t b0 = lds32(wt), b1 = lds32(wt + G::WEIGHT_TILE);
+                    const uint32_t at = st + t * G::TILE + p * kTileBytes + kPartBytes + c * 128 + ((g ^ (2 * c)) << 4);
+                    const uint4 x = lds128(at), y = lds128(at + G::TILE);
+                    mma_unsigned(sums[p][0], even_codes(x.x), odd_codes(x.x), even_codes(y.x), odd_codes(y.x), b0, b1);
+                    mma_unsigned(sums[p][1], even_codes(x.y), odd_codes(x.y), even_codes(y.y), odd_codes(y.y), b0, b1);
+                    mma_unsigned(sums[p][2], even_codes(x.z), odd_codes(x.z), even_codes(y.z), odd_codes(y.z), b0, b1);
+                    mma_unsigned(sums[p][3], even_codes(x.w), odd_codes(x.w), even_codes(y.w), odd_codes(y.w), b0, b1);
+                    mma_unsigned(eights[p], 0x08080808u, 0x80808080u, 0x08080808u, 0x80808080u, b0, b1);
                 }
             }
             // The stage and the weights have been read by every lane before either is written again; what was put into the stage
@@ -514,22 +517,41 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
             last = __shfl_sync(0xffffffffu, last, 0);
             if (last) {   // every part of (b,h) has written: fold the partials (normalised, weight 2^lse each)
                 __threadfence();
-                const int sub = lane % LPR;
-                SoftmaxState state;
-                state.init();
-                for (int s2 = lane / LPR; s2 < a.splits; s2 += 32 / LPR) {
-                    const float* part = a.ws + ((size_t)w.bh * a.splits + s2) * (HD + 4);
-                    const float lse = __ldcg(part + HD);
-                    const float4 x = __ldcg(reinterpret_cast<const float4*>(part + sub * 8));
-                    const float4 y = __ldcg(reinterpret_cast<const float4*>(part + sub * 8 + 4));
-                    const float a2[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                    state.merge(lse, 1.f, a2);
+                // their weights first, two parts a lane at most (splits <= 64), then HD / 32 dimensions a lane, the loads independent of one another
+                constexpr int DIMS = HD / 32;
+                const float* parts = a.ws + (size_t)w.bh * a.splits * (HD + 4);
+                float lse0 = lane < a.splits ? __ldcg(parts + lane * (HD + 4) + HD) : kNegInf;
+                float lse1 = lane + 32 < a.splits ? __ldcg(parts + (lane + 32) * (HD + 4) + HD) : kNegInf;
+                const float ref = softmax_reference(warp_max(fmaxf(lse0, lse1)));
+                lse0 = ex2(lse0 - ref);
+                lse1 = ex2(lse1 - ref);
+                float total = lse0 + lse1;
+#pragma unroll
+                for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+                float f[DIMS];
+#pragma unroll
+                for (int i = 0; i < DIMS; ++i) f[i] = 0.f;
+#pragma unroll 6
+                for (int s2 = 0; s2 < a.splits; ++s2) {
+                    const float weight = __shfl_sync(0xffffffffu, s2 < 32 ? lse0 : lse1, s2 & 31);
+                    const float* part = parts + s2 * (HD + 4) + lane * DIMS;
+                    if constexpr (DIMS == 4) {
+                        const float4 x = __ldcg(reinterpret_cast<const float4*>(part));
+                        f[0] = fmaf(weight, x.x, f[0]);
+                        f[1] = fmaf(weight, x.y, f[1]);
+                        f[2] = fmaf(weight, x.z, f[2]);
+                        f[3] = fmaf(weight, x.w, f[3]);
+                    } else {
+                        const float2 x = __ldcg(reinterpret_cast<const float2*>(part));
+                        f[0] = fmaf(weight, x.x, f[0]);
+                        f[1] = fmaf(weight, x.y, f[1]);
+                    }
                 }
-                state.merge_row_groups<LPR>();
-                if (lane < LPR) {
-                    float f[8];
-                    state.normalised(f);
-                    *reinterpret_cast<uint4*>(out + sub * 8) = pack8(f);
+                const float inv = inverse_sum(total);
+#pragma unroll
+                for (int i = 0; i < DIMS; i += 2) {
+                    const __nv_bfloat162 pair = __floats2bfloat162_rn(f[i] * inv, f[i + 1] * inv);
+                    *reinterpret_cast<__nv_bfloat162*>(out + lane * DIMS + i) = pair;
                 }
                 if (lane == 0) a.counters[w.bh] = 0;
             }
@@ -557,9 +579,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
 
 #ifndef BT_KV4_WARPS_64
 #define BT_KV4_WARPS_64 16
-#define BT_KV4_STAGES_64 3
+#define BT_KV4_STAGES_64 2
 #define BT_KV4_WARPS_128 8
-#define BT_KV4_STAGES_128 3
+#define BT_KV4_STAGES_128 2
 #endif
 
 template <int HD, int STAGES, int MAX_WARPS>
@@ -574,8 +596,20 @@ static cudaError_t launch_t(const Kv4DecodeArgs& a, cudaStream_t stream)
     const long long items = (long long)a.B * a.H * a.splits;
     if (items > 0x7fffffffLL - 4096) return cudaErrorInvalidConfiguration;
     const long long grid = items < sms ? items : sms;
+    // Items are dealt whole: of the warp counts down to five eighths of the most, the one that leaves the fewest warps without an item in
+    // the last round (4096 items on 148 SMs: 14 warps, 1.98 rounds of two; 16 warps 1.73).
+    int warps = MAX_WARPS;
+    double best = 0.0;
+    for (int w = MAX_WARPS; w >= MAX_WARPS * 5 / 8; --w) {
+        const long long slots = grid * w, rounds = (items + slots - 1) / slots;
+        const double fill = (double)items / (double)(rounds * slots);
+        if (fill > best + 1e-9) {
+            best = fill;
+            warps = w;
+        }
+    }
     const long long each = (items + grid - 1) / grid;
-    const int warps = (int)(each < MAX_WARPS ? each : MAX_WARPS);
+    if (each < warps) warps = (int)each;
     return launch_pdl(block_decode_kv4_kernel<HD, STAGES, MAX_WARPS>, dim3((unsigned)grid), dim3(warps * 32), (size_t)smem_bytes<HD>(warps, STAGES), stream, a);
 }
 
