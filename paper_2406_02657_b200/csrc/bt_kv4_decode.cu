@@ -28,8 +28,6 @@
 namespace bt {
 namespace kv4 {
 
-using ring::Cursor;
-
 constexpr int kChunkTiles = 4, kChunkRows = kChunkTiles * kTileRows;
 constexpr uint32_t kPollLimit = 1u << 24;   // polls of one wait before giving up (each poll suspends briefly)
 
@@ -103,6 +101,7 @@ __device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4])
 }
 constexpr int kChunksPerSum = 512;       // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
 constexpr float kHeadroom = 4.f;         // how far (log2) scores may exceed what weights are relative to before that changes
+constexpr int kJoin = 16;               // partial results requested at once
 constexpr int kWeightTo = 27;            // the largest step of V to 2^27 .. 2^28, weights up to 2^4 times that
 // the largest of a warp's values that are numbers
 __device__ __forceinline__ float warp_max(float x)
@@ -111,34 +110,50 @@ __device__ __forceinline__ float warp_max(float x)
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
     return m;
 }
-// Rows r0 .. r1 - 1 of a work item; n counts the new row, which is row n - 1 and lies here when new_row is set.
+// Division of numbers below 2^31 by a launch's constant: the high word of a product with ceil(2^k / d), k = 31 + bits of d - 1.
+struct Divisor {
+    uint32_t mul, shift;   // mul == 0: by one
+};
+inline Divisor divisor_of(uint32_t d)
+{
+    if (d <= 1) return {0u, 0u};
+    uint32_t bits = 0;
+    while ((1ull << bits) < d) ++bits;
+    return {(uint32_t)(((1ull << (31 + bits)) + d - 1) / d), bits - 1};
+}
+__device__ __forceinline__ int divide(int n, const Divisor& d) { return d.mul ? (int)(__umulhi((uint32_t)n, d.mul) >> d.shift) : n; }
+
+struct Params : Kv4DecodeArgs {
+    Divisor by_splits, by_heads;
+};
+
+// Work item (b, h, part): its rows r0 .. r1 - 1; n counts the new row, which is row n - 1 and lies here when new_row is set.
 struct Work {
     int bh, sp, b, n, r0, r1;
     bool new_row, overflow;
 };
-__device__ __forceinline__ Work work_of(const Cursor& c, const Kv4DecodeArgs& a, int n)   // n: the sequence's length
+__device__ __forceinline__ int sequence_of(int item, const Params& a) { return divide(divide(item, a.by_splits), a.by_heads); }
+__device__ __forceinline__ Work work_of(int item, const Params& a, int n)   // n: the sequence's length
 {
     Work w;
-    w.bh = c.bh;
-    w.sp = c.sp;
-    w.b = c.b;
+    w.bh = divide(item, a.by_splits);
+    w.sp = item - w.bh * a.splits;
+    w.b = divide(w.bh, a.by_heads);
     n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
     const bool append = a.k_new != nullptr && n < a.n_max;   // a full cache takes no row: flagged, attended as it is
     w.overflow = a.k_new != nullptr && !append;
     n += append ? 1 : 0;
     w.n = n;
     // whole chunks per part, as even as that goes (trailing parts may be empty)
-    const int chunks = (n + kChunkRows - 1) / kChunkRows;
-    const int per = a.splits == 1 ? chunks : (chunks + a.splits - 1) / a.splits;
-    w.r0 = min(n, w.sp * per * kChunkRows);
-    w.r1 = min(n, w.r0 + per * kChunkRows);
+    const int per = divide((n + kChunkRows - 1) / kChunkRows + a.splits - 1, a.by_splits) * kChunkRows;
+    w.r0 = min(n, w.sp * per);
+    w.r1 = min(n, w.r0 + per);
     w.new_row = append && w.r1 == n && w.r0 < n;
     return w;
 }
-__device__ __forceinline__ Work work_at(const Cursor& c, const Kv4DecodeArgs& a) { return work_of(c, a, a.len[c.b]); }
 
 template <int HD, int STAGES, int MAX_WARPS>
-__global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4DecodeArgs a)
+__global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(const __grid_constant__ Params a)
 {
     using G = Geo<HD>;
     constexpr int PLANES = G::PLANES, LPR = HD / 8;
@@ -164,43 +179,41 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
     const int stride = n_warps * gridDim.x;
     const int first = warp * gridDim.x + blockIdx.x;   // neighbouring items go to different SMs
     uint8_t* const kv = reinterpret_cast<uint8_t*>(a.kv);
-    const ring::Step step = ring::step_of(stride, a);
-    Cursor pc = ring::cursor_at(first < n_items ? first : 0, a);
-    pc.item = first;
     // While the kernel before this one drains, have the chunks that this warp will request first brought into L2: which those are comes
     // from a look at the length that may be out of date (read past L1), so it is a hint and decides nothing.
     if (first < n_items && lane == 0) {
-        const Work h = work_of(pc, a, __ldcg(a.len + pc.b));
+        const Work h = work_of(first, a, __ldcg(a.len + sequence_of(first, a)));
         const uint32_t bytes = (uint32_t)((min(STAGES * kChunkRows, h.r1 - h.r0) + kTileRows - 1) / kTileRows) * G::TILE;
         if (bytes > 0)
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(kv + (size_t)h.bh * a.slab_bytes + (size_t)(h.r0 / kTileRows) * G::TILE), "r"(bytes) : "memory");
     }
     pdl_wait();
 
-    // ---- producer cursor (kept by every lane, acted on by lane 0): next chunk to request
-    int p_row = 0;
-    Work pw = {};
-    auto p_seek = [&]() {   // move to the next item that has rows
-        for (; pc.item < n_items; ring::advance(pc, step, a)) {
-            pw = work_at(pc, a);
-            p_row = pw.r0;
-            if (pw.r0 < pw.r1) return;
+    // ---- producer (kept by every lane, acted on by lane 0): where the next chunk to request lies
+    int p_item = first, p_left = 0;   // rows of that item not yet requested
+    const uint8_t* p_from = kv;
+    auto p_seek = [&]() {   // to an item that has rows
+        for (; p_item < n_items; p_item += stride) {
+            const Work w = work_of(p_item, a, a.len[sequence_of(p_item, a)]);
+            p_left = w.r1 - w.r0;
+            p_from = kv + (size_t)w.bh * a.slab_bytes + (size_t)(w.r0 / kTileRows) * G::TILE;
+            if (p_left > 0) return;
         }
     };
     uint32_t issued = 0, consumed = 0;
     auto issue_one = [&]() {
-        if (pc.item >= n_items) return;
+        if (p_left <= 0) return;
         const uint32_t st = issued % STAGES;
         if (lane == 0) {
-            const uint32_t bytes = (uint32_t)((min(kChunkRows, pw.r1 - p_row) + kTileRows - 1) / kTileRows) * G::TILE;
+            const uint32_t bytes = (uint32_t)((min(kChunkRows, p_left) + kTileRows - 1) / kTileRows) * G::TILE;
             mbar_expect_tx(bar0 + 8 * st, bytes);
-            ring::bulk_load(ring0 + st * G::STAGE, kv + (size_t)pw.bh * a.slab_bytes + (size_t)(p_row / kTileRows) * G::TILE, bytes,
-                            bar0 + 8 * st, policy);
+            ring::bulk_load(ring0 + st * G::STAGE, p_from, bytes, bar0 + 8 * st, policy);
         }
         ++issued;
-        p_row += kChunkRows;
-        if (p_row >= pw.r1) {
-            ring::advance(pc, step, a);
+        p_from += G::STAGE;
+        p_left -= kChunkRows;
+        if (p_left <= 0) {
+            p_item += stride;
             p_seek();
         }
     };
@@ -209,8 +222,6 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
 
     // ---- consumer: whole items, chunk by chunk
     bool alive = true;
-    Cursor cc = ring::cursor_at(first < n_items ? first : 0, a);
-    cc.item = first;
     // The length update of an item is settled one item later: the count it depends on comes back from L2.  (lane 0 only)
     int pend_arrival = -1, pend_b = 0, pend_n = 0;
     bool pend_overflow = false;
@@ -230,11 +241,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
 #pragma unroll
             for (int i = 0; i < 2; ++i) q_next[p][i] = ld_plain(Qall + (size_t)bh * HD + p * 64 + c * 16 + i * 8);
     };
-    if (first < n_items) fetch_q(cc.bh);
-    for (; alive && cc.item < n_items;) {
-        const Work w = work_at(cc, a);
-        Cursor cn = cc;
-        ring::advance(cn, step, a);
+    if (first < n_items) fetch_q(divide(first, a.by_splits));
+    for (int item = first; item < n_items; item += stride) {
+        const Work w = work_of(item, a, a.len[sequence_of(item, a)]);
         // An item counts itself in as soon as its own read of the length has returned (the increment is computed from it).
         int seq_arrival = -1;
         if (a.k_new != nullptr && lane == 0) {
@@ -285,7 +294,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
                 q_off[p][1] = c < 2 ? other : sum;
             }
         }
-        if (cn.item < n_items) fetch_q(cn.bh);
+        if (item + stride < n_items) fetch_q(divide(item + stride, a.by_splits));
         float m = kNegInf, l = 0.f;                // what scores are relative to, the sum of 2^(score - m)
         float t_most = 0.f, t_to = power_to<kWeightTo>(0.f);   // the largest step of V so far and the power of two for it
         float o[PLANES][4][2], bad[PLANES][2];     // even | odd dimension; not a number once a step of V was none
@@ -531,20 +540,24 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
                 float f[DIMS];
 #pragma unroll
                 for (int i = 0; i < DIMS; ++i) f[i] = 0.f;
-#pragma unroll 6
-                for (int s2 = 0; s2 < a.splits; ++s2) {
-                    const float weight = __shfl_sync(0xffffffffu, s2 < 32 ? lse0 : lse1, s2 & 31);
-                    const float* part = parts + s2 * (HD + 4) + lane * DIMS;
-                    if constexpr (DIMS == 4) {
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(part));
-                        f[0] = fmaf(weight, x.x, f[0]);
-                        f[1] = fmaf(weight, x.y, f[1]);
-                        f[2] = fmaf(weight, x.z, f[2]);
-                        f[3] = fmaf(weight, x.w, f[3]);
-                    } else {
-                        const float2 x = __ldcg(reinterpret_cast<const float2*>(part));
-                        f[0] = fmaf(weight, x.x, f[0]);
-                        f[1] = fmaf(weight, x.y, f[1]);
+                for (int s0 = 0; s0 < a.splits; s0 += kJoin) {
+                    float x[kJoin][DIMS];
+#pragma unroll
+                    for (int i = 0; i < kJoin; ++i) {
+                        const float* part = parts + min(s0 + i, a.splits - 1) * (HD + 4) + lane * DIMS;
+                        if constexpr (DIMS == 4) {
+                            const float4 v = __ldcg(reinterpret_cast<const float4*>(part));
+                            x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
+                        } else {
+                            const float2 v = __ldcg(reinterpret_cast<const float2*>(part));
+                            x[i][0] = v.x, x[i][1] = v.y;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kJoin; ++i) {
+                        const float weight = __shfl_sync(0xffffffffu, s0 < 32 ? lse0 : lse1, (s0 + i) & 31);   // 0 past the last part
+#pragma unroll
+                        for (int j = 0; j < DIMS; ++j) f[j] = fmaf(weight, x[i][j], f[j]);
                     }
                 }
                 const float inv = inverse_sum(total);
@@ -556,7 +569,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
                 if (lane == 0) a.counters[w.bh] = 0;
             }
         }
-        if (w.sp == 0 && cc.h == 0 && lane == 0) {
+        if (w.sp == 0 && w.bh == w.b * a.H && lane == 0) {
             if (w.n == 0) raise_status(a.dev_status, BT_DEV_EMPTY);
             if (w.overflow) raise_status(a.dev_status, BT_DEV_OVERFLOW);
         }
@@ -565,7 +578,6 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(Kv4
         pend_b = w.b;
         pend_n = w.n;
         pend_overflow = w.overflow;
-        cc = cn;
     }
     settle();
     if (!alive) {
@@ -595,6 +607,10 @@ static cudaError_t launch_t(const Kv4DecodeArgs& a, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     const long long items = (long long)a.B * a.H * a.splits;
     if (items > 0x7fffffffLL - 4096) return cudaErrorInvalidConfiguration;
+    Params p;
+    static_cast<Kv4DecodeArgs&>(p) = a;
+    p.by_splits = divisor_of((uint32_t)a.splits);
+    p.by_heads = divisor_of((uint32_t)a.H);
     const long long grid = items < sms ? items : sms;
     // Items are dealt whole: of the warp counts down to five eighths of the most, the one that leaves the fewest warps without an item in
     // the last round (4096 items on 148 SMs: 14 warps, 1.98 rounds of two; 16 warps 1.73).
@@ -610,7 +626,7 @@ static cudaError_t launch_t(const Kv4DecodeArgs& a, cudaStream_t stream)
     }
     const long long each = (items + grid - 1) / grid;
     if (each < warps) warps = (int)each;
-    return launch_pdl(block_decode_kv4_kernel<HD, STAGES, MAX_WARPS>, dim3((unsigned)grid), dim3(warps * 32), (size_t)smem_bytes<HD>(warps, STAGES), stream, a);
+    return launch_pdl(block_decode_kv4_kernel<HD, STAGES, MAX_WARPS>, dim3((unsigned)grid), dim3(warps * 32), (size_t)smem_bytes<HD>(warps, STAGES), stream, p);
 }
 
 }  // namespace kv4
