@@ -52,65 +52,95 @@ __device__ __forceinline__ uint4 transpose4x4(const uint4& r)
     return make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632), __byte_perm(c, d, 0x5410), __byte_perm(c, d, 0x7632));
 }
 
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
+// The larger magnitudes of two pairs of bf16 (their signs mean nothing), NaN where one is.
+__device__ __forceinline__ uint32_t magnitude_max(uint32_t a, uint32_t b)
 {
     uint32_t d;
-    asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
-// Magnitudes of bf16 values compare like their bits, infinities and NaN above all numbers.
-__device__ __forceinline__ uint32_t magnitude_max8(const uint4& r)
+__device__ __forceinline__ uint32_t magnitude_max8(const uint4& r) { return magnitude_max(magnitude_max(r.x, r.y), magnitude_max(r.z, r.w)); }
+// the largest of both halves, as the bits of a magnitude: 0x7f80 and above where it is not finite
+__device__ __forceinline__ uint32_t magnitude_of(uint32_t pair)
 {
-    const uint32_t m = 0x7fff7fffu;
-    return max_u16x2(max_u16x2(r.x & m, r.y & m), max_u16x2(r.z & m, r.w & m));
+    pair &= 0x7fff7fffu;
+    return max(pair & 0xffffu, pair >> 16);
 }
 
-// Step of a group and what its values are multiplied with to get codes; `packed` holds magnitudes in both halves.
+__device__ __forceinline__ float reciprocal(float x)   // 2^-23 off at most; x normal
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Step of a group with this largest magnitude, and what its values are multiplied with to get codes.  (The product with 1 / MOST in place of a
+// division: A / MOST, A a number of 8 bits, is never half-way between two of those, and 2^-16 of it or more away, so the rounding to
+// bf16 is the quotient's.)
 struct Step {
     uint32_t bits;   // bf16
     float inv;
     bool finite;
 };
 template <int MOST>
-__device__ __forceinline__ Step step_of_group(uint32_t packed)
+__device__ __forceinline__ Step step_of_group(uint32_t magnitude)
 {
-    const uint32_t mag = max(packed & 0xffffu, packed >> 16);
     Step st;
-    st.finite = mag < 0x7f80u;
-    const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(mag << 16), (float)MOST)));
+    st.finite = magnitude < 0x7f80u;
+    const float s = __bfloat162float(__float2bfloat16_rn(__uint_as_float(magnitude << 16) * (1.0f / MOST)));
     const bool some = st.finite && s >= kLeastStep;
     st.bits = !st.finite ? 0x7fffu : some ? __float_as_uint(s) >> 16 : 0u;
-    st.inv = some ? __frcp_rn(s) * kRoundUpHalves : 0.f;
+    st.inv = some ? reciprocal(s) * kRoundUpHalves : 0.f;
     return st;
 }
 
-// 8 values -> 8 codes of four bits.  Adding 1.5 * 2^23 (+ 8) leaves the whole number nearest in the low bits.
-__device__ __forceinline__ uint32_t codes8(const uint4& r, const Step& st)
+// 8 finite values -> 8 codes of four bits.  Adding 1.5 * 2^23 + 8 leaves the code in the low bits, of which two make a byte.
+__device__ __forceinline__ uint32_t codes8(const uint4& r, float inv)
 {
     constexpr float kWhole = 12582912.0f + 8.0f;
     float f[8];
     unpack8(r, f);
-    uint32_t w = 0;
+    uint32_t t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w |= (__float_as_uint(fmaf(f[i], st.inv, kWhole)) & 15u) << (4 * i);
-    return st.finite ? w : kZeroCodes;
+    for (int i = 0; i < 8; ++i) t[i] = __float_as_uint(fmaf(f[i], inv, kWhole));
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) t[i] += t[i + 1] * 16u;   // the low byte
+    return __byte_perm(__byte_perm(t[0], t[2], 0x0040), __byte_perm(t[4], t[6], 0x0040), 0x5410);
 }
 
 // Four lanes hold a group (8 values each): its step, on all four of them.
 __device__ __forceinline__ Step step_of_lanes(const uint4& r)
 {
     uint32_t m = magnitude_max8(r);
-    m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    return step_of_group<7>(m);
+    m = magnitude_max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = magnitude_max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    return step_of_group<7>(magnitude_of(m));
 }
 
-// 8 codes -> values
-__device__ __forceinline__ void values8(uint32_t codes, float step, float (&f)[8])
+// 8 codes -> 8 bf16 values: code - 8 is exact in bf16 (as 128 + code less 136), the product with the step is rounded once.
+__device__ __forceinline__ uint4 values8(uint32_t codes, uint32_t step)
 {
+    const uint32_t s2 = __byte_perm(step, 0u, 0x1010);
+    uint32_t v[4];   // dimensions i and i + 4
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = step * (float)((int)((codes >> (4 * i)) & 15u) - 8);
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = ((codes >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+        asm("{\n\t.reg .b32 u;\n\tsub.rn.bf16x2 u, %1, %2;\n\tmul.rn.bf16x2 %0, u, %3;\n\t}" : "=r"(v[i]) : "r"(x), "r"(0x43084308u), "r"(s2));
+    }
+    return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
 }
+
+// Division of numbers below 2^31 by a launch's constant: the high word of a product with ceil(2^k / d), k = 31 + bits of d - 1.
+struct Divisor {
+    uint32_t mul, shift;   // mul == 0: by one
+};
+inline Divisor divisor_of(uint32_t d)
+{
+    if (d <= 1) return {0u, 0u};
+    uint32_t bits = 0;
+    while ((1ull << bits) < d) ++bits;
+    return {(uint32_t)(((1ull << (31 + bits)) + d - 1) / d), bits - 1};
+}
+__device__ __forceinline__ int divide(int n, const Divisor& d) { return d.mul ? (int)(__umulhi((uint32_t)n, d.mul) >> d.shift) : n; }
 
 }  // namespace kv4
 }  // namespace bt

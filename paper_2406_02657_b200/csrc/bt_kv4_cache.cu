@@ -13,22 +13,26 @@ namespace kv4 {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
+struct Params : Kv4Args {
+    int tiles, planes, items;   // tiles of a slab that the call may touch; all the call's
+    Divisor by_tiles, by_planes, by_heads;
+};
 // where item (slab, tile, plane) of a call lies; items count planes fastest
 struct Item {
     int slab, tile, plane;
 };
-__device__ __forceinline__ Item item_at(long long i, int tiles, int planes)
+__device__ __forceinline__ Item item_at(int i, const Params& a)
 {
     Item it;
-    const long long t = i / planes;
-    it.plane = (int)(i - t * planes);
-    it.slab = (int)(t / tiles);
-    it.tile = (int)(t - (long long)it.slab * tiles);
+    const int t = divide(i, a.by_planes);
+    it.plane = i - t * a.planes;
+    it.slab = divide(t, a.by_tiles);
+    it.tile = t - it.slab * a.tiles;
     return it;
 }
 
 // Rows start .. start + n_rows - 1 of a slab, as far as they lie in its `tile`-th tile from start's on.
-__device__ __forceinline__ void write_tile(const Kv4Args& a, const Item& it, int start, int lane)
+__device__ __forceinline__ void write_tile(const Params& a, const Item& it, int start, int lane)
 {
     const int tile = start / kTileRows + it.tile;
     const int first = tile * kTileRows, end = start + a.n_rows;
@@ -48,61 +52,74 @@ __device__ __forceinline__ void write_tile(const Kv4Args& a, const Item& it, int
             v[i] = ld_stream(reinterpret_cast<const bf16*>(a.v) + src);
         }
     }
-    uint8_t* dst = reinterpret_cast<uint8_t*>(a.kv) + (size_t)it.slab * a.slab_bytes + (size_t)(tile * (a.hd / 64) + it.plane) * kTileBytes;
+    uint8_t* dst = reinterpret_cast<uint8_t*>(a.kv) + (size_t)it.slab * a.slab_bytes + ((size_t)tile * a.planes + it.plane) * kTileBytes;
     const bool all = there[0] && there[3];
+    // Largest magnitudes, K's and V's of a row in one word, over the four lanes of a group, so that lane j of them ends up with row j's:
+    // it works out both steps of that row.
+    uint32_t m[4];
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        uint32_t steps[4], codes[4];
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t mk = magnitude_max8(k[i]), mv = magnitude_max8(v[i]);
+        m[i] = magnitude_max(__byte_perm(mk, mv, 0x5410), __byte_perm(mk, mv, 0x7632));
+    }
+    const bool up2 = (lane & 2) != 0, up1 = (lane & 1) != 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) m[i] = magnitude_max(up2 ? m[i + 2] : m[i], __shfl_xor_sync(0xffffffffu, up2 ? m[i] : m[i + 2], 2));
+    m[0] = magnitude_max(up1 ? m[1] : m[0], __shfl_xor_sync(0xffffffffu, up1 ? m[0] : m[1], 1)) & 0x7fff7fffu;
+    const Step sk = step_of_group<7>(m[0] & 0xffffu), sv = step_of_group<7>(m[0] >> 16);
+    {
+        const int r = first + g * 4 + (lane & 3);
+        if (r >= start && r < end) {
+            uint16_t* at = reinterpret_cast<uint16_t*>(dst + kStepsAt) + (g * 4 + (lane & 3)) * 2 + (sub >> 2);
+            at[0] = (uint16_t)sk.bits;
+            at[32] = (uint16_t)sv.bits;
+        }
+    }
+    uint32_t ck[4], cv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        ck[i] = codes8(k[i], __shfl_sync(0xffffffffu, sk.inv, (lane & 28) + i));
+        cv[i] = codes8(v[i], __shfl_sync(0xffffffffu, sv.inv, (lane & 28) + i));
+    }
+    // groups that are not finite: the warp looks for them together, hardly ever finds one
+    const uint32_t bad_k = __ballot_sync(0xffffffffu, !sk.finite), bad_v = __ballot_sync(0xffffffffu, !sv.finite);
+    if (bad_k | bad_v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4& x = part == 0 ? k[i] : v[i];
-            const Step st = step_of_lanes(x);
-            codes[i] = codes8(x, st);
-            steps[i] = st.bits | __shfl_down_sync(0xffffffffu, st.bits, 4) << 16;   // both groups' (lanes 0 of eight)
+            if (bad_k >> ((lane & 28) + i) & 1u) ck[i] = kZeroCodes;
+            if (bad_v >> ((lane & 28) + i) & 1u) cv[i] = kZeroCodes;
         }
-        if (part == 0) {
+    }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (there[i]) *reinterpret_cast<uint32_t*>(dst + k_codes_at(g * 4 + i, sub)) = codes[i];
-        } else if (all) {
-            *reinterpret_cast<uint4*>(dst + v_unit_at(g, sub)) = transpose4x4(make_uint4(codes[0], codes[1], codes[2], codes[3]));
-        } else {
+    for (int i = 0; i < 4; ++i)
+        if (there[i]) *reinterpret_cast<uint32_t*>(dst + k_codes_at(g * 4 + i, sub)) = ck[i];
+    if (all) {
+        *reinterpret_cast<uint4*>(dst + v_unit_at(g, sub)) = transpose4x4(make_uint4(cv[0], cv[1], cv[2], cv[3]));
+    } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (there[i])
+        for (int i = 0; i < 4; ++i)
+            if (there[i])
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) dst[v_codes_at(g * 4 + i, sub) + 4 * j] = (uint8_t)(codes[i] >> (8 * j));
-        }
-        if (sub == 0) {
-            uint32_t* at = reinterpret_cast<uint32_t*>(dst + kStepsAt + part * 64) + g * 4;
-            if (all) {
-                *reinterpret_cast<uint4*>(at) = make_uint4(steps[0], steps[1], steps[2], steps[3]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (there[i]) at[i] = steps[i];
-            }
-        }
+                for (int j = 0; j < 4; ++j) dst[v_codes_at(g * 4 + i, sub) + 4 * j] = (uint8_t)(cv[i] >> (8 * j));
     }
 }
 
 // FUSED: CTA = sequence, which raises its own length; else any warp takes any tile, and the length is raised by a launch behind
 // this one - or by this one, when the rows start anew and no warp looks at the old length.
 template <bool FUSED>
-__global__ void __launch_bounds__(kThreads) kv4_append_kernel(Kv4Args a, int tiles)
+__global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_constant__ Params a)
 {
     pdl_launch_dependents();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, planes = a.hd / 64;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    if constexpr (FUSED) {
+    if constexpr (FUSED) {   // items: those of one sequence
         const int b = blockIdx.x;
         const int start = a.len[b];
         const bool ok = start >= 0 && start <= a.cap - a.n_rows;
         __syncthreads();
-        const int items = a.H * tiles * planes;
         if (ok)
-            for (int i = warp; i < items; i += kWarps) {
-                Item it = item_at(i, tiles, planes);
+            for (int i = warp; i < a.items; i += kWarps) {
+                Item it = item_at(i, a);
                 it.slab += b * a.H;
                 write_tile(a, it, start, lane);
             }
@@ -111,10 +128,10 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(Kv4Args a, int til
             else raise_status(a.dev_status, BT_DEV_OVERFLOW);
         }
     } else {
-        const long long i = (long long)blockIdx.x * kWarps + warp;
-        if (i >= (long long)a.B * a.H * tiles * planes) return;
-        const Item it = item_at(i, tiles, planes);
-        const int b = it.slab / a.H;
+        const int i = (int)blockIdx.x * kWarps + warp;
+        if (i >= a.items) return;
+        const Item it = item_at(i, a);
+        const int b = divide(it.slab, a.by_heads);
         const int start = a.reset ? 0 : a.len[b];
         if (start < 0 || start > a.cap - a.n_rows) return;   // flagged by the launch that raises the lengths
         write_tile(a, it, start, lane);
@@ -133,20 +150,19 @@ __global__ void kv4_len_kernel(int32_t* len, int B, int n, int cap, uint32_t* de
     else raise_status(dev_status, BT_DEV_OVERFLOW);
 }
 
-__global__ void __launch_bounds__(kThreads) kv4_read_kernel(Kv4Args a, int tiles)
+__global__ void __launch_bounds__(kThreads) kv4_read_kernel(const __grid_constant__ Params a)
 {
     pdl_launch_dependents();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, planes = a.hd / 64;
-    const long long i = (long long)blockIdx.x * kWarps + warp;
+    const int lane = threadIdx.x & 31, i = (int)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const Item it = item_at(i, a);
     pdl_wait();
-    if (i >= (long long)a.B * a.H * tiles * planes) return;
-    const Item it = item_at(i, tiles, planes);
-    const int len = a.len[it.slab / a.H];
+    if (i >= a.items) return;
+    const int len = a.len[divide(it.slab, a.by_heads)];
     const int end = min(min(len, a.cap), a.first + a.n_rows);
     const int tile = a.first / kTileRows + it.tile, row0 = tile * kTileRows;
     if (row0 >= end) return;
     const int g = lane >> 3, sub = lane & 7;
-    const uint8_t* src = reinterpret_cast<const uint8_t*>(a.kv) + (size_t)it.slab * a.slab_bytes + (size_t)(tile * planes + it.plane) * kTileBytes;
+    const uint8_t* src = reinterpret_cast<const uint8_t*>(a.kv) + (size_t)it.slab * a.slab_bytes + ((size_t)tile * a.planes + it.plane) * kTileBytes;
     uint32_t codes[2][4], steps[2][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) codes[0][j] = *reinterpret_cast<const uint32_t*>(src + k_codes_at(g * 4 + j, sub));
@@ -171,36 +187,48 @@ __global__ void __launch_bounds__(kThreads) kv4_read_kernel(Kv4Args a, int tiles
         for (int j = 0; j < 4; ++j) {
             const int r = row0 + g * 4 + j;
             if (r < a.first || r >= end) continue;
-            float f[8];
-            values8(codes[part][j], sub < 4 ? bf_lo(steps[part][j]) : bf_hi(steps[part][j]), f);
-            *reinterpret_cast<uint4*>(out + dst0 + (size_t)(r - a.first) * a.hd) = pack8(f);
+            *reinterpret_cast<uint4*>(out + dst0 + (size_t)(r - a.first) * a.hd) =
+                values8(codes[part][j], sub < 4 ? steps[part][j] & 0xffffu : steps[part][j] >> 16);
         }
     }
 }
+
+// false: more items than 31 bits count (no device holds such a cache)
+static bool fill(Params& p, const Kv4Args& a, long long tiles, long long slabs)
+{
+    static_cast<Kv4Args&>(p) = a;
+    p.planes = a.hd / 64;
+    const long long items = slabs * tiles * p.planes;
+    if (items > 0x7fffffffLL - kThreads) return false;
+    p.tiles = (int)tiles;
+    p.items = (int)items;
+    p.by_tiles = divisor_of((uint32_t)tiles);
+    p.by_planes = divisor_of((uint32_t)p.planes);
+    p.by_heads = divisor_of((uint32_t)a.H);
+    return true;
+}
+static dim3 grid_of(const Params& p) { return dim3((unsigned)((p.items + kWarps - 1) / kWarps)); }
 
 }  // namespace kv4
 
 cudaError_t launch_kv4_append(const Kv4Args& a, cudaStream_t stream)
 {
-    const int planes = a.hd / 64;
     // rows that start inside a tile may reach into one more
-    const int tiles = (int)(((long long)a.n_rows + (a.reset ? 1 : 2) * (kv4::kTileRows - 1)) / kv4::kTileRows);
-    const long long per_sequence = (long long)a.H * tiles * planes, items = per_sequence * a.B;
-    if (!a.reset && per_sequence <= 8 * kv4::kWarps)
-        return launch_pdl(kv4::kv4_append_kernel<true>, dim3(a.B), dim3(kv4::kThreads), 0, stream, a, tiles);
-    const long long ctas = (items + kv4::kWarps - 1) / kv4::kWarps;
-    if (ctas > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = launch_pdl(kv4::kv4_append_kernel<false>, dim3((unsigned)ctas), dim3(kv4::kThreads), 0, stream, a, tiles);
+    const long long tiles = ((long long)a.n_rows + (a.reset ? 1 : 2) * (kv4::kTileRows - 1)) / kv4::kTileRows;
+    const bool fused = !a.reset && a.H * tiles * (a.hd / 64) <= 8 * kv4::kWarps;
+    kv4::Params p;
+    if (!kv4::fill(p, a, tiles, fused ? a.H : (long long)a.B * a.H)) return cudaErrorInvalidConfiguration;
+    if (fused) return launch_pdl(kv4::kv4_append_kernel<true>, dim3(a.B), dim3(kv4::kThreads), 0, stream, p);
+    const cudaError_t e = launch_pdl(kv4::kv4_append_kernel<false>, kv4::grid_of(p), dim3(kv4::kThreads), 0, stream, p);
     if (e != cudaSuccess || a.reset) return e;
     return launch_pdl(kv4::kv4_len_kernel, dim3((a.B + 255) / 256), dim3(256), 0, stream, a.len, a.B, a.n_rows, a.cap, a.dev_status);
 }
 
 cudaError_t launch_kv4_read(const Kv4Args& a, cudaStream_t stream)
 {
-    const int tiles = (a.first + a.n_rows - 1) / kv4::kTileRows - a.first / kv4::kTileRows + 1;
-    const long long items = (long long)a.B * a.H * tiles * (a.hd / 64), ctas = (items + kv4::kWarps - 1) / kv4::kWarps;
-    if (ctas > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    return launch_pdl(kv4::kv4_read_kernel, dim3((unsigned)ctas), dim3(kv4::kThreads), 0, stream, a, tiles);
+    kv4::Params p;
+    if (!kv4::fill(p, a, (a.first + a.n_rows - 1) / kv4::kTileRows - a.first / kv4::kTileRows + 1, (long long)a.B * a.H)) return cudaErrorInvalidConfiguration;
+    return launch_pdl(kv4::kv4_read_kernel, kv4::grid_of(p), dim3(kv4::kThreads), 0, stream, p);
 }
 
 }  // namespace bt

@@ -110,19 +110,6 @@ __device__ __forceinline__ float warp_max(float x)
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
     return m;
 }
-// Division of numbers below 2^31 by a launch's constant: the high word of a product with ceil(2^k / d), k = 31 + bits of d - 1.
-struct Divisor {
-    uint32_t mul, shift;   // mul == 0: by one
-};
-inline Divisor divisor_of(uint32_t d)
-{
-    if (d <= 1) return {0u, 0u};
-    uint32_t bits = 0;
-    while ((1ull << bits) < d) ++bits;
-    return {(uint32_t)(((1ull << (31 + bits)) + d - 1) / d), bits - 1};
-}
-__device__ __forceinline__ int divide(int n, const Divisor& d) { return d.mul ? (int)(__umulhi((uint32_t)n, d.mul) >> d.shift) : n; }
-
 struct Params : Kv4DecodeArgs {
     Divisor by_splits, by_heads;
 };
@@ -259,8 +246,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         {
             uint32_t top = 0;
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) top = max_u16x2(top, max_u16x2(magnitude_max8(q_next[p][0]), magnitude_max8(q_next[p][1])));
-            top = max(top & 0xffffu, top >> 16);
+            for (int p = 0; p < PLANES; ++p) top = magnitude_max(top, magnitude_max(magnitude_max8(q_next[p][0]), magnitude_max8(q_next[p][1])));
+            top = magnitude_of(top);
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const float to = power_to<21>(__uint_as_float(top << 16));
@@ -341,7 +328,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                 const int part = (lane / LPR) & 1, piece = lane % LPR;
                 const uint4 x = ld_plain(reinterpret_cast<const bf16*>(part == 0 ? a.k_new : a.v_new) + (size_t)w.bh * HD + piece * 8);
                 const Step sg = step_of_lanes(x);
-                const uint32_t codes = codes8(x, sg);
+                const uint32_t codes = sg.finite ? codes8(x, sg.inv) : kZeroCodes;
                 if (lane < 2 * LPR) {
                     const int r = w.n - 1 - row, in_tile = r % kTileRows, j = piece & 7;
                     const uint32_t tile = (uint32_t)(r / kTileRows) * G::TILE + (piece / 8) * kTileBytes;

@@ -179,14 +179,14 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
         for (int i = 0; i < 4; ++i) {
             const uint32_t* v = w + grp * 16 + i * 4;
             x[i] = make_uint4(v[0], v[1], v[2], v[3]);
-            m = kv4::max_u16x2(m, kv4::magnitude_max8(x[i]));
+            m = kv4::magnitude_max(m, kv4::magnitude_max8(x[i]));
         }
-        const kv4::Step st = kv4::step_of_group<7>(m);
+        const kv4::Step st = kv4::step_of_group<7>(kv4::magnitude_of(m));
         steps |= st.bits << (16 * grp);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int j = grp * 4 + i;
-            const uint32_t codes = kv4::codes8(x[i], st);
+            const uint32_t codes = st.finite ? kv4::codes8(x[i], st.inv) : kv4::kZeroCodes;
             if (part == 0) {
                 *reinterpret_cast<uint32_t*>(tile + kv4::k_codes_at(at, j)) = codes;
             } else {

@@ -50,9 +50,8 @@ __global__ void __launch_bounds__(kThreads) rows_quantize_kernel(const bf16* __r
         r[i] = at < pieces ? ld_stream(x + at * 8) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) m = kv4::max_u16x2(m, kv4::magnitude_max8(r[i]));
-    m = max(m & 0xffffu, m >> 16);
-    m = __reduce_max_sync(0xffffffffu, m);
+    for (int i = 0; i < PIECES; ++i) m = kv4::magnitude_max(m, kv4::magnitude_max8(r[i]));
+    m = __reduce_max_sync(0xffffffffu, kv4::magnitude_of(m));
     const kv4::Step st = kv4::step_of_group<127>(m);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
