@@ -90,17 +90,20 @@ __device__ __forceinline__ void write_tile(const Params& a, const Item& it, int 
             if (bad_v >> ((lane & 28) + i) & 1u) cv[i] = kZeroCodes;
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (there[i]) *reinterpret_cast<uint32_t*>(dst + k_codes_at(g * 4 + i, sub)) = ck[i];
+    // a 16-byte unit of K is two rows' codes of two neighbouring lanes: the even lane takes the first two rows, the odd one the others
+    const uint32_t x = __shfl_xor_sync(0xffffffffu, up1 ? ck[0] : ck[2], 1), y = __shfl_xor_sync(0xffffffffu, up1 ? ck[1] : ck[3], 1);
     if (all) {
+        const uint4 unit = up1 ? make_uint4(x, ck[2], y, ck[3]) : make_uint4(ck[0], x, ck[1], y);
+        *reinterpret_cast<uint4*>(dst + k_codes_at(g * 4 + (up1 ? 2 : 0), sub & 6)) = unit;
         *reinterpret_cast<uint4*>(dst + v_unit_at(g, sub)) = transpose4x4(make_uint4(cv[0], cv[1], cv[2], cv[3]));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (there[i])
+            if (there[i]) {
+                *reinterpret_cast<uint32_t*>(dst + k_codes_at(g * 4 + i, sub)) = ck[i];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) dst[v_codes_at(g * 4 + i, sub) + 4 * j] = (uint8_t)(cv[i] >> (8 * j));
+            }
     }
 }
 
@@ -164,8 +167,14 @@ __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const __grid_constan
     const int g = lane >> 3, sub = lane & 7;
     const uint8_t* src = reinterpret_cast<const uint8_t*>(a.kv) + (size_t)it.slab * a.slab_bytes + ((size_t)tile * a.planes + it.plane) * kTileBytes;
     uint32_t codes[2][4], steps[2][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) codes[0][j] = *reinterpret_cast<const uint32_t*>(src + k_codes_at(g * 4 + j, sub));
+    // a 16-byte unit of K is two rows' codes of two neighbouring lanes: the even lane reads the first two rows, the odd one the others
+    const bool odd = (lane & 1) != 0;
+    const uint4 two = *reinterpret_cast<const uint4*>(src + k_codes_at(g * 4 + (odd ? 2 : 0), sub & 6));
+    const uint32_t x = __shfl_xor_sync(0xffffffffu, odd ? two.x : two.y, 1), y = __shfl_xor_sync(0xffffffffu, odd ? two.z : two.w, 1);
+    codes[0][0] = odd ? x : two.x;
+    codes[0][1] = odd ? y : two.z;
+    codes[0][2] = odd ? two.y : x;
+    codes[0][3] = odd ? two.w : y;
     const uint4 unit = transpose4x4(*reinterpret_cast<const uint4*>(src + v_unit_at(g, sub)));
     codes[1][0] = unit.x;
     codes[1][1] = unit.y;
