@@ -33,7 +33,9 @@
 // so 32 bits hold them), which the epilogue multiplies with both steps.
 //
 // With the 4-bit block cache as the target (kProjectQkvKv4) the epilogue thread that holds 64 values of a K or V row, rounded to bf16
-// as they would be cached, quantises them (two groups of 32) and stores codes and steps itself: 32 + 4 bytes instead of 128.
+// as they would be cached, quantises them (two groups of 32); the warp then stores the codes of its 32 rows, whose bytes are interleaved
+// with those of neighbouring rows, through its shared-memory patch: four rows of a tile at once as 128 contiguous bytes where they are there,
+// else a row at a time.
 #include <cuda.h>
 
 #include "bt_common.cuh"
@@ -164,12 +166,24 @@ __device__ __forceinline__ uint32_t cluster_cta_rank()
     return r;
 }
 
-// 64 bf16 values of a K (part 0) or V (part 1) row, in w[0..31]: quantised and stored into the 4-bit cache by one thread.
-__device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (&w)[64], size_t slab, int row, int plane, int part)
+__device__ __forceinline__ uint32_t lds32(uint32_t addr)
 {
-    uint8_t* tile = reinterpret_cast<uint8_t*>(a.cache.k) + slab * a.cache.slab_stride +
-                    (size_t)(row / kv4::kTileRows * (a.hd / 64) + plane) * kv4::kTileBytes;
-    const int at = row % kv4::kTileRows;
+    uint32_t x;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+    return x;
+}
+__device__ __forceinline__ int64_t shfl64(int64_t x, int lane)
+{
+    const uint32_t lo = __shfl_sync(0xffffffffu, (uint32_t)x, lane), hi = __shfl_sync(0xffffffffu, (uint32_t)(x >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+constexpr int kCodeRow = 48;   // a row's 32 bytes of codes in the patch, 16 apart from the next so that the rows spread over the banks
+
+// K (part 0) or V (part 1) of a warp's rows into the 4-bit cache: 64 bf16 values of this lane's row in w[0..31]; the row is row rc (-1: it
+// goes nowhere) of the slab whose tile with that row lies `off` bytes into the cache; quads: lanes whose four neighbours hold the four rows of a quad.
+__device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (&w)[64], int64_t off, int rc, uint32_t quads, int part, uint32_t patch, int lane)
+{
+    uint8_t* const cache = reinterpret_cast<uint8_t*>(a.cache.k);
     uint32_t steps = 0;
 #pragma unroll
     for (int grp = 0; grp < 2; ++grp) {
@@ -183,23 +197,44 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
         }
         const kv4::Step st = kv4::step_of_group<7>(kv4::magnitude_of(m));
         steps |= st.bits << (16 * grp);
+        uint32_t codes[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = grp * 4 + i;
-            const uint32_t codes = st.finite ? kv4::codes8(x[i], st.inv) : kv4::kZeroCodes;
-            if (part == 0) {
-                *reinterpret_cast<uint32_t*>(tile + kv4::k_codes_at(at, j)) = codes;
-            } else {
-                uint8_t* bytes = tile + kv4::v_codes_at(at, j);   // a byte for each pair of dimensions: the row's neighbours lie between
-#pragma unroll
-                for (int q = 0; q < 4; ++q) bytes[4 * q] = (uint8_t)(codes >> (8 * q));
+        for (int i = 0; i < 4; ++i) codes[i] = st.finite ? kv4::codes8(x[i], st.inv) : kv4::kZeroCodes;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                     ::"r"(patch + lane * kCodeRow + grp * 16), "r"(codes[0]), "r"(codes[1]), "r"(codes[2]), "r"(codes[3]) : "memory");
+    }
+    if (rc >= 0) *reinterpret_cast<uint32_t*>(cache + off + kv4::kStepsAt + part * 64 + rc % kv4::kTileRows * 4) = steps;
+    __syncwarp();
+    const int j = lane >> 2, byte = lane & 3;
+#pragma unroll 1
+    for (int i = 0; i < 32; i += 4) {
+        const uint32_t rows = patch + i * kCodeRow;
+        if ((quads >> i & 15u) == 15u) {
+            const int at = __shfl_sync(0xffffffffu, rc, i) % kv4::kTileRows;
+            uint8_t* dst = cache + shfl64(off, i) + lane * 4;
+            if (part == 0) {   // a word: half a unit of one of the rows
+                *reinterpret_cast<uint32_t*>(dst + kv4::k_codes_at(at, 0)) = lds32(rows + (lane >> 4 << 1 | (lane >> 1 & 1)) * kCodeRow + ((lane >> 2 & 3) * 2 + (lane & 1)) * 4);
+            } else {           // a word: one byte of each of the rows
+                const uint32_t from = rows + (j ^ (at >> 2 << 1)) * 4;
+                const uint32_t x[4] = {lds32(from), lds32(from + kCodeRow), lds32(from + 2 * kCodeRow), lds32(from + 3 * kCodeRow)};
+                const uint32_t pick = byte | (4 + byte) << 4;
+                *reinterpret_cast<uint32_t*>(dst + kv4::kPartBytes + (at >> 2) * 128) = __byte_perm(__byte_perm(x[0], x[1], pick), __byte_perm(x[2], x[3], pick), 0x5410);
             }
+            continue;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int at = __shfl_sync(0xffffffffu, rc, i + r);
+            uint8_t* dst = cache + shfl64(off, i + r);
+            if (at < 0) continue;
+            const uint32_t codes = lds32(rows + r * kCodeRow + j * 4);
+            if (part == 1) dst[kv4::v_codes_at(at % kv4::kTileRows, j) + 4 * byte] = (uint8_t)(codes >> (8 * byte));
+            else if (byte == 0) *reinterpret_cast<uint32_t*>(dst + kv4::k_codes_at(at % kv4::kTileRows, j)) = codes;
         }
     }
-    *reinterpret_cast<uint32_t*>(tile + kv4::kStepsAt + part * 64 + at * 4) = steps;
 }
 
-template <int BN, int kCtas, bool kInt8>
+template <int BN, int kCtas, bool kInt8, bool kKv4>
 __global__ void __launch_bounds__(kThreads, 1)
 project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, Params p)
 {
@@ -350,18 +385,30 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
         for (int tile = unit; tile < n_tiles; tile += n_units, ++t) {
             const int tm = tile / p.tiles_n, tn = tile - tm * p.tiles_n;
             const uint32_t acc = t & 1;
-            // this lane's own row: which sequence, which of its n rows, and where the row lands in the cache
+            // This lane's own row: where it goes among the rows of Q (or of the plain output) and in the cache, without head and
+            // dimension (elements; bytes in the 4-bit cache); -1: nowhere.
             const int m = tm * (BM * kCtas) + (int)rank * BM + wq * 32 + lane;
-            int row_b = -1, row_i = 0, row_rc = -1;
-            if (m < a.M) {
-                if (a.mode == kProjectPlain) {
-                    row_b = m;
-                } else {
+            int64_t off_q = -1, off_c = -1;
+            int row_rc = -1;
+            uint32_t quads = 0;
+            if (m < a.M && a.mode == kProjectPlain) off_q = (int64_t)m * a.N;
+            if (a.mode != kProjectPlain) {
+                int row_b = -1;
+                if (m < a.M) {
                     row_b = m / a.n_rows;
-                    row_i = m - row_b * a.n_rows;
+                    const int row_i = m - row_b * a.n_rows;
+                    off_q = ((int64_t)row_b * a.H * a.n_rows + row_i) * a.hd;
                     const bool rst = a.reset_mask ? (a.reset_mask[row_b] != 0) : (a.reset_first != 0);
                     const int len_old = rst ? 0 : a.cache.len[row_b];
-                    if (len_old >= 0 && len_old + a.n_rows <= a.cache.cap) row_rc = len_old + row_i;  // else: no room, K and V are dropped
+                    if (len_old >= 0 && len_old + a.n_rows <= a.cache.cap) {   // else: no room, K and V are dropped
+                        row_rc = len_old + row_i;
+                        off_c = (int64_t)row_b * a.H * a.cache.slab_stride +
+                                (!kKv4 ? (int64_t)row_rc * a.cache.row_stride : (int64_t)(row_rc / kv4::kTileRows) * (a.hd / 64) * kv4::kTileBytes);
+                    }
+                }
+                if constexpr (kKv4) {
+                    const int b0 = __shfl_sync(0xffffffffu, row_b, lane & 28), rc0 = __shfl_sync(0xffffffffu, row_rc, lane & 28);
+                    quads = __ballot_sync(0xffffffffu, row_rc >= 0 && row_b == b0 && row_rc == rc0 + (lane & 3) && (rc0 & 3) == 0);
                 }
             }
             float x_step = 0.f;
@@ -383,38 +430,41 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 tmem_ld_fence32(r + 32);
                 // Where the piece goes.  head_dim is a multiple of 64 and so is col0: the 64 columns lie inside one
                 // head of one of Q, K, V, so everything but the row is the same for the whole warp.
-                int part = 0, piece_h = 0, piece_d = 0;            // part 0: Q, 1: K, 2: V
+                int part = 0;                                      // 0: Q or the plain output, 1: K, 2: V
+                int64_t off = off_q, add = col0;
                 if (a.mode != kProjectPlain) {
                     part = col0 / D;
-                    const int cc = col0 - part * D;
-                    piece_h = cc / a.hd;
-                    piece_d = cc - piece_h * a.hd;
+                    const int cc = col0 - part * D, h = cc / a.hd, d = cc - h * a.hd;
+                    add = (part == 0 ? (int64_t)h * a.n_rows * a.hd : (int64_t)h * a.cache.slab_stride) + d;
+                    if (part != 0) off = off_c;
+                    if (kKv4 && part != 0) add += d / 64 * kv4::kTileBytes - d;
                 }
+                const bool to_kv4 = kKv4 && part != 0;
+                off = off < 0 ? -1 : off + add;
                 // + bias, -> bf16, into the patch: row `lane`, 16-byte piece q8 at (q8 ^ (lane & 7)) - or, bound for the 4-bit
                 // cache, back into registers
-                const bool to_kv4 = a.mode == kProjectQkvKv4 && part != 0;
 #pragma unroll
                 for (int q8 = 0; q8 < 8; ++q8) {
                     float f[8];
                     const int col = col0 + q8 * 8;
-                    if constexpr (kInt8) {
-                        float4 s0 = make_float4(0.f, 0.f, 0.f, 0.f), s1 = s0;
-                        if (col < a.N) {
-                            s0 = *reinterpret_cast<const float4*>(a.w_steps + col);
-                            s1 = *reinterpret_cast<const float4*>(a.w_steps + col + 4);
-                        }
-                        const float ws[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+                    float bf[8] = {};
+                    if (bias != nullptr) unpack8(*reinterpret_cast<const uint4*>(bias + col), bf);
+                    if constexpr (kInt8) {   // sum * (x_step * w_step) + bias
+                        const uint64_t xs = pack2(x_step, x_step);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = (float)(int)r[q8 * 8 + i] * (x_step * ws[i]);
+                        for (int i = 0; i < 8; i += 4) {
+                            const float4 ws = *reinterpret_cast<const float4*>(a.w_steps + col + i);
+                            const int* sum = reinterpret_cast<const int*>(r + q8 * 8 + i);
+                            unpack2(ffma2(pack2((float)sum[0], (float)sum[1]), fmul2(xs, pack2(ws.x, ws.y)), pack2(bf[i], bf[i + 1])), f[i], f[i + 1]);
+                            unpack2(ffma2(pack2((float)sum[2], (float)sum[3]), fmul2(xs, pack2(ws.z, ws.w)), pack2(bf[i + 2], bf[i + 3])), f[i + 2], f[i + 3]);
+                        }
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r[q8 * 8 + i]);
-                    }
-                    if (bias != nullptr && col < a.N) {
-                        float bf[8];
-                        unpack8(*reinterpret_cast<const uint4*>(bias + col), bf);
+                        if (bias != nullptr) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] += bf[i];
+                            for (int i = 0; i < 8; ++i) f[i] += bf[i];
+                        }
                     }
                     const uint4 w = pack8(f);
                     if (to_kv4) {
@@ -428,41 +478,18 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
                 }
                 if (to_kv4) {
-                    if (row_rc >= 0) store_kv4(a, r, (size_t)row_b * a.H + piece_h, row_rc, piece_d / 64, part - 1);
-                    continue;
-                }
-                __syncwarp();
-                bf16* piece_base = reinterpret_cast<bf16*>(a.out);
-                size_t slab_elems = 0, row_elems = 0;     // element strides: per (sequence, head) slab, per row
-                const bool to_cache = part != 0;
-                if (a.mode != kProjectPlain) {
-                    if (to_cache) {
-                        piece_base = reinterpret_cast<bf16*>(part == 1 ? a.cache.k : a.cache.v);
-                        slab_elems = (size_t)a.cache.slab_stride;
-                        row_elems = (size_t)a.cache.row_stride;
-                    } else {
-                        slab_elems = (size_t)a.n_rows * a.hd;
-                        row_elems = (size_t)a.hd;
-                    }
-                }
-                // out of the patch: 8 lanes take one row's 128 bytes, so every store instruction writes 4 whole lines
+                    if constexpr (kKv4) store_kv4(a, r, off, row_rc, quads, part - 1, patch, lane);
+                } else {
+                    __syncwarp();
+                    bf16* const base_out = reinterpret_cast<bf16*>(part == 0 ? a.out : part == 1 ? a.cache.k : a.cache.v) + (lane & 7) * 8;
+                    // out of the patch: 8 lanes take one row's 128 bytes, so every store instruction writes 4 whole lines
 #pragma unroll
-                for (int itr = 0; itr < 8; ++itr) {
-                    const int rr = itr * 4 + (lane >> 3), q8 = lane & 7;
-                    const int b = __shfl_sync(0xffffffffu, row_b, rr);
-                    const int i = __shfl_sync(0xffffffffu, row_i, rr);
-                    const int rc = __shfl_sync(0xffffffffu, row_rc, rr);
-                    uint4 w;
-                    const uint32_t src = patch + rr * 128 + ((q8 ^ (rr & 7)) << 4);
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(src) : "memory");
-                    const int col = col0 + q8 * 8;
-                    if (b < 0 || col >= a.N) continue;
-                    bf16* dst = nullptr;
-                    if (a.mode == kProjectPlain)
-                        dst = piece_base + (size_t)b * a.N + col;
-                    else if (!to_cache || rc >= 0)   // Q row i of the sequence, or cache row rc (absent when there is no room)
-                        dst = piece_base + ((size_t)b * a.H + piece_h) * slab_elems + (size_t)(to_cache ? rc : i) * row_elems + piece_d + q8 * 8;
-                    if (dst) *reinterpret_cast<uint4*>(dst) = w;
+                    for (int itr = 0; itr < 8; ++itr) {
+                        const int rr = itr * 4 + (lane >> 3), q8 = lane & 7;
+                        const int64_t to = shfl64(off, rr);   // of that row; none where there is no room
+                        const uint4 w = lds128(patch + rr * 128 + ((q8 ^ (rr & 7)) << 4));
+                        if (to >= 0) *reinterpret_cast<uint4*>(base_out + to) = w;
+                    }
                 }
                 __syncwarp();  // the patch is free for the next piece
             }
@@ -496,12 +523,12 @@ __global__ void project_len_advance_kernel(int32_t* len, int B, int n, int cap, 
     if (b < B) advance_len(len, b, n, cap, reset_first, reset_mask, dev_status);
 }
 
-template <int BN, int kCtas, bool kInt8>
+template <int BN, int kCtas, bool kInt8, bool kKv4>
 static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_t stream)
 {
     using C = Cfg<BN, kCtas>;
     static PerDeviceOnce limit_raised;
-    cudaError_t e = raise_smem_limit_once(limit_raised, dev, project_tc_kernel<BN, kCtas, kInt8>, C::kSmemBytes);
+    cudaError_t e = raise_smem_limit_once(limit_raised, dev, project_tc_kernel<BN, kCtas, kInt8, kKv4>, C::kSmemBytes);
     if (e != cudaSuccess) return e;
     CUtensorMap mx, mw;
     if constexpr (kInt8) {
@@ -531,19 +558,20 @@ static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = kCtas == 2 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, project_tc_kernel<BN, kCtas, kInt8>, mx, mw, p);
+    return cudaLaunchKernelEx(&cfg, project_tc_kernel<BN, kCtas, kInt8, kKv4>, mx, mw, p);
 }
 
 template <int BN, int kCtas>
 static cudaError_t launch_type(const ProjectArgs& a, int dev, int sms, cudaStream_t stream)
 {
-    return a.x_steps ? launch_bn<BN, kCtas, true>(a, dev, sms, stream) : launch_bn<BN, kCtas, false>(a, dev, sms, stream);
+    if (a.mode == kProjectQkvKv4) return a.x_steps ? launch_bn<BN, kCtas, true, true>(a, dev, sms, stream) : launch_bn<BN, kCtas, false, true>(a, dev, sms, stream);
+    return a.x_steps ? launch_bn<BN, kCtas, true, false>(a, dev, sms, stream) : launch_bn<BN, kCtas, false, false>(a, dev, sms, stream);
 }
 
 }  // namespace proj
 
-// rows are copied in 16-byte pieces
-bool project_supported(const ProjectArgs& a) { return a.K % (a.x_steps ? 16 : 8) == 0 && a.N % 8 == 0 && tensor_map_encode_fn() != nullptr; }
+// rows are copied in 16-byte pieces; output features come in pieces of 64 (head_dim is a multiple of 64)
+bool project_supported(const ProjectArgs& a) { return a.K % (a.x_steps ? 16 : 8) == 0 && a.N % 64 == 0 && tensor_map_encode_fn() != nullptr; }
 
 cudaError_t launch_project(const ProjectArgs& a, cudaStream_t stream)
 {
