@@ -7,14 +7,14 @@
 //     local cache, so no separate append pass touches them.
 //
 // One persistent CTA per SM, warp-specialised:
-//   warps 0-7       : epilogue - thread = accumulator row (= tensor-memory lane), two warps per lane quarter
-//                     taking alternate 64-column pieces.  64 columns at a time:
+//   warps 0-7       : epilogue - thread = accumulator row (= tensor-memory lane), two warps per lane quarter (four, warps
+//                     0-15, where the 4-bit cache is the target) taking alternate 64-column pieces.  64 columns at a time:
 //                     tensor memory -> registers, + bias, -> bf16, through a per-warp swizzled
 //                     shared-memory patch so that the global stores are whole 128-byte lines (8 lanes
 //                     per row piece: one head of one cache row at head_dim 64), then to q / the cache /
 //                     the plain [M][N] output
-//   warp 8 (1 lane) : TMA producer - x tile [128 x 64] and W tile [BN x 64] per stage, 128-byte swizzle
-//   warp 9 (1 lane) : tcgen05.mma issuer - 128 x BN x 16 instructions, fp32 accumulators in tensor
+//   next warp (1 lane): TMA producer - x tile [128 x 64] and W tile [BN x 64] per stage, 128-byte swizzle
+//   last warp (1 lane): tcgen05.mma issuer - 128 x BN x 16 instructions, fp32 accumulators in tensor
 //                     memory, double-buffered so that the epilogue of a tile runs under the next
 //                     tile's products
 // BN (64, 128 or 256 output features per tile) is chosen per launch so that there are enough tiles
@@ -53,8 +53,6 @@ using namespace tc;
 
 constexpr int BM = 128;                  // rows of x per tile (= tensor-memory lanes)
 constexpr int kRowBytes = 128;           // bytes of K per stage and row: one swizzle atom (64 bf16, 128 8-bit values)
-constexpr int kEpilogueWarps = 8, kProducerWarp = 8, kMmaWarp = 9;
-constexpr int kThreads = 320;
 constexpr uint32_t kABytes = BM * kRowBytes;
 constexpr uint32_t kSpinLimit = 1u << 26;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s: far beyond any legitimate wait
@@ -62,14 +60,19 @@ constexpr uint32_t kPatchBytes = 32 * 128;         // per epilogue warp: 32 rows
 
 constexpr uint32_t kPeerBitMask = 0xFEFFFFFFu;   // clears the bit that tells the two CTAs of a pair apart in a shared::cluster address
 
-template <int BN, int kCtas>
+// kKv4 (the 4-bit cache is the target): 16 epilogue warps, which have twice the arithmetic to do, for 8, and a stage less for their patches
+// (197 us with 8 at 16384 rows x 2048 x 6144 in 8 bits, where the product into a bf16 cache takes 140).
+template <int BN, int kCtas, bool kKv4>
 struct Cfg {
+    static constexpr int kEpilogueWarps = kKv4 ? 16 : 8, kProducerWarp = kEpilogueWarps, kMmaWarp = kEpilogueWarps + 1;
+    static constexpr int kThreads = (kEpilogueWarps + 2) * 32;
     static constexpr uint32_t kBBytes = (BN / kCtas) * kRowBytes;   // a CTA of a pair holds half of the W tile
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = kStageBytes == 48 * 1024 ? 4 : (kStageBytes == 32 * 1024 ? 6 : 8);
+    static constexpr int kStages = kStageBytes == 48 * 1024 ? (kKv4 ? 3 : 4) : kStageBytes == 32 * 1024 ? (kKv4 ? 5 : 6) : (kKv4 ? 6 : 8);
     static constexpr uint32_t kTmemCols = 2 * BN;   // two accumulators
     static constexpr int kBarriers = 2 * kStages + 4;
     static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kEpilogueWarps * kPatchBytes + kBarriers * 8 + 16;
+    static_assert(kSmemBytes <= 227 * 1024, "a CTA's shared memory");
 };
 
 struct Params {
@@ -179,9 +182,9 @@ __device__ __forceinline__ int64_t shfl64(int64_t x, int lane)
 }
 constexpr int kCodeRow = 48;   // a row's 32 bytes of codes in the patch, 16 apart from the next so that the rows spread over the banks
 
-// K (part 0) or V (part 1) of a warp's rows into the 4-bit cache: 64 bf16 values of this lane's row in w[0..31]; the row is row rc (-1: it
+// K (part 0) or V (part 1) of a warp's rows into the 4-bit cache: 64 bf16 values of this lane's row in w; the row is row rc (-1: it
 // goes nowhere) of the slab whose tile with that row lies `off` bytes into the cache; quads: lanes whose four neighbours hold the four rows of a quad.
-__device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (&w)[64], int64_t off, int rc, uint32_t quads, int part, uint32_t patch, int lane)
+__device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (&w)[32], int64_t off, int rc, uint32_t quads, int part, uint32_t patch, int lane)
 {
     uint8_t* const cache = reinterpret_cast<uint8_t*>(a.cache.k);
     uint32_t steps = 0;
@@ -206,22 +209,31 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
     if (rc >= 0) *reinterpret_cast<uint32_t*>(cache + off + kv4::kStepsAt + part * 64 + rc % kv4::kTileRows * 4) = steps;
     __syncwarp();
     const int j = lane >> 2, byte = lane & 3;
+    auto quad = [&](int i) {   // rows i .. i + 3 of the warp: a quad of a tile, a word a lane
+        const uint32_t rows = patch + i * kCodeRow;
+        const int at = __shfl_sync(0xffffffffu, rc, i) % kv4::kTileRows;
+        uint8_t* dst = cache + shfl64(off, i) + lane * 4;
+        if (part == 0) {   // half a unit of one of the rows
+            *reinterpret_cast<uint32_t*>(dst + kv4::k_codes_at(at, 0)) = lds32(rows + (lane >> 4 << 1 | (lane >> 1 & 1)) * kCodeRow + ((lane >> 2 & 3) * 2 + (lane & 1)) * 4);
+        } else {           // one byte of each of the rows
+            const uint32_t from = rows + (j ^ (at >> 2 << 1)) * 4;
+            const uint32_t x[4] = {lds32(from), lds32(from + kCodeRow), lds32(from + 2 * kCodeRow), lds32(from + 3 * kCodeRow)};
+            const uint32_t pick = byte | (4 + byte) << 4;
+            *reinterpret_cast<uint32_t*>(dst + kv4::kPartBytes + (at >> 2) * 128) = __byte_perm(__byte_perm(x[0], x[1], pick), __byte_perm(x[2], x[3], pick), 0x5410);
+        }
+    };
+    if (quads == 0xffffffffu) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) quad(i);
+        return;
+    }
 #pragma unroll 1
     for (int i = 0; i < 32; i += 4) {
-        const uint32_t rows = patch + i * kCodeRow;
         if ((quads >> i & 15u) == 15u) {
-            const int at = __shfl_sync(0xffffffffu, rc, i) % kv4::kTileRows;
-            uint8_t* dst = cache + shfl64(off, i) + lane * 4;
-            if (part == 0) {   // a word: half a unit of one of the rows
-                *reinterpret_cast<uint32_t*>(dst + kv4::k_codes_at(at, 0)) = lds32(rows + (lane >> 4 << 1 | (lane >> 1 & 1)) * kCodeRow + ((lane >> 2 & 3) * 2 + (lane & 1)) * 4);
-            } else {           // a word: one byte of each of the rows
-                const uint32_t from = rows + (j ^ (at >> 2 << 1)) * 4;
-                const uint32_t x[4] = {lds32(from), lds32(from + kCodeRow), lds32(from + 2 * kCodeRow), lds32(from + 3 * kCodeRow)};
-                const uint32_t pick = byte | (4 + byte) << 4;
-                *reinterpret_cast<uint32_t*>(dst + kv4::kPartBytes + (at >> 2) * 128) = __byte_perm(__byte_perm(x[0], x[1], pick), __byte_perm(x[2], x[3], pick), 0x5410);
-            }
+            quad(i);
             continue;
         }
+        const uint32_t rows = patch + i * kCodeRow;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int at = __shfl_sync(0xffffffffu, rc, i + r);
@@ -235,11 +247,11 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
 }
 
 template <int BN, int kCtas, bool kInt8, bool kKv4>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<BN, kCtas, kKv4>::kThreads, 1)
 project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, Params p)
 {
-    using C = Cfg<BN, kCtas>;
-    constexpr int S = C::kStages;
+    using C = Cfg<BN, kCtas, kKv4>;
+    constexpr int S = C::kStages, kEpilogueWarps = C::kEpilogueWarps, kProducerWarp = C::kProducerWarp, kMmaWarp = C::kMmaWarp;
     constexpr uint32_t IDESC = kInt8 ? make_idesc_s8(BM * kCtas, BN) : make_idesc(BM * kCtas, BN, false);
     constexpr int BK = kInt8 ? kRowBytes : kRowBytes / 2;   // elements of K per stage
     const ProjectArgs& a = p.a;
@@ -372,8 +384,8 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
         }
     } else {
         // ------------------------------------------------------------------ epilogue: thread = output row
-        // warps 0-7: warp e drains tensor-memory lane quarter e % 4 (the quarter a warp may access is its index
-        // modulo 4) and every other 64-column piece, starting at piece e / 4
+        // warp e drains tensor-memory lane quarter e % 4 (the quarter a warp may access is its index modulo 4) and every second 64-column
+        // piece (every fourth with 16 warps), starting at piece e / 4
         const int wq = warp & 3, half = warp >> 2;
         const uint32_t lane_base = tmem + ((uint32_t)(wq * 32) << 16);
         const uint32_t patch = sPatch + warp * kPatchBytes;
@@ -419,15 +431,9 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
-            for (int c0 = half * 64; c0 < BN; c0 += 128) {
+            for (int c0 = half * 64; c0 < BN; c0 += kEpilogueWarps * 16) {
                 const int col0 = tn * BN + c0;                 // first output feature of this 64-column piece
                 if (col0 >= a.N) break;                        // warp-uniform
-                uint32_t r[64];
-                tmem_ld32_issue(lane_base + acc * BN + c0, r);
-                tmem_ld32_issue(lane_base + acc * BN + c0 + 32, r + 32);
-                tmem_wait_ld();
-                tmem_ld_fence32(r);
-                tmem_ld_fence32(r + 32);
                 // Where the piece goes.  head_dim is a multiple of 64 and so is col0: the 64 columns lie inside one
                 // head of one of Q, K, V, so everything but the row is the same for the whole warp.
                 int part = 0;                                      // 0: Q or the plain output, 1: K, 2: V
@@ -443,42 +449,53 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 off = off < 0 ? -1 : off + add;
                 // + bias, -> bf16, into the patch: row `lane`, 16-byte piece q8 at (q8 ^ (lane & 7)) - or, bound for the 4-bit
                 // cache, back into registers
+                constexpr int kAtOnce = kKv4 ? 32 : 64;        // accumulators in registers (16 warps leave 112 registers a thread)
+                uint32_t packed[32];                           // kKv4
 #pragma unroll
-                for (int q8 = 0; q8 < 8; ++q8) {
-                    float f[8];
-                    const int col = col0 + q8 * 8;
-                    float bf[8] = {};
-                    if (bias != nullptr) unpack8(*reinterpret_cast<const uint4*>(bias + col), bf);
-                    if constexpr (kInt8) {   // sum * (x_step * w_step) + bias
-                        const uint64_t xs = pack2(x_step, x_step);
+                for (int c1 = 0; c1 < 64; c1 += kAtOnce) {
+                    uint32_t r[kAtOnce];
 #pragma unroll
-                        for (int i = 0; i < 8; i += 4) {
-                            const float4 ws = *reinterpret_cast<const float4*>(a.w_steps + col + i);
-                            const int* sum = reinterpret_cast<const int*>(r + q8 * 8 + i);
-                            unpack2(ffma2(pack2((float)sum[0], (float)sum[1]), fmul2(xs, pack2(ws.x, ws.y)), pack2(bf[i], bf[i + 1])), f[i], f[i + 1]);
-                            unpack2(ffma2(pack2((float)sum[2], (float)sum[3]), fmul2(xs, pack2(ws.z, ws.w)), pack2(bf[i + 2], bf[i + 3])), f[i + 2], f[i + 3]);
+                    for (int i = 0; i < kAtOnce; i += 32) tmem_ld32_issue(lane_base + acc * BN + c0 + c1 + i, r + i);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < kAtOnce; i += 32) tmem_ld_fence32(r + i);
+#pragma unroll
+                    for (int e = 0; e < kAtOnce / 8; ++e) {
+                        float f[8];
+                        const int q8 = c1 / 8 + e, col = col0 + q8 * 8;
+                        float bf[8] = {};
+                        if (bias != nullptr) unpack8(*reinterpret_cast<const uint4*>(bias + col), bf);
+                        if constexpr (kInt8) {   // sum * (x_step * w_step) + bias
+                            const uint64_t xs = pack2(x_step, x_step);
+#pragma unroll
+                            for (int i = 0; i < 8; i += 4) {
+                                const float4 ws = *reinterpret_cast<const float4*>(a.w_steps + col + i);
+                                const int* sum = reinterpret_cast<const int*>(r + e * 8 + i);
+                                unpack2(ffma2(pack2((float)sum[0], (float)sum[1]), fmul2(xs, pack2(ws.x, ws.y)), pack2(bf[i], bf[i + 1])), f[i], f[i + 1]);
+                                unpack2(ffma2(pack2((float)sum[2], (float)sum[3]), fmul2(xs, pack2(ws.z, ws.w)), pack2(bf[i + 2], bf[i + 3])), f[i + 2], f[i + 3]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r[e * 8 + i]);
+                            if (bias != nullptr) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) f[i] += bf[i];
+                            }
                         }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r[q8 * 8 + i]);
-                        if (bias != nullptr) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) f[i] += bf[i];
+                        const uint4 w = pack8(f);
+                        if (to_kv4) {
+                            packed[q8 * 4] = w.x;
+                            packed[q8 * 4 + 1] = w.y;
+                            packed[q8 * 4 + 2] = w.z;
+                            packed[q8 * 4 + 3] = w.w;
+                            continue;
                         }
+                        const uint32_t dst = patch + lane * 128 + ((q8 ^ (lane & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
                     }
-                    const uint4 w = pack8(f);
-                    if (to_kv4) {
-                        r[q8 * 4] = w.x;
-                        r[q8 * 4 + 1] = w.y;
-                        r[q8 * 4 + 2] = w.z;
-                        r[q8 * 4 + 3] = w.w;
-                        continue;
-                    }
-                    const uint32_t dst = patch + lane * 128 + ((q8 ^ (lane & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
                 }
                 if (to_kv4) {
-                    if constexpr (kKv4) store_kv4(a, r, off, row_rc, quads, part - 1, patch, lane);
+                    if constexpr (kKv4) store_kv4(a, packed, off, row_rc, quads, part - 1, patch, lane);
                 } else {
                     __syncwarp();
                     bf16* const base_out = reinterpret_cast<bf16*>(part == 0 ? a.out : part == 1 ? a.cache.k : a.cache.v) + (lane & 7) * 8;
@@ -526,7 +543,7 @@ __global__ void project_len_advance_kernel(int32_t* len, int B, int n, int cap, 
 template <int BN, int kCtas, bool kInt8, bool kKv4>
 static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_t stream)
 {
-    using C = Cfg<BN, kCtas>;
+    using C = Cfg<BN, kCtas, kKv4>;
     static PerDeviceOnce limit_raised;
     cudaError_t e = raise_smem_limit_once(limit_raised, dev, project_tc_kernel<BN, kCtas, kInt8, kKv4>, C::kSmemBytes);
     if (e != cudaSuccess) return e;
@@ -546,7 +563,7 @@ static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_
     const int grid = (int)(tiles < units ? tiles : units) * kCtas;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(C::kThreads);
     cfg.dynamicSmemBytes = (size_t)C::kSmemBytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
