@@ -12,8 +12,6 @@
 namespace bt {
 namespace quant {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-
 // 8 values -> 8 codes of eight bits
 __device__ __forceinline__ uint2 bytes8(const uint4& r, float inv)
 {
@@ -29,15 +27,15 @@ __device__ __forceinline__ uint2 bytes8(const uint4& r, float inv)
     return w;
 }
 
-// PIECES 8-value pieces a lane: rows of up to 256 * PIECES values
-template <int PIECES>
-__global__ void __launch_bounds__(kThreads) rows_quantize_kernel(const bf16* __restrict__ x, long long rows, int cols, int8_t* __restrict__ x8,
+// PIECES 8-value pieces a lane: rows of up to 256 * PIECES values; WARPS rows a CTA
+template <int PIECES, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) rows_quantize_kernel(const bf16* __restrict__ x, long long rows, int cols, int8_t* __restrict__ x8,
                                                                  float* __restrict__ steps)
 {
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const long long row = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
     if (row >= rows) return;
     x += row * cols;
     x8 += row * cols;
@@ -61,12 +59,12 @@ __global__ void __launch_bounds__(kThreads) rows_quantize_kernel(const bf16* __r
     if (lane == 0) steps[row] = __uint_as_float(st.bits << 16);
 }
 
-template <int PIECES>
+template <int PIECES, int WARPS>
 static cudaError_t launch_p(const void* x, long long rows, int cols, void* x8, float* steps, cudaStream_t stream)
 {
-    const long long ctas = (rows + kWarps - 1) / kWarps;
+    const long long ctas = (rows + WARPS - 1) / WARPS;
     if (ctas > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    return launch_pdl(rows_quantize_kernel<PIECES>, dim3((unsigned)ctas), dim3(kThreads), 0, stream, reinterpret_cast<const bf16*>(x), rows, cols,
+    return launch_pdl(rows_quantize_kernel<PIECES, WARPS>, dim3((unsigned)ctas), dim3(WARPS * 32), 0, stream, reinterpret_cast<const bf16*>(x), rows, cols,
                       reinterpret_cast<int8_t*>(x8), steps);
 }
 
@@ -74,9 +72,10 @@ static cudaError_t launch_p(const void* x, long long rows, int cols, void* x8, f
 
 cudaError_t launch_rows_quantize(const void* x, long long rows, int cols, void* x8, float* steps, cudaStream_t stream)
 {
-    if (cols <= 512) return quant::launch_p<2>(x, rows, cols, x8, steps, stream);
-    if (cols <= 1024) return quant::launch_p<4>(x, rows, cols, x8, steps, stream);
-    return quant::launch_p<8>(x, rows, cols, x8, steps, stream);
+    // 16 rows a CTA where rows are long (16384 x 2048: 16.8 us, with 8 19.5; floor 15.3), 8 where they are short (4096 x 1024: 2.9 us, with 16 3.2)
+    if (cols <= 512) return quant::launch_p<2, 8>(x, rows, cols, x8, steps, stream);
+    if (cols <= 1024) return quant::launch_p<4, 8>(x, rows, cols, x8, steps, stream);
+    return quant::launch_p<8, 16>(x, rows, cols, x8, steps, stream);
 }
 
 }  // namespace bt
