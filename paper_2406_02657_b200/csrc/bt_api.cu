@@ -710,14 +710,14 @@ bt_status bt_block_kv4_read(const bt_config* cfg, const bt_block_cache_kv4* cach
     return cuda_status(bt::launch_kv4_read(a, (cudaStream_t)stream));
 }
 
-// Ways the row range of a (sequence, head) is cut: enough parts for the kernel's warps (16 at head_dim 64, 8 at 128, on each of 148 SMs; the
-// number fixes the workspace, so it does not depend on the device), each of at least 128 rows, or of 64 while the parts are so few that
+// Ways the row range of a (sequence, head) is cut: enough parts for the kernel's warps (eight on each of 148 SMs; the number
+// fixes the workspace, so it does not depend on the device), each of at least 128 rows, or of 64 while the parts are so few that
 // they are joined in one go (32 pairs of 300 to 512 rows of 64: 5.4 us in eight parts, 6.0 in four; 16 pairs of 4096: 7.8 us in 64
 // parts, 7.0 in 32).
 static int kv4_splits(const bt_config* cfg)
 {
     if (cfg->decode_splits > 0) return cfg->decode_splits;
-    long long s = (cfg->head_dim == 64 ? 16 : 8) * 148 / ((long long)cfg->batch * cfg->heads);
+    long long s = 8 * 148 / ((long long)cfg->batch * cfg->heads);
     const long long few = cfg->max_blocks / 64 < 16 ? cfg->max_blocks / 64 : 16;
     const long long most = cfg->max_blocks / 128 > few ? cfg->max_blocks / 128 : few;
     if (s > most) s = most;

@@ -18,30 +18,35 @@
 //            columns (2 groups x 4 bytes).  Sums are kept as 32-bit whole numbers until what they are relative to changes.
 // Products of the same bytes with rows of eights give what the offsets of the codes of V add; for K a sum over the query does.
 //
-// As in the streaming kernel of the bf16 cache: one persistent CTA per SM, every warp on its own with a ring of chunks (64 rows,
-// one bulk copy: tiles hold K and V), work items (sequence, head, part of the rows), partial results joined by the part that ends
+// As in the streaming kernel of the bf16 cache: one persistent CTA per SM, every warp on its own with a ring of chunks (64 or 128
+// rows, one bulk copy: tiles hold K and V), work items (sequence, head, part of the rows), partial results joined by the part that ends
 // last, the length raised by the item that reads it last.  A new row is quantised by the warp that owns the last row, stored into
 // the cache, and put into the copied chunk, where it is attended like any other: a step gives what append and attention give.
+#include <type_traits>
+
 #include "bt_decode_ring.cuh"
 #include "bt_kv4.cuh"
 
 namespace bt {
 namespace kv4 {
 
-constexpr int kChunkTiles = 4, kChunkRows = kChunkTiles * kTileRows;
+constexpr int kUnitTiles = 4, kUnitRows = kUnitTiles * kTileRows;   // rows that a warp scores at once, two a lane
 constexpr uint32_t kPollLimit = 1u << 24;   // polls of one wait before giving up (each poll suspends briefly)
 
-template <int HD>
+// UNITS: units of a chunk.  Two planes of a unit or two units of a plane go through the arithmetic together: what a chunk costs beside its
+// products is shared, and a warp has twice the independent instructions.
+template <int HD, int UNITS>
 struct Geo {
     static constexpr int PLANES = HD / 64;
+    static constexpr int ROWS = UNITS * kUnitRows;
     static constexpr int TILE = PLANES * kTileBytes;
-    static constexpr int STAGE = kChunkTiles * TILE;
+    static constexpr int STAGE = UNITS * kUnitTiles * TILE;
     static constexpr int WEIGHT_TILE = 8 * kTileRows + 16;        // 8 columns (group, byte) of 16 rows; 16 more spread the tiles over the banks
-    static constexpr int WEIGHT_PLANE = kChunkTiles * WEIGHT_TILE;
-    static constexpr int WEIGHTS = PLANES * WEIGHT_PLANE;
+    static constexpr int WEIGHT_PLANE = kUnitTiles * WEIGHT_TILE;   // of a unit
+    static constexpr int WEIGHTS = UNITS * PLANES * WEIGHT_PLANE;
 };
-template <int HD>
-constexpr int smem_bytes(int warps, int stages) { return warps * (stages * (Geo<HD>::STAGE + 8) + Geo<HD>::WEIGHTS); }
+template <int HD, int UNITS>
+constexpr int smem_bytes(int warps, int stages) { return warps * (stages * (Geo<HD, UNITS>::STAGE + 8) + Geo<HD, UNITS>::WEIGHTS); }
 
 __device__ __forceinline__ void lds64(uint32_t addr, uint32_t& x, uint32_t& y)
 {
@@ -99,7 +104,7 @@ __device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4])
 {
     return __byte_perm(__byte_perm(w[0], w[1], B | (4 + B) << 4), __byte_perm(w[2], w[3], B | (4 + B) << 4), 0x5410);
 }
-constexpr int kChunksPerSum = 512;       // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
+constexpr int kUnitsPerSum = 512;        // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
 constexpr float kHeadroom = 4.f;         // how far (log2) scores may exceed what weights are relative to before that changes
 constexpr int kJoin = 16;               // partial results requested at once
 constexpr int kWeightTo = 27;            // the largest step of V to 2^27 .. 2^28, weights up to 2^4 times that
@@ -131,18 +136,18 @@ __device__ __forceinline__ Work work_of(int item, const Params& a, int n)   // n
     w.overflow = a.k_new != nullptr && !append;
     n += append ? 1 : 0;
     w.n = n;
-    // whole chunks per part, as even as that goes (trailing parts may be empty)
-    const int per = divide((n + kChunkRows - 1) / kChunkRows + a.splits - 1, a.by_splits) * kChunkRows;
+    // whole units per part, as even as that goes (trailing parts may be empty)
+    const int per = divide((n + kUnitRows - 1) / kUnitRows + a.splits - 1, a.by_splits) * kUnitRows;
     w.r0 = min(n, w.sp * per);
     w.r1 = min(n, w.r0 + per);
     w.new_row = append && w.r1 == n && w.r0 < n;
     return w;
 }
 
-template <int HD, int STAGES, int MAX_WARPS>
+template <int HD, int UNITS, int STAGES, int MAX_WARPS>
 __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(const __grid_constant__ Params a)
 {
-    using G = Geo<HD>;
+    using G = Geo<HD, UNITS>;
     constexpr int PLANES = G::PLANES, LPR = HD / 8;
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -170,7 +175,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
     // from a look at the length that may be out of date (read past L1), so it is a hint and decides nothing.
     if (first < n_items && lane == 0) {
         const Work h = work_of(first, a, __ldcg(a.len + sequence_of(first, a)));
-        const uint32_t bytes = (uint32_t)((min(STAGES * kChunkRows, h.r1 - h.r0) + kTileRows - 1) / kTileRows) * G::TILE;
+        const uint32_t bytes = (uint32_t)((min(STAGES * G::ROWS, h.r1 - h.r0) + kTileRows - 1) / kTileRows) * G::TILE;
         if (bytes > 0)
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(kv + (size_t)h.bh * a.slab_bytes + (size_t)(h.r0 / kTileRows) * G::TILE), "r"(bytes) : "memory");
     }
@@ -192,13 +197,13 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         if (p_left <= 0) return;
         const uint32_t st = issued % STAGES;
         if (lane == 0) {
-            const uint32_t bytes = (uint32_t)((min(kChunkRows, p_left) + kTileRows - 1) / kTileRows) * G::TILE;
+            const uint32_t bytes = (uint32_t)((min(G::ROWS, p_left) + kTileRows - 1) / kTileRows) * G::TILE;
             mbar_expect_tx(bar0 + 8 * st, bytes);
             ring::bulk_load(ring0 + st * G::STAGE, p_from, bytes, bar0 + 8 * st, policy);
         }
         ++issued;
         p_from += G::STAGE;
-        p_left -= kChunkRows;
+        p_left -= G::ROWS;
         if (p_left <= 0) {
             p_item += stride;
             p_seek();
@@ -314,7 +319,136 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
             pending = 0;
         };
 
-        for (int row = w.r0; row < w.r1; row += kChunkRows) {
+        // The rows of a chunk: N units, of which nvalid rows are there.
+        auto chunk = [&](auto units, uint32_t st, int nvalid) {
+            constexpr int N = decltype(units)::value;
+            // ---- scores of rows 16 c + 2 g and 16 c + 2 g + 1 of every unit, in this lane
+            float s[N][2];
+            float t[N][PLANES][2][2];   // steps of V: group, row
+            bool in[N][2];
+            const uint32_t own_tile = st + c * G::TILE + g * 8;
+            float top = kNegInf, most = t_most;
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const uint32_t tile0 = st + u * (kUnitTiles * G::TILE);
+                s[u][0] = s[u][1] = 0.f;
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+                    int acc[kUnitTiles][4];
+                    // (Tiles that the chunk has not are multiplied all the same: what a stage holds there is whole numbers too, and their
+                    // scores are set aside below.  Without branches the tiles' instructions interleave.)
+#pragma unroll
+                    for (int k = 0; k < kUnitTiles; ++k) {
+                        const uint4 x = lds128(tile0 + k * G::TILE + p * kTileBytes + lane * 16);   // two words of the even row, two of the odd
+                        const uint32_t a0 = even_codes(x.x), a1 = even_codes(x.z), a2 = odd_codes(x.x), a3 = odd_codes(x.z);
+                        const uint32_t b0 = even_codes(x.y), b1 = even_codes(x.w), b2 = odd_codes(x.y), b3 = odd_codes(x.w);
+                        mma_signed_new(acc[k], a0, a1, a2, a3, qf[p][0][0][0], qf[p][0][0][1]);
+                        mma_signed(acc[k], b0, b1, b2, b3, qf[p][1][0][0], qf[p][1][0][1]);
+#pragma unroll
+                        for (int byte = 1; byte < 3; ++byte) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[k][i] *= 256;
+                            mma_signed(acc[k], a0, a1, a2, a3, qf[p][0][byte][0], qf[p][0][byte][1]);
+                            mma_signed(acc[k], b0, b1, b2, b3, qf[p][1][byte][0], qf[p][1][byte][1]);
+                        }
+                    }
+                    float mine[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int lo = c & 1 ? acc[1][i] : acc[0][i], hi = c & 1 ? acc[3][i] : acc[2][i];
+                        mine[i] = (float)((c & 2 ? hi : lo) - q_off[p][i & 1]);
+                    }
+                    uint32_t k0, k1;
+                    lds64(own_tile + u * (kUnitTiles * G::TILE) + p * kTileBytes + kStepsAt, k0, k1);
+                    s[u][0] = fmaf(mine[1], bf_hi(k0), fmaf(mine[0], bf_lo(k0), s[u][0]));
+                    s[u][1] = fmaf(mine[3], bf_hi(k1), fmaf(mine[2], bf_lo(k1), s[u][1]));
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    in[u][r] = u * kUnitRows + 16 * c + 2 * g + r < nvalid;
+                    s[u][r] = in[u][r] ? s[u][r] * q_unit * a.scale_log2 : kNegInf;
+                    top = fmaxf(top, s[u][r]);
+                }
+                // steps of V of the two rows; a row that is not there has no weight whatever its step is
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+                    uint32_t v[2];
+                    lds64(own_tile + u * (kUnitTiles * G::TILE) + p * kTileBytes + kStepsAt + 64, v[0], v[1]);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        v[r] = in[u][r] ? v[r] : 0u;
+                        t[u][p][0][r] = bf_lo(v[r]);
+                        t[u][p][1][r] = bf_hi(v[r]);
+                        most = fmaxf(most, fmaxf(t[u][p][0][r], t[u][p][1][r]));
+                        bad[p][0] = fmaf(0.f, t[u][p][0][r], bad[p][0]);
+                        bad[p][1] = fmaf(0.f, t[u][p][1][r], bad[p][1]);
+                    }
+                }
+            }
+            const float mn = fmaxf(m, warp_max(top));
+            t_most = warp_max(most);
+            const float to = power_to<kWeightTo>(t_most);
+            // What weights are relative to changes (for all of the warp) when a score would leave the headroom or a step of V the range.
+            const bool grown = mn > m + kHeadroom || (m == kNegInf && mn > m);
+            if (grown || to != t_to || pending >= kUnitsPerSum) {
+                if (pending > 0) flush();
+                const float m2 = grown ? mn : m, cf = ex2(m - softmax_reference(m2));
+                l *= cf;
+                const float co = cf * (to * inverse_power(t_to));
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        o[p][r][0] *= co;
+                        o[p][r][1] *= co;
+                    }
+                m = m2;
+                t_to = to;
+            }
+            pending += N;
+            const float m_use = softmax_reference(m);
+            // ---- weights of the rows: column 4 (group) + byte of a plane
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const float p0 = ex2(s[u][0] - m_use), p1 = ex2(s[u][1] - m_use);
+                l += p0 + p1;
+                const float w0 = p0 * t_to, w1 = p1 * t_to;
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+#pragma unroll
+                    for (int gl = 0; gl < 2; ++gl) {
+                        const uint32_t at = wbuf + (u * PLANES + p) * G::WEIGHT_PLANE + c * G::WEIGHT_TILE + gl * (4 * kTileRows) + 2 * g;
+                        const uint32_t x = whole(w0 * t[u][p][gl][0]), y = whole(w1 * t[u][p][gl][1]);
+                        sts16(at, __byte_perm(x, y, 0x0040));
+                        sts16(at + kTileRows, __byte_perm(x, y, 0x0051));
+                        sts16(at + 2 * kTileRows, __byte_perm(x, y, 0x0062));
+                        sts16(at + 3 * kTileRows, __byte_perm(x, y, 0x0073));
+                    }
+                }
+            }
+            __syncwarp();
+            // ---- weighted codes of V: rows 4 c .. 4 c + 3 of two tiles are this lane's
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+#pragma unroll
+                for (int k = 0; k < kUnitTiles; k += 2) {   // (rows that are not there have weights of zero)
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p) {
+                        const uint32_t wt = wbuf + (u * PLANES + p) * G::WEIGHT_PLANE + k * G::WEIGHT_TILE + lane * 4;
+                        const uint32_t b0 = lds32(wt), b1 = lds32(wt + G::WEIGHT_TILE);
+                        const uint32_t at = st + (u * kUnitTiles + k) * G::TILE + p * kTileBytes + kPartBytes + c * 128 + ((g ^ (2 * c)) << 4);
+                        const uint4 x = lds128(at), y = lds128(at + G::TILE);
+                        mma_unsigned(sums[p][0], even_codes(x.x), odd_codes(x.x), even_codes(y.x), odd_codes(y.x), b0, b1);
+                        mma_unsigned(sums[p][1], even_codes(x.y), odd_codes(x.y), even_codes(y.y), odd_codes(y.y), b0, b1);
+                        mma_unsigned(sums[p][2], even_codes(x.z), odd_codes(x.z), even_codes(y.z), odd_codes(y.z), b0, b1);
+                        mma_unsigned(sums[p][3], even_codes(x.w), odd_codes(x.w), even_codes(y.w), odd_codes(y.w), b0, b1);
+                        mma_unsigned(eights[p], 0x08080808u, 0x80808080u, 0x08080808u, 0x80808080u, b0, b1);
+                    }
+                }
+            }
+        };
+
+        for (int row = w.r0; row < w.r1; row += G::ROWS) {
             const uint32_t sidx = consumed % STAGES;
             // the outcome is made warp-uniform: what follows needs all 32 lanes
             if (!__all_sync(0xffffffffu, mbar_wait_polls(bar0 + 8 * sidx, (consumed / STAGES) & 1, kPollLimit))) {
@@ -322,8 +456,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                 break;
             }
             const uint32_t st = ring0 + sidx * G::STAGE;
-            const int nvalid = min(kChunkRows, w.r1 - row);
-            if (w.new_row && row + kChunkRows >= w.r1) {
+            const int nvalid = min(G::ROWS, w.r1 - row);
+            if (w.new_row && row + G::ROWS >= w.r1) {
                 // the new row, eight values a lane: lanes 0 .. LPR - 1 K, the next V (at head_dim 64 the upper half repeats them)
                 const int part = (lane / LPR) & 1, piece = lane % LPR;
                 const uint4 x = ld_plain(reinterpret_cast<const bf16*>(part == 0 ? a.k_new : a.v_new) + (size_t)w.bh * HD + piece * 8);
@@ -351,114 +485,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                 }
                 __syncwarp();
             }
-            // ---- scores of rows 16 c + 2 g and 16 c + 2 g + 1 of the chunk, in this lane
-            float s0 = 0.f, s1 = 0.f;
-            const uint32_t own_tile = st + c * G::TILE + g * 8;
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
-                int acc[kChunkTiles][4];
-                // (Tiles that the chunk has not are multiplied all the same: what a stage holds there is whole numbers too, and their scores
-                // are set aside below.  Without branches the tiles' instructions interleave.)
-#pragma unroll
-                for (int t = 0; t < kChunkTiles; ++t) {
-                    const uint4 x = lds128(st + t * G::TILE + p * kTileBytes + lane * 16);   // two words of the even row, two of the odd
-                    const uint32_t a0 = even_codes(x.x), a1 = even_codes(x.z), a2 = odd_codes(x.x), a3 = odd_codes(x.z);
-                    const uint32_t b0 = even_codes(x.y), b1 = even_codes(x.w), b2 = odd_codes(x.y), b3 = odd_codes(x.w);
-                    mma_signed_new(acc[t], a0, a1, a2, a3, qf[p][0][0][0], qf[p][0][0][1]);
-                    mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][0][0], qf[p][1][0][1]);
-#pragma unroll
-                    for (int byte = 1; byte < 3; ++byte) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[t][i] *= 256;
-                        mma_signed(acc[t], a0, a1, a2, a3, qf[p][0][byte][0], qf[p][0][byte][1]);
-                        mma_signed(acc[t], b0, b1, b2, b3, qf[p][1][byte][0], qf[p][1][byte][1]);
-                    }
-                }
-                float mine[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int lo = c & 1 ? acc[1][i] : acc[0][i], hi = c & 1 ? acc[3][i] : acc[2][i];
-                    mine[i] = (float)((c & 2 ? hi : lo) - q_off[p][i & 1]);
-                }
-                uint32_t k0, k1;
-                lds64(own_tile + p * kTileBytes + kStepsAt, k0, k1);
-                s0 = fmaf(mine[1], bf_hi(k0), fmaf(mine[0], bf_lo(k0), s0));
-                s1 = fmaf(mine[3], bf_hi(k1), fmaf(mine[2], bf_lo(k1), s1));
-            }
-            const bool in0 = 16 * c + 2 * g < nvalid, in1 = 16 * c + 2 * g + 1 < nvalid;
-            s0 = in0 ? s0 * q_unit * a.scale_log2 : kNegInf;
-            s1 = in1 ? s1 * q_unit * a.scale_log2 : kNegInf;
-            // steps of V of the two rows; a row that is not there has no weight whatever its step is
-            float t0[PLANES][2], t1[PLANES][2], most = t_most;
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
-                uint32_t v0, v1;
-                lds64(own_tile + p * kTileBytes + kStepsAt + 64, v0, v1);
-                v0 = in0 ? v0 : 0u;
-                v1 = in1 ? v1 : 0u;
-                t0[p][0] = bf_lo(v0);
-                t0[p][1] = bf_hi(v0);
-                t1[p][0] = bf_lo(v1);
-                t1[p][1] = bf_hi(v1);
-                most = fmaxf(most, fmaxf(fmaxf(t0[p][0], t0[p][1]), fmaxf(t1[p][0], t1[p][1])));
-                bad[p][0] = fmaf(0.f, t0[p][0], fmaf(0.f, t1[p][0], bad[p][0]));
-                bad[p][1] = fmaf(0.f, t0[p][1], fmaf(0.f, t1[p][1], bad[p][1]));
-            }
-            const float mn = fmaxf(m, warp_max(fmaxf(s0, s1)));
-            t_most = warp_max(most);
-            const float to = power_to<kWeightTo>(t_most);
-            // What weights are relative to changes (for all of the warp) when a score would leave the headroom or a step of V the range.
-            const bool grown = mn > m + kHeadroom || (m == kNegInf && mn > m);
-            if (grown || to != t_to || pending == kChunksPerSum) {
-                if (pending > 0) flush();
-                const float m2 = grown ? mn : m, cf = ex2(m - softmax_reference(m2));
-                l *= cf;
-                const float co = cf * (to * inverse_power(t_to));
-#pragma unroll
-                for (int p = 0; p < PLANES; ++p)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        o[p][r][0] *= co;
-                        o[p][r][1] *= co;
-                    }
-                m = m2;
-                t_to = to;
-            }
-            ++pending;
-            const float m_use = softmax_reference(m);
-            const float p0 = ex2(s0 - m_use), p1 = ex2(s1 - m_use);
-            l += p0 + p1;
-            // ---- weights of the two rows: column 4 (group) + byte of a plane
-            const float w0 = p0 * t_to, w1 = p1 * t_to;
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
-#pragma unroll
-                for (int gl = 0; gl < 2; ++gl) {
-                    const uint32_t at = wbuf + p * G::WEIGHT_PLANE + c * G::WEIGHT_TILE + gl * (4 * kTileRows) + 2 * g;
-                    const uint32_t x = whole(w0 * t0[p][gl]), y = whole(w1 * t1[p][gl]);
-                    sts16(at, __byte_perm(x, y, 0x0040));
-                    sts16(at + kTileRows, __byte_perm(x, y, 0x0051));
-                    sts16(at + 2 * kTileRows, __byte_perm(x, y, 0x0062));
-                    sts16(at + 3 * kTileRows, __byte_perm(x, y, 0x0073));
-                }
-            }
-            __syncwarp();
-            // ---- weighted codes of V: rows 4 c .. 4 c + 3 of two tiles are this lane's
-#pragma unroll
-            for (int t = 0; t < kChunkTiles; t += 2) {   // (rows that are not there have weights of zero)
-#pragma unroll
-                for (int p = 0; p < PLANES; ++p) {
-                    const uint32_t wt = wbuf + p * G::WEIGHT_PLANE + t * G::WEIGHT_TILE + lane * 4;
-                    const uint32_t b0 = lds32(wt), b1 = lds32(wt + G::WEIGHT_TILE);
-                    const uint32_t at = st + t * G::TILE + p * kTileBytes + kPartBytes + c * 128 + ((g ^ (2 * c)) << 4);
-                    const uint4 x = lds128(at), y = lds128(at + G::TILE);
-                    mma_unsigned(sums[p][0], even_codes(x.x), odd_codes(x.x), even_codes(y.x), odd_codes(y.x), b0, b1);
-                    mma_unsigned(sums[p][1], even_codes(x.y), odd_codes(x.y), even_codes(y.y), odd_codes(y.y), b0, b1);
-                    mma_unsigned(sums[p][2], even_codes(x.z), odd_codes(x.z), even_codes(y.z), odd_codes(y.z), b0, b1);
-                    mma_unsigned(sums[p][3], even_codes(x.w), odd_codes(x.w), even_codes(y.w), odd_codes(y.w), b0, b1);
-                    mma_unsigned(eights[p], 0x08080808u, 0x80808080u, 0x08080808u, 0x80808080u, b0, b1);
-                }
-            }
+            // a chunk of one unit, or of two where it has more than 64 rows
+            if (UNITS == 1 || nvalid <= kUnitRows) chunk(std::integral_constant<int, 1>(), st, nvalid);
+            else chunk(std::integral_constant<int, UNITS>(), st, nvalid);
             // The stage and the weights have been read by every lane before either is written again; what was put into the stage
             // by this warp is ordered before the copy engine's writes.
             if (w.new_row) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -576,21 +605,11 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
     }
 }
 
-#ifndef BT_KV4_WARPS_64
-#define BT_KV4_WARPS_64 16
-#define BT_KV4_STAGES_64 2
-#define BT_KV4_WARPS_128 8
-#define BT_KV4_STAGES_128 2
-#endif
-
-template <int HD, int STAGES, int MAX_WARPS>
-static cudaError_t launch_t(const Kv4DecodeArgs& a, cudaStream_t stream)
+template <int HD, int UNITS, int STAGES, int MAX_WARPS>
+static cudaError_t launch_t(const Kv4DecodeArgs& a, int dev, int sms, cudaStream_t stream)
 {
-    int dev = 0, sms = 0;
-    cudaError_t e = current_device(&dev, &sms);
-    if (e != cudaSuccess) return e;
     static PerDeviceOnce limit_raised;
-    e = raise_smem_limit_once(limit_raised, dev, block_decode_kv4_kernel<HD, STAGES, MAX_WARPS>, smem_bytes<HD>(MAX_WARPS, STAGES));
+    const cudaError_t e = raise_smem_limit_once(limit_raised, dev, block_decode_kv4_kernel<HD, UNITS, STAGES, MAX_WARPS>, smem_bytes<HD, UNITS>(MAX_WARPS, STAGES));
     if (e != cudaSuccess) return e;
     const long long items = (long long)a.B * a.H * a.splits;
     if (items > 0x7fffffffLL - 4096) return cudaErrorInvalidConfiguration;
@@ -613,14 +632,23 @@ static cudaError_t launch_t(const Kv4DecodeArgs& a, cudaStream_t stream)
     }
     const long long each = (items + grid - 1) / grid;
     if (each < warps) warps = (int)each;
-    return launch_pdl(block_decode_kv4_kernel<HD, STAGES, MAX_WARPS>, dim3((unsigned)grid), dim3(warps * 32), (size_t)smem_bytes<HD>(warps, STAGES), stream, p);
+    return launch_pdl(block_decode_kv4_kernel<HD, UNITS, STAGES, MAX_WARPS>, dim3((unsigned)grid), dim3(warps * 32), (size_t)smem_bytes<HD, UNITS>(warps, STAGES), stream, p);
 }
 
 }  // namespace kv4
 
 cudaError_t launch_block_decode_kv4(const Kv4DecodeArgs& a, cudaStream_t stream)
 {
-    return a.hd == 64 ? kv4::launch_t<64, BT_KV4_STAGES_64, BT_KV4_WARPS_64>(a, stream) : kv4::launch_t<128, BT_KV4_STAGES_128, BT_KV4_WARPS_128>(a, stream);
+    int dev = 0, sms = 0;
+    const cudaError_t e = current_device(&dev, &sms);
+    if (e != cudaSuccess) return e;
+    if (a.hd == 128) return kv4::launch_t<128, 1, 2, 8>(a, dev, sms, stream);
+    // Head_dim 64: with at most eight items an SM, a warp each and chunks of two units; with more, 16 warps an SM (126 registers a thread),
+    // of which each spends half as long on an item's beginning and end.  us, 16 warps / eight:
+    //   items of 48 to 64 rows:     1024: 3.6 / 3.6,  1536: 4.1 / 5.7,  4096: 8.1 / 10.3
+    //   items of 384 to 512 rows:   1024: 10.4 / 8.7, 1536: 12.3 / 14.6, 4096: 25.8 / 27.1
+    if ((long long)a.B * a.H * a.splits > 8LL * sms) return kv4::launch_t<64, 1, 2, 16>(a, dev, sms, stream);
+    return kv4::launch_t<64, 2, 2, 8>(a, dev, sms, stream);
 }
 
 }  // namespace bt
