@@ -135,16 +135,25 @@ def _ptr(t):
 # The current stream's handle without building a Stream object around it: 0.2 against 3.3 us, where the smallest calls spend
 # 4 us on the GPU.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)   # (a call's tensors are on a GPU: torch is initialised)
 
 
 def _stream(stream):
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))
+
+
+def _stream_of(t, stream):
+    """The stream for a call over `t`, which has to be on the current device: the kernels run there, and would read another's memory, or
+    the host's, as their own."""
+    if t.get_device() < 0 or t.get_device() != _device():
+        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {t.device}, not on the current device")
+    return _stream(stream)
 
 
 def _check(code: int, where: str):
@@ -430,7 +439,7 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
     n_new = k_new.shape[2] if n_new is None else n_new
     src_stride = k_new.shape[2] if src_stride is None else src_stride
     _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(k_new), _ptr(v_new), _i32(n_new), src_stride,
-                                    1 if reset_first else 0, _ptr(dev_status), _stream(stream)), "bt_block_kv4_append")
+                                    1 if reset_first else 0, _ptr(dev_status), _stream_of(k_new, stream)), "bt_block_kv4_append")
 
 
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
@@ -438,39 +447,39 @@ def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n
     n_rows = k_out.shape[2] if n_rows is None else n_rows
     dst_stride = k_out.shape[2] if dst_stride is None else dst_stride
     _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _i32(first), _i32(n_rows), _ptr(k_out), _ptr(v_out),
-                                  dst_stride, _stream(stream)), "bt_block_kv4_read")
+                                  dst_stride, _stream_of(k_out, stream)), "bt_block_kv4_read")
 
 
 def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace, dev_status=None, stream=None):
     """Decode attention over the 4-bit cache."""
     _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(out), *_ws(workspace),
-                                         _ptr(dev_status), _stream(stream)), "bt_block_decode_attn_kv4")
+                                         _ptr(dev_status), _stream_of(q, stream)), "bt_block_decode_attn_kv4")
 
 
 def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, out, workspace, dev_status=None, stream=None):
     """Quantise and append the new block's row, then attend over the 4-bit cache including it, in one launch."""
     _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
-                                         *_ws(workspace), _ptr(dev_status), _stream(stream)), "bt_block_decode_step_kv4")
+                                         *_ws(workspace), _ptr(dev_status), _stream_of(q, stream)), "bt_block_decode_step_kv4")
 
 
 def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, bias, q_out, n_rows=None, dev_status=None, stream=None):
     """bt_block_qkv_project_append into the 4-bit cache."""
     n_rows = x.shape[1] if n_rows is None else n_rows
     _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x), _i32(n_rows), _ptr(w_qkv), _ptr(bias),
-                                                _ptr(q_out), _ptr(dev_status), _stream(stream)), "bt_block_qkv_project_append_kv4")
+                                                _ptr(q_out), _ptr(dev_status), _stream_of(x, stream)), "bt_block_qkv_project_append_kv4")
 
 
 def bt_rows_quantize_i8(x, x8, steps, stream=None):
     """Rows of x bf16 [..., n_cols] -> int8 of the same shape and fp32 steps [...]."""
     n_cols = x.shape[-1]
-    _check(_lib.bt_rows_quantize_i8(_ptr(x), x.numel() // max(n_cols, 1), _i32(n_cols), _ptr(x8), _ptr(steps), _stream(stream)),
+    _check(_lib.bt_rows_quantize_i8(_ptr(x), x.numel() // max(n_cols, 1), _i32(n_cols), _ptr(x8), _ptr(steps), _stream_of(x, stream)),
            "bt_rows_quantize_i8")
 
 
 def bt_prefix_project_i8(cfg, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status=None, stream=None):
     """bt_prefix_project of 8-bit operands and their steps."""
     _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), _ptr(ctx8), _ptr(ctx_steps), _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(prefix_out),
-                                     _ptr(dev_status), _stream(stream)), "bt_prefix_project_i8")
+                                     _ptr(dev_status), _stream_of(ctx8, stream)), "bt_prefix_project_i8")
 
 
 def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
@@ -478,7 +487,7 @@ def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w
     """bt_block_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
     _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
-                                               _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream(stream)),
+                                               _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream_of(x8, stream)),
            "bt_block_qkv_project_append_i8")
 
 
@@ -488,7 +497,7 @@ def bt_local_qkv_project_append_i8(cfg, cache: LocalCache, layer, x8, x_steps, w
     n_rows = x8.shape[1] if n_rows is None else n_rows
     _check(_lib.bt_local_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
                                                _ptr(w_steps), _ptr(bias), 1 if reset_first else 0, _ptr(reset_mask), _ptr(q_out),
-                                               _ptr(dev_status), _stream(stream)), "bt_local_qkv_project_append_i8")
+                                               _ptr(dev_status), _stream_of(x8, stream)), "bt_local_qkv_project_append_i8")
 
 
 def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
@@ -496,7 +505,7 @@ def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_s
     """bt_block_qkv_project_append of 8-bit operands and their steps into the 4-bit cache."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
     _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows),
-                                                   _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream(stream)),
+                                                   _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream_of(x8, stream)),
            "bt_block_qkv_project_append_i8_kv4")
 
 

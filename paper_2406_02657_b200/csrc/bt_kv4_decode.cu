@@ -13,9 +13,10 @@
 //            all of them after the other is multiplied into the same sums, which are shifted in between.  A column has the values of one
 //            group only and zeros elsewhere; columns alternate between the two groups of 64 dimensions, so that all four lanes that share
 //            a row hold its two sums, and lane c of them goes on with tile c of a chunk.
-//   output:  A = codes of V transposed, 16 dimensions x 32 rows; B = the weights p t of a group as whole numbers of 32 bits, relative to
-//            2^28 .. 2^32 for the largest (so that the rounding, 2^-29 of the largest, does not add up over a million rows), a byte in each of four
-//            columns (2 groups x 4 bytes).  Sums are kept as 32-bit whole numbers until what they are relative to changes.
+//   output:  A = codes of V transposed, 16 dimensions x 32 rows; B = the weights p t of a group as whole numbers of 32 bits, times a power
+//            of two that has the largest of them so far at 2^28 .. 2^32 (so that the rounding, 2^-29 of the largest, does not add up over a
+//            million rows), a byte in each of four columns (2 groups x 4 bytes).  Sums are kept as 32-bit whole numbers until what they are
+//            relative to changes.
 // Products of the same bytes with rows of eights give what the offsets of the codes of V add; for K a sum over the query does.
 //
 // As in the streaming kernel of the bf16 cache: one persistent CTA per SM, every warp on its own with a ring of chunks (64 or 128
@@ -107,7 +108,8 @@ __device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4])
 constexpr int kUnitsPerSum = 512;        // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
 constexpr float kHeadroom = 4.f;         // how far (log2) scores may exceed what weights are relative to before that changes
 constexpr int kJoin = 16;               // partial results requested at once
-constexpr int kWeightTo = 27;            // the largest step of V to 2^27 .. 2^28, weights up to 2^4 times that
+constexpr int kWeightTo = 28;            // the largest weight to 2^28 .. 2^29; it may grow until ...
+constexpr float kWeightEnd = 4294967296.f;
 // the largest of a warp's values that are numbers
 __device__ __forceinline__ float warp_max(float x)
 {
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         }
         if (item + stride < n_items) fetch_q(divide(item + stride, a.by_splits));
         float m = kNegInf, l = 0.f;                // what scores are relative to, the sum of 2^(score - m)
-        float t_most = 0.f, t_to = power_to<kWeightTo>(0.f);   // the largest step of V so far and the power of two for it
+        float w_most = 0.f, w_to = power_to<kWeightTo>(0.f);   // the largest weight p t so far and the power of two for it
         float o[PLANES][4][2], bad[PLANES][2];     // even | odd dimension; not a number once a step of V was none
         int sums[PLANES][4][4], eights[PLANES][4], pending = 0;
 #pragma unroll
@@ -324,10 +326,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
             constexpr int N = decltype(units)::value;
             // ---- scores of rows 16 c + 2 g and 16 c + 2 g + 1 of every unit, in this lane
             float s[N][2];
-            float t[N][PLANES][2][2];   // steps of V: group, row
+            float t[N][PLANES][2][2];   // steps of V, then weights: group, row
             bool in[N][2];
             const uint32_t own_tile = st + c * G::TILE + g * 8;
-            float top = kNegInf, most = t_most;
+            float top = kNegInf;
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const uint32_t tile0 = st + u * (kUnitTiles * G::TILE);
@@ -379,22 +381,38 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                         v[r] = in[u][r] ? v[r] : 0u;
                         t[u][p][0][r] = bf_lo(v[r]);
                         t[u][p][1][r] = bf_hi(v[r]);
-                        most = fmaxf(most, fmaxf(t[u][p][0][r], t[u][p][1][r]));
                         bad[p][0] = fmaf(0.f, t[u][p][0][r], bad[p][0]);
                         bad[p][1] = fmaf(0.f, t[u][p][1][r], bad[p][1]);
                     }
                 }
             }
+            // What scores are relative to changes (for all of the warp) when one would leave the headroom.
             const float mn = fmaxf(m, warp_max(top));
-            t_most = warp_max(most);
-            const float to = power_to<kWeightTo>(t_most);
-            // What weights are relative to changes (for all of the warp) when a score would leave the headroom or a step of V the range.
             const bool grown = mn > m + kHeadroom || (m == kNegInf && mn > m);
-            if (grown || to != t_to || pending >= kUnitsPerSum) {
+            const float cf = grown ? ex2(m - mn) : 1.f;
+            m = grown ? mn : m;
+            const float m_use = softmax_reference(m);
+            l *= cf;
+            float most = w_most * cf;
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const float p0 = ex2(s[u][0] - m_use), p1 = ex2(s[u][1] - m_use);
+                l += p0 + p1;
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                    for (int gl = 0; gl < 2; ++gl) {
+                        t[u][p][gl][0] *= p0;
+                        t[u][p][gl][1] *= p1;
+                        most = fmaxf(most, fmaxf(t[u][p][gl][0], t[u][p][gl][1]));
+                    }
+            }
+            // ... and what weights are relative to, then and when one would leave 32 bits.
+            w_most = warp_max(most);
+            if (grown || w_most * w_to >= kWeightEnd || pending >= kUnitsPerSum) {
                 if (pending > 0) flush();
-                const float m2 = grown ? mn : m, cf = ex2(m - softmax_reference(m2));
-                l *= cf;
-                const float co = cf * (to * inverse_power(t_to));
+                const float to = power_to<kWeightTo>(w_most);
+                const float co = cf * to * inverse_power(w_to);   // at most 2, in this order
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p)
 #pragma unroll
@@ -402,23 +420,18 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                         o[p][r][0] *= co;
                         o[p][r][1] *= co;
                     }
-                m = m2;
-                t_to = to;
+                w_to = to;
             }
             pending += N;
-            const float m_use = softmax_reference(m);
             // ---- weights of the rows: column 4 (group) + byte of a plane
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const float p0 = ex2(s[u][0] - m_use), p1 = ex2(s[u][1] - m_use);
-                l += p0 + p1;
-                const float w0 = p0 * t_to, w1 = p1 * t_to;
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p) {
 #pragma unroll
                     for (int gl = 0; gl < 2; ++gl) {
                         const uint32_t at = wbuf + (u * PLANES + p) * G::WEIGHT_PLANE + c * G::WEIGHT_TILE + gl * (4 * kTileRows) + 2 * g;
-                        const uint32_t x = whole(w0 * t[u][p][gl][0]), y = whole(w1 * t[u][p][gl][1]);
+                        const uint32_t x = whole(t[u][p][gl][0] * w_to), y = whole(t[u][p][gl][1] * w_to);
                         sts16(at, __byte_perm(x, y, 0x0040));
                         sts16(at + kTileRows, __byte_perm(x, y, 0x0051));
                         sts16(at + 2 * kTileRows, __byte_perm(x, y, 0x0062));
@@ -503,7 +516,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         // the high ones in those of odd c.  They count where that is the dimensions' group, and are added up here.
         const bool own_piece = c == 2 * (g >> 2);
         const float high = c & 1 ? 65536.f : 1.f;
-        const float unit = inverse_power(t_to) * inverse_sum(l);
+        const float unit = inverse_power(w_to) * inverse_sum(l);
         auto piece = [&](int p, float (&f)[8]) {
             const bool bad0 = __any_sync(0xffffffffu, bad[p][0] != 0.f), bad1 = __any_sync(0xffffffffu, bad[p][1] != 0.f);
             const float u = (g < 4 ? bad0 : bad1) ? __uint_as_float(0x7fffffffu) : unit;

@@ -191,3 +191,22 @@ def test_integer_projection_agrees_with_brute_force():
         for n in range(4):
             want = sum(int(x8[m, i]) * int(w8[n, i]) for i in range(16)) * xs[m] * ws[n] + bias[n]
             assert abs(y[m, n] - want) < 1e-9 and tol[m, n] > 2.0 ** -9 * abs(want)
+
+
+def test_host_tensors_are_refused(bt):
+    """Memory of the host, or of another device than the current one, does not reach a kernel."""
+    import torch
+
+    cfg = bt.make_config(2, 2, 64, 4, 1, 16, 1)
+    cache, ws = bt.BlockCacheKV4(cfg, device="cpu"), torch.zeros(bt.bt_workspace_bytes_kv4(cfg), dtype=torch.uint8)
+    q, rows = torch.zeros((2, 2, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 3, 64), dtype=torch.bfloat16)
+    x8, xs = torch.zeros((2, 1, 128), dtype=torch.int8), torch.zeros((2, 1))
+    x, w8 = torch.zeros((2, 1, 128), dtype=torch.bfloat16), torch.zeros((384, 128), dtype=torch.int8)
+    for call in (lambda: bt.bt_block_kv4_append(cfg, cache, 0, rows, rows), lambda: bt.bt_block_kv4_read(cfg, cache, 0, rows, rows),
+                 lambda: bt.bt_block_decode_attn_kv4(cfg, cache, 0, q, q, ws), lambda: bt.bt_block_decode_step_kv4(cfg, cache, 0, q, q, q, q, ws),
+                 lambda: bt.bt_rows_quantize_i8(x, x8, xs), lambda: bt.bt_prefix_project_i8(cfg, x8, xs, w8, xs, None, q),
+                 lambda: bt.bt_block_qkv_project_append_kv4(cfg, cache, 0, x, x, None, q),
+                 lambda: bt.bt_block_qkv_project_append_i8_kv4(cfg, cache, 0, x8, xs, w8, xs, None, q)):
+        with pytest.raises(bt.BtError) as e:
+            call()
+        assert e.value.code == bt.BT_ERR_UNSUPPORTED

@@ -241,6 +241,31 @@ def test_large_scores_keep_their_precision(bt, hd):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_rows_of_unlike_size(bt, hd, splits):
+    """V of sizes from 2^-90 to 2^90 under weights that make up for it or not: a huge row that gets next to no weight takes no precision from
+    the others, tiny rows alone keep theirs, and the size grows and shrinks along the rows."""
+    B, H, N = 4, 2, 330
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    q, k, v = f64(rnd(18, 3, (B, H, hd))), f64(rnd(18, 1, (B, H, N, hd))), f64(rnd(18, 2, (B, H, N, hd)))
+    q[..., 0] = 8.0
+    k[..., 0] = 0.0
+    k[0, :, 17, 0], v[0, :, 17] = -90.0, v[0, :, 17] * 2.0 ** 60      # weight about 2^-100: huge all the same
+    k[0, :, 18, 0], v[0, :, 18] = -60.0, v[0, :, 18] * 2.0 ** 30
+    v[1] *= 2.0 ** -90
+    v[2] *= 2.0 ** np.linspace(-90, 90, N)[None, :, None]             # and the scores fall as the rows grow
+    k[2, :, :, 0] = -np.linspace(0, 90, N) / 2
+    v[3] *= 2.0 ** np.linspace(40, -40, N)[None, :, None]
+    q, k, v = bits(q), bits(k), bits(v)
+    lens = [N, N, N, 301]
+    cache = filled(bt, cfg, k, v, lens)
+    out, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), bt.alloc_workspace_kv4(cfg)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, to_dev(q), out, ws)
+    ref, tol = lb.decode(f64(q), lb.held(f64(k)), lb.held(f64(v)), lens)
+    check(out, ref, tol, "unlike rows")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("splits", [1, 4])
 def test_values_that_are_not_finite(bt, hd, splits):
     B, H, N = 6, 2, 200
