@@ -105,6 +105,8 @@ __device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4])
 {
     return __byte_perm(__byte_perm(w[0], w[1], B | (4 + B) << 4), __byte_perm(w[2], w[3], B | (4 + B) << 4), 0x5410);
 }
+constexpr float kWholeAt = 12582912.f;   // 1.5 * 2^23
+constexpr uint32_t kWholeBits = 0x4B400000u;
 constexpr int kUnitsPerSum = 512;        // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
 constexpr float kHeadroom = 4.f;         // how far (log2) scores may exceed what weights are relative to before that changes
 constexpr int kJoin = 16;               // partial results requested at once
@@ -263,7 +265,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
             const uint32_t own_group = (g & 1) == (c >> 1) ? 0xffffffffu : 0u;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
-                int sum = 0;
+                // Adding 1.5 * 2^23 rounds to whole numbers and leaves them in the low bits: kWholeBits + n.
+                uint32_t by_parity[2] = {0u, 0u};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     float f[8];
@@ -272,16 +275,16 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                     for (int h = 0; h < 2; ++h) {
                         uint32_t x[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int n = __float2int_rn(f[2 * j + h] * (h ? to * 0.0625f : to));
-                            sum += n * (h ? 128 : 8);
-                            x[j] = (uint32_t)n + 0x00808080u;    // bytes 0 .. 255 for digits -128 .. 127
-                        }
+                        for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(fmaf(f[2 * j + h], h ? to * 0.0625f : to, kWholeAt));
+                        by_parity[h] += x[0] + x[1] + x[2] + x[3];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] += 0x00808080u - kWholeBits;    // bytes 0 .. 255 for digits -128 .. 127
                         qf[p][i][0][h] = (gather_byte<2>(x) ^ 0x80808080u) & own_group;
                         qf[p][i][1][h] = (gather_byte<1>(x) ^ 0x80808080u) & own_group;
                         qf[p][i][2][h] = (gather_byte<0>(x) ^ 0x80808080u) & own_group;
                     }
                 }
+                int sum = (int)(8u * (by_parity[0] - 8u * kWholeBits) + 128u * (by_parity[1] - 8u * kWholeBits));
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);      // the two lanes of a group
                 const int other = __shfl_xor_sync(0xffffffffu, sum, 2);
                 q_off[p][0] = c < 2 ? sum : other;
