@@ -9,15 +9,16 @@
 // what 16-bit floats would take; unpacking to those also takes seven integer instructions for eight values instead of two).
 // The other operand becomes whole numbers cut into bytes, and the sums are exact:
 //   scores:  A = codes of 16 rows x 32 dimensions; B = the query, times a power of two that brings its largest value to 2^21 .. 2^22 (odd
-//            dimensions to 2^17 .. 2^18: half a step of the rounding is 2^-18 of the largest value at most), as three signed bytes.  One byte of
-//            all of them after the other is multiplied into the same sums, which are shifted in between.  A column has the values of one
-//            group only and zeros elsewhere; columns alternate between the two groups of 64 dimensions, so that all four lanes that share
-//            a row hold its two sums, and lane c of them goes on with tile c of a chunk.
+//            dimensions to 2^17 .. 2^18: half a step of the rounding is 2^-18 of the largest value at most), as three signed bytes, of which each has
+//            two columns: the values of one group of a plane and zeros elsewhere, and the other's.  The lanes that share a row then hold
+//            the sums of one byte each; two exchanges between them, with shifts, give lane c the whole sums of tile c of a unit.
+//            (Every byte in every column, one after the other into the same sums, needs no exchange but three times the products: 128 us where
+//            this takes 121 over 24 x 16 items of 12001 to 16000 rows of 128, at the clock that the power limit leaves.)
 //   output:  A = codes of V transposed, 16 dimensions x 32 rows; B = the weights p t of a group as whole numbers of 32 bits, times a power
 //            of two that has the largest of them so far at 2^28 .. 2^32 (so that the rounding, 2^-29 of the largest, does not add up over a
 //            million rows), a byte in each of four columns (2 groups x 4 bytes).  Sums are kept as 32-bit whole numbers until what they are
 //            relative to changes.
-// Products of the same bytes with rows of eights give what the offsets of the codes of V add; for K a sum over the query does.
+// Products of the same bytes with rows of eights give what the offsets of the codes add.
 //
 // As in the streaming kernel of the bf16 cache: one persistent CTA per SM, every warp on its own with a ring of chunks (64 or 128
 // rows, one bulk copy: tiles hold K and V), work items (sequence, head, part of the rows), partial results joined by the part that ends
@@ -73,11 +74,11 @@ __device__ __forceinline__ void mma_signed(int (&d)[4], uint32_t a0, uint32_t a1
                  : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_signed_new(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma_signed_from(int (&d)[4], int even, int odd, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-                 : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(0));
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(even), "r"(odd));
 }
 __device__ __forceinline__ void mma_unsigned(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -99,12 +100,13 @@ __device__ __forceinline__ uint32_t whole(float x)
     asm("cvt.rni.u32.f32 %0, %1;" : "=r"(w) : "f"(x));
     return w;
 }
-// byte B of four words
-template <int B>
-__device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4])
+// a byte of each of four words
+__device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4], int byte)
 {
-    return __byte_perm(__byte_perm(w[0], w[1], B | (4 + B) << 4), __byte_perm(w[2], w[3], B | (4 + B) << 4), 0x5410);
+    const uint32_t pick = byte | (4 + byte) << 4;
+    return __byte_perm(__byte_perm(w[0], w[1], pick), __byte_perm(w[2], w[3], pick), 0x5410);
 }
+constexpr uint32_t kEightsEven = 0x08080808u, kEightsOdd = 0x80808080u;   // what even_codes and odd_codes give for codes of 0
 constexpr float kWholeAt = 12582912.f;   // 1.5 * 2^23
 constexpr uint32_t kWholeBits = 0x4B400000u;
 constexpr int kUnitsPerSum = 512;        // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
@@ -156,6 +158,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, c = lane & 3;   // row and column of a fragment
+    const int own_by_2 = c & 2 ? 65536 : 1, got_by_2 = c & 2 ? 1 : 65536, own_by_1 = c & 1 ? 256 : 1, got_by_1 = c & 1 ? 1 : 256;   // byte c of a sum
     const int n_warps = blockDim.x >> 5;
     const uint32_t ring0 = smem_u32(smem) + warp * (STAGES * G::STAGE);
     const uint32_t wbuf = smem_u32(smem) + n_warps * (STAGES * G::STAGE) + warp * G::WEIGHTS;
@@ -247,11 +250,11 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
             asm volatile("and.b32 %0, %1, 0;\n\tadd.s32 %0, %0, 1;" : "=r"(one) : "r"(w.n));
             seq_arrival = atomicAdd(a.counters + (size_t)a.B * a.H + w.b, one);
         }
-        // Query fragments: lane c holds dimensions 16 c .. 16 c + 15 of a plane, in the order of the codes of two words; in the
-        // columns of the other group it holds zeros.
-        uint32_t qf[PLANES][2][3][2];      // word, byte (highest first), even | odd dimensions
-        int q_off[PLANES][2];              // what the eights of a group's codes add to its sum
-        float q_unit;                      // what a sum has to be multiplied with
+        // Query fragments: lane (g, c) holds, of dimensions 16 c .. 16 c + 15 of a plane in the order of the codes of two words, byte g >> 1 for
+        // the column of group g & 1: zeros where the dimensions are the other group's, and in the two columns that are left.
+        uint32_t qf[PLANES][2][2];         // word, even | odd dimensions
+        int q_from[PLANES][2];             // what the sums of a byte of a group (columns 2 c, 2 c + 1) start from, so that the codes' eights are taken out
+        float q_unit;                      // what a whole sum has to be multiplied with
         {
             uint32_t top = 0;
 #pragma unroll
@@ -262,33 +265,28 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
             const float to = power_to<21>(__uint_as_float(top << 16));
             // a query with a value that is not finite gives NaN throughout
             q_unit = top < 0x7f80u ? inverse_power(to) : __uint_as_float(0x7fffffffu);
-            const uint32_t own_group = (g & 1) == (c >> 1) ? 0xffffffffu : 0u;
+            const uint32_t own = (g & 1) == (c >> 1) && g < 6 ? 0xffffffffu : 0u;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
-                // Adding 1.5 * 2^23 rounds to whole numbers and leaves them in the low bits: kWholeBits + n.
-                uint32_t by_parity[2] = {0u, 0u};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     float f[8];
                     unpack8(q_next[p][i], f);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
+                        // Adding 1.5 * 2^23 rounds to whole numbers and leaves them in the low bits: kWholeBits + n.  Bytes 0 .. 255 then stand
+                        // for digits -128 .. 127.
                         uint32_t x[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(fmaf(f[2 * j + h], h ? to * 0.0625f : to, kWholeAt));
-                        by_parity[h] += x[0] + x[1] + x[2] + x[3];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] += 0x00808080u - kWholeBits;    // bytes 0 .. 255 for digits -128 .. 127
-                        qf[p][i][0][h] = (gather_byte<2>(x) ^ 0x80808080u) & own_group;
-                        qf[p][i][1][h] = (gather_byte<1>(x) ^ 0x80808080u) & own_group;
-                        qf[p][i][2][h] = (gather_byte<0>(x) ^ 0x80808080u) & own_group;
+                        for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(fmaf(f[2 * j + h], h ? to * 0.0625f : to, kWholeAt)) + (0x00808080u - kWholeBits);
+                        qf[p][i][h] = (gather_byte(x, g >> 1) ^ 0x80808080u) & own;
                     }
                 }
-                int sum = (int)(8u * (by_parity[0] - 8u * kWholeBits) + 128u * (by_parity[1] - 8u * kWholeBits));
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);      // the two lanes of a group
-                const int other = __shfl_xor_sync(0xffffffffu, sum, 2);
-                q_off[p][0] = c < 2 ? sum : other;
-                q_off[p][1] = c < 2 ? other : sum;
+                int off[4];
+                mma_signed_from(off, 0, 0, kEightsEven, kEightsEven, kEightsOdd, kEightsOdd, qf[p][0][0], qf[p][0][1]);
+                mma_signed(off, kEightsEven, kEightsEven, kEightsOdd, kEightsOdd, qf[p][1][0], qf[p][1][1]);
+                q_from[p][0] = -off[0];
+                q_from[p][1] = -off[1];
             }
         }
         if (item + stride < n_items) fetch_q(divide(item + stride, a.by_splits));
@@ -347,21 +345,26 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                         const uint4 x = lds128(tile0 + k * G::TILE + p * kTileBytes + lane * 16);   // two words of the even row, two of the odd
                         const uint32_t a0 = even_codes(x.x), a1 = even_codes(x.z), a2 = odd_codes(x.x), a3 = odd_codes(x.z);
                         const uint32_t b0 = even_codes(x.y), b1 = even_codes(x.w), b2 = odd_codes(x.y), b3 = odd_codes(x.w);
-                        mma_signed_new(acc[k], a0, a1, a2, a3, qf[p][0][0][0], qf[p][0][0][1]);
-                        mma_signed(acc[k], b0, b1, b2, b3, qf[p][1][0][0], qf[p][1][0][1]);
-#pragma unroll
-                        for (int byte = 1; byte < 3; ++byte) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[k][i] *= 256;
-                            mma_signed(acc[k], a0, a1, a2, a3, qf[p][0][byte][0], qf[p][0][byte][1]);
-                            mma_signed(acc[k], b0, b1, b2, b3, qf[p][1][byte][0], qf[p][1][byte][1]);
-                        }
+                        mma_signed_from(acc[k], q_from[p][0], q_from[p][1], a0, a1, a2, a3, qf[p][0][0], qf[p][0][1]);
+                        mma_signed(acc[k], b0, b1, b2, b3, qf[p][1][0], qf[p][1][1]);
                     }
+                    // Lane c has byte c of all tiles' sums (lane 3: zeros) and needs all bytes of tile c's: tiles are exchanged with lane c ^ 2,
+                    // two bytes away, then with lane c ^ 1.
+                    int two[2][4];
                     float mine[4];
 #pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int keep = c & 2 ? acc[2 + k][i] : acc[k][i];
+                            const int got = __shfl_xor_sync(0xffffffffu, c & 2 ? acc[k][i] : acc[2 + k][i], 2);
+                            two[k][i] = keep * own_by_2 + got * got_by_2;
+                        }
+#pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int lo = c & 1 ? acc[1][i] : acc[0][i], hi = c & 1 ? acc[3][i] : acc[2][i];
-                        mine[i] = (float)((c & 2 ? hi : lo) - q_off[p][i & 1]);
+                        const int keep = c & 1 ? two[1][i] : two[0][i];
+                        const int got = __shfl_xor_sync(0xffffffffu, c & 1 ? two[0][i] : two[1][i], 1);
+                        mine[i] = (float)(keep * own_by_1 + got * got_by_1);
                     }
                     uint32_t k0, k1;
                     lds64(own_tile + u * (kUnitTiles * G::TILE) + p * kTileBytes + kStepsAt, k0, k1);
@@ -458,7 +461,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                         mma_unsigned(sums[p][1], even_codes(x.y), odd_codes(x.y), even_codes(y.y), odd_codes(y.y), b0, b1);
                         mma_unsigned(sums[p][2], even_codes(x.z), odd_codes(x.z), even_codes(y.z), odd_codes(y.z), b0, b1);
                         mma_unsigned(sums[p][3], even_codes(x.w), odd_codes(x.w), even_codes(y.w), odd_codes(y.w), b0, b1);
-                        mma_unsigned(eights[p], 0x08080808u, 0x80808080u, 0x08080808u, 0x80808080u, b0, b1);
+                        mma_unsigned(eights[p], kEightsEven, kEightsOdd, kEightsEven, kEightsOdd, b0, b1);
                     }
                 }
             }
