@@ -712,17 +712,20 @@ bt_status bt_block_kv4_read(const bt_config* cfg, const bt_block_cache_kv4* cach
 
 // Ways the row range of a (sequence, head) is cut: enough parts for the kernel's warps (eight on each of 148 SMs; the number
 // fixes the workspace, so it does not depend on the device), each of at least 128 rows, or of 64 while the parts are so few that
-// they are joined in one go (32 pairs of 300 to 512 rows of 64: 5.4 us in eight parts, 6.0 in four; 16 pairs of 4096: 7.8 us in 64
-// parts, 7.0 in 32).
+// they are joined in one go (32 pairs of 300 to 512 rows of 64: 5.2 us in eight parts, 5.5 in four; 16 pairs of 4096: 7.6 us in 64
+// parts, 6.2 in 32).  Joining costs 3 us, as long as a warp takes for seven times 64 rows at head_dim 64 and for five times at 128: where
+// cutting does not save a warp as many, nothing is cut (512 pairs of 512 rows of 64: 6.1 us, in two parts 8.1; 64 pairs of 200 to 256:
+// 4.0 us, in four 5.3; 256 pairs of 1500 to 2048, which gain: 16.5 us, in four 10.8).
 static int kv4_splits(const bt_config* cfg)
 {
     if (cfg->decode_splits > 0) return cfg->decode_splits;
     long long s = 8 * 148 / ((long long)cfg->batch * cfg->heads);
-    const long long few = cfg->max_blocks / 64 < 16 ? cfg->max_blocks / 64 : 16;
-    const long long most = cfg->max_blocks / 128 > few ? cfg->max_blocks / 128 : few;
+    const long long units = cfg->max_blocks / 64;
+    const long long few = units < 16 ? units : 16;
+    const long long most = units / 2 > few ? units / 2 : few;
     if (s > most) s = most;
     if (s > 64) s = 64;
-    return s < 1 ? 1 : (int)s;
+    return s < 1 || units * (s - 1) < (cfg->head_dim == 64 ? 7 : 5) * s ? 1 : (int)s;
 }
 
 size_t bt_workspace_bytes_kv4(const bt_config* cfg)

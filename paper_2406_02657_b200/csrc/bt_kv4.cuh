@@ -9,10 +9,8 @@
 // half exactly away from zero, without a division for each value.
 //
 // A tile is 16 rows of 64 dimensions of K and of V, 1152 contiguous bytes (nine 128-byte lines, so a range of rows is one
-// bulk copy).  A byte holds dimension 2i in its low half and 2i + 1 in its high half, as u + 8 (1 .. 15): such a number in a byte of its
-// own is also an 8-bit float with four exponent bits, of value (u + 8) 2^-9, so that the attention feeds codes to the tensor cores
-// after one mask (low halves) or a shift and a mask (high halves) for four of them.  Bytes lie where the attention's matrix
-// fragments want them:
+// bulk copy).  A byte holds dimension 2i in its low half and 2i + 1 in its high half, as u + 8 (1 .. 15), so that one mask gives the attention
+// four codes as bytes.  Bytes lie where its matrix fragments want them:
 //   bytes    0 ..  511   K: two rows together, 16 dimensions of the even row, the same of the odd one, and so on
 //   bytes  512 .. 1023   V: four rows together, their bytes of two dimensions side by side; the eight 16-byte units of a row quad q (eight
 //                        dimensions each) in the order unit ^ 2q, which spreads the four quads over the shared-memory banks

@@ -13,7 +13,7 @@
 //            two columns: the values of one group of a plane and zeros elsewhere, and the other's.  The lanes that share a row then hold
 //            the sums of one byte each; two exchanges between them, with shifts, give lane c the whole sums of tile c of a unit.
 //            (Every byte in every column, one after the other into the same sums, needs no exchange but three times the products: 128 us where
-//            this takes 121 over 24 x 16 items of 12001 to 16000 rows of 128, at the clock that the power limit leaves.)
+//            this takes 118 over 24 x 16 items of 12001 to 16000 rows of 128, at the clock that the power limit leaves.)
 //   output:  A = codes of V transposed, 16 dimensions x 32 rows; B = the weights p t of a group as whole numbers of 32 bits, times a power
 //            of two that has the largest of them so far at 2^28 .. 2^32 (so that the rounding, 2^-29 of the largest, does not add up over a
 //            million rows), a byte in each of four columns (2 groups x 4 bytes).  Sums are kept as 32-bit whole numbers until what they are
@@ -664,8 +664,8 @@ cudaError_t launch_block_decode_kv4(const Kv4DecodeArgs& a, cudaStream_t stream)
     if (a.hd == 128) return kv4::launch_t<128, 1, 2, 8>(a, dev, sms, stream);
     // Head_dim 64: with at most eight items an SM, a warp each and chunks of two units; with more, 16 warps an SM (126 registers a thread),
     // of which each spends half as long on an item's beginning and end.  us, 16 warps / eight:
-    //   items of 48 to 64 rows:     1024: 3.6 / 3.6,  1536: 4.1 / 5.7,  4096: 8.1 / 10.3
-    //   items of 384 to 512 rows:   1024: 10.4 / 8.7, 1536: 12.3 / 14.6, 4096: 25.8 / 27.1
+    //   items of 48 to 64 rows:     1024: 3.5 / 3.5,  1536: 3.8 / 5.3,   4096: 7.1 / 9.5
+    //   items of 384 to 512 rows:   1024: 9.2 / 8.3,  1536: 11.0 / 13.9, 4096: 23.5 / 26.5
     if ((long long)a.B * a.H * a.splits > 8LL * sms) return kv4::launch_t<64, 1, 2, 16>(a, dev, sms, stream);
     return kv4::launch_t<64, 2, 2, 8>(a, dev, sms, stream);
 }
