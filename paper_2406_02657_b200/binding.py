@@ -151,9 +151,10 @@ def _stream(stream):
 def _stream_of(t, stream):
     """The stream for a call over `t`, which has to be on the current device: the kernels run there, and would read another's memory, or
     the host's, as their own."""
-    if t.get_device() < 0 or t.get_device() != _device():
+    device = t.get_device()
+    if device < 0 or device != _device():
         raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {t.device}, not on the current device")
-    return _stream(stream)
+    return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(device)
 
 
 def _check(code: int, where: str):
@@ -436,16 +437,18 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
                         stream=None):
     """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
     slabs of k_new, v_new (a bf16 block cache has N_max)."""
-    n_new = k_new.shape[2] if n_new is None else n_new
-    src_stride = k_new.shape[2] if src_stride is None else src_stride
+    if n_new is None or src_stride is None:
+        rows = k_new.shape[2]
+        n_new, src_stride = rows if n_new is None else n_new, rows if src_stride is None else src_stride
     _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(k_new), _ptr(v_new), _i32(n_new), src_stride,
                                     1 if reset_first else 0, _ptr(dev_status), _stream_of(k_new, stream)), "bt_block_kv4_append")
 
 
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
     """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
-    n_rows = k_out.shape[2] if n_rows is None else n_rows
-    dst_stride = k_out.shape[2] if dst_stride is None else dst_stride
+    if n_rows is None or dst_stride is None:
+        rows = k_out.shape[2]
+        n_rows, dst_stride = rows if n_rows is None else n_rows, rows if dst_stride is None else dst_stride
     _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _i32(first), _i32(n_rows), _ptr(k_out), _ptr(v_out),
                                   dst_stride, _stream_of(k_out, stream)), "bt_block_kv4_read")
 
