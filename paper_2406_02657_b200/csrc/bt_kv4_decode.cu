@@ -60,8 +60,6 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
     return x;
 }
-__device__ __forceinline__ void sts32(uint32_t addr, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(x) : "memory"); }
-
 __device__ __forceinline__ void sts16(uint32_t addr, uint32_t x) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"((uint16_t)x) : "memory"); }
 
 // four codes of a word as bytes: u + 8 of the even dimensions, 16 (u + 8) of the odd ones
@@ -368,13 +366,14 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                     }
                     uint32_t k0, k1;
                     lds64(own_tile + u * (kUnitTiles * G::TILE) + p * kTileBytes + kStepsAt, k0, k1);
-                    s[u][0] = fmaf(mine[1], bf_hi(k0), fmaf(mine[0], bf_lo(k0), s[u][0]));
-                    s[u][1] = fmaf(mine[3], bf_hi(k1), fmaf(mine[2], bf_lo(k1), s[u][1]));
+                    // (the query's power of two goes to the step, so that nothing between is larger than the products themselves)
+                    s[u][0] = fmaf(mine[1], bf_hi(k0) * q_unit, fmaf(mine[0], bf_lo(k0) * q_unit, s[u][0]));
+                    s[u][1] = fmaf(mine[3], bf_hi(k1) * q_unit, fmaf(mine[2], bf_lo(k1) * q_unit, s[u][1]));
                 }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     in[u][r] = u * kUnitRows + 16 * c + 2 * g + r < nvalid;
-                    s[u][r] = in[u][r] ? s[u][r] * q_unit * a.scale_log2 : kNegInf;
+                    s[u][r] = in[u][r] ? s[u][r] * a.scale_log2 : kNegInf;
                     top = fmaxf(top, s[u][r]);
                 }
                 // steps of V of the two rows; a row that is not there has no weight whatever its step is

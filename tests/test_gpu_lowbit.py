@@ -266,6 +266,21 @@ def test_rows_of_unlike_size(bt, hd, splits):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("up", [-100, 100])
+def test_queries_and_keys_of_unlike_size(bt, hd, up):
+    """Products of ordinary size of a tiny query and huge keys, and the other way round."""
+    B, H, N = 2, 2, 90
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
+    q, k, v = f64(rnd(19, 3, (B, H, hd))) * 2.0 ** -up, f64(rnd(19, 1, (B, H, N, hd))) * 2.0 ** up, rnd(19, 2, (B, H, N, hd))
+    q, k = bits(q), bits(k)
+    cache = filled(bt, cfg, k, v, [N, 41])
+    out, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), bt.alloc_workspace_kv4(cfg)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, to_dev(q), out, ws)
+    ref, tol = lb.decode(f64(q), lb.held(f64(k)), lb.held(f64(v)), [N, 41])
+    check(out, ref, tol, "unlike query and keys")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("splits", [1, 4])
 def test_values_that_are_not_finite(bt, hd, splits):
     B, H, N = 6, 2, 200
