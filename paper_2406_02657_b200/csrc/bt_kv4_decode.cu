@@ -520,15 +520,16 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         // Lane (g, c) holds dimensions 8 g .. 8 g + 7 of a plane under two bytes of the weights of group c >> 1: the low ones in lanes of even c,
         // the high ones in those of odd c.  They count where that is the dimensions' group, and are added up here.
         const bool own_piece = c == 2 * (g >> 2);
-        const float high = c & 1 ? 65536.f : 1.f;
-        const float unit = inverse_power(w_to) * inverse_sum(l);
+        // (The sum of the weights divides first: with the weights' power of two it could leave the normal numbers.)
+        const float share = (c & 1 ? 65536.f : 1.f) * inverse_sum(l);
+        const float unit = inverse_power(w_to);
         auto piece = [&](int p, float (&f)[8]) {
             const bool bad0 = __any_sync(0xffffffffu, bad[p][0] != 0.f), bad1 = __any_sync(0xffffffffu, bad[p][1] != 0.f);
             const float u = (g < 4 ? bad0 : bad1) ? __uint_as_float(0x7fffffffu) : unit;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                f[2 * r] = o[p][r][0] * high;
-                f[2 * r + 1] = o[p][r][1] * (high * 0.0625f);
+                f[2 * r] = o[p][r][0] * share;
+                f[2 * r + 1] = o[p][r][1] * (share * 0.0625f);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = (f[i] + __shfl_xor_sync(0xffffffffu, f[i], 1)) * u;

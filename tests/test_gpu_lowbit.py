@@ -281,6 +281,23 @@ def test_queries_and_keys_of_unlike_size(bt, hd, up):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+def test_small_values_over_many_rows(bt, hd):
+    """Values near 2^-97 under 409200 equal weights: the weights' power of two is at its end there, and with the sum of the weights it would
+    be 20.5 times the least number of fp32.  Exact here: all rows are alike, so an output is its value."""
+    n = 409200
+    cfg = bt.make_config(1, 1, hd, 4, 1, n, 1, decode_splits=1)
+    value = np.ldexp(np.tile(np.arange(-7.0, 8.0), hd)[:hd], -100)
+    value[::32] = np.ldexp(7.0, -100)     # the step is 2^-100
+    row = torch.from_numpy(value).to("cuda", torch.bfloat16)
+    rows = row.expand(1, 1, n, hd).contiguous()
+    cache, q, out = empty_cache(bt, cfg), torch.zeros((1, 1, hd), dtype=torch.bfloat16, device="cuda"), torch.empty((1, 1, hd), dtype=torch.bfloat16, device="cuda")
+    bt.bt_block_kv4_append(cfg, cache, 0, rows, rows)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, q, out, bt.alloc_workspace_kv4(cfg))
+    # sums in fp32, flushed n / 64 / 512 = 13 times with four roundings of 2^-24 each, far below the half step of the result, 2^-8
+    check(out, value[None, None], 1.01 * 2.0 ** -8 * np.abs(value), "out")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("splits", [1, 4])
 def test_values_that_are_not_finite(bt, hd, splits):
     B, H, N = 6, 2, 200
@@ -561,6 +578,77 @@ def test_generation_in_few_bits(bt, hd, H):
             # against the rows as read back, whose rounding to bf16 moves scores and values by 2^-8 at most
             ref, tol = lb.decode(to_f64(bufs["q"][layer][:, :, 0]), K[layer], V[layer], [n] * B)
             check(bufs["o"][layer], ref, tol + 0.02 + 0.02 * np.abs(ref), f"step {i} layer {layer}")
+
+
+def test_strided_rows(bt):
+    """Views of larger slabs are taken as they lie (append) and written as they lie (read); what no slab stride says is refused."""
+    hd, N, n = 64, 40, 21
+    for B, H in ((3, 4), (1, 4), (3, 1), (1, 1)):
+        cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
+        K, V = to_dev(rnd(71, 1, (B, H, N, hd))), to_dev(rnd(71, 2, (B, H, N, hd)))
+        a, b = empty_cache(bt, cfg), empty_cache(bt, cfg)
+        bt.bt_block_kv4_append(cfg, a, 0, K[:, :, 5:5 + n], V[:, :, 7:7 + n], reset_first=True)
+        bt.bt_block_kv4_append(cfg, b, 0, K[:, :, 5:5 + n].contiguous(), V[:, :, 7:7 + n].contiguous(), reset_first=True)
+        assert torch.equal(a.kv, b.kv) and torch.equal(a.len, b.len)
+        packed = [torch.empty((B, H, n, hd), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        wide = [torch.full((B, H, N, hd), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        bt.bt_block_kv4_read(cfg, a, 0, *packed)
+        bt.bt_block_kv4_read(cfg, a, 0, *[x[:, :, 3:3 + n] for x in wide])
+        for x, y in zip(packed, wide):
+            assert torch.equal(x, y[:, :, 3:3 + n]) and (y[:, :, :3] == 9).all() and (y[:, :, 3 + n:] == 9).all()
+    cfg = bt.make_config(3, 4, hd, 4, 1, N, 1)
+    K = to_dev(rnd(71, 3, (3, 4, N, hd)))
+    cache = empty_cache(bt, cfg)
+    by_row = K.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)[:, :, :n]   # [B][n][H][hd] in memory
+    for k, v in ((by_row, by_row), (K[:, :, ::2], K[:, :, ::2]), (K[:, :, :n], K[:, :, :n].contiguous()), (K[:, :2, :n], K[:, :2, :n]),
+                 (K[:, :1, :n].expand(3, 4, n, hd), K[:, :, :n])):
+        with pytest.raises(bt.BtError) as e:
+            bt.bt_block_kv4_append(cfg, cache, 0, k, v)
+        assert e.value.code == bt.BT_ERR_UNSUPPORTED
+    torch.cuda.synchronize()
+    assert (cache.len == 0).all()
+
+
+def test_tensors_elsewhere_and_not_packed_are_refused(bt):
+    """Each tensor of a call in turn in the host's memory, or with strides: refused before anything is launched."""
+    B, H, hd, N = 2, 2, 64, 8
+    cfg, D = bt.make_config(B, H, hd, 4, 1, N, 1), H * hd
+    cache, block, local, ws = bt.BlockCacheKV4(cfg), bt.BlockCache(cfg), bt.LocalCache(cfg), bt.alloc_workspace_kv4(cfg)
+
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.zeros(shape, dtype=dtype, device="cuda")
+
+    q, x, w, bias, qo = t(B, H, hd), t(B, 1, D), t(3 * D, D), t(3 * D), t(B, H, 1, hd)
+    x8, w8, xs, wsteps = t(B, 1, D, dtype=torch.int8), t(3 * D, D, dtype=torch.int8), t(B, 1, dtype=torch.float32), t(3 * D, dtype=torch.float32)
+    status, mask = t(1, dtype=torch.int32), t(B, dtype=torch.uint8)
+    calls = [
+        (lambda *a: bt.bt_block_decode_attn_kv4(cfg, cache, 0, *a), [q, q, ws, status]),
+        (lambda *a: bt.bt_block_decode_step_kv4(cfg, cache, 0, *a), [q, q, q, q, ws, status]),
+        (lambda a, b, c, d, s: bt.bt_block_qkv_project_append_kv4(cfg, cache, 0, a, b, c, d, dev_status=s), [x, w, bias, qo, status]),
+        (bt.bt_rows_quantize_i8, [x, x8, xs]),
+        (lambda *a: bt.bt_prefix_project_i8(cfg, *a), [x8, xs, w8[:D], wsteps[:D], bias[:D], x, status]),
+        (lambda *a: bt.bt_block_qkv_project_append_i8(cfg, block, 0, *a[:-1], dev_status=a[-1]), [x8, xs, w8, wsteps, bias, qo, status]),
+        (lambda *a: bt.bt_local_qkv_project_append_i8(cfg, local, 0, *a[:-2], reset_mask=a[-2], dev_status=a[-1]),
+         [x8, xs, w8, wsteps, bias, qo, mask, status]),
+        (lambda *a: bt.bt_block_qkv_project_append_i8_kv4(cfg, cache, 0, *a[:-1], dev_status=a[-1]), [x8, xs, w8, wsteps, bias, qo, status]),
+    ]
+    for call, args in calls:
+        for i, arg in enumerate(args):
+            bad = [arg.cpu()]
+            if arg.numel() > 1:
+                bad.append(torch.stack([arg, arg], -1)[..., 0])
+            for b in bad:
+                with pytest.raises(bt.BtError) as e:
+                    call(*args[:i], b, *args[i + 1:])
+                assert e.value.code == bt.BT_ERR_UNSUPPORTED
+    rows = t(B, H, 1, hd)
+    for call in (bt.bt_block_kv4_append, bt.bt_block_kv4_read):
+        for k, v in ((rows.cpu(), rows), (rows, rows.cpu())):
+            with pytest.raises(bt.BtError) as e:
+                call(cfg, cache, 0, k, v)
+            assert e.value.code == bt.BT_ERR_UNSUPPORTED
+    torch.cuda.synchronize()
+    assert (cache.len == 0).all() and (block.len == 0).all() and (local.len == 0).all()
 
 
 def test_other_streams_and_two_calls_at_once(bt):
