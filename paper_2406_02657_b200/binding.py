@@ -148,13 +148,37 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
-def _stream_of(t, stream):
-    """The stream for a call over `t`, which has to be on the current device: the kernels run there, and would read another's memory, or
-    the host's, as their own."""
-    device = t.get_device()
+def _stream_of(stream, cache, *tensors, packed=True):
+    """The stream for a call over these tensors (None: not given), the first of which is there, and a 4-bit cache or None.  They have to be on the
+    current device: the kernels run there, and would read another's memory, or the host's, as their own; and packed, as a call knows no strides."""
+    device = tensors[0].get_device()
     if device < 0 or device != _device():
-        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {t.device}, not on the current device")
-    return _stream(stream) if stream is not None or _raw_stream is None else _raw_stream(device)
+        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {tensors[0].device}, not on the current device")
+    if cache is not None and cache.device != device:
+        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {tensors[0].device}, cache on {cache.kv.device}")
+    for t in tensors:
+        if t is not None:
+            if t.get_device() != device:
+                raise BtError(BT_ERR_UNSUPPORTED, f"tensors on {tensors[0].device} and {t.device}")
+            if packed and not t.is_contiguous():
+                raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of strides {tuple(t.stride())} and shape {tuple(t.shape)}")
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
+
+
+def _slab_stride(k, v):
+    """Rows between the slabs of k, v [B,H,n,hd], which may be the first rows of larger slabs."""
+    if k.is_contiguous() and v.is_contiguous():
+        return k.shape[2]
+    found = []
+    for t in (k, v):
+        (B, H, n, hd), (by_b, by_h, by_n, by_d) = t.shape, t.stride()
+        slab = by_h if H > 1 else by_b if B > 1 else n * hd
+        if by_d != 1 or (n > 1 and by_n != hd) or slab % hd != 0 or (B > 1 and H > 1 and by_b != H * by_h):
+            raise BtError(BT_ERR_UNSUPPORTED, f"rows of strides {tuple(t.stride())} and shape {tuple(t.shape)}")
+        found.append(slab // hd)
+    if found[0] != found[1]:
+        raise BtError(BT_ERR_UNSUPPORTED, f"slabs of k every {found[0]} rows, of v every {found[1]}")
+    return found[0]
 
 
 def _check(code: int, where: str):
@@ -202,6 +226,8 @@ class BlockCacheKV4:
         self.kv = torch.zeros(shape, dtype=torch.uint8, device=device) if kv is None else kv
         self.len = torch.zeros((cfg.n_layers, cfg.batch), dtype=torch.int32, device=device) if length is None else length
         assert self.kv.shape == shape and self.kv.is_contiguous() and self.len.is_contiguous()
+        self.device = self.kv.get_device()
+        assert self.len.get_device() == self.device
         self.c = bt_block_cache_kv4(self.kv.data_ptr(), self.len.data_ptr())
 
 
@@ -436,61 +462,71 @@ def alloc_workspace_kv4(cfg, device="cuda"):
 def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=None, src_stride=None, reset_first=False, dev_status=None,
                         stream=None):
     """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
-    slabs of k_new, v_new (a bf16 block cache has N_max)."""
-    if n_new is None or src_stride is None:
-        rows = k_new.shape[2]
-        n_new, src_stride = rows if n_new is None else n_new, rows if src_stride is None else src_stride
+    slabs of k_new, v_new (a bf16 block cache has N_max), theirs where it is not given."""
+    if n_new is None:
+        n_new = k_new.shape[2]
+    if src_stride is None:
+        src_stride = _slab_stride(k_new, v_new)
+    on = _stream_of(stream, cache, k_new, v_new, dev_status, packed=False)
     _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(k_new), _ptr(v_new), _i32(n_new), src_stride,
-                                    1 if reset_first else 0, _ptr(dev_status), _stream_of(k_new, stream)), "bt_block_kv4_append")
+                                    1 if reset_first else 0, _ptr(dev_status), on), "bt_block_kv4_append")
 
 
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
     """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
-    if n_rows is None or dst_stride is None:
-        rows = k_out.shape[2]
-        n_rows, dst_stride = rows if n_rows is None else n_rows, rows if dst_stride is None else dst_stride
+    if n_rows is None:
+        n_rows = k_out.shape[2]
+    if dst_stride is None:
+        dst_stride = _slab_stride(k_out, v_out)
+    on = _stream_of(stream, cache, k_out, v_out, packed=False)
     _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _i32(first), _i32(n_rows), _ptr(k_out), _ptr(v_out),
-                                  dst_stride, _stream_of(k_out, stream)), "bt_block_kv4_read")
+                                  dst_stride, on), "bt_block_kv4_read")
 
 
 def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace, dev_status=None, stream=None):
     """Decode attention over the 4-bit cache."""
+    on = _stream_of(stream, cache, q, out, workspace, dev_status)
     _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(out), *_ws(workspace),
-                                         _ptr(dev_status), _stream_of(q, stream)), "bt_block_decode_attn_kv4")
+                                         _ptr(dev_status), on), "bt_block_decode_attn_kv4")
 
 
 def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, out, workspace, dev_status=None, stream=None):
     """Quantise and append the new block's row, then attend over the 4-bit cache including it, in one launch."""
+    on = _stream_of(stream, cache, q, k_new, v_new, out, workspace, dev_status)
     _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
-                                         *_ws(workspace), _ptr(dev_status), _stream_of(q, stream)), "bt_block_decode_step_kv4")
+                                         *_ws(workspace), _ptr(dev_status), on), "bt_block_decode_step_kv4")
 
 
 def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, bias, q_out, n_rows=None, dev_status=None, stream=None):
     """bt_block_qkv_project_append into the 4-bit cache."""
     n_rows = x.shape[1] if n_rows is None else n_rows
+    on = _stream_of(stream, cache, x, w_qkv, bias, q_out, dev_status)
     _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x), _i32(n_rows), _ptr(w_qkv), _ptr(bias),
-                                                _ptr(q_out), _ptr(dev_status), _stream_of(x, stream)), "bt_block_qkv_project_append_kv4")
+                                                _ptr(q_out), _ptr(dev_status), on), "bt_block_qkv_project_append_kv4")
 
 
 def bt_rows_quantize_i8(x, x8, steps, stream=None):
     """Rows of x bf16 [..., n_cols] -> int8 of the same shape and fp32 steps [...]."""
     n_cols = x.shape[-1]
-    _check(_lib.bt_rows_quantize_i8(_ptr(x), x.numel() // max(n_cols, 1), _i32(n_cols), _ptr(x8), _ptr(steps), _stream_of(x, stream)),
+    on = _stream_of(stream, None, x, x8, steps)
+    _check(_lib.bt_rows_quantize_i8(_ptr(x), x.numel() // max(n_cols, 1), _i32(n_cols), _ptr(x8), _ptr(steps), on),
            "bt_rows_quantize_i8")
 
 
 def bt_prefix_project_i8(cfg, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status=None, stream=None):
     """bt_prefix_project of 8-bit operands and their steps."""
+    on = _stream_of(stream, None, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status)
     _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), _ptr(ctx8), _ptr(ctx_steps), _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(prefix_out),
-                                     _ptr(dev_status), _stream_of(ctx8, stream)), "bt_prefix_project_i8")
+                                     _ptr(dev_status), on), "bt_prefix_project_i8")
 
 
 def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
                                    stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
+    on = _stream_of(stream, None, x8, x_steps, w8, w_steps, bias, q_out, cache.k, cache.v, cache.len, dev_status)
     _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
-                                               _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream_of(x8, stream)),
+                                               _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), on),
            "bt_block_qkv_project_append_i8")
 
 
@@ -498,17 +534,19 @@ def bt_local_qkv_project_append_i8(cfg, cache: LocalCache, layer, x8, x_steps, w
                                    reset_mask=None, dev_status=None, stream=None):
     """bt_local_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
+    on = _stream_of(stream, None, x8, x_steps, w8, w_steps, bias, q_out, cache.kv, cache.len, reset_mask, dev_status)
     _check(_lib.bt_local_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
                                                _ptr(w_steps), _ptr(bias), 1 if reset_first else 0, _ptr(reset_mask), _ptr(q_out),
-                                               _ptr(dev_status), _stream_of(x8, stream)), "bt_local_qkv_project_append_i8")
+                                               _ptr(dev_status), on), "bt_local_qkv_project_append_i8")
 
 
 def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
                                        stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps into the 4-bit cache."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
+    on = _stream_of(stream, cache, x8, x_steps, w8, w_steps, bias, q_out, dev_status)
     _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows),
-                                                   _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), _stream_of(x8, stream)),
+                                                   _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), on),
            "bt_block_qkv_project_append_i8_kv4")
 
 
