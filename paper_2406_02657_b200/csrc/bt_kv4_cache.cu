@@ -12,6 +12,7 @@ namespace bt {
 namespace kv4 {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kFusedWarps = 16;   // at most: a warp for every tile of a sequence
 
 struct Params : Kv4Args {
     int tiles, planes, items;   // tiles of a slab that the call may touch; all the call's
@@ -110,22 +111,21 @@ __device__ __forceinline__ void write_tile(const Params& a, const Item& it, int 
 // FUSED: CTA = sequence, which raises its own length; else any warp takes any tile, and the length is raised by a launch behind
 // this one - or by this one, when the rows start anew and no warp looks at the old length.
 template <bool FUSED>
-__global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_constant__ Params a)
+__global__ void __launch_bounds__(FUSED ? kFusedWarps * 32 : kThreads) kv4_append_kernel(const __grid_constant__ Params a)
 {
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    if constexpr (FUSED) {   // items: those of one sequence
+    if constexpr (FUSED) {   // items: those of one sequence, one for each warp
         const int b = blockIdx.x;
         const int start = a.len[b];
         const bool ok = start >= 0 && start <= a.cap - a.n_rows;
         __syncthreads();
-        if (ok)
-            for (int i = warp; i < a.items; i += kWarps) {
-                Item it = item_at(i, a);
-                it.slab += b * a.H;
-                write_tile(a, it, start, lane);
-            }
+        if (ok) {
+            Item it = item_at(warp, a);
+            it.slab += b * a.H;
+            write_tile(a, it, start, lane);
+        }
         if (threadIdx.x == 0) {
             if (ok) a.len[b] = start + a.n_rows;
             else raise_status(a.dev_status, BT_DEV_OVERFLOW);
@@ -224,10 +224,15 @@ cudaError_t launch_kv4_append(const Kv4Args& a, cudaStream_t stream)
 {
     // rows that start inside a tile may reach into one more
     const long long tiles = ((long long)a.n_rows + (a.reset ? 1 : 2) * (kv4::kTileRows - 1)) / kv4::kTileRows;
-    const bool fused = !a.reset && a.H * tiles * (a.hd / 64) <= 8 * kv4::kWarps;
+    const long long each = a.H * tiles * (a.hd / 64);   // items of a sequence
+    // One launch where a CTA has a warp for every item of a sequence.  us, one launch / two:
+    //   one item a warp, a row of 16 heads of 64:     32 sequences: 2.8 / 3.1,   256: 4.1 / 4.9
+    //   two items a warp, a row of 16 heads of 128:   32 sequences: 4.4 / 3.1,   256: 6.8 / 7.1;   16 rows of 16 heads of 64, 64 sequences: 5.1 / 3.7
+    // (Eight CTAs, a cluster, a sequence: 6.5 us over 13 x 7 x 487 rows of 64, two launches 4.4.)
+    const bool fused = !a.reset && each <= kv4::kFusedWarps;
     kv4::Params p;
     if (!kv4::fill(p, a, tiles, fused ? a.H : (long long)a.B * a.H)) return cudaErrorInvalidConfiguration;
-    if (fused) return launch_pdl(kv4::kv4_append_kernel<true>, dim3(a.B), dim3(kv4::kThreads), 0, stream, p);
+    if (fused) return launch_pdl(kv4::kv4_append_kernel<true>, dim3(a.B), dim3((unsigned)each * 32), 0, stream, p);
     const cudaError_t e = launch_pdl(kv4::kv4_append_kernel<false>, kv4::grid_of(p), dim3(kv4::kThreads), 0, stream, p);
     if (e != cudaSuccess || a.reset) return e;
     return launch_pdl(kv4::kv4_len_kernel, dim3((a.B + 255) / 256), dim3(256), 0, stream, a.len, a.B, a.n_rows, a.cap, a.dev_status);
