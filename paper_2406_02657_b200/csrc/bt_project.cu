@@ -99,6 +99,10 @@ __device__ __forceinline__ void advance_len(int32_t* len, int b, int n, int cap,
         raise_status(dev_status, BT_DEV_OVERFLOW);  // the sequence keeps its rows and its length
 }
 
+// Every sequence starts with the call's rows, for which there is room: no tile looks at an old length, and the one with a sequence's first
+// row sets the new one, so that no launch has to follow.
+__host__ __device__ __forceinline__ bool starts_anew(const ProjectArgs& a) { return a.reset_first != 0 && a.reset_mask == nullptr; }
+
 // ---- the forms that differ between one CTA and a pair
 template <int kCtas>
 __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t cols)
@@ -391,6 +395,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
         const uint32_t patch = sPatch + warp * kPatchBytes;
         const bf16* bias = reinterpret_cast<const bf16*>(a.bias);
         const int D = a.H * a.hd;
+        const bool anew = !kKv4 && starts_anew(a);
         uint32_t t = 0;
         bool ok = true;
         pdl_wait();
@@ -412,6 +417,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     off_q = ((int64_t)row_b * a.H * a.n_rows + row_i) * a.hd;
                     const bool rst = a.reset_mask ? (a.reset_mask[row_b] != 0) : (a.reset_first != 0);
                     const int len_old = rst ? 0 : a.cache.len[row_b];
+                    if (anew && tn == 0 && half == 0 && row_i == 0) a.cache.len[row_b] = a.n_rows;
                     if (len_old >= 0 && len_old + a.n_rows <= a.cache.cap) {   // else: no room, K and V are dropped
                         row_rc = len_old + row_i;
                         off_c = (int64_t)row_b * a.H * a.cache.slab_stride +
@@ -449,7 +455,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 off = off < 0 ? -1 : off + add;
                 // + bias, -> bf16, into the patch: row `lane`, 16-byte piece q8 at (q8 ^ (lane & 7)) - or, bound for the 4-bit
                 // cache, back into registers
-                constexpr int kAtOnce = kKv4 ? 32 : 64;        // accumulators in registers (16 warps leave 112 registers a thread)
+                constexpr int kAtOnce = kKv4 ? 32 : 64;        // accumulators in registers (18 warps are five on one of an SM's four schedulers, which leaves 96 registers a thread)
                 uint32_t packed[32];                           // kKv4
 #pragma unroll
                 for (int c1 = 0; c1 < 64; c1 += kAtOnce) {
@@ -528,7 +534,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
     }
 }
 
-// The lengths go up once every tile has read the old ones: a second, tiny launch behind the product (it starts
+// The lengths go up once every tile has read the old ones (where it needs them): a second, tiny launch behind the product (it starts
 // under programmatic dependent launch while the product drains; counting the product's CTAs in on a word in
 // global memory and letting the last one advance the lengths was measured 2 us slower per step).
 __global__ void project_len_advance_kernel(int32_t* len, int B, int n, int cap, int reset_first, const uint8_t* reset_mask,
@@ -625,7 +631,7 @@ cudaError_t launch_project(const ProjectArgs& a, cudaStream_t stream)
         case 2: e = proj::launch_type<128, 1>(a, dev, sms, stream); break;
         default: e = proj::launch_type<64, 1>(a, dev, sms, stream); break;
     }
-    if (e != cudaSuccess || a.mode == kProjectPlain) return e;
+    if (e != cudaSuccess || a.mode == kProjectPlain || proj::starts_anew(a)) return e;
     const int B = a.M / a.n_rows;
     return launch_pdl(proj::project_len_advance_kernel, dim3((B + 255) / 256), dim3(256), 0, stream, a.cache.len, B, a.n_rows,
                       a.cache.cap, a.reset_first, a.reset_mask, a.dev_status);
