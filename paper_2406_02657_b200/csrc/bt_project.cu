@@ -187,7 +187,7 @@ __device__ __forceinline__ int64_t shfl64(int64_t x, int lane)
 constexpr int kCodeRow = 48;   // a row's 32 bytes of codes in the patch, 16 apart from the next so that the rows spread over the banks
 
 // K (part 0) or V (part 1) of a warp's rows into the 4-bit cache: 64 bf16 values of this lane's row in w; the row is row rc (-1: it
-// goes nowhere) of the slab whose tile with that row lies `off` bytes into the cache; quads: lanes whose four neighbours hold the four rows of a quad.
+// goes nowhere) of the slab whose tile with that row lies `off` bytes into the cache; quads: lanes that, with the three behind them, hold the four rows of a quad.
 __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (&w)[32], int64_t off, int rc, uint32_t quads, int part, uint32_t patch, int lane)
 {
     uint8_t* const cache = reinterpret_cast<uint8_t*>(a.cache.k);
@@ -213,10 +213,13 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
     if (rc >= 0) *reinterpret_cast<uint32_t*>(cache + off + kv4::kStepsAt + part * 64 + rc % kv4::kTileRows * 4) = steps;
     __syncwarp();
     const int j = lane >> 2, byte = lane & 3;
+    constexpr int64_t kOffset = ((int64_t)1 << 56) - 1;
+    const int64_t where = rc < 0 ? -1 : (int64_t)(rc % kv4::kTileRows) << 56 | off;   // row of the tile and where that lies
     auto quad = [&](int i) {   // rows i .. i + 3 of the warp: a quad of a tile, a word a lane
         const uint32_t rows = patch + i * kCodeRow;
-        const int at = __shfl_sync(0xffffffffu, rc, i) % kv4::kTileRows;
-        uint8_t* dst = cache + shfl64(off, i) + lane * 4;
+        const int64_t to = shfl64(where, i);
+        const int at = (int)(to >> 56);
+        uint8_t* dst = cache + (to & kOffset) + lane * 4;
         if (part == 0) {   // half a unit of one of the rows
             *reinterpret_cast<uint32_t*>(dst + kv4::k_codes_at(at, 0)) = lds32(rows + (lane >> 4 << 1 | (lane >> 1 & 1)) * kCodeRow + ((lane >> 2 & 3) * 2 + (lane & 1)) * 4);
         } else {           // one byte of each of the rows
@@ -226,26 +229,31 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
             *reinterpret_cast<uint32_t*>(dst + kv4::kPartBytes + (at >> 2) * 128) = __byte_perm(__byte_perm(x[0], x[1], pick), __byte_perm(x[2], x[3], pick), 0x5410);
         }
     };
-    if (quads == 0xffffffffu) {
+    if (quads == 0x11111111u) {
 #pragma unroll
         for (int i = 0; i < 32; i += 4) quad(i);
         return;
     }
+    const uint32_t done = quads * 15u;   // (no two start within four rows of each other)
+#pragma unroll 1
+    for (; quads; quads &= quads - 1) quad(__ffs(quads) - 1);
 #pragma unroll 1
     for (int i = 0; i < 32; i += 4) {
-        if ((quads >> i & 15u) == 15u) {
-            quad(i);
-            continue;
-        }
-        const uint32_t rows = patch + i * kCodeRow;
+        if ((done >> i & 15u) == 15u) continue;
+        // eight lanes a row, a word of its codes each
+        const int r = i + (lane >> 3), q = lane & 7;
+        const int64_t to = shfl64(where, r);
+        if (to >= 0 && !(done >> r & 1u)) {
+            const int at = (int)(to >> 56);
+            uint8_t* dst = cache + (to & kOffset);
+            const uint32_t codes = lds32(patch + r * kCodeRow + q * 4);
+            if (part == 0) {
+                *reinterpret_cast<uint32_t*>(dst + kv4::k_codes_at(at, q)) = codes;
+            } else {
+                dst += kv4::v_codes_at(at, q);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int at = __shfl_sync(0xffffffffu, rc, i + r);
-            uint8_t* dst = cache + shfl64(off, i + r);
-            if (at < 0) continue;
-            const uint32_t codes = lds32(rows + r * kCodeRow + j * 4);
-            if (part == 1) dst[kv4::v_codes_at(at % kv4::kTileRows, j) + 4 * byte] = (uint8_t)(codes >> (8 * byte));
-            else if (byte == 0) *reinterpret_cast<uint32_t*>(dst + kv4::k_codes_at(at % kv4::kTileRows, j)) = codes;
+                for (int b = 0; b < 4; ++b) dst[4 * b] = (uint8_t)(codes >> (8 * b));
+            }
         }
     }
 }
@@ -424,9 +432,9 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                                 (!kKv4 ? (int64_t)row_rc * a.cache.row_stride : (int64_t)(row_rc / kv4::kTileRows) * (a.hd / 64) * kv4::kTileBytes);
                     }
                 }
-                if constexpr (kKv4) {
-                    const int b0 = __shfl_sync(0xffffffffu, row_b, lane & 28), rc0 = __shfl_sync(0xffffffffu, row_rc, lane & 28);
-                    quads = __ballot_sync(0xffffffffu, row_rc >= 0 && row_b == b0 && row_rc == rc0 + (lane & 3) && (rc0 & 3) == 0);
+                if constexpr (kKv4) {   // rows of a sequence follow one another
+                    const int b3 = __shfl_down_sync(0xffffffffu, row_b, 3);
+                    quads = __ballot_sync(0xffffffffu, lane <= 28 && row_rc >= 0 && row_b == b3 && (row_rc & 3) == 0);
                 }
             }
             float x_step = 0.f;
