@@ -26,7 +26,8 @@
 // one MMA thread issues 256 x BN x 16 instructions that read both halves of W from the two CTAs' shared
 // memory and accumulate each CTA's 128 rows in that CTA's tensor memory; commits are multicast to both CTAs'
 // barriers; each CTA drains its own accumulator and reports to the leader.  Per CTA this moves a third less
-// operand data from L2 into shared memory for the same products.
+// operand data from L2 into shared memory for the same products.  Where few tiles are left for the last round, they are cut into
+// two or four parts along their output features, a part a pair.
 //
 // 8-bit operands (kInt8: a step per row of x and per output feature) run through the same stages and tiles: 128 bytes of a row are
 // 128 values of K instead of 64, an instruction takes 32 of them, and the sums are whole numbers (at most 2048 * 128 * 128 = 2^25,
@@ -78,7 +79,28 @@ struct Cfg {
 struct Params {
     ProjectArgs a;
     int tiles_m, tiles_n;
+    int whole, parts, items;   // tiles worked whole; parts that each of the others is cut into along its output features; both together
 };
+// Item i of a launch: rows of tile tm, `width` output features from `col`.
+struct Piece {
+    int tm, col, width;
+};
+template <int BN, int kCtas>
+__device__ __forceinline__ Piece piece_of(int i, const Params& p)
+{
+    Piece w;
+    int part = 0;
+    w.width = BN;
+    if (kCtas == 2 && i >= p.whole) {   // parts: 2 or 4
+        const int shift = p.parts >> 1, s = i - p.whole;
+        part = s & (p.parts - 1);
+        i = p.whole + (s >> shift);
+        w.width = BN >> shift;
+    }
+    w.tm = i / p.tiles_n;
+    w.col = (i - w.tm * p.tiles_n) * BN + part * w.width;
+    return w;
+}
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* dev_status)
 {
@@ -260,7 +282,7 @@ __device__ __forceinline__ void store_kv4(const ProjectArgs& a, const uint32_t (
 
 template <int BN, int kCtas, bool kInt8, bool kKv4>
 __global__ void __launch_bounds__(Cfg<BN, kCtas, kKv4>::kThreads, 1)
-project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, Params p)
+project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapPart, Params p)
 {
     using C = Cfg<BN, kCtas, kKv4>;
     constexpr int S = C::kStages, kEpilogueWarps = C::kEpilogueWarps, kProducerWarp = C::kProducerWarp, kMmaWarp = C::kMmaWarp;
@@ -309,7 +331,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
     // reads or writes global memory (the descriptor prefetch below touches only the kernel's own parameters).
     pdl_launch_dependents();
 
-    const int n_tiles = p.tiles_m * p.tiles_n;     // tiles of BM * kCtas rows
+    const int n_items = p.items;                   // tiles of BM * kCtas rows, or parts of them
     const int n_kb = (a.K + BK - 1) / BK;
 
     if (warp == kProducerWarp) {
@@ -319,8 +341,9 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
             pdl_wait();
             uint32_t it = 0;
             bool ok = true;
-            for (int tile = unit; ok && tile < n_tiles; tile += n_units) {
-                const int tm = tile / p.tiles_n, tn = tile - tm * p.tiles_n;
+            for (int item = unit; ok && item < n_items; item += n_units) {
+                const Piece w = piece_of<BN, kCtas>(item, p);
+                const CUtensorMap* const from = kCtas == 1 || w.width == BN ? &mapW : &mapPart;
                 for (int kb = 0; kb < n_kb; ++kb, ++it) {
                     const uint32_t s = it % S;
                     ok = wait(empty(s), ((it / S) & 1) ^ 1, abort_flag, a.dev_status);
@@ -328,14 +351,14 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     const uint32_t dst = base + s * C::kStageBytes;
                     if constexpr (kCtas == 1) {
                         mbar_expect_tx(full(s), C::kStageBytes);
-                        tma_load_3d(dst, &mapX, full(s), kb * BK, tm * BM, 0);
-                        tma_load_3d(dst + kABytes, &mapW, full(s), kb * BK, tn * BN, 0);
+                        tma_load_3d(dst, &mapX, full(s), kb * BK, w.tm * BM, 0);
+                        tma_load_3d(dst + kABytes, from, full(s), kb * BK, w.col, 0);
                     } else {
                         // both CTAs' bytes are counted on the leader's barrier, which the leader arms
-                        if (leader) mbar_expect_tx(full(s), 2 * C::kStageBytes);
+                        if (leader) mbar_expect_tx(full(s), 2 * kABytes + w.width * kRowBytes);
                         const uint32_t bar = full(s) & kPeerBitMask;
-                        tma_load_3d_pair(dst, &mapX, bar, kb * BK, tm * (2 * BM) + (int)rank * BM, 0);
-                        tma_load_3d_pair(dst + kABytes, &mapW, bar, kb * BK, tn * BN + (int)rank * (BN / 2), 0);
+                        tma_load_3d_pair(dst, &mapX, bar, kb * BK, w.tm * (2 * BM) + (int)rank * BM, 0);
+                        tma_load_3d_pair(dst + kABytes, from, bar, kb * BK, w.col + (int)rank * (w.width / 2), 0);
                     }
                 }
             }
@@ -359,8 +382,9 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
             auto wait_all = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity, abort_flag, a.dev_status)) != 0; };
             uint32_t it = 0, t = 0;
             bool ok = true;
-            for (int tile = unit; ok && tile < n_tiles; tile += n_units, ++t) {
+            for (int item = unit; ok && item < n_items; item += n_units, ++t) {
                 const uint32_t acc = t & 1;
+                const uint32_t idesc = kCtas == 1 ? IDESC : with_n(IDESC, piece_of<BN, kCtas>(item, p).width);
                 ok = wait_all(acc_empty(acc), ((t >> 1) & 1) ^ 1);  // the epilogue has drained this accumulator
                 if (!ok) break;
                 tc_fence_after();
@@ -378,10 +402,10 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                         for (int kk = 0; kk < kRowBytes / 32; ++kk) {
                             const uint64_t da = desc_words(alo + kk * 2, kDescHiSw128), db = desc_words(blo + kk * 2, kDescHiSw128);
                             const uint32_t more = (kb > 0 || kk > 0) ? 1u : 0u;
-                            if constexpr (kInt8 && kCtas == 1) mma_s8(tmem + acc * BN, da, db, IDESC, more);
-                            else if constexpr (kInt8) mma_s8_pair(tmem + acc * BN, da, db, IDESC, more);
-                            else if constexpr (kCtas == 1) mma_bf16(tmem + acc * BN, da, db, IDESC, more);
-                            else mma_bf16_pair(tmem + acc * BN, da, db, IDESC, more);
+                            if constexpr (kInt8 && kCtas == 1) mma_s8(tmem + acc * BN, da, db, idesc, more);
+                            else if constexpr (kInt8) mma_s8_pair(tmem + acc * BN, da, db, idesc, more);
+                            else if constexpr (kCtas == 1) mma_bf16(tmem + acc * BN, da, db, idesc, more);
+                            else mma_bf16_pair(tmem + acc * BN, da, db, idesc, more);
                         }
                         if constexpr (kCtas == 1) mma_commit(empty(s));
                         else mma_commit_pair(empty(s));
@@ -407,12 +431,12 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
         uint32_t t = 0;
         bool ok = true;
         pdl_wait();
-        for (int tile = unit; tile < n_tiles; tile += n_units, ++t) {
-            const int tm = tile / p.tiles_n, tn = tile - tm * p.tiles_n;
+        for (int item = unit; item < n_items; item += n_units, ++t) {
+            const Piece w = piece_of<BN, kCtas>(item, p);
             const uint32_t acc = t & 1;
             // This lane's own row: where it goes among the rows of Q (or of the plain output) and in the cache, without head and
             // dimension (elements; bytes in the 4-bit cache); -1: nowhere.
-            const int m = tm * (BM * kCtas) + (int)rank * BM + wq * 32 + lane;
+            const int m = w.tm * (BM * kCtas) + (int)rank * BM + wq * 32 + lane;
             int64_t off_q = -1, off_c = -1;
             int row_rc = -1;
             uint32_t quads = 0;
@@ -425,7 +449,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     off_q = ((int64_t)row_b * a.H * a.n_rows + row_i) * a.hd;
                     const bool rst = a.reset_mask ? (a.reset_mask[row_b] != 0) : (a.reset_first != 0);
                     const int len_old = rst ? 0 : a.cache.len[row_b];
-                    if (anew && tn == 0 && half == 0 && row_i == 0) a.cache.len[row_b] = a.n_rows;
+                    if (anew && w.col == 0 && half == 0 && row_i == 0) a.cache.len[row_b] = a.n_rows;
                     if (len_old >= 0 && len_old + a.n_rows <= a.cache.cap) {   // else: no room, K and V are dropped
                         row_rc = len_old + row_i;
                         off_c = (int64_t)row_b * a.H * a.cache.slab_stride +
@@ -445,8 +469,8 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
-            for (int c0 = half * 64; c0 < BN; c0 += kEpilogueWarps * 16) {
-                const int col0 = tn * BN + c0;                 // first output feature of this 64-column piece
+            for (int c0 = half * 64; c0 < (kCtas == 1 ? BN : w.width); c0 += kEpilogueWarps * 16) {
+                const int col0 = w.col + c0;                 // first output feature of this 64-column piece
                 if (col0 >= a.N) break;                        // warp-uniform
                 // Where the piece goes.  head_dim is a multiple of 64 and so is col0: the 64 columns lie inside one
                 // head of one of Q, K, V, so everything but the row is the same for the whole warp.
@@ -496,16 +520,16 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                                 for (int i = 0; i < 8; ++i) f[i] += bf[i];
                             }
                         }
-                        const uint4 w = pack8(f);
+                        const uint4 y = pack8(f);
                         if (to_kv4) {
-                            packed[q8 * 4] = w.x;
-                            packed[q8 * 4 + 1] = w.y;
-                            packed[q8 * 4 + 2] = w.z;
-                            packed[q8 * 4 + 3] = w.w;
+                            packed[q8 * 4] = y.x;
+                            packed[q8 * 4 + 1] = y.y;
+                            packed[q8 * 4 + 2] = y.z;
+                            packed[q8 * 4 + 3] = y.w;
                             continue;
                         }
                         const uint32_t dst = patch + lane * 128 + ((q8 ^ (lane & 7)) << 4);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
                     }
                 }
                 if (to_kv4) {
@@ -518,8 +542,8 @@ project_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     for (int itr = 0; itr < 8; ++itr) {
                         const int rr = itr * 4 + (lane >> 3), q8 = lane & 7;
                         const int64_t to = shfl64(off, rr);   // of that row; none where there is no room
-                        const uint4 w = lds128(patch + rr * 128 + ((q8 ^ (rr & 7)) << 4));
-                        if (to >= 0) *reinterpret_cast<uint4*>(base_out + to) = w;
+                        const uint4 y = lds128(patch + rr * 128 + ((q8 ^ (rr & 7)) << 4));
+                        if (to >= 0) *reinterpret_cast<uint4*>(base_out + to) = y;
                     }
                 }
                 __syncwarp();  // the patch is free for the next piece
@@ -555,18 +579,20 @@ __global__ void project_len_advance_kernel(int32_t* len, int B, int n, int cap, 
 }
 
 template <int BN, int kCtas, bool kInt8, bool kKv4>
-static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_t stream)
+static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, int parts, cudaStream_t stream)
 {
     using C = Cfg<BN, kCtas, kKv4>;
     static PerDeviceOnce limit_raised;
     cudaError_t e = raise_smem_limit_once(limit_raised, dev, project_tc_kernel<BN, kCtas, kInt8, kKv4>, C::kSmemBytes);
     if (e != cudaSuccess) return e;
-    CUtensorMap mx, mw;
-    if constexpr (kInt8) {
-        if (!make_byte_map(&mx, a.x, a.K, a.M, BM) || !make_byte_map(&mw, a.w, a.K, a.N, BN / kCtas)) return cudaErrorInvalidValue;
-    } else {
-        if (!make_slab_map(&mx, a.x, a.K, a.M, a.M, 1, BM) || !make_slab_map(&mw, a.w, a.K, a.N, a.N, 1, BN / kCtas)) return cudaErrorInvalidValue;
-    }
+    CUtensorMap mx, mw, mp;
+    auto map_rows = [&a](CUtensorMap* m, const void* ptr, long long rows, int box_rows) {
+        if constexpr (kInt8) return make_byte_map(m, ptr, a.K, rows, box_rows);
+        else return make_slab_map(m, ptr, a.K, rows, rows, 1, box_rows);
+    };
+    if (!map_rows(&mx, a.x, a.M, BM) || !map_rows(&mw, a.w, a.N, BN / kCtas)) return cudaErrorInvalidValue;
+    mp = mw;
+    if (parts > 1 && !map_rows(&mp, a.w, a.N, BN / kCtas / parts)) return cudaErrorInvalidValue;
     Params p;
     p.a = a;
     p.tiles_m = (a.M + BM * kCtas - 1) / (BM * kCtas);
@@ -574,7 +600,10 @@ static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_
     const long long tiles = (long long)p.tiles_m * p.tiles_n;
     if (tiles > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
     const int units = sms / kCtas;
-    const int grid = (int)(tiles < units ? tiles : units) * kCtas;
+    p.parts = parts;
+    p.whole = (int)(parts > 1 ? tiles / units * units : tiles);
+    p.items = p.whole + (int)(tiles - p.whole) * parts;
+    const int grid = (p.items < units ? p.items : units) * kCtas;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(C::kThreads);
@@ -589,14 +618,15 @@ static cudaError_t launch_bn(const ProjectArgs& a, int dev, int sms, cudaStream_
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = kCtas == 2 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, project_tc_kernel<BN, kCtas, kInt8, kKv4>, mx, mw, p);
+    return cudaLaunchKernelEx(&cfg, project_tc_kernel<BN, kCtas, kInt8, kKv4>, mx, mw, mp, p);
 }
 
 template <int BN, int kCtas>
-static cudaError_t launch_type(const ProjectArgs& a, int dev, int sms, cudaStream_t stream)
+static cudaError_t launch_type(const ProjectArgs& a, int dev, int sms, int parts, cudaStream_t stream)
 {
-    if (a.mode == kProjectQkvKv4) return a.x_steps ? launch_bn<BN, kCtas, true, true>(a, dev, sms, stream) : launch_bn<BN, kCtas, false, true>(a, dev, sms, stream);
-    return a.x_steps ? launch_bn<BN, kCtas, true, false>(a, dev, sms, stream) : launch_bn<BN, kCtas, false, false>(a, dev, sms, stream);
+    if (a.mode == kProjectQkvKv4)
+        return a.x_steps ? launch_bn<BN, kCtas, true, true>(a, dev, sms, parts, stream) : launch_bn<BN, kCtas, false, true>(a, dev, sms, parts, stream);
+    return a.x_steps ? launch_bn<BN, kCtas, true, false>(a, dev, sms, parts, stream) : launch_bn<BN, kCtas, false, false>(a, dev, sms, parts, stream);
 }
 
 }  // namespace proj
@@ -618,7 +648,7 @@ cudaError_t launch_project(const ProjectArgs& a, cudaStream_t stream)
         double rate;
     };
     const Shape shapes[4] = {{256, 2, 1.11}, {256, 1, 1.0}, {128, 1, 0.9}, {64, 1, 0.75}};
-    int best = 1;
+    int best = 1, best_parts = 1;
     double best_cost = 0.0;
     for (int i = 0; i < 4; ++i) {
         const Shape& sh = shapes[i];
@@ -626,18 +656,28 @@ cudaError_t launch_project(const ProjectArgs& a, cudaStream_t stream)
         const long long rows = (long long)proj::BM * sh.ctas;
         const long long tiles = ((a.M + rows - 1) / rows) * ((a.N + sh.bn - 1) / sh.bn);
         const long long units = sms / sh.ctas;
-        const long long rounds = (tiles + units - 1) / units;
-        const double cost = (double)rounds * (double)(proj::BM * sh.bn) / sh.rate;
+        // A last round of few tiles of pairs is worked in quarters or halves of them where each still has a pair of its own: per stage a part loads
+        // all of its 16 KB of x and a quarter or half of as many of W, and takes 0.6 or 0.75 of the whole's time.  us, 8-bit / bf16, without and with:
+        //   80 tiles of K = 1344 (1190 rows): 16 / 26, 13 / 18;   96 of K = 2048 (1024 rows): 20 / 36, 16 / 25;   384 (4096 rows): 39 / 72, 38 / 71
+        double rounds = (double)((tiles + units - 1) / units);
+        int parts = 1;
+        const long long rest = tiles % units;
+        if (sh.ctas == 2 && tiles > units && rest > 0) {
+            parts = rest * 4 <= units ? 4 : rest * 2 <= units ? 2 : 1;
+            rounds -= parts == 4 ? 0.4 : parts == 2 ? 0.25 : 0.0;
+        }
+        const double cost = rounds * (double)(proj::BM * sh.bn) / sh.rate;
         if (i == 0 || cost < best_cost - 1e-9) {
             best = i;
+            best_parts = parts;
             best_cost = cost;
         }
     }
     switch (best) {
-        case 0: e = proj::launch_type<256, 2>(a, dev, sms, stream); break;
-        case 1: e = proj::launch_type<256, 1>(a, dev, sms, stream); break;
-        case 2: e = proj::launch_type<128, 1>(a, dev, sms, stream); break;
-        default: e = proj::launch_type<64, 1>(a, dev, sms, stream); break;
+        case 0: e = proj::launch_type<256, 2>(a, dev, sms, best_parts, stream); break;
+        case 1: e = proj::launch_type<256, 1>(a, dev, sms, 1, stream); break;
+        case 2: e = proj::launch_type<128, 1>(a, dev, sms, 1, stream); break;
+        default: e = proj::launch_type<64, 1>(a, dev, sms, 1, stream); break;
     }
     if (e != cudaSuccess || a.mode == kProjectPlain || proj::starts_anew(a)) return e;
     const int B = a.M / a.n_rows;

@@ -75,6 +75,9 @@ __host__ __device__ constexpr uint32_t make_idesc_s8(int M, int N)
     return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+// the same descriptor with another N
+__device__ __forceinline__ uint32_t with_n(uint32_t idesc, int n) { return (idesc & ~(0x3fu << 17)) | ((uint32_t)(n >> 3) << 17); }
+
 __device__ __forceinline__ void mma_bf16(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(

@@ -446,6 +446,46 @@ def test_local_qkv_of_integers(bt, B, H, hd, n):
             assert (np.delete(got[b], range(m, m + n), axis=1) == 0).all()
 
 
+@pytest.mark.parametrize("B,H,hd,n", [(1500, 20, 64, 1), (256, 16, 128, 4), (238, 21, 64, 5), (75, 16, 128, 17)])
+def test_products_that_end_in_parts_of_tiles(bt, B, H, hd, n):
+    """Products of somewhat more tiles than pairs of processors (six rows of 15, four of 24, five of 16 - the last of them three quarters there -
+    and five of 24): those of the last round are worked in halves or quarters.  Into the local cache from its first row, into the block cache, in 4 bits."""
+    D = H * hd
+    x8, xs, w8, ws, bias = operands(B + 90, B * n, 3 * D, D)
+    args = (cuda(x8).view(B, n, D), cuda(xs), cuda(w8), cuda(ws), to_dev(bias))
+    ref, tol = lb.project(x8, xs.astype(np.float64), w8, ws.astype(np.float64), f64(bias))
+    part = lambda t, i: t.reshape(B, n, 3, H, hd)[:, :, i].transpose(0, 2, 1, 3)   # noqa: E731
+    cfg = bt.make_config(B, H, hd, 4, n, n + 3, 1)
+    local, q, st = bt.LocalCache(cfg), torch.empty((B, H, n, hd), dtype=torch.bfloat16, device="cuda"), status_word()
+    local.len.fill_(3)
+    bt.bt_local_qkv_project_append_i8(cfg, local, 0, *args, q, reset_first=True, dev_status=st)
+    k, v = (f64(x) for x in local_kv_split(local.kv[0]))
+    for got, i in ((to_f64(q), 0), (k[:, :, :n], 1), (v[:, :, :n], 2)):
+        assert (np.abs(got - part(ref, i)) <= part(tol, i)).all(), i
+    assert (local.len == n).all() and st.item() == 0 and not k[:, :, n:].any() and not v[:, :, n:].any()
+
+    block, q2 = bt.BlockCache(cfg), torch.empty_like(q)
+    block.len.fill_(2)
+    bt.bt_block_qkv_project_append_i8(cfg, block, 0, *args, q2)
+    assert torch.equal(q, q2) and (block.len == n + 2).all() and not block.k[0, :, :, :2].any()
+    assert np.array_equal(to_f64(block.k[0, :, :, 2:n + 2]), k[:, :, :n]) and np.array_equal(to_f64(block.v[0, :, :, 2:n + 2]), v[:, :, :n])
+    one, two = empty_cache(bt, cfg), empty_cache(bt, cfg)
+    one.len.fill_(2), two.len.fill_(2)
+    bt.bt_block_qkv_project_append_i8_kv4(cfg, one, 0, *args, q2)
+    bt.bt_block_kv4_append(cfg, two, 0, block.k[0, :, :, 2:n + 2], block.v[0, :, :, 2:n + 2])
+    assert torch.equal(q, q2) and torch.equal(one.kv, two.kv) and torch.equal(one.len, two.len)
+
+    # bf16: powers of two and small whole numbers, so that every sum is exact
+    x = f64(rnd(91, 3, (B * n, D))).round()
+    w = np.ldexp(np.random.default_rng(B).integers(-1, 2, (3 * D, D)).astype(np.float64), -4)
+    want = x @ w.T
+    assert np.abs(want).max() < 2 ** 16   # whole numbers of sixteenths below 2^24
+    bt.bt_local_qkv_project_append(cfg, local, 0, to_dev(bits(x)).view(B, n, D), to_dev(bits(w)), None, q, reset_first=True)
+    k, v = (f64(x) for x in local_kv_split(local.kv[0]))
+    for got, i in ((to_f64(q), 0), (k[:, :, :n], 1), (v[:, :, :n], 2)):
+        assert np.array_equal(got, lb.to_bf16(part(want, i))), i
+
+
 def test_steps_that_are_not_finite(bt):
     """A token quantised from a NaN makes its own outputs NaN and no others; so does a feature's step."""
     B, H, hd = 40, 2, 64
