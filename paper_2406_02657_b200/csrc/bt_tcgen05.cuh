@@ -179,6 +179,21 @@ __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t* r)
         : "r"(taddr)
         : "memory");
 }
+// The same for 64 columns of 16 lanes, as fragments of 16 rows x 8 columns: of block i, lane (g, c) of the warp gets columns 2 c, 2 c + 1 of row g in
+// r[4 i], r[4 i + 1] and of row g + 8 in r[4 i + 2], r[4 i + 3].  taddr names the first of the 16 lanes.
+__device__ __forceinline__ void tmem_ld16x64_issue(uint32_t taddr, uint32_t* r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
 // Placed after tmem_wait_ld(): makes every later use of r[0..31] depend on a statement that follows
 // the wait, so no consumer can be scheduled ahead of it.  Emits no instruction.
 __device__ __forceinline__ void tmem_ld_fence32(uint32_t* r)
