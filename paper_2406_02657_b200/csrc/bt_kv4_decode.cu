@@ -109,7 +109,7 @@ constexpr float kWholeAt = 12582912.f;   // 1.5 * 2^23
 constexpr uint32_t kWholeBits = 0x4B400000u;
 constexpr int kUnitsPerSum = 512;        // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
 constexpr float kHeadroom = 4.f;         // how far (log2) scores may exceed what weights are relative to before that changes
-constexpr int kJoin = 16;               // partial results requested at once
+constexpr int kJoin = 32;               // partial results requested at once, a warp's weights
 constexpr int kWeightTo = 28;            // the largest weight to 2^28 .. 2^29; it may grow until ...
 constexpr float kWeightEnd = 4294967296.f;
 // the largest of a warp's values that are numbers
@@ -554,18 +554,42 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                 }
             }
             if (lane == 0) ws[HD] = l == 0.f ? kNegInf : m + log2f(l);
-            __threadfence();   // the partial is visible before this item counts itself in
+            // The partial is visible before this item counts itself in, and the others' partials to the item that comes last: release and acquire
+            // by the lane that counts, and for the other lanes by the warp's barriers before and after.
             __syncwarp();
             int last = 0;
-            if (lane == 0) last = atomicAdd(a.counters + w.bh, 1) == a.splits - 1;
+            if (lane == 0) {
+                int before;
+                asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(a.counters + w.bh) : "memory");
+                last = before == a.splits - 1;
+            }
             last = __shfl_sync(0xffffffffu, last, 0);
             if (last) {   // every part of (b,h) has written: fold the partials (normalised, weight 2^lse each)
-                __threadfence();
-                // their weights first, two parts a lane at most (splits <= 64), then HD / 32 dimensions a lane, the loads independent of one another
+                __syncwarp();
+                // HD / 32 dimensions a lane, of 32 parts at once, and the weights, two parts a lane at most (splits <= 64): all requested before any is used
                 constexpr int DIMS = HD / 32;
                 const float* parts = a.ws + (size_t)w.bh * a.splits * (HD + 4);
+                float x[kJoin][DIMS];
+                auto request = [&](int s0) {
+#pragma unroll
+                    for (int i = 0; i < kJoin; ++i) {
+#pragma unroll
+                        for (int j = 0; j < DIMS; ++j) x[i][j] = 0.f;
+                        if (s0 + i < a.splits) {
+                            const float* part = parts + (s0 + i) * (HD + 4) + lane * DIMS;
+                            if constexpr (DIMS == 4) {
+                                const float4 v = __ldcg(reinterpret_cast<const float4*>(part));
+                                x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
+                            } else {
+                                const float2 v = __ldcg(reinterpret_cast<const float2*>(part));
+                                x[i][0] = v.x, x[i][1] = v.y;
+                            }
+                        }
+                    }
+                };
                 float lse0 = lane < a.splits ? __ldcg(parts + lane * (HD + 4) + HD) : kNegInf;
                 float lse1 = lane + 32 < a.splits ? __ldcg(parts + (lane + 32) * (HD + 4) + HD) : kNegInf;
+                request(0);
                 const float ref = softmax_reference(warp_max(fmaxf(lse0, lse1)));
                 lse0 = ex2(lse0 - ref);
                 lse1 = ex2(lse1 - ref);
@@ -575,25 +599,18 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                 float f[DIMS];
 #pragma unroll
                 for (int i = 0; i < DIMS; ++i) f[i] = 0.f;
-                for (int s0 = 0; s0 < a.splits; s0 += kJoin) {
-                    float x[kJoin][DIMS];
+                auto add = [&](float weights) {   // of the 32 parts in x, one a lane; 0 past the last part
 #pragma unroll
                     for (int i = 0; i < kJoin; ++i) {
-                        const float* part = parts + min(s0 + i, a.splits - 1) * (HD + 4) + lane * DIMS;
-                        if constexpr (DIMS == 4) {
-                            const float4 v = __ldcg(reinterpret_cast<const float4*>(part));
-                            x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
-                        } else {
-                            const float2 v = __ldcg(reinterpret_cast<const float2*>(part));
-                            x[i][0] = v.x, x[i][1] = v.y;
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < kJoin; ++i) {
-                        const float weight = __shfl_sync(0xffffffffu, s0 < 32 ? lse0 : lse1, (s0 + i) & 31);   // 0 past the last part
+                        const float weight = __shfl_sync(0xffffffffu, weights, i);
 #pragma unroll
                         for (int j = 0; j < DIMS; ++j) f[j] = fmaf(weight, x[i][j], f[j]);
                     }
+                };
+                add(lse0);
+                if (a.splits > kJoin) {
+                    request(kJoin);
+                    add(lse1);
                 }
                 const float inv = inverse_sum(total);
 #pragma unroll
