@@ -148,21 +148,27 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
-def _stream_of(stream, cache, *tensors, packed=True):
-    """The stream for a call over these tensors (None: not given), the first of which is there, and a 4-bit cache or None.  They have to be on the
-    current device: the kernels run there, and would read another's memory, or the host's, as their own; and packed, as a call knows no strides."""
+def _over(stream, cache, *tensors, packed=True):
+    """The addresses of a call's tensors (None: not given), the first of which is there, and its stream.  The tensors, and a 4-bit cache or None, have
+    to be on the current device: the kernels run there, and would read another's memory, or the host's, as their own; and packed, as a call
+    knows no strides."""
     device = tensors[0].get_device()
     if device < 0 or device != _device():
         raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {tensors[0].device}, not on the current device")
     if cache is not None and cache.device != device:
         raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {tensors[0].device}, cache on {cache.kv.device}")
+    found = []
     for t in tensors:
-        if t is not None:
-            if t.get_device() != device:
-                raise BtError(BT_ERR_UNSUPPORTED, f"tensors on {tensors[0].device} and {t.device}")
-            if packed and not t.is_contiguous():
-                raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of strides {tuple(t.stride())} and shape {tuple(t.shape)}")
-    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
+        if t is None:
+            found.append(None)
+            continue
+        if t.get_device() != device:
+            raise BtError(BT_ERR_UNSUPPORTED, f"tensors on {tensors[0].device} and {t.device}")
+        if packed and not t.is_contiguous():
+            raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of strides {tuple(t.stride())} and shape {tuple(t.shape)}")
+        found.append(t.data_ptr())
+    found.append(_raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream))
+    return found
 
 
 def _slab_stride(k, v):
@@ -229,6 +235,7 @@ class BlockCacheKV4:
         self.device = self.kv.get_device()
         assert self.len.get_device() == self.device
         self.c = bt_block_cache_kv4(self.kv.data_ptr(), self.len.data_ptr())
+        self.ref = ctypes.byref(self.c)
 
 
 def bt_version() -> int:
@@ -467,9 +474,9 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
         n_new = k_new.shape[2]
     if src_stride is None:
         src_stride = _slab_stride(k_new, v_new)
-    on = _stream_of(stream, cache, k_new, v_new, dev_status, packed=False)
-    _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(k_new), _ptr(v_new), _i32(n_new), src_stride,
-                                    1 if reset_first else 0, _ptr(dev_status), on), "bt_block_kv4_append")
+    k, v, status, on = _over(stream, cache, k_new, v_new, dev_status, packed=False)
+    _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), cache.ref, layer, k, v, _i32(n_new), src_stride, 1 if reset_first else 0, status, on),
+           "bt_block_kv4_append")
 
 
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
@@ -478,55 +485,51 @@ def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n
         n_rows = k_out.shape[2]
     if dst_stride is None:
         dst_stride = _slab_stride(k_out, v_out)
-    on = _stream_of(stream, cache, k_out, v_out, packed=False)
-    _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _i32(first), _i32(n_rows), _ptr(k_out), _ptr(v_out),
-                                  dst_stride, on), "bt_block_kv4_read")
+    k, v, on = _over(stream, cache, k_out, v_out, packed=False)
+    _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), cache.ref, layer, _i32(first), _i32(n_rows), k, v, dst_stride, on), "bt_block_kv4_read")
 
 
 def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace, dev_status=None, stream=None):
     """Decode attention over the 4-bit cache."""
-    on = _stream_of(stream, cache, q, out, workspace, dev_status)
-    _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(out), *_ws(workspace),
-                                         _ptr(dev_status), on), "bt_block_decode_attn_kv4")
+    q, o, ws, status, on = _over(stream, cache, q, out, workspace, dev_status)
+    _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), cache.ref, layer, q, o, ws, 0 if ws is None else workspace.nbytes, status, on),
+           "bt_block_decode_attn_kv4")
 
 
 def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, out, workspace, dev_status=None, stream=None):
     """Quantise and append the new block's row, then attend over the 4-bit cache including it, in one launch."""
-    on = _stream_of(stream, cache, q, k_new, v_new, out, workspace, dev_status)
-    _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
-                                         *_ws(workspace), _ptr(dev_status), on), "bt_block_decode_step_kv4")
+    q, k, v, o, ws, status, on = _over(stream, cache, q, k_new, v_new, out, workspace, dev_status)
+    _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), cache.ref, layer, q, k, v, o, ws, 0 if ws is None else workspace.nbytes, status, on),
+           "bt_block_decode_step_kv4")
 
 
 def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, bias, q_out, n_rows=None, dev_status=None, stream=None):
     """bt_block_qkv_project_append into the 4-bit cache."""
     n_rows = x.shape[1] if n_rows is None else n_rows
-    on = _stream_of(stream, cache, x, w_qkv, bias, q_out, dev_status)
-    _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x), _i32(n_rows), _ptr(w_qkv), _ptr(bias),
-                                                _ptr(q_out), _ptr(dev_status), on), "bt_block_qkv_project_append_kv4")
+    x, w, b, q, status, on = _over(stream, cache, x, w_qkv, bias, q_out, dev_status)
+    _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), cache.ref, layer, x, _i32(n_rows), w, b, q, status, on),
+           "bt_block_qkv_project_append_kv4")
 
 
 def bt_rows_quantize_i8(x, x8, steps, stream=None):
     """Rows of x bf16 [..., n_cols] -> int8 of the same shape and fp32 steps [...]."""
     n_cols = x.shape[-1]
-    on = _stream_of(stream, None, x, x8, steps)
-    _check(_lib.bt_rows_quantize_i8(_ptr(x), x.numel() // max(n_cols, 1), _i32(n_cols), _ptr(x8), _ptr(steps), on),
-           "bt_rows_quantize_i8")
+    rows, out, st, on = _over(stream, None, x, x8, steps)
+    _check(_lib.bt_rows_quantize_i8(rows, x.numel() // max(n_cols, 1), _i32(n_cols), out, st, on), "bt_rows_quantize_i8")
 
 
 def bt_prefix_project_i8(cfg, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status=None, stream=None):
     """bt_prefix_project of 8-bit operands and their steps."""
-    on = _stream_of(stream, None, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status)
-    _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), _ptr(ctx8), _ptr(ctx_steps), _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(prefix_out),
-                                     _ptr(dev_status), on), "bt_prefix_project_i8")
+    x, xs, w, ws, b, out, status, on = _over(stream, None, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status)
+    _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), x, xs, w, ws, b, out, status, on), "bt_prefix_project_i8")
 
 
 def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
                                    stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    on = _stream_of(stream, None, x8, x_steps, w8, w_steps, bias, q_out, cache.k, cache.v, cache.len, dev_status)
-    _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
-                                               _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), on),
+    x, xs, w, ws, b, q, status, *_, on = _over(stream, None, x8, x_steps, w8, w_steps, bias, q_out, dev_status, cache.k, cache.v, cache.len)
+    _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
            "bt_block_qkv_project_append_i8")
 
 
@@ -534,19 +537,17 @@ def bt_local_qkv_project_append_i8(cfg, cache: LocalCache, layer, x8, x_steps, w
                                    reset_mask=None, dev_status=None, stream=None):
     """bt_local_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    on = _stream_of(stream, None, x8, x_steps, w8, w_steps, bias, q_out, cache.kv, cache.len, reset_mask, dev_status)
-    _check(_lib.bt_local_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows), _ptr(w8),
-                                               _ptr(w_steps), _ptr(bias), 1 if reset_first else 0, _ptr(reset_mask), _ptr(q_out),
-                                               _ptr(dev_status), on), "bt_local_qkv_project_append_i8")
+    x, xs, w, ws, b, q, mask, status, *_, on = _over(stream, None, x8, x_steps, w8, w_steps, bias, q_out, reset_mask, dev_status, cache.kv, cache.len)
+    _check(_lib.bt_local_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, x, xs, _i32(n_rows), w, ws, b,
+                                               1 if reset_first else 0, mask, q, status, on), "bt_local_qkv_project_append_i8")
 
 
 def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
                                        stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps into the 4-bit cache."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    on = _stream_of(stream, cache, x8, x_steps, w8, w_steps, bias, q_out, dev_status)
-    _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), ctypes.byref(cache.c), layer, _ptr(x8), _ptr(x_steps), _i32(n_rows),
-                                                   _ptr(w8), _ptr(w_steps), _ptr(bias), _ptr(q_out), _ptr(dev_status), on),
+    x, xs, w, ws, b, q, status, on = _over(stream, cache, x8, x_steps, w8, w_steps, bias, q_out, dev_status)
+    _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), cache.ref, layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
            "bt_block_qkv_project_append_i8_kv4")
 
 
