@@ -171,12 +171,20 @@ def _over(stream, cache, *tensors, packed=True):
     return found
 
 
+def _rows(t):
+    """n of [B,H,n,hd]."""
+    if t.dim() != 4:
+        raise BtError(BT_ERR_SHAPE, f"rows of shape {tuple(t.shape)}, not [B,H,n,hd]")
+    return t.shape[2]
+
+
 def _slab_stride(k, v):
     """Rows between the slabs of k, v [B,H,n,hd], which may be the first rows of larger slabs."""
     if k.is_contiguous() and v.is_contiguous():
-        return k.shape[2]
+        return _rows(k)
     found = []
     for t in (k, v):
+        _rows(t)
         (B, H, n, hd), (by_b, by_h, by_n, by_d) = t.shape, t.stride()
         slab = by_h if H > 1 else by_b if B > 1 else n * hd
         if by_d != 1 or (n > 1 and by_n != hd) or slab % hd != 0 or (B > 1 and H > 1 and by_b != H * by_h):
@@ -471,7 +479,7 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
     """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
     slabs of k_new, v_new (a bf16 block cache has N_max), theirs where it is not given."""
     if n_new is None:
-        n_new = k_new.shape[2]
+        n_new = _rows(k_new)
     if src_stride is None:
         src_stride = _slab_stride(k_new, v_new)
     k, v, status, on = _over(stream, cache, k_new, v_new, dev_status, packed=False)
@@ -482,7 +490,7 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
     """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
     if n_rows is None:
-        n_rows = k_out.shape[2]
+        n_rows = _rows(k_out)
     if dst_stride is None:
         dst_stride = _slab_stride(k_out, v_out)
     k, v, on = _over(stream, cache, k_out, v_out, packed=False)

@@ -210,3 +210,17 @@ def test_host_tensors_are_refused(bt):
         with pytest.raises(bt.BtError) as e:
             call()
         assert e.value.code == bt.BT_ERR_UNSUPPORTED
+
+
+def test_rows_without_their_axis_are_refused(bt):
+    """[B,H,hd], as the decode step takes a row: its last axis is not taken for a number of rows."""
+    import torch
+
+    cfg = bt.make_config(2, 2, 64, 4, 1, 16, 1)
+    cache, row = bt.BlockCacheKV4(cfg, device="cpu"), torch.zeros((2, 2, 64), dtype=torch.bfloat16)
+    for call in (lambda k: bt.bt_block_kv4_append(cfg, cache, 0, k, k), lambda k: bt.bt_block_kv4_append(cfg, cache, 0, k, k, n_new=1),
+                 lambda k: bt.bt_block_kv4_read(cfg, cache, 0, k, k), lambda k: bt.bt_block_kv4_read(cfg, cache, 0, k, k, n_rows=1)):
+        for k in (row, row.transpose(0, 1)):
+            with pytest.raises(bt.BtError) as e:
+                call(k)
+            assert e.value.code == bt.BT_ERR_SHAPE
