@@ -108,7 +108,8 @@ constexpr uint32_t kEightsEven = 0x08080808u, kEightsOdd = 0x80808080u;   // wha
 constexpr float kWholeAt = 12582912.f;   // 1.5 * 2^23
 constexpr uint32_t kWholeBits = 0x4B400000u;
 constexpr int kUnitsPerSum = 512;        // 64 rows add at most 64 * 240 * 255 to a sum of bytes: 2^31 holds 548 times that
-constexpr float kHeadroom = 4.f;         // how far (log2) scores may exceed what weights are relative to before that changes
+constexpr float kHeadroom = 2.f;         // how far (log2) scores may exceed what weights are relative to before that changes: a weight is 4
+                                         // at most then, and its product with the largest step there is, 146 * 2^118, a number of fp32
 constexpr int kJoin = 32;               // partial results requested at once, a warp's weights
 constexpr int kWeightTo = 28;            // the largest weight to 2^28 .. 2^29; it may grow until ...
 constexpr float kWeightEnd = 4294967296.f;

@@ -1,0 +1,49 @@
+"""Attention over the 4-bit cache where values are as large as bf16 goes, against its float64 definition."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import lowbit as lb
+
+from test_gpu_lowbit import bits, check, f64, filled, rnd
+from util import status_word, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def bt():
+    import paper_2406_02657_b200 as bt
+    assert torch.cuda.is_available()
+    return bt
+
+
+def keys_of(levels, hd):
+    """Rows K [..., hd] that a query with 8 in its first dimension scores with `levels` (base 2), under the usual scale."""
+    k = np.zeros((*levels.shape, hd))
+    k[..., 0] = levels * np.log(2.0) * np.sqrt(hd) / 8.0
+    return k
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rise", [0.9, 1.9, 2.6, 3.6, 7.0])
+def test_values_near_the_end_of_bf16(bt, hd, rise):
+    """V of 1e38 to 3.3e38 under scores that rise from 128 rows to the next 128, more or less than weights may before all become relative to
+    something else: a weight above one times such a step has to stay a number."""
+    B, H, N = 3, 2, 700
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=1)
+    rng = np.random.default_rng(int(10 * rise))
+    q = f64(rnd(31, 3, (B, H, hd)))
+    q[..., 0] = 8.0
+    k = keys_of(np.broadcast_to(rise * (np.arange(N) // 128), (B, H, N)), hd)
+    v = rng.uniform(1e38, 3.3e38, (B, H, N, hd))
+    v[1] *= rng.choice([-1.0, 1.0], (H, N, hd))
+    v[2, :, :300] *= 1e-30                       # the huge ones come late
+    q, k, v = bits(q), bits(k), bits(v)
+    lens = [N, 517, 400]
+    cache, st = filled(bt, cfg, k, v, lens), status_word()
+    out, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), bt.alloc_workspace_kv4(cfg)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, to_dev(q), out, ws, dev_status=st)
+    ref, tol = lb.decode(f64(q), lb.held(f64(k)), lb.held(f64(v)), lens)
+    check(out, ref, tol, f"rise {rise}")
+    assert st.item() == 0
