@@ -597,6 +597,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                 float total = lse0 + lse1;
 #pragma unroll
                 for (int off = 16; off >= 1; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+                // (the weights' sum divides them before they meet a partial: several partials near the end of fp32 add up to one)
+                const float inv = inverse_sum(total);
+                lse0 *= inv;
+                lse1 *= inv;
                 float f[DIMS];
 #pragma unroll
                 for (int i = 0; i < DIMS; ++i) f[i] = 0.f;
@@ -613,10 +617,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                     request(kJoin);
                     add(lse1);
                 }
-                const float inv = inverse_sum(total);
 #pragma unroll
                 for (int i = 0; i < DIMS; i += 2) {
-                    const __nv_bfloat162 pair = __floats2bfloat162_rn(f[i] * inv, f[i + 1] * inv);
+                    const __nv_bfloat162 pair = __floats2bfloat162_rn(f[i], f[i + 1]);
                     *reinterpret_cast<__nv_bfloat162*>(out + lane * DIMS + i) = pair;
                 }
                 if (lane == 0) a.counters[w.bh] = 0;

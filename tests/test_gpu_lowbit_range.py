@@ -47,3 +47,26 @@ def test_values_near_the_end_of_bf16(bt, hd, rise):
     ref, tol = lb.decode(f64(q), lb.held(f64(k)), lb.held(f64(v)), lens)
     check(out, ref, tol, f"rise {rise}")
     assert st.item() == 0
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("splits", [2, 3, 40])
+@pytest.mark.parametrize("rise", [0.0, 1.9, 3.6])
+def test_parts_near_the_end_of_bf16_are_joined(bt, hd, splits, rise):
+    """Parts whose results are 1e38 to 3.3e38 each: their weighted sum is no larger than the largest of them."""
+    B, H, N = 2, 2, 2600
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    rng = np.random.default_rng(splits)
+    q = f64(rnd(32, 3, (B, H, hd)))
+    q[..., 0] = 8.0
+    k = keys_of(np.broadcast_to(rise * (np.arange(N) // 900), (B, H, N)), hd)
+    v = rng.uniform(1e38, 3.3e38, (B, H, N, hd))
+    v[1] *= -1.0
+    q, k, v = bits(q), bits(k), bits(v)
+    lens = [N, 1111]
+    cache, st = filled(bt, cfg, k, v, lens), status_word()
+    out, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), bt.alloc_workspace_kv4(cfg)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, to_dev(q), out, ws, dev_status=st)
+    ref, tol = lb.decode(f64(q), lb.held(f64(k)), lb.held(f64(v)), lens)
+    check(out, ref, tol, f"{splits} parts, rise {rise}")
+    assert st.item() == 0
