@@ -15,7 +15,7 @@
 //            (Every byte in every column, one after the other into the same sums, needs no exchange but three times the products: 128 us where
 //            this takes 118 over 24 x 16 items of 12001 to 16000 rows of 128, at the clock that the power limit leaves.)
 //   output:  A = codes of V transposed, 16 dimensions x 32 rows; B = the weights p t of a group as whole numbers of 32 bits, times a power
-//            of two that has the largest of them so far at 2^28 .. 2^32 (so that the rounding, 2^-29 of the largest, does not add up over a
+//            of two that has the group's largest so far at 2^28 .. 2^32 (so that the rounding, 2^-29 of the largest, does not add up over a
 //            million rows), a byte in each of four columns (2 groups x 4 bytes).  Sums are kept as 32-bit whole numbers until what they are
 //            relative to changes.
 // Products of the same bytes with rows of eights give what the offsets of the codes add.
@@ -290,12 +290,15 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         }
         if (item + stride < n_items) fetch_q(divide(item + stride, a.by_splits));
         float m = kNegInf, l = 0.f;                // what scores are relative to, the sum of 2^(score - m)
-        float w_most = 0.f, w_to = power_to<kWeightTo>(0.f);   // the largest weight p t so far and the power of two for it
+        // of every group: the largest weight p t that this lane has had, and the power of two for the largest of all lanes'
+        float w_most[PLANES][2], w_to[PLANES][2];
         float o[PLANES][4][2], bad[PLANES][2];     // even | odd dimension; not a number once a step of V was none
         int sums[PLANES][4][4], eights[PLANES][4], pending = 0;
 #pragma unroll
         for (int p = 0; p < PLANES; ++p) {
             bad[p][0] = bad[p][1] = 0.f;
+            w_most[p][0] = w_most[p][1] = 0.f;
+            w_to[p][0] = w_to[p][1] = power_to<kWeightTo>(0.f);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 o[p][r][0] = o[p][r][1] = 0.f;
@@ -399,7 +402,11 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
             m = grown ? mn : m;
             const float m_use = softmax_reference(m);
             l *= cf;
-            float most = w_most * cf;
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+                w_most[p][0] *= cf;
+                w_most[p][1] *= cf;
+            }
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const float p0 = ex2(s[u][0] - m_use), p1 = ex2(s[u][1] - m_use);
@@ -410,23 +417,31 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                     for (int gl = 0; gl < 2; ++gl) {
                         t[u][p][gl][0] *= p0;
                         t[u][p][gl][1] *= p1;
-                        most = fmaxf(most, fmaxf(t[u][p][gl][0], t[u][p][gl][1]));
+                        w_most[p][gl] = fmaxf(w_most[p][gl], fmaxf(t[u][p][gl][0], t[u][p][gl][1]));
                     }
             }
-            // ... and what weights are relative to, then and when one would leave 32 bits.
-            w_most = warp_max(most);
-            if (grown || w_most * w_to >= kWeightEnd || pending >= kUnitsPerSum) {
-                if (pending > 0) flush();
-                const float to = power_to<kWeightTo>(w_most);
-                const float co = cf * to * inverse_power(w_to);   // at most 2, in this order
+            // ... and what the weights of a group are relative to, then and when one would leave 32 bits.  (A power of two for all
+            // groups would take the precision of those whose steps are small beside another's.)
+            float end = 0.f;
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p)
+            for (int p = 0; p < PLANES; ++p) end = fmaxf(end, fmaxf(w_most[p][0] * w_to[p][0], w_most[p][1] * w_to[p][1]));
+            if (grown || pending >= kUnitsPerSum || __any_sync(0xffffffffu, end >= kWeightEnd)) {
+                if (pending > 0) flush();
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+                    float co = 0.f;   // of the group whose weights this lane's outputs are under
+#pragma unroll
+                    for (int gl = 0; gl < 2; ++gl) {
+                        const float to = power_to<kWeightTo>(warp_max(w_most[p][gl]));
+                        if (gl == c >> 1) co = cf * to * inverse_power(w_to[p][gl]);   // at most 2, in this order
+                        w_to[p][gl] = to;
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         o[p][r][0] *= co;
                         o[p][r][1] *= co;
                     }
-                w_to = to;
+                }
             }
             pending += N;
             // ---- weights of the rows: column 4 (group) + byte of a plane
@@ -437,7 +452,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
 #pragma unroll
                     for (int gl = 0; gl < 2; ++gl) {
                         const uint32_t at = wbuf + (u * PLANES + p) * G::WEIGHT_PLANE + c * G::WEIGHT_TILE + gl * (4 * kTileRows) + 2 * g;
-                        const uint32_t x = whole(t[u][p][gl][0] * w_to), y = whole(t[u][p][gl][1] * w_to);
+                        const uint32_t x = whole(t[u][p][gl][0] * w_to[p][gl]), y = whole(t[u][p][gl][1] * w_to[p][gl]);
                         sts16(at, __byte_perm(x, y, 0x0040));
                         sts16(at + kTileRows, __byte_perm(x, y, 0x0051));
                         sts16(at + 2 * kTileRows, __byte_perm(x, y, 0x0062));
@@ -523,10 +538,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         const bool own_piece = c == 2 * (g >> 2);
         // (The sum of the weights divides first: with the weights' power of two it could leave the normal numbers.)
         const float share = (c & 1 ? 65536.f : 1.f) * inverse_sum(l);
-        const float unit = inverse_power(w_to);
         auto piece = [&](int p, float (&f)[8]) {
             const bool bad0 = __any_sync(0xffffffffu, bad[p][0] != 0.f), bad1 = __any_sync(0xffffffffu, bad[p][1] != 0.f);
-            const float u = (g < 4 ? bad0 : bad1) ? __uint_as_float(0x7fffffffu) : unit;
+            const float u = (g < 4 ? bad0 : bad1) ? __uint_as_float(0x7fffffffu) : inverse_power(c & 2 ? w_to[p][1] : w_to[p][0]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 f[2 * r] = o[p][r][0] * share;

@@ -1,4 +1,4 @@
-"""Attention over the 4-bit cache where values are as large as bf16 goes, against its float64 definition."""
+"""Attention over the 4-bit cache where values are as large as bf16 goes or of unlike size in groups of dimensions, against its float64 definition."""
 import numpy as np
 import pytest
 import torch
@@ -70,3 +70,32 @@ def test_parts_near_the_end_of_bf16_are_joined(bt, hd, splits, rise):
     ref, tol = lb.decode(f64(q), lb.held(f64(k)), lb.held(f64(v)), lens)
     check(out, ref, tol, f"{splits} parts, rise {rise}")
     assert st.item() == 0
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("apart", [10, 20, 30, 60])
+def test_groups_of_unlike_size_keep_their_own_precision(bt, hd, splits, apart):
+    """V whose groups of 32 dimensions are 2^apart and more from each other, within a plane of 64 dimensions and across the two, and change
+    places along the rows of one sequence: each has the bound of its own size."""
+    B, H, N = 3, 4, 600
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    q, k, v = f64(rnd(33, 3, (B, H, hd))), f64(rnd(33, 1, (B, H, N, hd))), f64(rnd(33, 2, (B, H, N, hd)))
+    groups = hd // 32
+    for h in range(H):
+        size = np.repeat(2.0 ** -(apart * ((np.arange(groups) + h) % groups)), 32)
+        v[:, h] *= size
+        v[1, h, 300:] = v[1, h, 300:] / size * size[::-1]
+    v[2, :, :, :32] = 0.0                        # a group without any size
+    q, k, v = bits(q), bits(k), bits(v)
+    lens = [N, 587, 130]
+    cache = filled(bt, cfg, k, v, lens)
+    out, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), bt.alloc_workspace_kv4(cfg)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, to_dev(q), out, ws)
+    held = lb.held(f64(v))
+    ref, tol = lb.decode(f64(q), lb.held(f64(k)), held, lens)
+    check(out, ref, tol, f"{apart} apart")
+    # what the bound itself is worth: a hundredth of the largest value of the group, at most
+    for b, n in enumerate(lens):
+        largest = np.abs(held[b, :, :n]).max(1).reshape(H, groups, 32).max(2)
+        assert (tol[b].reshape(H, groups, 32) <= 0.01 * largest[..., None] + 2e-30).all()
