@@ -396,9 +396,9 @@ bt_status bt_block_kv4_read(const bt_config* cfg, const bt_block_cache_kv4* cach
                             void* v_out, int64_t dst_stride, void* stream);
 
 /*
- * bt_block_decode_attn and bt_block_decode_step over the 4-bit cache: K and V are the values s u.  The query is rounded to whole
- * numbers (by 2^-18 of its largest value at most: values down to 2^-10 of that stay what they are), and so are the products of a row's
- * weight and a step of V (by 2^-29 of the largest such product of the 32 dimensions in question), neither by less than 2^-123 and 2^-127; sums of
+ * bt_block_decode_attn and bt_block_decode_step over the 4-bit cache: K and V are the values s u.  For every 32 dimensions on their own
+ * the query is rounded to whole numbers (by 2^-18 of its largest value there at most: values down to 2^-10 of that stay what they are), and so are
+ * the products of a row's weight and a step of V (by 2^-29 of the largest such product), neither by less than 2^-123 and 2^-127; sums of
  * products of whole numbers are exact, the rest is fp32.  The step quantises the new row, stores it and attends over it as it is stored: it gives what
  * bt_block_kv4_append and bt_block_decode_attn_kv4 give.
  * Values that are not finite: as for the contexts calls above, where a NaN in V is in all 32 dimensions of its step; a query that

@@ -79,7 +79,7 @@ def write_tiles(tiles, row0, k, v):
 
 def decode(q, K, V, n):
     """q [B,H,hd], K, V [B,H,N,hd] as held, n [B]: (out, tol).  Beside what contexts.attend allows: the query is rounded to whole
-    numbers, by 2^-18 of its largest value at most (a score error of e moves a weight by a factor within exp(+-e), in numerator and
+    numbers, by 2^-18 of the largest value of its group of 32 dimensions at most (a score error of e moves a weight by a factor within exp(+-e), in numerator and
     denominator), and so are the products of a weight and a step of V, by 2^-29 of the largest one of their group of 32 dimensions, for a
     code of up to 7."""
     out, tol = np.zeros(q.shape), np.zeros(q.shape)
@@ -88,7 +88,8 @@ def decode(q, K, V, n):
             k, v = K[b, h, :n[b]], V[b, h, :n[b]]
             o, p, e, _ = ctx.attend(q[b, h], k, v)
             if n[b]:
-                score = np.abs(k).sum(1).max() * np.abs(q[b, h]).max() * 2.0 ** -18 / np.sqrt(q.shape[2])
+                sizes = np.abs(k).reshape(n[b], -1, 32).sum(2) @ np.abs(q[b, h]).reshape(-1, 32).max(1)
+                score = sizes.max() * 2.0 ** -18 / np.sqrt(q.shape[2])
                 largest = (p[:, None] * np.abs(v)).max(0).reshape(-1, 32).max(1)
                 e += 2 * score * (p @ np.abs(v)) + n[b] * 2.0 ** -29 * 1.01 * np.repeat(largest, 32)
             out[b, h], tol[b, h] = o, e

@@ -8,8 +8,8 @@
 // bytes, another those of four odd ones as 16 (u + 8), and warp-level m16n8k32 integer instructions multiply them (8 cycles each, half of
 // what 16-bit floats would take; unpacking to those also takes seven integer instructions for eight values instead of two).
 // The other operand becomes whole numbers cut into bytes, and the sums are exact:
-//   scores:  A = codes of 16 rows x 32 dimensions; B = the query, times a power of two that brings its largest value to 2^21 .. 2^22 (odd
-//            dimensions to 2^17 .. 2^18: half a step of the rounding is 2^-18 of the largest value at most), as three signed bytes, of which each has
+//   scores:  A = codes of 16 rows x 32 dimensions; B = the query, times a power of two that brings a group's largest value to 2^21 .. 2^22 (odd
+//            dimensions to 2^17 .. 2^18: half a step of the rounding is 2^-18 of the group's largest at most), as three signed bytes, of which each has
 //            two columns: the values of one group of a plane and zeros elsewhere, and the other's.  The lanes that share a row then hold
 //            the sums of one byte each; two exchanges between them, with shifts, give lane c the whole sums of tile c of a unit.
 //            (Every byte in every column, one after the other into the same sums, needs no exchange but three times the products: 128 us where
@@ -253,20 +253,19 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
         // the column of group g & 1: zeros where the dimensions are the other group's, and in the two columns that are left.
         uint32_t qf[PLANES][2][2];         // word, even | odd dimensions
         int q_from[PLANES][2];             // what the sums of a byte of a group (columns 2 c, 2 c + 1) start from, so that the codes' eights are taken out
-        float q_unit;                      // what a whole sum has to be multiplied with
+        float q_unit[PLANES][2];           // what a group's whole sum has to be multiplied with
         {
-            uint32_t top = 0;
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) top = magnitude_max(top, magnitude_max(magnitude_max8(q_next[p][0]), magnitude_max8(q_next[p][1])));
-            top = magnitude_of(top);
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const float to = power_to<21>(__uint_as_float(top << 16));
-            // a query with a value that is not finite gives NaN throughout
-            q_unit = top < 0x7f80u ? inverse_power(to) : __uint_as_float(0x7fffffffu);
             const uint32_t own = (g & 1) == (c >> 1) && g < 6 ? 0xffffffffu : 0u;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
+                // (lanes c and c ^ 1 have the dimensions of one group, lanes c ^ 2 the other's)
+                uint32_t top = magnitude_of(magnitude_max(magnitude_max8(q_next[p][0]), magnitude_max8(q_next[p][1])));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                const float to = power_to<21>(__uint_as_float(top << 16));
+                // a query with a value that is not finite gives NaN throughout
+                const float unit = top < 0x7f80u ? inverse_power(to) : __uint_as_float(0x7fffffffu), other = __shfl_xor_sync(0xffffffffu, unit, 2);
+                q_unit[p][0] = c & 2 ? other : unit;
+                q_unit[p][1] = c & 2 ? unit : other;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     float f[8];
@@ -371,8 +370,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                     uint32_t k0, k1;
                     lds64(own_tile + u * (kUnitTiles * G::TILE) + p * kTileBytes + kStepsAt, k0, k1);
                     // (the query's power of two goes to the step, so that nothing between is larger than the products themselves)
-                    s[u][0] = fmaf(mine[1], bf_hi(k0) * q_unit, fmaf(mine[0], bf_lo(k0) * q_unit, s[u][0]));
-                    s[u][1] = fmaf(mine[3], bf_hi(k1) * q_unit, fmaf(mine[2], bf_lo(k1) * q_unit, s[u][1]));
+                    s[u][0] = fmaf(mine[1], bf_hi(k0) * q_unit[p][1], fmaf(mine[0], bf_lo(k0) * q_unit[p][0], s[u][0]));
+                    s[u][1] = fmaf(mine[3], bf_hi(k1) * q_unit[p][1], fmaf(mine[2], bf_lo(k1) * q_unit[p][0], s[u][1]));
                 }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {

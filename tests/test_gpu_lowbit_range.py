@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import contexts as ctx
 from oracle import lowbit as lb
 
 from test_gpu_lowbit import bits, check, f64, filled, rnd
@@ -99,3 +100,53 @@ def test_groups_of_unlike_size_keep_their_own_precision(bt, hd, splits, apart):
     for b, n in enumerate(lens):
         largest = np.abs(held[b, :, :n]).max(1).reshape(H, groups, 32).max(2)
         assert (tol[b].reshape(H, groups, 32) <= 0.01 * largest[..., None] + 2e-30).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("apart", [10, 18, 30])
+def test_groups_of_a_query_keep_their_own_precision(bt, hd, splits, apart):
+    """Queries whose groups of 32 dimensions are 2^apart and more from each other, and keys that are so the other way round: every group
+    has its part in the scores."""
+    B, H, N = 2, 4, 300
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1, decode_splits=splits)
+    q, k, v = f64(rnd(36, 3, (B, H, hd))), f64(rnd(36, 1, (B, H, N, hd))), rnd(36, 2, (B, H, N, hd))
+    for h in range(H):
+        size = np.repeat(2.0 ** -(apart * ((np.arange(hd // 32) + h) % (hd // 32))), 32)
+        q[:, h] *= size
+        k[:, h] /= size
+    q, k = bits(q), bits(k)
+    lens = [N, 177]
+    cache = filled(bt, cfg, k, v, lens)
+    out, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), bt.alloc_workspace_kv4(cfg)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, to_dev(q), out, ws)
+    ref, tol = lb.decode(f64(q), lb.held(f64(k)), lb.held(f64(v)), lens)
+    check(out, ref, tol, f"{apart} apart")
+    assert tol.max() < 0.03                      # what the bound itself is worth
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("where", ["another group"])
+def test_huge_queries_and_keys_that_do_not_meet(bt, hd, where):
+    """A query and keys of 2^80 in different dimensions, of the same group of 32 or not: their products are zeros, and the scores come from the rest."""
+    B, H, N = 2, 2, 150
+    cfg = bt.make_config(B, H, hd, 4, 1, N, 1)
+    q, k, v = np.zeros((B, H, hd)), np.zeros((B, H, N, hd)), rnd(37, 2, (B, H, N, hd))
+    q[..., 3], q[..., 40] = 2.0 ** 80, 2.0
+    k[..., 40] = f64(rnd(37, 1, (B, H, N)))
+    k[..., 20 if where == "the same group" else 50] = 2.0 ** 80
+    if where == "another group":
+        q[..., 40], q[..., 5], k[..., 40] = 0.0, 2.0, 0.0
+        k[..., 3] = f64(rnd(37, 1, (B, H, N))) * 2.0 ** -80
+    q, k = bits(q), bits(k)
+    lens = [N, 99]
+    cache = filled(bt, cfg, k, v, lens)
+    out, ws = torch.empty((B, H, hd), dtype=torch.bfloat16, device="cuda"), bt.alloc_workspace_kv4(cfg)
+    bt.bt_block_decode_attn_kv4(cfg, cache, 0, to_dev(q), out, ws)
+    q, K, V = f64(q), lb.held(f64(k)), lb.held(f64(v))
+    assert np.ptp((K * q[:, :, None]).sum(-1)) > 4.0 / np.sqrt(hd)
+    # the definition over what meets: the query's rounding leaves powers of two and zeros what they are, so that it adds nothing here
+    for b, n in enumerate(lens):
+        for h in range(H):
+            ref, _, tol, _ = ctx.attend(q[b, h], np.where(q[b, h] != 0, K[b, h, :n], 0.0), V[b, h, :n])
+            check(out[b, h], ref, tol + n * 2.0 ** -29 * 1.01 * np.abs(V[b, h, :n]).max(), where)
