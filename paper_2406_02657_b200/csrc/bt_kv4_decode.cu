@@ -98,6 +98,13 @@ __device__ __forceinline__ uint32_t whole(float x)
     asm("cvt.rni.u32.f32 %0, %1;" : "=r"(w) : "f"(x));
     return w;
 }
+// x, NaN included, but no infinity above
+__device__ __forceinline__ float at_most_largest(float x)
+{
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(3.40282347e38f));
+    return y;
+}
 // a byte of each of four words
 __device__ __forceinline__ uint32_t gather_byte(const uint32_t (&w)[4], int byte)
 {
@@ -370,8 +377,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                     uint32_t k0, k1;
                     lds64(own_tile + u * (kUnitTiles * G::TILE) + p * kTileBytes + kStepsAt, k0, k1);
                     // (the query's power of two goes to the step, so that nothing between is larger than the products themselves)
-                    s[u][0] = fmaf(mine[1], bf_hi(k0) * q_unit[p][1], fmaf(mine[0], bf_lo(k0) * q_unit[p][0], s[u][0]));
-                    s[u][1] = fmaf(mine[3], bf_hi(k1) * q_unit[p][1], fmaf(mine[2], bf_lo(k1) * q_unit[p][0], s[u][1]));
+                    s[u][0] = fmaf(mine[1], at_most_largest(bf_hi(k0) * q_unit[p][1]), fmaf(mine[0], at_most_largest(bf_lo(k0) * q_unit[p][0]), s[u][0]));
+                    s[u][1] = fmaf(mine[3], at_most_largest(bf_hi(k1) * q_unit[p][1]), fmaf(mine[2], at_most_largest(bf_lo(k1) * q_unit[p][0]), s[u][1]));
                 }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {

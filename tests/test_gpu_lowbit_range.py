@@ -126,7 +126,7 @@ def test_groups_of_a_query_keep_their_own_precision(bt, hd, splits, apart):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
-@pytest.mark.parametrize("where", ["another group"])
+@pytest.mark.parametrize("where", ["another group", "the same group"])
 def test_huge_queries_and_keys_that_do_not_meet(bt, hd, where):
     """A query and keys of 2^80 in different dimensions, of the same group of 32 or not: their products are zeros, and the scores come from the rest."""
     B, H, N = 2, 2, 150
