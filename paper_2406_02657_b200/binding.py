@@ -171,20 +171,38 @@ def _over(stream, cache, *tensors, packed=True):
     return found
 
 
-def _rows(t):
-    """n of [B,H,n,hd]."""
-    if t.dim() != 4:
-        raise BtError(BT_ERR_SHAPE, f"rows of shape {tuple(t.shape)}, not [B,H,n,hd]")
-    return t.shape[2]
+def _slabs(cfg, k, v, n, stride):
+    """How many rows of k, v a call takes (n, or all of them), and how many lie between their slabs (stride, or as they lie: [B,H,rows,hd] of the config,
+    packed or the first rows of larger slabs).  What the call touches is there."""
+    if k is None or v is None:
+        raise BtError(BT_ERR_NULL, "rows")
+    if stride is not None:   # the caller's word for the layout: k and v have to reach as far
+        if n is None:
+            n = k.shape[2] if k.dim() == 4 else 0
+        need = ((cfg.batch * cfg.heads - 1) * stride + n) * cfg.head_dim
+        for t in (k, v):
+            if stride < n or (t.numel() if t.is_contiguous() else _span(t)) < need:
+                raise BtError(BT_ERR_SHAPE, f"rows of strides {tuple(t.stride())} and shape {tuple(t.shape)}, taken every {stride} of them")
+        return n, stride
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape:
+        raise BtError(BT_ERR_SHAPE, f"rows of shapes {tuple(shape)} and {tuple(v.shape)}, not both [B,H,n,hd]")
+    rows = shape[2]
+    stride = rows if k.is_contiguous() and v.is_contiguous() else _slab_stride(k, v)
+    if (cfg.batch, cfg.heads, rows, cfg.head_dim) != shape or (n is not None and n > rows):
+        raise BtError(BT_ERR_SHAPE, f"rows of shape {tuple(shape)} for {cfg.batch} sequences, {cfg.heads} heads of {cfg.head_dim}, {n} rows")
+    return rows if n is None else n, stride
+
+
+def _span(t):
+    """Elements from a tensor's first to its last in memory."""
+    return 1 + sum((size - 1) * by for size, by in zip(t.shape, t.stride())) if t.numel() else 0
 
 
 def _slab_stride(k, v):
     """Rows between the slabs of k, v [B,H,n,hd], which may be the first rows of larger slabs."""
-    if k.is_contiguous() and v.is_contiguous():
-        return _rows(k)
     found = []
     for t in (k, v):
-        _rows(t)
         (B, H, n, hd), (by_b, by_h, by_n, by_d) = t.shape, t.stride()
         slab = by_h if H > 1 else by_b if B > 1 else n * hd
         if by_d != 1 or (n > 1 and by_n != hd) or slab % hd != 0 or (B > 1 and H > 1 and by_b != H * by_h):
@@ -478,10 +496,7 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
                         stream=None):
     """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
     slabs of k_new, v_new (a bf16 block cache has N_max), theirs where it is not given."""
-    if n_new is None:
-        n_new = _rows(k_new)
-    if src_stride is None:
-        src_stride = _slab_stride(k_new, v_new)
+    n_new, src_stride = _slabs(cfg, k_new, v_new, n_new, src_stride)
     k, v, status, on = _over(stream, cache, k_new, v_new, dev_status, packed=False)
     _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), cache.ref, layer, k, v, _i32(n_new), src_stride, 1 if reset_first else 0, status, on),
            "bt_block_kv4_append")
@@ -489,10 +504,7 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
 
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
     """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
-    if n_rows is None:
-        n_rows = _rows(k_out)
-    if dst_stride is None:
-        dst_stride = _slab_stride(k_out, v_out)
+    n_rows, dst_stride = _slabs(cfg, k_out, v_out, n_rows, dst_stride)
     k, v, on = _over(stream, cache, k_out, v_out, packed=False)
     _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), cache.ref, layer, _i32(first), _i32(n_rows), k, v, dst_stride, on), "bt_block_kv4_read")
 

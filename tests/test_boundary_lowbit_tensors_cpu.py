@@ -1,0 +1,119 @@
+"""The binding refuses tensors that do not hold what a call over the low-bit operators would read or write, before the library is called (no GPU
+needed: the tensors are in the host's memory and say that they are on the current device; the library's calls are recorded)."""
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def bt():
+    import paper_2406_02657_b200 as bt
+    return bt
+
+
+class OnDevice:
+    """A tensor that says it is on the current device."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 0
+
+
+class Recorder:
+    def __init__(self, lib):
+        self.calls, self.bt_status_string = [], lib.bt_status_string
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or 0
+
+
+@pytest.fixture
+def lib(bt, monkeypatch):
+    rec = Recorder(bt.lib())
+    monkeypatch.setattr(bt.binding, "_lib", rec)
+    monkeypatch.setattr(bt.binding, "_device", lambda: 0)
+    monkeypatch.setattr(bt.binding, "_raw_stream", lambda device: 0)
+    return rec
+
+
+def t(*shape, dtype=torch.bfloat16):
+    return OnDevice(torch.zeros(shape, dtype=dtype))
+
+
+def view(shape, f, dtype=torch.bfloat16):
+    return OnDevice(f(torch.zeros(shape, dtype=dtype)))
+
+
+B, H, HD, N = 2, 3, 64, 16
+
+
+def config(bt, **other):
+    size = dict(batch=B, heads=H, head_dim=HD, block_len=4, prefix_len=2, max_blocks=N, n_layers=2)
+    return bt.make_config(**{**size, **other})
+
+
+def kv4(bt, cfg):
+    cache = bt.BlockCacheKV4(cfg, device="cpu")
+    cache.device = 0
+    return cache
+
+
+def refused(bt, lib, code, call, *args, **kwargs):
+    before = len(lib.calls)
+    with pytest.raises(bt.BtError) as e:
+        call(*args, **kwargs)
+    assert e.value.code == code and len(lib.calls) == before, e.value
+
+
+def passed(lib, call, *args, **kwargs):
+    before = len(lib.calls)
+    call(*args, **kwargs)
+    assert len(lib.calls) == before + 1
+    return lib.calls[-1]
+
+
+def test_rows_of_k_and_v_are_there(bt, lib):
+    """Append and read: k and v of one shape, of the config's sizes, with as many rows as the call takes."""
+    cfg = config(bt)
+    cache, k = kv4(bt, cfg), t(B, H, 5, HD)
+    for call, stride, n in ((bt.bt_block_kv4_append, "src_stride", "n_new"), (bt.bt_block_kv4_read, "dst_stride", "n_rows")):
+        name, args = passed(lib, call, cfg, cache, 0, k, t(B, H, 5, HD))
+        assert name == call.__name__ and 5 in args
+        passed(lib, call, cfg, cache, 0, k, k, **{n: 3})
+        wide = view((B, H, N, HD), lambda x: x[:, :, 2:7])
+        passed(lib, call, cfg, cache, 0, wide, wide)
+        # v has fewer rows, no rows' axis, next to nothing; and the other way round
+        for other in (t(B, H, 3, HD), t(B, H, HD), t(1), t(B, H, 0, HD), t(B, H - 1, 5, HD), t(B, H, 5, HD // 2), t(B * H, 5, HD)):
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, other)
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, other, k)
+        # both alike, but not what the config says
+        for both in (t(B - 1, H, 5, HD), t(B, H - 1, 5, HD), t(B, H, 5, 2 * HD), t(B, H, HD), t(H, B, 5, HD)):
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, both, both)
+        # more rows than there are, packed or in a larger slab, whose last one would be left behind
+        refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, k, **{n: 6})
+        refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, wide, wide, **{n: 6})
+        for missing in ((None, k), (k, None)):
+            refused(bt, lib, bt.BT_ERR_NULL, call, cfg, cache, 0, *missing)
+
+
+def test_rows_under_a_given_stride_are_there(bt, lib):
+    """A stride that the caller gives: k and v reach to the last row of the last slab."""
+    cfg = config(bt)
+    cache, k = kv4(bt, cfg), t(B, H, N, HD)
+    flat, short = t(B * H * N - 11, HD), t(B * H * N - 12, HD)          # five rows of the last slab, four
+    last = view((B, H, N, HD), lambda x: x[:, :, 11:])                  # a view that starts eleven rows into the first slab
+    for call, stride, n in ((bt.bt_block_kv4_append, "src_stride", "n_new"), (bt.bt_block_kv4_read, "dst_stride", "n_rows")):
+        for ok in (k, flat, last):
+            passed(lib, call, cfg, cache, 0, ok, k, **{stride: N, n: 5})
+            passed(lib, call, cfg, cache, 0, k, ok, **{stride: N, n: 5})
+        for bad, rows in ((short, 5), (last, 6), (t(B, H, 5, HD), 5), (t(1), 1), (t(0), 1)):
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, bad, k, **{stride: N, n: rows})
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, bad, **{stride: N, n: rows})
+        refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, k, **{stride: N + 1, n: N})
+        refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, k, **{stride: N - 1, n: N})
+        for wrapped in (2 ** 64 + N, N - 2 ** 64):                      # no numbers of 64 bits
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, k, **{stride: wrapped, n: 5})
