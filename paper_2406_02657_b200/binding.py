@@ -148,27 +148,37 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
-def _over(stream, cache, *tensors, packed=True):
-    """The addresses of a call's tensors (None: not given), the first of which is there, and its stream.  The tensors, and a 4-bit cache or None, have
-    to be on the current device: the kernels run there, and would read another's memory, or the host's, as their own; and packed, as a call
-    knows no strides."""
-    device = tensors[0].get_device()
+def _over(stream, cache, wanted, packed=True):
+    """The addresses of a call's tensors, and its stream.  wanted: (tensor or None, the type of its elements or None for any, the bytes that the call
+    takes of it), of which the first has to be there.  The tensors, and a 4-bit cache or None, have to be on the current device: the kernels run
+    there, and would read another's memory, or the host's, as their own; packed, as a call knows no strides; of their type; and no smaller."""
+    first = wanted[0][0]
+    if first is None:
+        raise BtError(BT_ERR_NULL, "tensor")
+    device = first.get_device()
     if device < 0 or device != _device():
-        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {tensors[0].device}, not on the current device")
+        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {first.device}, not on the current device")
     if cache is not None and cache.device != device:
-        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {tensors[0].device}, cache on {cache.kv.device}")
+        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {first.device}, cache on {cache.kv.device}")
     found = []
-    for t in tensors:
+    for t, kind, size in wanted:
         if t is None:
             found.append(None)
-            continue
-        if t.get_device() != device:
-            raise BtError(BT_ERR_UNSUPPORTED, f"tensors on {tensors[0].device} and {t.device}")
-        if packed and not t.is_contiguous():
+        elif t.get_device() != device:
+            raise BtError(BT_ERR_UNSUPPORTED, f"tensors on {first.device} and {t.device}")
+        elif packed and not t.is_contiguous():
             raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of strides {tuple(t.stride())} and shape {tuple(t.shape)}")
-        found.append(t.data_ptr())
+        elif kind is not None and t.dtype is not kind:
+            raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of {t.dtype} for one of {kind}")
+        elif t.nbytes < size:
+            raise BtError(BT_ERR_SHAPE, f"a tensor of shape {tuple(t.shape)} for {size} bytes")
+        else:
+            found.append(t.data_ptr())
     found.append(_raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream))
     return found
+
+
+_BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 
 
 def _slabs(cfg, k, v, n, stride):
@@ -497,7 +507,7 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
     """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
     slabs of k_new, v_new (a bf16 block cache has N_max), theirs where it is not given."""
     n_new, src_stride = _slabs(cfg, k_new, v_new, n_new, src_stride)
-    k, v, status, on = _over(stream, cache, k_new, v_new, dev_status, packed=False)
+    k, v, status, on = _over(stream, cache, ((k_new, _BF16, 0), (v_new, _BF16, 0), (dev_status, None, 4)), packed=False)
     _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), cache.ref, layer, k, v, _i32(n_new), src_stride, 1 if reset_first else 0, status, on),
            "bt_block_kv4_append")
 
@@ -505,20 +515,23 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
     """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
     n_rows, dst_stride = _slabs(cfg, k_out, v_out, n_rows, dst_stride)
-    k, v, on = _over(stream, cache, k_out, v_out, packed=False)
+    k, v, on = _over(stream, cache, ((k_out, _BF16, 0), (v_out, _BF16, 0)), packed=False)
     _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), cache.ref, layer, _i32(first), _i32(n_rows), k, v, dst_stride, on), "bt_block_kv4_read")
 
 
 def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace, dev_status=None, stream=None):
     """Decode attention over the 4-bit cache."""
-    q, o, ws, status, on = _over(stream, cache, q, out, workspace, dev_status)
+    n = 2 * cfg.batch * cfg.heads * cfg.head_dim
+    q, o, ws, status, on = _over(stream, cache, ((q, _BF16, n), (out, _BF16, n), (workspace, None, 0), (dev_status, None, 4)))
     _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), cache.ref, layer, q, o, ws, 0 if ws is None else workspace.nbytes, status, on),
            "bt_block_decode_attn_kv4")
 
 
 def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, out, workspace, dev_status=None, stream=None):
     """Quantise and append the new block's row, then attend over the 4-bit cache including it, in one launch."""
-    q, k, v, o, ws, status, on = _over(stream, cache, q, k_new, v_new, out, workspace, dev_status)
+    n = 2 * cfg.batch * cfg.heads * cfg.head_dim
+    q, k, v, o, ws, status, on = _over(stream, cache, ((q, _BF16, n), (k_new, _BF16, n), (v_new, _BF16, n), (out, _BF16, n), (workspace, None, 0),
+                                                       (dev_status, None, 4)))
     _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), cache.ref, layer, q, k, v, o, ws, 0 if ws is None else workspace.nbytes, status, on),
            "bt_block_decode_step_kv4")
 
@@ -526,7 +539,9 @@ def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, 
 def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, bias, q_out, n_rows=None, dev_status=None, stream=None):
     """bt_block_qkv_project_append into the 4-bit cache."""
     n_rows = x.shape[1] if n_rows is None else n_rows
-    x, w, b, q, status, on = _over(stream, cache, x, w_qkv, bias, q_out, dev_status)
+    D = cfg.heads * cfg.head_dim
+    n = 2 * cfg.batch * n_rows * D
+    x, w, b, q, status, on = _over(stream, cache, ((x, _BF16, n), (w_qkv, _BF16, 6 * D * D), (bias, _BF16, 6 * D), (q_out, _BF16, n), (dev_status, None, 4)))
     _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), cache.ref, layer, x, _i32(n_rows), w, b, q, status, on),
            "bt_block_qkv_project_append_kv4")
 
@@ -534,13 +549,18 @@ def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, 
 def bt_rows_quantize_i8(x, x8, steps, stream=None):
     """Rows of x bf16 [..., n_cols] -> int8 of the same shape and fp32 steps [...]."""
     n_cols = x.shape[-1]
-    rows, out, st, on = _over(stream, None, x, x8, steps)
-    _check(_lib.bt_rows_quantize_i8(rows, x.numel() // max(n_cols, 1), _i32(n_cols), out, st, on), "bt_rows_quantize_i8")
+    n = x.numel()
+    n_rows = n // max(n_cols, 1)
+    rows, out, st, on = _over(stream, None, ((x, _BF16, 0), (x8, _I8, n), (steps, _F32, 4 * n_rows)))
+    _check(_lib.bt_rows_quantize_i8(rows, n_rows, _i32(n_cols), out, st, on), "bt_rows_quantize_i8")
 
 
 def bt_prefix_project_i8(cfg, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status=None, stream=None):
     """bt_prefix_project of 8-bit operands and their steps."""
-    x, xs, w, ws, b, out, status, on = _over(stream, None, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status)
+    B, D = cfg.batch, cfg.heads * cfg.head_dim
+    n = cfg.prefix_len * D
+    x, xs, w, ws, b, out, status, on = _over(stream, None, ((ctx8, _I8, B * D), (ctx_steps, _F32, 4 * B), (w8, _I8, n * D), (w_steps, _F32, 4 * n),
+                                                            (bias, _BF16, 2 * n), (prefix_out, _BF16, 2 * B * n), (dev_status, None, 4)))
     _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), x, xs, w, ws, b, out, status, on), "bt_prefix_project_i8")
 
 
@@ -548,7 +568,12 @@ def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w
                                    stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    x, xs, w, ws, b, q, status, *_, on = _over(stream, None, x8, x_steps, w8, w_steps, bias, q_out, dev_status, cache.k, cache.v, cache.len)
+    B, D = cfg.batch, cfg.heads * cfg.head_dim
+    rows, lens = B * n_rows, cfg.n_layers * B
+    held = 2 * lens * cfg.max_blocks * D
+    x, xs, w, ws, b, q, status, *_, on = _over(stream, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
+                                                              (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D), (dev_status, None, 4),
+                                                              (cache.k, _BF16, held), (cache.v, _BF16, held), (cache.len, _I32, 4 * lens)))
     _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
            "bt_block_qkv_project_append_i8")
 
@@ -557,7 +582,15 @@ def bt_local_qkv_project_append_i8(cfg, cache: LocalCache, layer, x8, x_steps, w
                                    reset_mask=None, dev_status=None, stream=None):
     """bt_local_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    x, xs, w, ws, b, q, mask, status, *_, on = _over(stream, None, x8, x_steps, w8, w_steps, bias, q_out, reset_mask, dev_status, cache.kv, cache.len)
+    if reset_mask is not None and reset_mask.element_size() != 1:
+        raise BtError(BT_ERR_UNSUPPORTED, f"a mask of {reset_mask.dtype}")
+    B, D = cfg.batch, cfg.heads * cfg.head_dim
+    rows, lens = B * n_rows, cfg.n_layers * B
+    x, xs, w, ws, b, q, mask, status, *_, on = _over(stream, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D),
+                                                                    (w_steps, _F32, 12 * D), (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D),
+                                                                    (reset_mask, None, B), (dev_status, None, 4),
+                                                                    (cache.kv, _BF16, 4 * lens * (cfg.prefix_len + cfg.block_len) * D),
+                                                                    (cache.len, _I32, 4 * lens)))
     _check(_lib.bt_local_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, x, xs, _i32(n_rows), w, ws, b,
                                                1 if reset_first else 0, mask, q, status, on), "bt_local_qkv_project_append_i8")
 
@@ -566,7 +599,10 @@ def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_s
                                        stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps into the 4-bit cache."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    x, xs, w, ws, b, q, status, on = _over(stream, cache, x8, x_steps, w8, w_steps, bias, q_out, dev_status)
+    D = cfg.heads * cfg.head_dim
+    rows = cfg.batch * n_rows
+    x, xs, w, ws, b, q, status, on = _over(stream, cache, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
+                                                           (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D), (dev_status, None, 4)))
     _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), cache.ref, layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
            "bt_block_qkv_project_append_i8_kv4")
 

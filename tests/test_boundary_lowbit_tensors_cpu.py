@@ -117,3 +117,56 @@ def test_rows_under_a_given_stride_are_there(bt, lib):
         refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, k, **{stride: N - 1, n: N})
         for wrapped in (2 ** 64 + N, N - 2 ** 64):                      # no numbers of 64 bits
             refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, k, k, **{stride: wrapped, n: 5})
+
+
+def every_call(bt, n=1):
+    """(call, its tensors in order) of every call over the low-bit operators that takes packed tensors."""
+    cfg, D, P = config(bt), H * HD, 2
+    cache, block, local = kv4(bt, cfg), bt.BlockCache(cfg, device="cpu"), bt.LocalCache(cfg, device="cpu")
+    for c in (block, local):
+        for name in ("k", "v", "kv", "len"):
+            if hasattr(c, name):
+                setattr(c, name, OnDevice(getattr(c, name)))
+    q, x, w, bias, qo, st = t(B, H, HD), t(B, n, D), t(3 * D, D), t(3 * D), t(B, H, n, HD), t(1, dtype=torch.int32)
+    x8, w8, xs, ws = t(B, n, D, dtype=torch.int8), t(3 * D, D, dtype=torch.int8), t(B, n, dtype=torch.float32), t(3 * D, dtype=torch.float32)
+    c8, cs, p8, ps, pb, po = t(B, D, dtype=torch.int8), t(B, dtype=torch.float32), t(P * D, D, dtype=torch.int8), t(P * D, dtype=torch.float32), t(P * D), t(B, P, D)
+    space, mask = t(bt.bt_workspace_bytes_kv4(cfg), dtype=torch.uint8), t(B, dtype=torch.uint8)
+    return [
+        (lambda a, o, s: bt.bt_block_decode_attn_kv4(cfg, cache, 1, a, o, space, dev_status=s), [q, q, st]),
+        (lambda a, k, v, o, s: bt.bt_block_decode_step_kv4(cfg, cache, 1, a, k, v, o, space, dev_status=s), [q, q, q, q, st]),
+        (lambda a, b, c, d, s: bt.bt_block_qkv_project_append_kv4(cfg, cache, 1, a, b, c, d, n_rows=n, dev_status=s), [x, w, bias, qo, st]),
+        (lambda b, c: bt.bt_rows_quantize_i8(x, b, c), [x8, xs]),
+        (lambda *a: bt.bt_prefix_project_i8(cfg, *a), [c8, cs, p8, ps, pb, po, st]),
+        (lambda *a: bt.bt_block_qkv_project_append_i8(cfg, block, 1, *a[:-1], n_rows=n, dev_status=a[-1]), [x8, xs, w8, ws, bias, qo, st]),
+        (lambda *a: bt.bt_local_qkv_project_append_i8(cfg, local, 1, *a[:-2], n_rows=n, reset_mask=a[-2], dev_status=a[-1]), [x8, xs, w8, ws, bias, qo, mask, st]),
+        (lambda *a: bt.bt_block_qkv_project_append_i8_kv4(cfg, cache, 1, *a[:-1], n_rows=n, dev_status=a[-1]), [x8, xs, w8, ws, bias, qo, st]),
+    ]
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_every_tensor_is_as_large_as_the_call_takes(bt, lib, n):
+    """One element less than the call reads or writes is refused; more than that is not (a buffer for the most rows serves fewer)."""
+    for call, args in every_call(bt, n):
+        passed(lib, call, *args)
+        for i in range(len(args)):
+            less, more = t(args[i].numel() - 1, dtype=args[i].dtype), t(args[i].numel() + 1, dtype=args[i].dtype)
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, *args[:i], less, *args[i + 1:])
+            passed(lib, call, *args[:i], more, *args[i + 1:])
+
+
+def test_every_tensor_has_its_type(bt, lib):
+    for call, args in every_call(bt):
+        for i, arg in enumerate(args):
+            if arg.dtype is torch.int32:
+                continue                                     # the status word: any four bytes
+            for kind in (torch.float32, torch.float16, torch.int8, torch.uint8, torch.bfloat16, torch.int64):
+                if kind is arg.dtype or (arg.dtype is torch.uint8 and kind is torch.int8):
+                    continue
+                refused(bt, lib, bt.BT_ERR_UNSUPPORTED, call, *args[:i], t(*arg.shape, dtype=kind), *args[i + 1:])
+    x8, steps = t(4, 64, dtype=torch.int8), t(4, dtype=torch.float32)
+    refused(bt, lib, bt.BT_ERR_UNSUPPORTED, bt.bt_rows_quantize_i8, t(4, 64, dtype=torch.float32), x8, steps)
+    rows = t(B, H, 1, HD, dtype=torch.float32)
+    cfg = config(bt)
+    for call in (bt.bt_block_kv4_append, bt.bt_block_kv4_read):
+        for k, v in ((rows, t(B, H, 1, HD)), (t(B, H, 1, HD), rows)):
+            refused(bt, lib, bt.BT_ERR_UNSUPPORTED, call, cfg, kv4(bt, cfg), 0, k, v)
