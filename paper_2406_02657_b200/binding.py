@@ -148,10 +148,11 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
-def _over(stream, cache, wanted, packed=True):
+def _over(stream, cfg, cache, wanted, packed=True):
     """The addresses of a call's tensors, and its stream.  wanted: (tensor or None, the type of its elements or None for any, the bytes that the call
     takes of it), of which the first has to be there.  The tensors, and a 4-bit cache or None, have to be on the current device: the kernels run
-    there, and would read another's memory, or the host's, as their own; packed, as a call knows no strides; of their type; and no smaller."""
+    there, and would read another's memory, or the host's, as their own; packed, as a call knows no strides; of their type; and no smaller.  The
+    4-bit cache has to be one of the config's."""
     first = wanted[0][0]
     if first is None:
         raise BtError(BT_ERR_NULL, "tensor")
@@ -160,6 +161,8 @@ def _over(stream, cache, wanted, packed=True):
         raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {first.device}, not on the current device")
     if cache is not None and cache.device != device:
         raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {first.device}, cache on {cache.kv.device}")
+    if cache is not None and ((cfg.batch, cfg.heads, cfg.head_dim, cfg.max_blocks) != cache.sizes or cfg.n_layers > cache.n_layers):
+        raise BtError(BT_ERR_SHAPE, f"a cache of shape {tuple(cache.kv.shape)}, not of the config")
     found = []
     for t, kind, size in wanted:
         if t is None:
@@ -267,7 +270,9 @@ class BlockCacheKV4:
         shape = (cfg.n_layers, cfg.batch, cfg.heads, -(-cfg.max_blocks // KV4_TILE_ROWS), cfg.head_dim // 64, KV4_TILE_BYTES)
         self.kv = torch.zeros(shape, dtype=torch.uint8, device=device) if kv is None else kv
         self.len = torch.zeros((cfg.n_layers, cfg.batch), dtype=torch.int32, device=device) if length is None else length
-        assert self.kv.shape == shape and self.kv.is_contiguous() and self.len.is_contiguous()
+        assert self.kv.shape == shape and self.kv.is_contiguous() and self.kv.dtype is torch.uint8
+        assert self.len.shape == shape[:2] and self.len.is_contiguous() and self.len.dtype is torch.int32
+        self.sizes, self.n_layers = (cfg.batch, cfg.heads, cfg.head_dim, cfg.max_blocks), cfg.n_layers
         self.device = self.kv.get_device()
         assert self.len.get_device() == self.device
         self.c = bt_block_cache_kv4(self.kv.data_ptr(), self.len.data_ptr())
@@ -507,7 +512,7 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
     """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
     slabs of k_new, v_new (a bf16 block cache has N_max), theirs where it is not given."""
     n_new, src_stride = _slabs(cfg, k_new, v_new, n_new, src_stride)
-    k, v, status, on = _over(stream, cache, ((k_new, _BF16, 0), (v_new, _BF16, 0), (dev_status, None, 4)), packed=False)
+    k, v, status, on = _over(stream, cfg, cache, ((k_new, _BF16, 0), (v_new, _BF16, 0), (dev_status, None, 4)), packed=False)
     _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), cache.ref, layer, k, v, _i32(n_new), src_stride, 1 if reset_first else 0, status, on),
            "bt_block_kv4_append")
 
@@ -515,14 +520,14 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
     """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
     n_rows, dst_stride = _slabs(cfg, k_out, v_out, n_rows, dst_stride)
-    k, v, on = _over(stream, cache, ((k_out, _BF16, 0), (v_out, _BF16, 0)), packed=False)
+    k, v, on = _over(stream, cfg, cache, ((k_out, _BF16, 0), (v_out, _BF16, 0)), packed=False)
     _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), cache.ref, layer, _i32(first), _i32(n_rows), k, v, dst_stride, on), "bt_block_kv4_read")
 
 
 def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace, dev_status=None, stream=None):
     """Decode attention over the 4-bit cache."""
     n = 2 * cfg.batch * cfg.heads * cfg.head_dim
-    q, o, ws, status, on = _over(stream, cache, ((q, _BF16, n), (out, _BF16, n), (workspace, None, 0), (dev_status, None, 4)))
+    q, o, ws, status, on = _over(stream, cfg, cache, ((q, _BF16, n), (out, _BF16, n), (workspace, None, 0), (dev_status, None, 4)))
     _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), cache.ref, layer, q, o, ws, 0 if ws is None else workspace.nbytes, status, on),
            "bt_block_decode_attn_kv4")
 
@@ -530,7 +535,7 @@ def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace
 def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, out, workspace, dev_status=None, stream=None):
     """Quantise and append the new block's row, then attend over the 4-bit cache including it, in one launch."""
     n = 2 * cfg.batch * cfg.heads * cfg.head_dim
-    q, k, v, o, ws, status, on = _over(stream, cache, ((q, _BF16, n), (k_new, _BF16, n), (v_new, _BF16, n), (out, _BF16, n), (workspace, None, 0),
+    q, k, v, o, ws, status, on = _over(stream, cfg, cache, ((q, _BF16, n), (k_new, _BF16, n), (v_new, _BF16, n), (out, _BF16, n), (workspace, None, 0),
                                                        (dev_status, None, 4)))
     _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), cache.ref, layer, q, k, v, o, ws, 0 if ws is None else workspace.nbytes, status, on),
            "bt_block_decode_step_kv4")
@@ -541,7 +546,7 @@ def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, 
     n_rows = x.shape[1] if n_rows is None else n_rows
     D = cfg.heads * cfg.head_dim
     n = 2 * cfg.batch * n_rows * D
-    x, w, b, q, status, on = _over(stream, cache, ((x, _BF16, n), (w_qkv, _BF16, 6 * D * D), (bias, _BF16, 6 * D), (q_out, _BF16, n), (dev_status, None, 4)))
+    x, w, b, q, status, on = _over(stream, cfg, cache, ((x, _BF16, n), (w_qkv, _BF16, 6 * D * D), (bias, _BF16, 6 * D), (q_out, _BF16, n), (dev_status, None, 4)))
     _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), cache.ref, layer, x, _i32(n_rows), w, b, q, status, on),
            "bt_block_qkv_project_append_kv4")
 
@@ -551,7 +556,7 @@ def bt_rows_quantize_i8(x, x8, steps, stream=None):
     n_cols = x.shape[-1]
     n = x.numel()
     n_rows = n // max(n_cols, 1)
-    rows, out, st, on = _over(stream, None, ((x, _BF16, 0), (x8, _I8, n), (steps, _F32, 4 * n_rows)))
+    rows, out, st, on = _over(stream, None, None, ((x, _BF16, 0), (x8, _I8, n), (steps, _F32, 4 * n_rows)))
     _check(_lib.bt_rows_quantize_i8(rows, n_rows, _i32(n_cols), out, st, on), "bt_rows_quantize_i8")
 
 
@@ -559,7 +564,7 @@ def bt_prefix_project_i8(cfg, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, de
     """bt_prefix_project of 8-bit operands and their steps."""
     B, D = cfg.batch, cfg.heads * cfg.head_dim
     n = cfg.prefix_len * D
-    x, xs, w, ws, b, out, status, on = _over(stream, None, ((ctx8, _I8, B * D), (ctx_steps, _F32, 4 * B), (w8, _I8, n * D), (w_steps, _F32, 4 * n),
+    x, xs, w, ws, b, out, status, on = _over(stream, None, None, ((ctx8, _I8, B * D), (ctx_steps, _F32, 4 * B), (w8, _I8, n * D), (w_steps, _F32, 4 * n),
                                                             (bias, _BF16, 2 * n), (prefix_out, _BF16, 2 * B * n), (dev_status, None, 4)))
     _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), x, xs, w, ws, b, out, status, on), "bt_prefix_project_i8")
 
@@ -571,7 +576,7 @@ def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w
     B, D = cfg.batch, cfg.heads * cfg.head_dim
     rows, lens = B * n_rows, cfg.n_layers * B
     held = 2 * lens * cfg.max_blocks * D
-    x, xs, w, ws, b, q, status, *_, on = _over(stream, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
+    x, xs, w, ws, b, q, status, *_, on = _over(stream, None, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
                                                               (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D), (dev_status, None, 4),
                                                               (cache.k, _BF16, held), (cache.v, _BF16, held), (cache.len, _I32, 4 * lens)))
     _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
@@ -586,7 +591,7 @@ def bt_local_qkv_project_append_i8(cfg, cache: LocalCache, layer, x8, x_steps, w
         raise BtError(BT_ERR_UNSUPPORTED, f"a mask of {reset_mask.dtype}")
     B, D = cfg.batch, cfg.heads * cfg.head_dim
     rows, lens = B * n_rows, cfg.n_layers * B
-    x, xs, w, ws, b, q, mask, status, *_, on = _over(stream, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D),
+    x, xs, w, ws, b, q, mask, status, *_, on = _over(stream, None, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D),
                                                                     (w_steps, _F32, 12 * D), (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D),
                                                                     (reset_mask, None, B), (dev_status, None, 4),
                                                                     (cache.kv, _BF16, 4 * lens * (cfg.prefix_len + cfg.block_len) * D),
@@ -601,7 +606,7 @@ def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_s
     n_rows = x8.shape[1] if n_rows is None else n_rows
     D = cfg.heads * cfg.head_dim
     rows = cfg.batch * n_rows
-    x, xs, w, ws, b, q, status, on = _over(stream, cache, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
+    x, xs, w, ws, b, q, status, on = _over(stream, cfg, cache, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
                                                            (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D), (dev_status, None, 4)))
     _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), cache.ref, layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
            "bt_block_qkv_project_append_i8_kv4")

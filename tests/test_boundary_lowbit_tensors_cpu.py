@@ -170,3 +170,49 @@ def test_every_tensor_has_its_type(bt, lib):
     for call in (bt.bt_block_kv4_append, bt.bt_block_kv4_read):
         for k, v in ((rows, t(B, H, 1, HD)), (t(B, H, 1, HD), rows)):
             refused(bt, lib, bt.BT_ERR_UNSUPPORTED, call, cfg, kv4(bt, cfg), 0, k, v)
+
+
+def test_caches_are_the_config_s(bt, lib):
+    """A cache made for another config is refused: other sizes, or fewer layers; one that differs in what the cache does not depend on is taken."""
+    cfg, D = config(bt), H * HD
+    q, x, w, rows, x8, xs = t(3, 4, 2 * HD), t(3, 1, D), t(3 * D, D), t(B, H, 1, HD), t(B, 1, D, dtype=torch.int8), t(B, dtype=torch.float32)
+    w8, ws, qo, space = t(3 * D, D, dtype=torch.int8), t(3 * D, dtype=torch.float32), t(B, H, 1, HD), t(1 << 20, dtype=torch.uint8)
+
+    def calls(cache):
+        return ((bt.bt_block_kv4_append, cfg, cache, 0, rows, rows), (bt.bt_block_kv4_read, cfg, cache, 0, rows, rows),
+                (bt.bt_block_decode_attn_kv4, cfg, cache, 0, q, q, space), (bt.bt_block_decode_step_kv4, cfg, cache, 0, q, q, q, q, space),
+                (bt.bt_block_qkv_project_append_kv4, cfg, cache, 0, x, w, None, qo),
+                (bt.bt_block_qkv_project_append_i8_kv4, cfg, cache, 0, x8, xs, w8, ws, None, qo))
+
+    for other in (dict(batch=B - 1), dict(batch=B + 1), dict(heads=H + 1), dict(head_dim=128), dict(max_blocks=N - 1), dict(max_blocks=N + 1), dict(n_layers=1)):
+        for call, *args in calls(kv4(bt, config(bt, **other))):
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, *args)
+    for other in (dict(), dict(n_layers=3), dict(block_len=7), dict(prefix_len=1), dict(decode_splits=5), dict(softmax_scale=0.5)):
+        for call, *args in calls(kv4(bt, config(bt, **other))):
+            passed(lib, call, *args)
+
+
+def test_caches_of_16_bits_hold_what_integers_are_projected_into(bt, lib):
+    cfg, D = config(bt), H * HD
+    x8, xs, w8, ws, qo = t(B, 1, D, dtype=torch.int8), t(B, dtype=torch.float32), t(3 * D, D, dtype=torch.int8), t(3 * D, dtype=torch.float32), t(B, H, 1, HD)
+    for other, code in ((dict(), 0), (dict(n_layers=3), 0), (dict(batch=B - 1), bt.BT_ERR_SHAPE), (dict(n_layers=1), bt.BT_ERR_SHAPE),
+                        (dict(max_blocks=N - 1, block_len=3), bt.BT_ERR_SHAPE)):
+        made = config(bt, **other)
+        block, local = bt.BlockCache(made, device="cpu"), bt.LocalCache(made, device="cpu")
+        block.k, block.v, block.len, local.kv, local.len = (OnDevice(x) for x in (block.k, block.v, block.len, local.kv, local.len))
+        for call, cache in ((bt.bt_block_qkv_project_append_i8, block), (bt.bt_local_qkv_project_append_i8, local)):
+            if code:
+                refused(bt, lib, code, call, cfg, cache, 0, x8, xs, w8, ws, None, qo)
+            else:
+                passed(lib, call, cfg, cache, 0, x8, xs, w8, ws, None, qo)
+            # [B,D]: its last axis is not taken for a number of rows
+            refused(bt, lib, bt.BT_ERR_SHAPE, call, cfg, cache, 0, t(B, D, dtype=torch.int8), xs, w8, ws, None, qo)
+
+
+def test_cache_tensors_are_what_they_should_be(bt):
+    cfg = config(bt)
+    good = bt.BlockCacheKV4(cfg, device="cpu")
+    bt.BlockCacheKV4(cfg, device="cpu", kv=good.kv, length=good.len)
+    for bad in (dict(kv=good.kv.to(torch.int8)), dict(length=good.len.long()), dict(length=good.len[:1]), dict(length=good.len.reshape(-1))):
+        with pytest.raises(AssertionError):
+            bt.BlockCacheKV4(cfg, device="cpu", **bad)
