@@ -38,6 +38,19 @@ class bt_config(ctypes.Structure):
                 ("n_layers", ctypes.c_int32), ("decode_splits", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("prefill_plain", ctypes.c_int32)]
 
+    # What the calls compare tensors and caches with, worked out when it is first asked for and again when a field has changed: reading five fields
+    # takes a small call 0.2 us of host time.
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        self.__dict__.clear()
+
+    def __getattr__(self, name):
+        if name not in ("sizes", "local_sizes", "model_dim"):
+            raise AttributeError(name)
+        B, H, hd = self.batch, self.heads, self.head_dim
+        self.__dict__.update(sizes=(B, H, hd, self.max_blocks), local_sizes=(B, H, hd, self.prefix_len + self.block_len), model_dim=H * hd)
+        return self.__dict__[name]
+
 
 class bt_block_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("len", ctypes.c_void_p)]
@@ -148,40 +161,54 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
-def _over(stream, cfg, cache, wanted, packed=True):
-    """The addresses of a call's tensors, and its stream.  wanted: (tensor or None, the type of its elements or None for any, the bytes that the call
-    takes of it), of which the first has to be there.  The tensors, and a 4-bit cache or None, have to be on the current device: the kernels run
+def _over(stream, cfg, cache, sizes, status, wanted, packed=True):
+    """The addresses of a call's tensors and status word, and its stream.  wanted: (tensor or None, the type of its elements, the bytes that the call
+    takes of it), of which the first has to be there.  The tensors, and a cache or None, have to be on the current device: the kernels run
     there, and would read another's memory, or the host's, as their own; packed, as a call knows no strides; of their type; and no smaller.  The
-    4-bit cache has to be one of the config's."""
+    cache has to be one of the config's."""
     first = wanted[0][0]
     if first is None:
         raise BtError(BT_ERR_NULL, "tensor")
     device = first.get_device()
     if device < 0 or device != _device():
         raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {first.device}, not on the current device")
-    if cache is not None and cache.device != device:
-        raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {first.device}, cache on {cache.kv.device}")
-    if cache is not None and ((cfg.batch, cfg.heads, cfg.head_dim, cfg.max_blocks) != cache.sizes or cfg.n_layers > cache.n_layers):
-        raise BtError(BT_ERR_SHAPE, f"a cache of shape {tuple(cache.kv.shape)}, not of the config")
+    if cache is not None:
+        if cache.device != device:
+            raise BtError(BT_ERR_UNSUPPORTED, f"tensor on {first.device}, cache elsewhere or not of packed bf16 rows and int32 lengths")
+        if cache.sizes != sizes or cfg.n_layers > cache.n_layers:
+            raise BtError(BT_ERR_SHAPE, f"a cache of {cache.n_layers} layers of {cache.sizes}, not of the config")
     found = []
     for t, kind, size in wanted:
         if t is None:
             found.append(None)
-        elif t.get_device() != device:
-            raise BtError(BT_ERR_UNSUPPORTED, f"tensors on {first.device} and {t.device}")
-        elif packed and not t.is_contiguous():
-            raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of strides {tuple(t.stride())} and shape {tuple(t.shape)}")
-        elif kind is not None and t.dtype is not kind:
-            raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of {t.dtype} for one of {kind}")
-        elif t.nbytes < size:
-            raise BtError(BT_ERR_SHAPE, f"a tensor of shape {tuple(t.shape)} for {size} bytes")
-        else:
+        elif t.dtype is kind and t.nbytes >= size and t.is_contiguous() and t.get_device() == device:
             found.append(t.data_ptr())
+        else:
+            found.append(_unlike(t, kind, size, first, packed))
+    found.append(status if status is None else _unlike(status, status.dtype, 4, first, True))
     found.append(_raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream))
     return found
 
 
-_BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
+def _type_of(t):
+    """Whatever its elements are (a workspace, a mask)."""
+    return None if t is None else t.dtype
+
+
+def _unlike(t, kind, size, first, packed):
+    """A tensor's address, or what is wrong with it."""
+    if t.get_device() != first.get_device():
+        raise BtError(BT_ERR_UNSUPPORTED, f"tensors on {first.device} and {t.device}")
+    if packed and not t.is_contiguous():
+        raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of strides {tuple(t.stride())} and shape {tuple(t.shape)}")
+    if t.dtype is not kind:
+        raise BtError(BT_ERR_UNSUPPORTED, f"a tensor of {t.dtype} for one of {kind}")
+    if t.nbytes < size:
+        raise BtError(BT_ERR_SHAPE, f"a tensor of shape {tuple(t.shape)} for {size} bytes")
+    return t.data_ptr()
+
+
+_BF16, _F32, _I8 = torch.bfloat16, torch.float32, torch.int8
 
 
 def _slabs(cfg, k, v, n, stride):
@@ -202,7 +229,8 @@ def _slabs(cfg, k, v, n, stride):
         raise BtError(BT_ERR_SHAPE, f"rows of shapes {tuple(shape)} and {tuple(v.shape)}, not both [B,H,n,hd]")
     rows = shape[2]
     stride = rows if k.is_contiguous() and v.is_contiguous() else _slab_stride(k, v)
-    if (cfg.batch, cfg.heads, rows, cfg.head_dim) != shape or (n is not None and n > rows):
+    B, H, hd, _ = cfg.sizes
+    if (B, H, rows, hd) != shape or (n is not None and n > rows):
         raise BtError(BT_ERR_SHAPE, f"rows of shape {tuple(shape)} for {cfg.batch} sequences, {cfg.heads} heads of {cfg.head_dim}, {n} rows")
     return rows if n is None else n, stride
 
@@ -237,6 +265,13 @@ def make_config(batch, heads, head_dim, block_len, prefix_len, max_blocks, n_lay
                      softmax_scale, prefill_plain)
 
 
+def _home(rows, kind, lengths):
+    """The device of a cache's tensors; none (-2) where they are on several, or not what the kernels take them for."""
+    device = lengths.get_device()
+    fine = lengths.dtype is torch.int32 and lengths.is_contiguous() and lengths.numel() >= rows[0].shape[0] * rows[0].shape[1]
+    return device if fine and all(t.dtype is kind and t.get_device() == device for t in rows) else -2
+
+
 class BlockCache:
     """Caller-owned block KV cache: k, v bf16 [layers,B,H,N_max,hd], len int32 [layers,B]."""
 
@@ -246,6 +281,7 @@ class BlockCache:
         self.v = torch.zeros(shape, dtype=torch.bfloat16, device=device) if v is None else v
         self.len = torch.zeros((cfg.n_layers, cfg.batch), dtype=torch.int32, device=device) if length is None else length
         assert self.k.shape == shape and self.v.shape == shape and self.k.is_contiguous() and self.v.is_contiguous()
+        self.sizes, self.n_layers, self.device = cfg.sizes, cfg.n_layers, _home((self.k, self.v), torch.bfloat16, self.len)
         self.c = bt_block_cache(self.k.data_ptr(), self.v.data_ptr(), self.len.data_ptr())
 
 
@@ -257,6 +293,7 @@ class LocalCache:
         self.kv = torch.zeros((cfg.n_layers, cfg.batch, cfg.heads, cap, 2, cfg.head_dim), dtype=torch.bfloat16,
                               device=device)
         self.len = torch.zeros((cfg.n_layers, cfg.batch), dtype=torch.int32, device=device)
+        self.sizes, self.n_layers, self.device = cfg.local_sizes, cfg.n_layers, _home((self.kv,), torch.bfloat16, self.len)
         self.c = bt_local_cache(self.kv.data_ptr(), self.len.data_ptr())
 
 
@@ -272,8 +309,7 @@ class BlockCacheKV4:
         self.len = torch.zeros((cfg.n_layers, cfg.batch), dtype=torch.int32, device=device) if length is None else length
         assert self.kv.shape == shape and self.kv.is_contiguous() and self.kv.dtype is torch.uint8
         assert self.len.shape == shape[:2] and self.len.is_contiguous() and self.len.dtype is torch.int32
-        self.sizes, self.n_layers = (cfg.batch, cfg.heads, cfg.head_dim, cfg.max_blocks), cfg.n_layers
-        self.device = self.kv.get_device()
+        self.sizes, self.n_layers, self.device = cfg.sizes, cfg.n_layers, _home((self.kv,), torch.uint8, self.len)
         assert self.len.get_device() == self.device
         self.c = bt_block_cache_kv4(self.kv.data_ptr(), self.len.data_ptr())
         self.ref = ctypes.byref(self.c)
@@ -512,42 +548,44 @@ def bt_block_kv4_append(cfg, cache: BlockCacheKV4, layer, k_new, v_new, n_new=No
     """Quantise n_new rows into the 4-bit cache, behind the rows there are or (reset_first) from row 0.  src_stride: rows between the
     slabs of k_new, v_new (a bf16 block cache has N_max), theirs where it is not given."""
     n_new, src_stride = _slabs(cfg, k_new, v_new, n_new, src_stride)
-    k, v, status, on = _over(stream, cfg, cache, ((k_new, _BF16, 0), (v_new, _BF16, 0), (dev_status, None, 4)), packed=False)
-    _check(_lib.bt_block_kv4_append(ctypes.byref(cfg), cache.ref, layer, k, v, _i32(n_new), src_stride, 1 if reset_first else 0, status, on),
+    k, v, status, on = _over(stream, cfg, cache, cfg.sizes, dev_status, ((k_new, _BF16, 0), (v_new, _BF16, 0)), packed=False)
+    _check(_lib.bt_block_kv4_append(cfg, cache.ref, layer, k, v, _i32(n_new), src_stride, 1 if reset_first else 0, status, on),
            "bt_block_kv4_append")
 
 
 def bt_block_kv4_read(cfg, cache: BlockCacheKV4, layer, k_out, v_out, first=0, n_rows=None, dst_stride=None, stream=None):
     """Rows first .. of the 4-bit cache as bf16 into rows 0 .. of k_out, v_out [B,H,n,hd]; rows that the cache has not stay as they are."""
     n_rows, dst_stride = _slabs(cfg, k_out, v_out, n_rows, dst_stride)
-    k, v, on = _over(stream, cfg, cache, ((k_out, _BF16, 0), (v_out, _BF16, 0)), packed=False)
-    _check(_lib.bt_block_kv4_read(ctypes.byref(cfg), cache.ref, layer, _i32(first), _i32(n_rows), k, v, dst_stride, on), "bt_block_kv4_read")
+    k, v, _, on = _over(stream, cfg, cache, cfg.sizes, None, ((k_out, _BF16, 0), (v_out, _BF16, 0)), packed=False)
+    _check(_lib.bt_block_kv4_read(cfg, cache.ref, layer, _i32(first), _i32(n_rows), k, v, dst_stride, on), "bt_block_kv4_read")
 
 
 def bt_block_decode_attn_kv4(cfg, cache: BlockCacheKV4, layer, q, out, workspace, dev_status=None, stream=None):
     """Decode attention over the 4-bit cache."""
-    n = 2 * cfg.batch * cfg.heads * cfg.head_dim
-    q, o, ws, status, on = _over(stream, cfg, cache, ((q, _BF16, n), (out, _BF16, n), (workspace, None, 0), (dev_status, None, 4)))
-    _check(_lib.bt_block_decode_attn_kv4(ctypes.byref(cfg), cache.ref, layer, q, o, ws, 0 if ws is None else workspace.nbytes, status, on),
+    n = 2 * cfg.batch * cfg.model_dim
+    wanted = (q, _BF16, n), (out, _BF16, n), (workspace, _type_of(workspace), 0)
+    q, o, ws, status, on = _over(stream, cfg, cache, cfg.sizes, dev_status, wanted)
+    _check(_lib.bt_block_decode_attn_kv4(cfg, cache.ref, layer, q, o, ws, 0 if ws is None else workspace.nbytes, status, on),
            "bt_block_decode_attn_kv4")
 
 
 def bt_block_decode_step_kv4(cfg, cache: BlockCacheKV4, layer, q, k_new, v_new, out, workspace, dev_status=None, stream=None):
     """Quantise and append the new block's row, then attend over the 4-bit cache including it, in one launch."""
-    n = 2 * cfg.batch * cfg.heads * cfg.head_dim
-    q, k, v, o, ws, status, on = _over(stream, cfg, cache, ((q, _BF16, n), (k_new, _BF16, n), (v_new, _BF16, n), (out, _BF16, n), (workspace, None, 0),
-                                                       (dev_status, None, 4)))
-    _check(_lib.bt_block_decode_step_kv4(ctypes.byref(cfg), cache.ref, layer, q, k, v, o, ws, 0 if ws is None else workspace.nbytes, status, on),
+    n = 2 * cfg.batch * cfg.model_dim
+    wanted = (q, _BF16, n), (k_new, _BF16, n), (v_new, _BF16, n), (out, _BF16, n), (workspace, _type_of(workspace), 0)
+    q, k, v, o, ws, status, on = _over(stream, cfg, cache, cfg.sizes, dev_status, wanted)
+    _check(_lib.bt_block_decode_step_kv4(cfg, cache.ref, layer, q, k, v, o, ws, 0 if ws is None else workspace.nbytes, status, on),
            "bt_block_decode_step_kv4")
 
 
 def bt_block_qkv_project_append_kv4(cfg, cache: BlockCacheKV4, layer, x, w_qkv, bias, q_out, n_rows=None, dev_status=None, stream=None):
     """bt_block_qkv_project_append into the 4-bit cache."""
     n_rows = x.shape[1] if n_rows is None else n_rows
-    D = cfg.heads * cfg.head_dim
+    D = cfg.model_dim
     n = 2 * cfg.batch * n_rows * D
-    x, w, b, q, status, on = _over(stream, cfg, cache, ((x, _BF16, n), (w_qkv, _BF16, 6 * D * D), (bias, _BF16, 6 * D), (q_out, _BF16, n), (dev_status, None, 4)))
-    _check(_lib.bt_block_qkv_project_append_kv4(ctypes.byref(cfg), cache.ref, layer, x, _i32(n_rows), w, b, q, status, on),
+    wanted = (x, _BF16, n), (w_qkv, _BF16, 6 * D * D), (bias, _BF16, 6 * D), (q_out, _BF16, n)
+    x, w, b, q, status, on = _over(stream, cfg, cache, cfg.sizes, dev_status, wanted)
+    _check(_lib.bt_block_qkv_project_append_kv4(cfg, cache.ref, layer, x, _i32(n_rows), w, b, q, status, on),
            "bt_block_qkv_project_append_kv4")
 
 
@@ -556,30 +594,28 @@ def bt_rows_quantize_i8(x, x8, steps, stream=None):
     n_cols = x.shape[-1]
     n = x.numel()
     n_rows = n // max(n_cols, 1)
-    rows, out, st, on = _over(stream, None, None, ((x, _BF16, 0), (x8, _I8, n), (steps, _F32, 4 * n_rows)))
+    rows, out, st, _, on = _over(stream, None, None, None, None, ((x, _BF16, 0), (x8, _I8, n), (steps, _F32, 4 * n_rows)))
     _check(_lib.bt_rows_quantize_i8(rows, n_rows, _i32(n_cols), out, st, on), "bt_rows_quantize_i8")
 
 
 def bt_prefix_project_i8(cfg, ctx8, ctx_steps, w8, w_steps, bias, prefix_out, dev_status=None, stream=None):
     """bt_prefix_project of 8-bit operands and their steps."""
-    B, D = cfg.batch, cfg.heads * cfg.head_dim
+    B, D = cfg.batch, cfg.model_dim
     n = cfg.prefix_len * D
-    x, xs, w, ws, b, out, status, on = _over(stream, None, None, ((ctx8, _I8, B * D), (ctx_steps, _F32, 4 * B), (w8, _I8, n * D), (w_steps, _F32, 4 * n),
-                                                            (bias, _BF16, 2 * n), (prefix_out, _BF16, 2 * B * n), (dev_status, None, 4)))
-    _check(_lib.bt_prefix_project_i8(ctypes.byref(cfg), x, xs, w, ws, b, out, status, on), "bt_prefix_project_i8")
+    wanted = (ctx8, _I8, B * D), (ctx_steps, _F32, 4 * B), (w8, _I8, n * D), (w_steps, _F32, 4 * n), (bias, _BF16, 2 * n), (prefix_out, _BF16, 2 * B * n)
+    x, xs, w, ws, b, out, status, on = _over(stream, None, None, None, dev_status, wanted)
+    _check(_lib.bt_prefix_project_i8(cfg, x, xs, w, ws, b, out, status, on), "bt_prefix_project_i8")
 
 
 def bt_block_qkv_project_append_i8(cfg, cache: BlockCache, layer, x8, x_steps, w8, w_steps, bias, q_out, n_rows=None, dev_status=None,
                                    stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    B, D = cfg.batch, cfg.heads * cfg.head_dim
-    rows, lens = B * n_rows, cfg.n_layers * B
-    held = 2 * lens * cfg.max_blocks * D
-    x, xs, w, ws, b, q, status, *_, on = _over(stream, None, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
-                                                              (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D), (dev_status, None, 4),
-                                                              (cache.k, _BF16, held), (cache.v, _BF16, held), (cache.len, _I32, 4 * lens)))
-    _check(_lib.bt_block_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
+    rows, D = cfg.batch * n_rows, cfg.model_dim
+    wanted = ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D), (bias, _BF16, 6 * D),
+              (q_out, _BF16, 2 * rows * D))
+    x, xs, w, ws, b, q, status, on = _over(stream, cfg, cache, cfg.sizes, dev_status, wanted)
+    _check(_lib.bt_block_qkv_project_append_i8(cfg, cache.c, layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
            "bt_block_qkv_project_append_i8")
 
 
@@ -589,14 +625,11 @@ def bt_local_qkv_project_append_i8(cfg, cache: LocalCache, layer, x8, x_steps, w
     n_rows = x8.shape[1] if n_rows is None else n_rows
     if reset_mask is not None and reset_mask.element_size() != 1:
         raise BtError(BT_ERR_UNSUPPORTED, f"a mask of {reset_mask.dtype}")
-    B, D = cfg.batch, cfg.heads * cfg.head_dim
-    rows, lens = B * n_rows, cfg.n_layers * B
-    x, xs, w, ws, b, q, mask, status, *_, on = _over(stream, None, None, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D),
-                                                                    (w_steps, _F32, 12 * D), (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D),
-                                                                    (reset_mask, None, B), (dev_status, None, 4),
-                                                                    (cache.kv, _BF16, 4 * lens * (cfg.prefix_len + cfg.block_len) * D),
-                                                                    (cache.len, _I32, 4 * lens)))
-    _check(_lib.bt_local_qkv_project_append_i8(ctypes.byref(cfg), ctypes.byref(cache.c), layer, x, xs, _i32(n_rows), w, ws, b,
+    rows, D = cfg.batch * n_rows, cfg.model_dim
+    wanted = ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D), (bias, _BF16, 6 * D),
+              (q_out, _BF16, 2 * rows * D), (reset_mask, _type_of(reset_mask), cfg.batch))
+    x, xs, w, ws, b, q, mask, status, on = _over(stream, cfg, cache, cfg.local_sizes, dev_status, wanted)
+    _check(_lib.bt_local_qkv_project_append_i8(cfg, cache.c, layer, x, xs, _i32(n_rows), w, ws, b,
                                                1 if reset_first else 0, mask, q, status, on), "bt_local_qkv_project_append_i8")
 
 
@@ -604,11 +637,11 @@ def bt_block_qkv_project_append_i8_kv4(cfg, cache: BlockCacheKV4, layer, x8, x_s
                                        stream=None):
     """bt_block_qkv_project_append of 8-bit operands and their steps into the 4-bit cache."""
     n_rows = x8.shape[1] if n_rows is None else n_rows
-    D = cfg.heads * cfg.head_dim
-    rows = cfg.batch * n_rows
-    x, xs, w, ws, b, q, status, on = _over(stream, cfg, cache, ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D),
-                                                           (bias, _BF16, 6 * D), (q_out, _BF16, 2 * rows * D), (dev_status, None, 4)))
-    _check(_lib.bt_block_qkv_project_append_i8_kv4(ctypes.byref(cfg), cache.ref, layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
+    rows, D = cfg.batch * n_rows, cfg.model_dim
+    wanted = ((x8, _I8, rows * D), (x_steps, _F32, 4 * rows), (w8, _I8, 3 * D * D), (w_steps, _F32, 12 * D), (bias, _BF16, 6 * D),
+              (q_out, _BF16, 2 * rows * D))
+    x, xs, w, ws, b, q, status, on = _over(stream, cfg, cache, cfg.sizes, dev_status, wanted)
+    _check(_lib.bt_block_qkv_project_append_i8_kv4(cfg, cache.ref, layer, x, xs, _i32(n_rows), w, ws, b, q, status, on),
            "bt_block_qkv_project_append_i8_kv4")
 
 

@@ -123,10 +123,7 @@ def every_call(bt, n=1):
     """(call, its tensors in order) of every call over the low-bit operators that takes packed tensors."""
     cfg, D, P = config(bt), H * HD, 2
     cache, block, local = kv4(bt, cfg), bt.BlockCache(cfg, device="cpu"), bt.LocalCache(cfg, device="cpu")
-    for c in (block, local):
-        for name in ("k", "v", "kv", "len"):
-            if hasattr(c, name):
-                setattr(c, name, OnDevice(getattr(c, name)))
+    block.device = local.device = 0
     q, x, w, bias, qo, st = t(B, H, HD), t(B, n, D), t(3 * D, D), t(3 * D), t(B, H, n, HD), t(1, dtype=torch.int32)
     x8, w8, xs, ws = t(B, n, D, dtype=torch.int8), t(3 * D, D, dtype=torch.int8), t(B, n, dtype=torch.float32), t(3 * D, dtype=torch.float32)
     c8, cs, p8, ps, pb, po = t(B, D, dtype=torch.int8), t(B, dtype=torch.float32), t(P * D, D, dtype=torch.int8), t(P * D, dtype=torch.float32), t(P * D), t(B, P, D)
@@ -199,7 +196,7 @@ def test_caches_of_16_bits_hold_what_integers_are_projected_into(bt, lib):
                         (dict(max_blocks=N - 1, block_len=3), bt.BT_ERR_SHAPE)):
         made = config(bt, **other)
         block, local = bt.BlockCache(made, device="cpu"), bt.LocalCache(made, device="cpu")
-        block.k, block.v, block.len, local.kv, local.len = (OnDevice(x) for x in (block.k, block.v, block.len, local.kv, local.len))
+        block.device = local.device = 0
         for call, cache in ((bt.bt_block_qkv_project_append_i8, block), (bt.bt_local_qkv_project_append_i8, local)):
             if code:
                 refused(bt, lib, code, call, cfg, cache, 0, x8, xs, w8, ws, None, qo)
@@ -216,3 +213,30 @@ def test_cache_tensors_are_what_they_should_be(bt):
     for bad in (dict(kv=good.kv.to(torch.int8)), dict(length=good.len.long()), dict(length=good.len[:1]), dict(length=good.len.reshape(-1))):
         with pytest.raises(AssertionError):
             bt.BlockCacheKV4(cfg, device="cpu", **bad)
+
+
+def test_a_config_that_changes(bt, lib):
+    """What is worked out from a config's fields follows them."""
+    cfg, rows = config(bt), t(B, H, 1, HD)
+    cache = kv4(bt, cfg)
+    passed(lib, bt.bt_block_kv4_append, cfg, cache, 0, rows, rows)
+    for name, value in (("batch", B + 1), ("heads", 1), ("head_dim", 128), ("max_blocks", N + 1), ("n_layers", 3)):
+        was = getattr(cfg, name)
+        setattr(cfg, name, value)
+        refused(bt, lib, bt.BT_ERR_SHAPE, bt.bt_block_kv4_append, cfg, cache, 0, rows, rows)
+        setattr(cfg, name, was)
+        passed(lib, bt.bt_block_kv4_append, cfg, cache, 0, rows, rows)
+    with pytest.raises(AttributeError):
+        cfg.no_such_field
+
+
+def test_a_cache_of_other_types_is_refused(bt, lib):
+    """A bf16 cache whose tensors the kernels would take for others: made as before, refused by the calls that look."""
+    cfg, D = config(bt), H * HD
+    good = bt.BlockCache(cfg, device="cpu")
+    x8, xs, w8, ws, qo = t(B, 1, D, dtype=torch.int8), t(B, dtype=torch.float32), t(3 * D, D, dtype=torch.int8), t(3 * D, dtype=torch.float32), t(B, H, 1, HD)
+    for bad in (dict(k=good.k.half()), dict(v=good.v.float()), dict(length=good.len.long()), dict(length=good.len[:1]),
+                dict(length=torch.zeros((B, 2), dtype=torch.int32).T)):
+        cache = bt.BlockCache(cfg, device="cpu", **{**dict(k=good.k, v=good.v, length=good.len), **bad})
+        assert cache.device == -2
+        refused(bt, lib, bt.BT_ERR_UNSUPPORTED, bt.bt_block_qkv_project_append_i8, cfg, cache, 0, x8, xs, w8, ws, None, qo)
