@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
             float end = 0.f;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) end = fmaxf(end, fmaxf(w_most[p][0] * w_to[p][0], w_most[p][1] * w_to[p][1]));
-            if (grown || pending >= kUnitsPerSum || __any_sync(0xffffffffu, end >= kWeightEnd)) {
+            if (__any_sync(0xffffffffu, grown || pending >= kUnitsPerSum || end >= kWeightEnd)) {
                 if (pending > 0) flush();
 #pragma unroll
                 for (int p = 0; p < PLANES; ++p) {
