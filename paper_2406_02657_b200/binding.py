@@ -42,7 +42,8 @@ class bt_config(ctypes.Structure):
     # takes a small call 0.2 us of host time.
     def __setattr__(self, name, value):
         super().__setattr__(name, value)
-        self.__dict__.clear()
+        for derived in ("sizes", "local_sizes", "model_dim"):
+            self.__dict__.pop(derived, None)
 
     def __getattr__(self, name):
         if name not in ("sizes", "local_sizes", "model_dim"):

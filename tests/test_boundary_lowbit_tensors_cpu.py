@@ -1,5 +1,7 @@
 """The binding refuses tensors that do not hold what a call over the low-bit operators would read or write, before the library is called (no GPU
 needed: the tensors are in the host's memory and say that they are on the current device; the library's calls are recorded)."""
+import copy
+
 import pytest
 import torch
 
@@ -228,6 +230,10 @@ def test_a_config_that_changes(bt, lib):
         passed(lib, bt.bt_block_kv4_append, cfg, cache, 0, rows, rows)
     with pytest.raises(AttributeError):
         cfg.no_such_field
+    cfg.note = "kept"                          # an attribute of the caller's own
+    cfg.batch, other = B, copy.copy(cfg)
+    other.batch = B + 1
+    assert cfg.note == "kept" and cfg.sizes == (B, H, HD, N) and other.sizes == (B + 1, H, HD, N)
 
 
 def test_a_cache_of_other_types_is_refused(bt, lib):
