@@ -362,7 +362,8 @@ bt_status bt_block_kv_evict(const bt_config* cfg, bt_block_cache* cache, float* 
  *
  * What a row is held as: for every 32 dimensions a step s = bf16(max|x| / 7) and codes u = round(x / s), halves away from zero
  * (-7 <= u <= 7); its value is s u.  Where s would be below 2^-126 the 32 values are held as zeros; where one of them is
- * not finite all 32 are held as NaN.
+ * not finite all 32 are held as NaN.  (The largest bf16 number, 0x7f7f, is held as 2^128 - 2^119, which as bf16 is infinite: what is
+ * read back, or comes out of attention over such rows alone, is then infinity.  0x7f7e and below are not.)
  *   kv  : uint8 [n_layers][B][H][ceil(N_max / 16)][hd / 64][BT_KV4_TILE_BYTES], 16-byte aligned; the last 16 rows may be there in
  *         part only, and their tiles are whole nevertheless.  A tile holds 16 rows x 64 dimensions of K and V, two codes a byte as
  *         u + 8 (dimension 2i in the low half, 2i + 1 in the high half); byte i of row r of the tile lies at
@@ -452,7 +453,8 @@ bt_status bt_prefix_project(const bt_config* cfg, const void* ctx, const void* w
  *   len[b] += n_rows.
  * A sequence without room for n_rows more rows keeps its cache and length, BT_DEV_OVERFLOW is raised
  * (its q_out rows are still written).  Two launches: the product with the cache-writing epilogue, then
- * a small one that advances the lengths once every tile has read the old ones.
+ * a small one that advances the lengths once every tile has read the old ones; one, where every sequence starts anew (the local
+ * form with reset_first and no mask): the product sets the lengths then.
  * Attention then runs over the cache as it stands: bt_block_decode_attn for the block decoder,
  * bt_token_decode_attn with k_new = v_new = NULL (n_q = n_rows) for the token decoder.
  * Returns BT_ERR_CAPACITY if n_rows exceeds the cache capacity.

@@ -712,11 +712,11 @@ bt_status bt_block_kv4_read(const bt_config* cfg, const bt_block_cache_kv4* cach
 
 // Ways the row range of a (sequence, head) is cut: enough parts for the kernel's warps (eight on each of 148 SMs; the number
 // fixes the workspace, so it does not depend on the device), each of at least 128 rows, or of 64 while there are at most 16 (head_dim 128, where a
-// warp takes longer for them: 32) parts: 32 pairs of 512 rows of 64 4.5 us in eight parts, 4.7 in four; 16 pairs of 4096 5.0 us in 32, 6.2 in 64; 16 pairs
-// of 2048 of 128 5.8 us in 32, 6.5 in 16.  32 parts are joined in one go; more are worth it only for 256 rows each (8 pairs of 16384 rows of 128: 9.5 us
+// warp takes longer for them: 32) parts: 32 pairs of 512 rows of 64 4.5 us in eight parts, 4.8 in four; 16 pairs of 4096 5.3 us in 32, 6.2 in 64; 16 pairs
+// of 2048 of 128 5.8 us in 32, 6.2 in 16.  32 parts are joined in one go; more are worth it only for 256 rows each (8 pairs of 16384 rows of 128: 9.4 us
 // in 64, 11.6 in 32; of 8192: 8.6, 8.4).  Joining costs 2 us and more, as long as a warp takes for seven times 64 rows at head_dim 64 and for
-// five times at 128: where cutting does not save a warp as many, nothing is cut (512 pairs of 512 rows of 64: 6.0 us, in two parts 7.2; 64 pairs of
-// 200 to 256: 4.0 us, in four 4.5; 256 pairs of 1024, which gain: 9.3 us, in four 7.4).
+// five times at 128: where cutting does not save a warp as many, nothing is cut (512 pairs of 512 rows of 64: 6.2 us, in two parts 7.7; 64 pairs of
+// 200 to 256: 4.0 us, in four 4.5; 256 pairs of 1024, which gain: 9.4 us, in four 7.5).
 static int kv4_splits(const bt_config* cfg)
 {
     if (cfg->decode_splits > 0) return cfg->decode_splits;

@@ -185,7 +185,8 @@ cudaError_t launch_rows_quantize(const void* x, long long rows, int cols, void* 
 //   kProjectQkv   : M = B * n_rows rows (sequence b, row i), N = 3 * H * hd output features ordered Q, K, V,
 //                   each (h, d): Q -> out [B][H][n_rows][hd]; K, V -> rows len_old[b] + i of `cache`
 //                   (len_old = 0 where the reset applies); a sequence without room for n_rows rows keeps
-//                   its cache.  A second launch then advances the lengths (and flags those sequences).
+//                   its cache.  A second launch then advances the lengths (and flags those sequences), unless every
+//                   sequence starts anew (reset_first without a mask).
 //   kProjectQkvKv4: the same into the 4-bit block cache: cache.k is its layer base, cache.slab_stride its slabs' bytes.
 enum { kProjectPlain = 0, kProjectQkv = 1, kProjectQkvKv4 = 2 };
 struct ProjectArgs {

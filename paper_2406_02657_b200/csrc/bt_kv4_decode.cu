@@ -427,7 +427,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) block_decode_kv4_kernel(con
                     }
             }
             // ... and what the weights of a group are relative to, then and when one would leave 32 bits.  (A power of two for all
-            // groups would take the precision of those whose steps are small beside another's.)
+            // groups would take the precision of those whose steps are small beside another's; it would save 0.9 of 60.6 us over 24 x 16 items of
+            // 12001 to 16000 rows of 64, 0.7 of 115.6 of 128.  One vote for all that leads here: three ways in are compiled as copies, and the code
+            // then outgrows what is near an SM: 5.2 us instead of 4.5 over 32 pairs of 512 rows in eight parts.)
             float end = 0.f;
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) end = fmaxf(end, fmaxf(w_most[p][0] * w_to[p][0], w_most[p][1] * w_to[p][1]));
@@ -705,8 +707,8 @@ cudaError_t launch_block_decode_kv4(const Kv4DecodeArgs& a, cudaStream_t stream)
     if (a.hd == 128) return kv4::launch_t<128, 1, 2, 8>(a, dev, sms, stream);
     // Head_dim 64: with at most eight items an SM, a warp each and chunks of two units; with more, 16 warps an SM (126 registers a thread),
     // of which each spends half as long on an item's beginning and end.  us, 16 warps / eight:
-    //   items of 48 to 64 rows:     1024: 3.5 / 3.5,  1536: 3.8 / 5.3,   4096: 7.1 / 9.5
-    //   items of 384 to 512 rows:   1024: 9.2 / 8.3,  1536: 11.0 / 13.9, 4096: 23.5 / 26.5
+    //   items of 48 to 64 rows:     1024: 3.4 / 3.5,  1536: 3.8 / 5.2,   4096: 7.2 / 9.4
+    //   items of 384 to 512 rows:   1024: 9.4 / 8.3,  1536: 11.1 / 13.9, 4096: 23.9 / 26.4
     if ((long long)a.B * a.H * a.splits > 8LL * sms) return kv4::launch_t<64, 1, 2, 16>(a, dev, sms, stream);
     return kv4::launch_t<64, 2, 2, 8>(a, dev, sms, stream);
 }
